@@ -126,8 +126,8 @@ def draw(rng):
 
 # ---------------------------------------------------------------------------------------------- inputs
 
-def _gen(seed, device=DEV):
-    g = torch.Generator(device=device)
+def _gen(seed, device=None):
+    g = torch.Generator(device=device or DEV)
     g.manual_seed(seed)
     return g
 
