@@ -21,7 +21,8 @@
  *    before anything is launched, so a failed call has no side effects on device memory.
  *  - A cache "slot" is a row index into the KV pool: slot = block_id * 16 + offset_in_block.
  *    The pool of one layer is addressed as  base + slot*stride_slot + kv_head*stride_head + c.
- *  - dtype: CS_F32 (float) or CS_BF16 (bfloat16 bit patterns, uint16_t storage).
+ *  - dtype: CS_F32 (float) or CS_BF16 (bfloat16 bit patterns, uint16_t storage).  Caches may also be held in
+ *    4 bits (CS_KV4, calls q1 .. q4 below).
  *  - Not checked on the device (caller's contract): slots lie inside the pool; destination
  *    slots are unique; for a repacking re-rotation the source and destination slot sets are
  *    disjoint; q_pos is non-decreasing inside a stream and smaller than that stream's kv_len.
@@ -44,6 +45,7 @@ extern "C" {
 
 #define CS_F32  0
 #define CS_BF16 1
+#define CS_KV4  2   /* caches only: 4-bit elements in blocks of 32 with a power of two each, see (q1) */
 
 #define CS_FRAME_P 0
 #define CS_FRAME_I 1
@@ -505,6 +507,170 @@ int cs_refresh_prefill_attn(const void* k_new, const void* v_new, const int32_t*
                             int64_t stride_slot, int64_t stride_head, float softmax_scale,
                             int32_t dtype, void* workspace, size_t workspace_bytes,
                             int32_t plan_mode, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * 4-bit window cache.  (No passage of the paper: its cache is 16-bit.  The calls below are those of (b), (c) and
+ *     (d) for a cache of a quarter of the size, with the rotary embedding of fresh tokens in the write.)
+ *
+ * A cache row is head_dim elements of 4 bits in blocks of 32, a scale per block:
+ *     element   sign (bit 3) and one of 0, .5, 1, 1.5, 2, 3, 4, 6 (bits 0..2); two elements a byte, the even one low
+ *     scale     one byte e: the element stands for its number times 2^(e - 127), e in 1..254 (0 is read as 1);
+ *               255: the block held a NaN or an infinity, all of its elements are read as NaN
+ * A block x of 32 numbers becomes: e the least in 1..254 with max |x| <= 7 * 2^(e - 127), elements the nearest numbers
+ * to x / 2^(e - 127), ties to the even code, saturating at 6 (a number past 3.5 * 2^126 becomes 2^128, which reads as infinity).  (So the stored numbers of a row are bf16 numbers, and
+ * a row that is written again unchanged keeps its numbers.)
+ * A pool is a tensor of codes and one of scales for K and the same for V, addressed by ONE set of strides in elements,
+ * multiples of 32: element (l, slot, h, c) is number i = l*stride_layer + slot*stride_slot + h*stride_head + c, its code
+ * in byte i/2 of the codes, its scale in byte i/32 of the scales.  Codes are 16-byte aligned.  Head-major pools
+ * (stride_slot = head_dim) are read in whole lines by attention, which takes one kv head at a time.
+ * ------------------------------------------------------------------------------------------ */
+
+/* ------------------------------------------------------------------------------------------
+ * (q1) Rotary embedding of fresh tokens with the refresh write.     Paper Sec. 3.5 (write), Sec. 4 (three-axis mRoPE).
+ *
+ * One layer, n_tok tokens as a projection leaves them, not yet rotated:
+ *     q_out[t][h] = R(pos[t]) q[t][h]
+ *     K[slot[t]][h] = R(pos[t]) k_new[t][h],  V[slot[t]][h] = v_new[t][h]      for slot[t] >= 0
+ * in a cache of dtype (as cs_kv_refresh_scatter writes it) or of 4 bits.  R as in cs_kv_rerotate; with axis_of_pair the
+ * position is a triple (t, h, w) and pair i is turned by pos[t][axis_of_pair[i]] * theta_i, as in cs_kv_rerotate_axes:
+ * images and video have their frame, row and column there, text the same number three times.  Angles are formed and
+ * reduced in double precision, cosine and sine rounded to single, products and sums are single precision, each rounded
+ * (not fused); bf16 results are rounded once, and 4-bit rows come from the single-precision ones.
+ * R(-p) is R(p) transposed: with negated positions the call undoes the rotation, and maps the gradient of its results
+ * to that of its inputs.
+ *
+ *  q             in   token t at t*stride_q, heads behind one another; 16-byte aligned; NULL iff n_q_heads == 0
+ *  q_out         out  [n_tok][n_q_heads][head_dim] contiguous, 16-byte aligned; or q itself (then with its stride)
+ *  k_new, v_new  in   token t at t*stride_k / stride_v; 16-byte aligned; NULL iff n_kv_heads == 0 (as slot and the caches)
+ *  slot          in   int32 [n_tok], unique where >= 0; a negative slot skips the token's write
+ *  pos           in   int32 [n_tok], or [n_tok][3] with axis_of_pair.  NULL: keys are written as they are (n_q_heads == 0)
+ *  axis_of_pair  in   uint8 [head_dim/2], values 0, 1, 2 (larger: read as 2), or NULL
+ *  k_cache_layer, v_cache_layer  i/o  pool of the layer (codes of a 4-bit cache), 16-byte aligned
+ *  k_scales_layer, v_scales_layer  i/o  scales of a 4-bit cache, else ignored
+ *  stride_q, stride_k, stride_v   elements from token to token, multiples of 16 bytes, no less than a token's heads
+ *  stride_slot, stride_head       elements of the cache
+ * Errors: CS_EINVAL (null pointer, negative size, no heads at all, tokens that overlap, queries without positions, rope_base not
+ *         a positive finite number), CS_EUNSUPPORTED (head_dim not a multiple of 16 (4-bit cache: 64) or > 256, unknown
+ *         dtype / rope_style, a cache_dtype that is neither dtype nor CS_KV4, strides or pointers that are not aligned, more than
+ *         65,535 heads), CS_EHIP.  n_tok == 0 returns CS_OK.
+ * ------------------------------------------------------------------------------------------ */
+int cs_rope_refresh_scatter(const void* q, void* q_out, const void* k_new, const void* v_new, const int32_t* slot,
+                            const int32_t* pos, const uint8_t* axis_of_pair, void* k_cache_layer, void* v_cache_layer,
+                            uint8_t* k_scales_layer, uint8_t* v_scales_layer, int64_t n_tok, int32_t n_q_heads,
+                            int32_t n_kv_heads, int32_t head_dim, int64_t stride_q, int64_t stride_k, int64_t stride_v,
+                            int64_t stride_slot, int64_t stride_head, float rope_base, int32_t rope_style,
+                            int32_t dtype, int32_t cache_dtype, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * (q2) Rows of a 4-bit cache as numbers.
+ *
+ *     k_out[l][i][h] = K[l][slot[i]][h],  v_out likewise       for slot[i] >= 0; other rows are left as they were
+ *
+ *  k_out, v_out  out  [n_layers][n_rows][n_kv_heads][head_dim] of dtype (exact in either), 16-byte aligned; one of them
+ *                     may be NULL (its pool then too)
+ * Errors: CS_EINVAL (null pointer, negative size), CS_EUNSUPPORTED (head_dim not a multiple of 64 or > 256, unknown dtype,
+ *         strides not multiples of 32, alignment), CS_EHIP.  n_rows == 0 or n_layers == 0 returns CS_OK.
+ * ------------------------------------------------------------------------------------------ */
+int cs_kv4_gather(const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* v_codes, const uint8_t* v_scales,
+                  const int32_t* slot, int64_t n_rows, int32_t n_layers, int32_t n_kv_heads, int32_t head_dim,
+                  int64_t stride_layer, int64_t stride_slot, int64_t stride_head, void* k_out, void* v_out, int32_t dtype,
+                  void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * (q3) Position-corrected reuse of 4-bit keys.       Paper Sec. 3.4.2, Eq. 6, as cs_kv_rerotate (axis_of_pair == NULL, delta
+ *     int32 [n_rows]) and cs_kv_rerotate_axes (delta int32 [n_rows][3]) on a 4-bit cache of all layers.
+ *
+ * A key's numbers are turned in single precision and written as 4-bit rows again, so a key that stays in a window for
+ * several slides is rounded once a slide (a shift of 0 keeps its numbers).  Values are copied code for code.
+ * dst_slot == NULL: keys in place, the v pools are not touched (may be NULL).  Rows with a negative src_slot or dst_slot
+ * are skipped; source and destination slot sets are disjoint, destination slots unique.
+ * Errors: as cs_kv_rerotate; CS_EUNSUPPORTED also for head_dim not a multiple of 64, strides not multiples of 32.
+ * ------------------------------------------------------------------------------------------ */
+int cs_kv4_rerotate(uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_codes, uint8_t* v_scales, const int32_t* src_slot,
+                    const int32_t* dst_slot, const int32_t* delta, const uint8_t* axis_of_pair, int64_t n_rows,
+                    int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int64_t stride_layer, int64_t stride_slot,
+                    int64_t stride_head, float rope_base, int32_t rope_style, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * (q4) Joint prefill attention, or attention of single tokens, over a 4-bit cache.       Paper Sec. 3.5.
+ *
+ * As cs_window_prefill_attn, with the same meaning of cu_q, q_pos, kv_len, block_table and of n_q as an upper bound; besides,
+ * q_pos needs no order inside a stream, and a negative q_pos is a query that sees nothing (out 0, lse -inf).
+ * q and out are CS_BF16 (bf16 operands, fp32 scores, statistics and sums; weights are rounded to bf16) or CS_F32 (fp32
+ * accuracy throughout).  Keys and values that are no numbers reach the queries that see them, and no others.
+ *
+ *  lse          out  float [n_q][n_q_heads] or NULL: log sum_j exp(softmax_scale * q[t][h] . K_j), natural logarithm
+ *  workspace         cs_kv4_window_attn_workspace() bytes, 16-byte aligned (may be 0, then NULL is accepted); contents need
+ *                    not be initialised.  Two calls that overlap in time must not share a workspace.
+ * Errors: CS_EINVAL (null pointer, negative size, n_q_heads not a multiple of n_kv_heads, softmax_scale not a positive
+ *         finite number), CS_EUNSUPPORTED (head_dim not in {64,128}, block_size != 16, n_q_heads/n_kv_heads > 16, strides not
+ *         multiples of 32, alignment, unknown dtype, n_q >= 2^27, n_kv_heads > 65,535), CS_EWORKSPACE, CS_EHIP.
+ *         n_q == 0 or n_streams == 0 returns CS_OK.
+ * ------------------------------------------------------------------------------------------ */
+size_t cs_kv4_window_attn_workspace(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads,
+                                    int32_t head_dim, int32_t max_blocks);
+
+int cs_kv4_window_attn(const void* q, const uint8_t* k_codes_layer, const uint8_t* k_scales_layer,
+                       const uint8_t* v_codes_layer, const uint8_t* v_scales_layer, const int32_t* cu_q,
+                       const int32_t* q_pos, const int32_t* kv_len, const int32_t* block_table, int32_t max_blocks,
+                       int32_t block_size, void* out, float* lse, int64_t n_q, int32_t n_streams, int32_t n_q_heads,
+                       int32_t n_kv_heads, int32_t head_dim, int64_t stride_slot, int64_t stride_head,
+                       float softmax_scale, int32_t dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * (w) Attention weight that every cache entry received.  (No passage of the paper: it prunes by codec metadata; this is
+ *     the measure of what the model reads, for cs_plan_evict.)
+ *
+ *     weight_out[s][j] = decay * weight_in[s][j] + sum_{t, h} exp(softmax_scale * q[t][h] . K_j - lse[t][h])
+ * over the queries t of stream s with j <= q_pos[t] and all query heads h, for the entries j < kv_len[s]; other places of
+ * weight_out are left as they were.  Arguments as in the attention calls; any order of q_pos, negative ones see nothing.
+ * The sums' order is fixed: the same call gives the same bits.
+ *
+ *  lse           in   float [n_q][n_q_heads] as cs_kv4_window_attn leaves them, or NULL: computed here (keys are read twice)
+ *  k_cache_layer, k_scales_layer   in   the layer's keys; cache_dtype is dtype (scales ignored) or CS_KV4
+ *  weight_in     in   float [n_streams][max_blocks * 16], or NULL (zeros); not read with decay == 0
+ *  weight_out    out  the same layout, may be weight_in
+ *  decay              0 .. 1: 1 sums up, less lets earlier steps fade, 0 starts anew
+ *  workspace          cs_attn_weights_workspace() bytes, 16-byte aligned, contents need not be initialised.  Two calls that
+ *                     overlap in time must not share a workspace.
+ * Errors: as cs_kv4_window_attn; CS_EINVAL also for a decay outside 0 .. 1, CS_EUNSUPPORTED for a cache_dtype that is neither
+ *         dtype nor CS_KV4.  n_streams == 0 returns CS_OK; n_q == 0 only lets weights fade.
+ * ------------------------------------------------------------------------------------------ */
+size_t cs_attn_weights_workspace(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                 int32_t max_blocks);
+
+int cs_attn_weights(const void* q, const float* lse, const void* k_cache_layer, const uint8_t* k_scales_layer,
+                    const int32_t* cu_q, const int32_t* q_pos, const int32_t* kv_len, const int32_t* block_table,
+                    int32_t max_blocks, int32_t block_size, const float* weight_in, float* weight_out, float decay,
+                    int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                    int64_t stride_slot, int64_t stride_head, float softmax_scale, int32_t dtype, int32_t cache_dtype,
+                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * (v) Eviction: which entries stay when windows are cut to a budget.     (Paper Sec. 3.5 for the lists: a frame-aware index
+ *     maps spans to physical slots; the choice by weight is not the paper's.)
+ *
+ * Stream s keeps m = min(kv_len[s], budget) entries: the first n_first, the last n_last, then those of the largest
+ * weight[s][j], equal weights by the lowest index, NaN below everything (where the budget does not hold the first and last
+ * ones, the earliest of them).  Kept entries stay in order; the i-th one, entry j of the old window, gives
+ *     kept[s][i] = j, src_slot = its slot by block_table_old, dst_slot = entry i's slot by block_table_new,
+ *     delta = renumber ? i - j : 0
+ * The lists are what cs_kv_rerotate, cs_kv4_rerotate (dst_slot != NULL) take with n_rows = n_streams * budget; the two tables must
+ * name different blocks.  Places i >= m hold kept, src_slot, dst_slot -1 and delta 0.
+ *
+ *  weight           in   float [n_streams][max_blocks_old * 16];   kv_len  in  int32 [n_streams] (clamped to the table's rows)
+ *  block_table_old, block_table_new   in   int32 [n_streams][max_blocks_old / _new]
+ *  kept, src_slot, dst_slot, delta    out  int32 [n_streams][budget]
+ *  kv_len_new       out  int32 [n_streams]: m
+ *  weight_new       out  float [n_streams][max_blocks_new * 16] or NULL: the kept entries' weights; places past m are left
+ * Bit exact.
+ * Errors: CS_EINVAL (null pointer, negative size, budget < 1, a block table without columns, a new table too narrow for what
+ *         may stay), CS_EUNSUPPORTED (tables of 2^27 columns), CS_EHIP.  n_streams == 0 returns CS_OK.
+ * ------------------------------------------------------------------------------------------ */
+int cs_plan_evict(const float* weight, const int32_t* kv_len, const int32_t* block_table_old, int32_t max_blocks_old,
+                  const int32_t* block_table_new, int32_t max_blocks_new, int32_t n_streams, int32_t budget,
+                  int32_t n_first, int32_t n_last, int32_t renumber, int32_t* kept, int32_t* src_slot, int32_t* dst_slot,
+                  int32_t* delta, int32_t* kv_len_new, float* weight_new, void* stream);
 
 #ifdef __cplusplus
 }

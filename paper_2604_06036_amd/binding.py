@@ -17,7 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcodecsight.so")
 
 CS_OK, CS_EINVAL, CS_EUNSUPPORTED, CS_EHIP, CS_EWORKSPACE = 0, -1, -2, -3, -4
-CS_F32, CS_BF16 = 0, 1
+CS_F32, CS_BF16, CS_KV4 = 0, 1, 2
 CS_ATTN_PLAN_BUILD, CS_ATTN_PLAN_REUSE, CS_ATTN_PLAN_ONLY = 0, 1, 2
 CS_ATTN_OWN_ROWS = 1 << 16
 CS_FRAME_P, CS_FRAME_I = 0, 1
@@ -31,7 +31,9 @@ EXPORTS = ("cs_version", "cs_last_hip_error", "cs_mfma_rate_probe", "cs_project_
            "cs_score_compact_noalloc",
            "cs_plan_refresh_workspace", "cs_plan_refresh", "cs_kv_rerotate", "cs_kv_rerotate_axes", "cs_kv_refresh_scatter",
            "cs_window_prefill_attn_workspace",
-           "cs_window_prefill_attn", "cs_refresh_prefill_attn_workspace", "cs_refresh_prefill_attn")
+           "cs_window_prefill_attn", "cs_refresh_prefill_attn_workspace", "cs_refresh_prefill_attn",
+           "cs_rope_refresh_scatter", "cs_kv4_gather", "cs_kv4_rerotate", "cs_kv4_window_attn_workspace", "cs_kv4_window_attn",
+           "cs_attn_weights_workspace", "cs_attn_weights", "cs_plan_evict")
 
 
 class CodecSightError(RuntimeError):
@@ -95,6 +97,22 @@ def lib() -> ctypes.CDLL:
     L.cs_refresh_prefill_attn.restype = c.c_int
     L.cs_refresh_prefill_attn.argtypes = [vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp, i64, i32, i32, i32,
                                           i32, i64, i64, f32, i32, vp, sz, i32, vp]
+    L.cs_rope_refresh_scatter.restype = c.c_int
+    L.cs_rope_refresh_scatter.argtypes = [vp] * 11 + [i64, i32, i32, i32, i64, i64, i64, i64, i64, f32, i32, i32, i32, vp]
+    L.cs_kv4_gather.restype = c.c_int
+    L.cs_kv4_gather.argtypes = [vp, vp, vp, vp, vp, i64, i32, i32, i32, i64, i64, i64, vp, vp, i32, vp]
+    L.cs_kv4_rerotate.restype = c.c_int
+    L.cs_kv4_rerotate.argtypes = [vp] * 8 + [i64, i32, i32, i32, i64, i64, i64, f32, i32, vp]
+    L.cs_kv4_window_attn_workspace.restype = sz
+    L.cs_kv4_window_attn_workspace.argtypes = [i64, i32, i32, i32, i32, i32]
+    L.cs_kv4_window_attn.restype = c.c_int
+    L.cs_kv4_window_attn.argtypes = [vp] * 9 + [i32, i32, vp, vp, i64, i32, i32, i32, i32, i64, i64, f32, i32, vp, sz, vp]
+    L.cs_attn_weights_workspace.restype = sz
+    L.cs_attn_weights_workspace.argtypes = [i64, i32, i32, i32, i32, i32]
+    L.cs_attn_weights.restype = c.c_int
+    L.cs_attn_weights.argtypes = [vp] * 8 + [i32, i32, vp, vp, f32, i64, i32, i32, i32, i32, i64, i64, f32, i32, i32, vp, sz, vp]
+    L.cs_plan_evict.restype = c.c_int
+    L.cs_plan_evict.argtypes = [vp, vp, vp, i32, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp]
     _lib = L
     return L
 
@@ -340,3 +358,105 @@ def cs_attn_status(workspace) -> int:
         return 0
     flat = workspace.view(-1).view(torch.uint8)
     return int(flat[CS_ATTN_STATUS_OFFSET:CS_ATTN_STATUS_OFFSET + 4].view(torch.int32).item())
+
+
+def _span(t: Optional[torch.Tensor], rows: int, stride: int, row: int) -> bool:
+    """Whether the memory from t's first element on holds `rows` rows of `row` elements, `stride` apart."""
+    if t is None or rows < 1:
+        return True
+    return (rows - 1) * stride + row <= t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+
+
+def cs_rope_refresh_scatter(q, q_out, k_new, v_new, slot, pos, axis_of_pair, k_cache_layer, v_cache_layer, k_scales_layer,
+                            v_scales_layer, n_tok, n_q_heads, n_kv_heads, head_dim, stride_q, stride_k, stride_v, stride_slot,
+                            stride_head, rope_base, rope_style, dtype, cache_dtype):
+    fn = "cs_rope_refresh_scatter"
+    _need(fn, slot, n_tok, "slot")
+    _need(fn, pos, n_tok if axis_of_pair is None else 3 * n_tok, "pos"); _need(fn, axis_of_pair, head_dim // 2, "axis_of_pair")
+    for t, stride, heads, what in ((q, stride_q, n_q_heads, "q"), (k_new, stride_k, n_kv_heads, "k_new"), (v_new, stride_v, n_kv_heads, "v_new")):
+        if not _span(t, n_tok, stride, heads * head_dim):
+            raise ValueError(f"{fn}: {what} holds fewer than {n_tok} tokens")
+    if q_out is not None and (q is None or q_out.data_ptr() != q.data_ptr()):
+        _need(fn, q_out, n_tok * n_q_heads * head_dim, "q_out")
+    _check(fn, lib().cs_rope_refresh_scatter(
+        _ptr(q), _ptr(q_out), _ptr(k_new), _ptr(v_new), _ptr(slot), _ptr(pos), _ptr(axis_of_pair), _ptr(k_cache_layer), _ptr(v_cache_layer),
+        _ptr(k_scales_layer), _ptr(v_scales_layer), n_tok, n_q_heads, n_kv_heads, head_dim, stride_q, stride_k, stride_v, stride_slot,
+        stride_head, rope_base, rope_style, dtype, cache_dtype, _stream()))
+
+
+def cs_kv4_gather(k_codes, k_scales, v_codes, v_scales, slot, n_rows, n_layers, n_kv_heads, head_dim, stride_layer, stride_slot,
+                  stride_head, k_out, v_out, dtype):
+    fn = "cs_kv4_gather"
+    _need(fn, slot, n_rows, "slot")
+    for t, what in ((k_out, "k_out"), (v_out, "v_out")):
+        _need(fn, t, n_layers * n_rows * n_kv_heads * head_dim, what)
+    _check(fn, lib().cs_kv4_gather(_ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales), _ptr(slot), n_rows, n_layers, n_kv_heads,
+                                   head_dim, stride_layer, stride_slot, stride_head, _ptr(k_out), _ptr(v_out), dtype, _stream()))
+
+
+def cs_kv4_rerotate(k_codes, k_scales, v_codes, v_scales, src_slot, dst_slot, delta, axis_of_pair, n_rows, n_layers, n_kv_heads,
+                    head_dim, stride_layer, stride_slot, stride_head, rope_base, rope_style):
+    fn = "cs_kv4_rerotate"
+    _need(fn, src_slot, n_rows, "src_slot"); _need(fn, dst_slot, n_rows, "dst_slot")
+    _need(fn, delta, n_rows if axis_of_pair is None else 3 * n_rows, "delta"); _need(fn, axis_of_pair, head_dim // 2, "axis_of_pair")
+    _check(fn, lib().cs_kv4_rerotate(_ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales), _ptr(src_slot), _ptr(dst_slot), _ptr(delta),
+                                     _ptr(axis_of_pair), n_rows, n_layers, n_kv_heads, head_dim, stride_layer, stride_slot, stride_head,
+                                     rope_base, rope_style, _stream()))
+
+
+def cs_kv4_window_attn_workspace(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, max_blocks) -> int:
+    return int(lib().cs_kv4_window_attn_workspace(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, max_blocks))
+
+
+def cs_kv4_window_attn(q, k_codes_layer, k_scales_layer, v_codes_layer, v_scales_layer, cu_q, q_pos, kv_len, block_table, max_blocks,
+                       block_size, out, lse, n_q, n_streams, n_q_heads, n_kv_heads, head_dim, stride_slot, stride_head, softmax_scale,
+                       dtype, workspace=None, workspace_bytes=None):
+    if workspace_bytes is None:
+        workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    fn = "cs_kv4_window_attn"
+    _need(fn, q, n_q * n_q_heads * head_dim, "q"); _need(fn, out, n_q * n_q_heads * head_dim, "out"); _need(fn, lse, n_q * n_q_heads, "lse")
+    _need(fn, cu_q, n_streams + 1, "cu_q"); _need(fn, q_pos, n_q, "q_pos"); _need(fn, kv_len, n_streams, "kv_len")
+    _need(fn, block_table, n_streams * max_blocks, "block_table")
+    if workspace is not None and workspace.numel() * workspace.element_size() < workspace_bytes:
+        raise ValueError(f"{fn}: workspace tensor smaller than workspace_bytes")
+    _check(fn, lib().cs_kv4_window_attn(
+        _ptr(q), _ptr(k_codes_layer), _ptr(k_scales_layer), _ptr(v_codes_layer), _ptr(v_scales_layer), _ptr(cu_q), _ptr(q_pos), _ptr(kv_len),
+        _ptr(block_table), max_blocks, block_size, _ptr(out), _ptr(lse), n_q, n_streams, n_q_heads, n_kv_heads, head_dim, stride_slot,
+        stride_head, softmax_scale, dtype, _ptr(workspace), workspace_bytes, _stream()))
+
+
+def cs_attn_weights_workspace(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, max_blocks) -> int:
+    return int(lib().cs_attn_weights_workspace(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, max_blocks))
+
+
+def cs_attn_weights(q, lse, k_cache_layer, k_scales_layer, cu_q, q_pos, kv_len, block_table, max_blocks, block_size, weight_in, weight_out,
+                    decay, n_q, n_streams, n_q_heads, n_kv_heads, head_dim, stride_slot, stride_head, softmax_scale, dtype, cache_dtype,
+                    workspace=None, workspace_bytes=None):
+    if workspace_bytes is None:
+        workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    fn = "cs_attn_weights"
+    _need(fn, q, n_q * n_q_heads * head_dim, "q"); _need(fn, lse, n_q * n_q_heads, "lse")
+    _need(fn, cu_q, n_streams + 1, "cu_q"); _need(fn, q_pos, n_q, "q_pos"); _need(fn, kv_len, n_streams, "kv_len")
+    _need(fn, block_table, n_streams * max_blocks, "block_table")
+    for t, what in ((weight_in, "weight_in"), (weight_out, "weight_out")):
+        _need(fn, t, n_streams * max_blocks * CS_KV_BLOCK, what)
+    if workspace is not None and workspace.numel() * workspace.element_size() < workspace_bytes:
+        raise ValueError(f"{fn}: workspace tensor smaller than workspace_bytes")
+    _check(fn, lib().cs_attn_weights(
+        _ptr(q), _ptr(lse), _ptr(k_cache_layer), _ptr(k_scales_layer), _ptr(cu_q), _ptr(q_pos), _ptr(kv_len), _ptr(block_table), max_blocks,
+        block_size, _ptr(weight_in), _ptr(weight_out), decay, n_q, n_streams, n_q_heads, n_kv_heads, head_dim, stride_slot, stride_head,
+        softmax_scale, dtype, cache_dtype, _ptr(workspace), workspace_bytes, _stream()))
+
+
+def cs_plan_evict(weight, kv_len, block_table_old, max_blocks_old, block_table_new, max_blocks_new, n_streams, budget, n_first, n_last,
+                  renumber, kept, src_slot, dst_slot, delta, kv_len_new, weight_new):
+    fn = "cs_plan_evict"
+    _need(fn, weight, n_streams * max_blocks_old * CS_KV_BLOCK, "weight"); _need(fn, kv_len, n_streams, "kv_len")
+    _need(fn, block_table_old, n_streams * max_blocks_old, "block_table_old")
+    _need(fn, block_table_new, n_streams * max_blocks_new, "block_table_new")
+    for t, what in ((kept, "kept"), (src_slot, "src_slot"), (dst_slot, "dst_slot"), (delta, "delta")):
+        _need(fn, t, n_streams * budget, what)
+    _need(fn, kv_len_new, n_streams, "kv_len_new"); _need(fn, weight_new, n_streams * max_blocks_new * CS_KV_BLOCK, "weight_new")
+    _check(fn, lib().cs_plan_evict(
+        _ptr(weight), _ptr(kv_len), _ptr(block_table_old), max_blocks_old, _ptr(block_table_new), max_blocks_new, n_streams, budget, n_first,
+        n_last, int(bool(renumber)), _ptr(kept), _ptr(src_slot), _ptr(dst_slot), _ptr(delta), _ptr(kv_len_new), _ptr(weight_new), _stream()))

@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcodecsight.so")
-SOURCES = ["library.hip", "calibrate.hip", "project_blocks.hip", "residual_proxy.hip", "score_compact.hip", "plan_refresh.hip", "kv_rerotate.hip", "window_attn.hip"]
+SOURCES = ["library.hip", "calibrate.hip", "project_blocks.hip", "residual_proxy.hip", "score_compact.hip", "plan_refresh.hip", "kv_rerotate.hip", "window_attn.hip",
+           "kv4_cache.hip", "kv4_attn.hip", "attn_weights.hip", "plan_evict.hip"]
 
 # Packed-fp32 VALU forms are switched off for device code (scalar fp32 code generation only).  Matrix instructions keep
 # their results in the vector registers unless the source says otherwise: the persistent attention kernel fills the

@@ -1,0 +1,436 @@
+// Attention weight that every cache entry received, summed over queries and query heads, gfx950.
+//
+// weight[s][j] = decay weight[s][j] + sum_{t, h} exp(scale q[t][h] . K_j - lse[t][h]) over the queries t of stream s that see j.
+// A wave holds 64 keys (32 of an fp32 cache) as matrix operands in registers for the whole launch, so that a key is read and,
+// from a 4-bit cache, converted once; query rows pass through LDS in steps of 32.  With S = Q K^T a lane owns one key and 16
+// rows: weights add up in a register, in a fixed order, and no two lanes add to the same place.  Shares of a stream's rows and
+// kv heads leave partial sums that a last launch adds in order, so results are the same bits from run to run.
+// Without statistics from the caller the same kernel computes S^T = K Q^T first (operands swapped: a lane owns one query and
+// 16 keys), which gives a row's maximum and sum over the workgroup's keys in registers; a second launch joins the key ranges.
+// fp32 operands are sums of three bf16 numbers: three products for 4-bit keys (exact in bf16), six for fp32 keys.
+#include <math.h>
+
+#include <type_traits>
+
+#include "kv4.h"
+
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
+struct Params {
+  const void* __restrict__ q;
+  const float* __restrict__ lse;         // natural logarithms [n_q][n_q_heads]
+  const void* __restrict__ k;
+  const uint8_t* __restrict__ k_scales;
+  const int32_t* __restrict__ cu_q;
+  const int32_t* __restrict__ q_pos;
+  const int32_t* __restrict__ kv_len;
+  const int32_t* __restrict__ block_table;
+  const float* weight_in;
+  float* weight_out;
+  float* ws_lse;                         // [n_q][n_q_heads]
+  cs::f32v2* ws_stat;                    // [n_q][n_q_heads][key_tiles]: maximum (log2 units), sum
+  float* ws_part;                        // [chunks][n_kv_heads][n_streams][max_blocks * 16]
+  int64_t n_q, stride_slot, stride_head;
+  int32_t max_blocks, n_streams, n_q_heads, n_kv_heads, group, key_tiles, chunks;
+  float scale_log2e, decay;
+};
+
+constexpr int kStep = 32;                // query rows of a step
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+constexpr int keys_per_wave(int cache) { return cache == CS_F32 ? 32 : 64; }
+constexpr int keys_per_tile(int cache) { return 4 * keys_per_wave(cache); }
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  const cs::f32v2 v = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, cs::bf16v2));
+}
+
+// The next bf16 part of eight numbers, taken off them.
+__device__ __forceinline__ cs::u32x4 next_part(float* x) {
+  cs::u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    w[i] = pack2(x[2 * i], x[2 * i + 1]);
+    x[2 * i] -= __uint_as_float(w[i] << 16);
+    x[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
+  }
+  return w;
+}
+
+__device__ __forceinline__ void load8(const float* p, float* x) {
+  const cs::u32x4 a = *reinterpret_cast<const cs::u32x4*>(p), b = *reinterpret_cast<const cs::u32x4*>(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[i] = __uint_as_float(a[i]);
+    x[4 + i] = __uint_as_float(b[i]);
+  }
+}
+
+__device__ __forceinline__ int stream_entries(const Params& p, int s) { return min(p.kv_len[s], p.max_blocks * CS_KV_BLOCK); }
+
+template <int D, int CACHE, int QP, bool STATS>
+__global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
+  constexpr int STEPS = D / 16, KP = CACHE == CS_F32 ? 3 : 1, KB = keys_per_wave(CACHE) / 32;
+  constexpr int TILE = keys_per_tile(CACHE);
+  constexpr int QROW = D + 8;                              // padded LDS row
+  constexpr int CHUNKS = kStep * D / 8 / 256;              // 8-element pieces of a step's rows a thread moves (D 64: 1, D 128: 2)
+  __shared__ __attribute__((aligned(16))) uint16_t s_q[2][QP][kStep * QROW];
+  __shared__ __attribute__((aligned(16))) float s_lse[2][kStep];
+  __shared__ __attribute__((aligned(16))) int s_pos[2][kStep];
+  __shared__ float s_m[2][4][kStep], s_l[2][4][kStep];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, h = lane >> 5;
+  // ---- which keys, which rows
+  int job = blockIdx.x;
+  const int chunk = job % p.chunks;
+  job /= p.chunks;
+  const int kt = job % p.key_tiles;
+  job /= p.key_tiles;
+  const int kvh = job % p.n_kv_heads, stream = job / p.n_kv_heads;
+  const int entries = stream_entries(p, stream);
+  if (kt * TILE >= entries) return;
+  const int q0 = p.cu_q[stream];
+  const int rows = max(0, min(p.cu_q[stream + 1], static_cast<int>(p.n_q)) - q0) * p.group;
+  const int steps = (rows + kStep - 1) / kStep, share = (steps + p.chunks - 1) / p.chunks;
+  const int step_begin = chunk * share, step_end = min(steps, step_begin + share);
+  const int tile0 = kt * TILE, key0 = tile0 + wave * 32 * KB;
+
+  // ---- keys: operand layout, lane n is a key, 8 h + 0..7 its elements of a step
+  bf16x8 kf[KP][KB][STEPS];
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) {
+    const int key = min(key0 + 32 * kb + n, entries - 1);
+    const int64_t at = (static_cast<int64_t>(p.block_table[static_cast<int64_t>(stream) * p.max_blocks + key / CS_KV_BLOCK]) * CS_KV_BLOCK + key % CS_KV_BLOCK) * p.stride_slot +
+                       static_cast<int64_t>(kvh) * p.stride_head + 8 * h;
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) {
+      if (CACHE == CS_KV4) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(p.k) + (at + 16 * st) / 2);
+        const uint32_t e = p.k_scales[(at + 16 * st) / cs::kKv4Block];
+        cs::u32x4 x = cs::kv4_unpack8_bf16(w, cs::kv4_scale(e));
+        if (e == cs::kKv4NoNumber) x = cs::u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+        kf[0][kb][st] = __builtin_bit_cast(bf16x8, x);
+      } else if (CACHE == CS_BF16) {
+        kf[0][kb][st] = *reinterpret_cast<const bf16x8*>(static_cast<const uint16_t*>(p.k) + at + 16 * st);
+      } else {
+        float x[8];
+        load8(static_cast<const float*>(p.k) + at + 16 * st, x);
+#pragma unroll
+        for (int part = 0; part < KP; ++part) kf[part][kb][st] = __builtin_bit_cast(bf16x8, next_part(x));
+      }
+    }
+  }
+
+  // ---- query rows: asked for a step ahead
+  cs::u32x4 raw[CHUNKS][QP == 1 ? 1 : 2];
+  int next_pos = -1;
+  float next_lse = 0.0f;
+  auto request = [&](int step) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      const int c = tid + 256 * i, r = min(step * kStep + c / (D / 8), rows - 1);
+      const int64_t at = (static_cast<int64_t>(q0 + r / p.group) * p.n_q_heads + kvh * p.group + r % p.group) * D + 8 * (c % (D / 8));
+      if (QP == 1) {
+        raw[i][0] = *reinterpret_cast<const cs::u32x4*>(static_cast<const uint16_t*>(p.q) + at);
+      } else {
+        raw[i][0] = *reinterpret_cast<const cs::u32x4*>(static_cast<const float*>(p.q) + at);
+        raw[i][QP == 1 ? 0 : 1] = *reinterpret_cast<const cs::u32x4*>(static_cast<const float*>(p.q) + at + 4);
+      }
+    }
+    if (tid < kStep) {
+      const int r = step * kStep + tid;
+      next_pos = -1;                                       // rows past the last: see nothing
+      if (r < rows) {
+        const int tok = q0 + r / p.group;
+        next_pos = min(p.q_pos[tok], entries - 1);
+        if (!STATS) next_lse = p.lse[static_cast<int64_t>(tok) * p.n_q_heads + kvh * p.group + r % p.group] * kLog2e;
+      }
+    }
+  };
+  // (STATS) a step's maxima and sums of the four waves joined, left for the launch that joins key ranges
+  auto join = [&](int step, int buf) __attribute__((always_inline)) {
+    const int r = step * kStep + tid;
+    if (tid < kStep && r < rows) {
+      float m = s_m[buf][0][tid];
+#pragma unroll
+      for (int w = 1; w < 4; ++w) m = fmaxf(m, s_m[buf][w][tid]);
+      float l = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) l += m == -INFINITY ? s_l[buf][w][tid] : s_l[buf][w][tid] * __builtin_amdgcn_exp2f(s_m[buf][w][tid] - m);
+      p.ws_stat[(static_cast<int64_t>(q0 + r / p.group) * p.n_q_heads + kvh * p.group + r % p.group) * p.key_tiles + kt] = cs::f32v2{m, l};
+    }
+  };
+
+  float acc[KB] = {};
+  if (step_begin < step_end) request(step_begin);
+  for (int step = step_begin; step < step_end; ++step) {
+    const int buf = (step - step_begin) & 1;
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      const int c = tid + 256 * i, at = (c / (D / 8)) * QROW + 8 * (c % (D / 8));
+      if (QP == 1) {
+        *reinterpret_cast<cs::u32x4*>(&s_q[buf][0][at]) = raw[i][0];
+      } else {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[e] = __uint_as_float(raw[i][0][e]);
+          x[4 + e] = __uint_as_float(raw[i][QP == 1 ? 0 : 1][e]);
+        }
+#pragma unroll
+        for (int part = 0; part < QP; ++part) *reinterpret_cast<cs::u32x4*>(&s_q[buf][part][at]) = next_part(x);
+      }
+    }
+    if (tid < kStep) {
+      s_pos[buf][tid] = next_pos;
+      if (!STATS) s_lse[buf][tid] = next_lse;
+    }
+    if (step + 1 < step_end) request(step + 1);
+    __syncthreads();
+    if (STATS && step > step_begin) join(step - 1, buf ^ 1);
+
+    const int my_pos = s_pos[buf][n];
+    const bool sees = __any(my_pos >= key0);               // some row of the step sees a key of this wave
+    const bool masked = __any(my_pos < key0 + 32 * KB - 1);
+    if (sees) {
+      f32x16 s[KB] = {};
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) {
+        bf16x8 qf[QP];
+#pragma unroll
+        for (int part = 0; part < QP; ++part) qf[part] = *reinterpret_cast<const bf16x8*>(&s_q[buf][part][n * QROW + 16 * st + 8 * h]);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int a = 0; a < QP; ++a)
+#pragma unroll
+            for (int b = 0; b < KP; ++b)
+              if (a + b < 3)                               // (what the others add is below fp32's last bit)
+                s[kb] = STATS ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[b][kb][st], qf[a], s[kb], 0, 0, 0)
+                              : __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[a], kf[b][kb][st], s[kb], 0, 0, 0);
+      }
+      if (STATS) {
+        float m = -INFINITY, l = 0.0f;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            s[kb][r] *= p.scale_log2e;
+            if (masked && key0 + 32 * kb + 8 * (r / 4) + 4 * h + r % 4 > my_pos) s[kb][r] = -INFINITY;
+            m = fmaxf(m, s[kb][r]);
+          }
+        m = fmaxf(m, __shfl_xor(m, 32));
+        const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) l += __builtin_amdgcn_exp2f(s[kb][r] - base);
+        l += __shfl_xor(l, 32);
+        if (h == 0) {
+          s_m[buf][wave][n] = m;
+          s_l[buf][wave][n] = l;
+        }
+      } else {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          const int key = key0 + 32 * kb + n;
+          float sum = 0.0f;
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {                    // rows 8 g + 4 h + 0..3
+            const cs::u32x4 lse = *reinterpret_cast<const cs::u32x4*>(&s_lse[buf][8 * g + 4 * h]);
+            const cs::u32x4 pos = *reinterpret_cast<const cs::u32x4*>(&s_pos[buf][8 * g + 4 * h]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float w = __builtin_amdgcn_exp2f(fmaf(s[kb][4 * g + i], p.scale_log2e, -__uint_as_float(lse[i])));
+              if (masked && key > static_cast<int>(pos[i])) w = 0.0f;
+              sum += w;
+            }
+          }
+          acc[kb] += sum;
+        }
+      }
+    } else if (STATS && h == 0) {
+      s_m[buf][wave][n] = -INFINITY;
+      s_l[buf][wave][n] = 0.0f;
+    }
+  }
+  if (STATS) {
+    if (step_begin < step_end) {
+      __syncthreads();
+      join(step_end - 1, (step_end - 1 - step_begin) & 1);
+    }
+    return;
+  }
+  float* part = p.ws_part + ((static_cast<int64_t>(chunk) * p.n_kv_heads + kvh) * p.n_streams + stream) * (static_cast<int64_t>(p.max_blocks) * CS_KV_BLOCK);
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) {
+    const float both = acc[kb] + __shfl_xor(acc[kb], 32);
+    const int key = key0 + 32 * kb + n;
+    if (h == 0 && key < entries) part[key] = both;
+  }
+}
+
+// log-sum-exp of every query row from its key ranges' maxima and sums.
+__global__ __launch_bounds__(256) void attn_weights_join_kernel(Params p, int tile) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= p.n_q * p.n_q_heads) return;
+  const int tok = static_cast<int>(i / p.n_q_heads);
+  int lo = 0, hi = p.n_streams;                            // the last stream that starts at or before the token and is not empty
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (p.cu_q[mid] <= tok) lo = mid;
+    else hi = mid;
+  }
+  if (tok < p.cu_q[lo] || tok >= p.cu_q[lo + 1]) return;
+  const int pos = min(p.q_pos[tok], stream_entries(p, lo) - 1);
+  if (pos < 0) return;
+  float m = -INFINITY, l = 0.0f;
+  const cs::f32v2* part = p.ws_stat + i * p.key_tiles;
+  for (int kt = 0; kt <= pos / tile; ++kt) {
+    const float pm = part[kt].x, pl = part[kt].y, top = fmaxf(m, pm);
+    l = (m == -INFINITY ? 0.0f : l * __builtin_amdgcn_exp2f(m - top)) + (pm == -INFINITY ? pl : pl * __builtin_amdgcn_exp2f(pm - top));
+    m = top;
+  }
+  p.ws_lse[i] = ((m == -INFINITY ? 0.0f : m) + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// Partial sums of shares and kv heads, added in order to what earlier calls left.
+__global__ __launch_bounds__(256) void attn_weights_sum_kernel(Params p) {
+  const int64_t row = static_cast<int64_t>(p.max_blocks) * CS_KV_BLOCK, all = row * p.n_streams;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= all) return;
+  const int stream = static_cast<int>(i / row);
+  if (i - stream * row >= stream_entries(p, stream)) return;
+  float sum = 0.0f;
+  for (int c = 0; c < p.chunks * p.n_kv_heads; ++c) sum += p.ws_part[c * all + i];
+  if (p.weight_in && p.decay != 0.0f) sum = fmaf(p.decay, p.weight_in[i], sum);
+  p.weight_out[i] = sum;
+}
+
+struct Layout {
+  int key_tiles, chunks;
+  size_t lse, stat, part, total;
+};
+Layout layout(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads, int32_t max_blocks, int tile) {
+  Layout w;
+  const int64_t entries = static_cast<int64_t>(max_blocks) * CS_KV_BLOCK;
+  w.key_tiles = static_cast<int>((entries + tile - 1) / tile);
+  // Shares of a stream's rows: until about four workgroups a CU are under way, but at least four steps of rows each.
+  const int64_t jobs = static_cast<int64_t>(w.key_tiles) * n_streams * n_kv_heads;
+  const int64_t steps = (n_q * (n_q_heads / n_kv_heads) / (n_streams > 0 ? n_streams : 1) + kStep - 1) / kStep;
+  int64_t c = jobs > 0 ? 1024 / jobs : 1;
+  if (c > steps / 4) c = steps / 4;
+  w.chunks = static_cast<int>(c < 1 ? 1 : c);
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  w.lse = 0;
+  w.stat = up(static_cast<size_t>(n_q) * n_q_heads * 4);
+  w.part = w.stat + up(static_cast<size_t>(n_q) * n_q_heads * w.key_tiles * 8);
+  w.total = w.part + up(static_cast<size_t>(w.chunks) * n_kv_heads * n_streams * entries * 4);
+  return w;
+}
+
+template <int D, int CACHE, int QP>
+int launch(Params p, const Layout& w, bool have_lse, hipStream_t st) {
+  const int64_t jobs = static_cast<int64_t>(p.n_streams) * p.n_kv_heads * w.key_tiles * w.chunks;
+  if (jobs > 0x7fffffffll) return CS_EUNSUPPORTED;
+  const dim3 grid(static_cast<unsigned>(jobs));
+  const int64_t all = static_cast<int64_t>(p.max_blocks) * CS_KV_BLOCK * p.n_streams;
+  if (!have_lse) {
+    hipLaunchKernelGGL((attn_weights_kernel<D, CACHE, QP, true>), grid, dim3(256), 0, st, p);
+    hipLaunchKernelGGL(attn_weights_join_kernel, dim3(static_cast<unsigned>((p.n_q * p.n_q_heads + 255) / 256)), dim3(256), 0, st, p, keys_per_tile(CACHE));
+    p.lse = p.ws_lse;
+  }
+  hipLaunchKernelGGL((attn_weights_kernel<D, CACHE, QP, false>), grid, dim3(256), 0, st, p);
+  hipLaunchKernelGGL(attn_weights_sum_kernel, dim3(static_cast<unsigned>((all + 255) / 256)), dim3(256), 0, st, p);
+  return cs::note_hip(hipGetLastError());
+}
+
+}  // namespace
+
+// (sized for the smaller tiles of an fp32 cache, whatever the cache)
+extern "C" size_t cs_attn_weights_workspace(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_blocks) {
+  (void)head_dim;
+  if (n_q < 1 || n_streams < 1 || n_q_heads < 1 || n_kv_heads < 1 || max_blocks < 1) return 0;
+  const Layout a = layout(n_q, n_streams, n_q_heads, n_kv_heads, max_blocks, keys_per_tile(CS_F32));
+  const Layout b = layout(n_q, n_streams, n_q_heads, n_kv_heads, max_blocks, keys_per_tile(CS_BF16));
+  return a.total > b.total ? a.total : b.total;
+}
+
+extern "C" int cs_attn_weights(const void* q, const float* lse, const void* k_cache_layer, const uint8_t* k_scales_layer, const int32_t* cu_q,
+                               const int32_t* q_pos, const int32_t* kv_len, const int32_t* block_table, int32_t max_blocks, int32_t block_size,
+                               const float* weight_in, float* weight_out, float decay, int64_t n_q, int32_t n_streams, int32_t n_q_heads,
+                               int32_t n_kv_heads, int32_t head_dim, int64_t stride_slot, int64_t stride_head, float softmax_scale, int32_t dtype,
+                               int32_t cache_dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  if (n_q < 0 || n_streams < 0 || n_q_heads < 1 || n_kv_heads < 1 || head_dim < 1 || max_blocks < 0 || stride_slot < 0 || stride_head < 0)
+    return CS_EINVAL;
+  if (n_q_heads % n_kv_heads) return CS_EINVAL;
+  if (!(softmax_scale > 0.0f && softmax_scale <= 3.0e38f) || !(decay >= 0.0f && decay <= 1.0f)) return CS_EINVAL;
+  if (dtype != CS_F32 && dtype != CS_BF16) return CS_EUNSUPPORTED;
+  if (cache_dtype != CS_KV4 && cache_dtype != dtype) return CS_EUNSUPPORTED;
+  if ((head_dim != 64 && head_dim != 128) || block_size != CS_KV_BLOCK || n_q_heads / n_kv_heads > 16) return CS_EUNSUPPORTED;
+  const int unit = cache_dtype == CS_KV4 ? cs::kKv4Block : cache_dtype == CS_BF16 ? 8 : 4;
+  if (stride_slot % unit || stride_head % unit) return CS_EUNSUPPORTED;
+  if (n_q > 0x7fffffffll / n_q_heads || max_blocks > 0x7fffffff / CS_KV_BLOCK) return CS_EUNSUPPORTED;
+  if (static_cast<int64_t>(max_blocks) * CS_KV_BLOCK * n_streams > 0x7fffffffll * 255) return CS_EUNSUPPORTED;
+  if (n_streams == 0) return CS_OK;
+  if (!kv_len || !weight_out || max_blocks < 1) return CS_EINVAL;
+  if (n_q == 0) {                        // earlier weights fade
+    Params p = {};
+    p.kv_len = kv_len;
+    p.weight_in = weight_in;
+    p.weight_out = weight_out;
+    p.max_blocks = max_blocks;
+    p.n_streams = n_streams;
+    p.decay = decay;
+    const int64_t all = static_cast<int64_t>(max_blocks) * CS_KV_BLOCK * n_streams;
+    hipLaunchKernelGGL(attn_weights_sum_kernel, dim3(static_cast<unsigned>((all + 255) / 256)), dim3(256), 0, cs::as_stream(stream), p);
+    return cs::note_hip(hipGetLastError());
+  }
+  if (!q || !k_cache_layer || !cu_q || !q_pos || !block_table) return CS_EINVAL;
+  if (cache_dtype == CS_KV4 && !k_scales_layer) return CS_EINVAL;
+  if (!cs::aligned16(q) || !cs::aligned16(k_cache_layer)) return CS_EUNSUPPORTED;
+  const size_t need = cs_attn_weights_workspace(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, max_blocks);
+  if (!workspace || workspace_bytes < need || !cs::aligned16(workspace)) return CS_EWORKSPACE;
+
+  const Layout w = layout(n_q, n_streams, n_q_heads, n_kv_heads, max_blocks, keys_per_tile(cache_dtype));
+  Params p;
+  p.q = q;
+  p.lse = lse;
+  p.k = k_cache_layer;
+  p.k_scales = k_scales_layer;
+  p.cu_q = cu_q;
+  p.q_pos = q_pos;
+  p.kv_len = kv_len;
+  p.block_table = block_table;
+  p.weight_in = weight_in;
+  p.weight_out = weight_out;
+  p.ws_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + w.lse);
+  p.ws_stat = reinterpret_cast<cs::f32v2*>(static_cast<char*>(workspace) + w.stat);
+  p.ws_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + w.part);
+  p.n_q = n_q;
+  p.stride_slot = stride_slot;
+  p.stride_head = stride_head;
+  p.max_blocks = max_blocks;
+  p.n_streams = n_streams;
+  p.n_q_heads = n_q_heads;
+  p.n_kv_heads = n_kv_heads;
+  p.group = n_q_heads / n_kv_heads;
+  p.key_tiles = w.key_tiles;
+  p.chunks = w.chunks;
+  p.scale_log2e = softmax_scale * kLog2e;
+  p.decay = decay;
+  hipStream_t st = cs::as_stream(stream);
+  const bool have = lse != nullptr;
+  if (head_dim == 128) {
+    if (cache_dtype == CS_F32) return launch<128, CS_F32, 3>(p, w, have, st);
+    if (cache_dtype == CS_BF16) return launch<128, CS_BF16, 1>(p, w, have, st);
+    return dtype == CS_BF16 ? launch<128, CS_KV4, 1>(p, w, have, st) : launch<128, CS_KV4, 3>(p, w, have, st);
+  }
+  if (cache_dtype == CS_F32) return launch<64, CS_F32, 3>(p, w, have, st);
+  if (cache_dtype == CS_BF16) return launch<64, CS_BF16, 1>(p, w, have, st);
+  return dtype == CS_BF16 ? launch<64, CS_KV4, 1>(p, w, have, st) : launch<64, CS_KV4, 3>(p, w, have, st);
+}
