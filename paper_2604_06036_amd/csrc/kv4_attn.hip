@@ -42,17 +42,17 @@ struct Params {
   const int32_t* __restrict__ block_table;
   void* __restrict__ out;
   float* __restrict__ lse;
-  float* __restrict__ ws_ml;             // [jobs][rows][2]: reference maximum (raw score), sum; jobs are (kv head, row tile, piece)
+  float* __restrict__ ws_ml;             // [jobs][rows][2]: reference maximum (raw score), sum; jobs are (row tile, piece, kv head)
   float* __restrict__ ws_o;              // [jobs][rows][D]: sums, not divided
   int64_t n_q, stride_slot, stride_head;
   int32_t max_blocks, n_streams, n_q_heads, n_kv_heads, group;
-  int32_t row_tiles, pieces, jobs, jobs_per_xcd;
+  int32_t pieces;
   float scale_log2e;
 };
 
 constexpr int kKeys = 64;                // entries of a tile
 constexpr int kRowsMany = 128;           // rows of a workgroup of the rows kernel
-constexpr int kRowsFew = 32;             // ... of the keys kernel
+constexpr int kRowsFew = 16;             // ... of the keys kernel
 constexpr float kSlack = 8.0f;           // log2 of how far weights may exceed the reference maximum's
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -66,9 +66,61 @@ __device__ __forceinline__ float other_half(float x) {     // the value of lane 
   return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
 }
 
-// The stream and row tile of the `target`-th row tile of the launch.  Every wave scans the streams for itself.
+__device__ __forceinline__ float other_quarter(float x) {  // the value of lane ^ 16
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 16) ? r[0] : r[1]);
+}
+
+// Eight numbers as sums of PARTS bf16 numbers, the first being the rounded ones.
+template <int PARTS>
+__device__ __forceinline__ void split8(float (&x)[8], bf16x8 (&part)[PARTS]) {
+#pragma unroll
+  for (int k = 0; k < PARTS; ++k) {
+    cs::u32x4 c;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      c[e] = pack2(x[2 * e], x[2 * e + 1]);
+      if (k + 1 < PARTS) {
+        x[2 * e] -= __uint_as_float(c[e] << 16);
+        x[2 * e + 1] -= __uint_as_float(c[e] & 0xffff0000u);
+      }
+    }
+    part[k] = __builtin_bit_cast(bf16x8, c);
+  }
+}
+
+// Eight elements of a query: bf16 (PARTS 1) or fp32.
+template <int PARTS>
+__device__ __forceinline__ void load_parts(const void* q, int64_t at, bf16x8 (&part)[PARTS]) {
+  if constexpr (PARTS == 1) {
+    part[0] = *reinterpret_cast<const bf16x8*>(static_cast<const uint16_t*>(q) + at);
+  } else {
+    const float* src = static_cast<const float*>(q) + at;
+    const cs::u32x4 a = *reinterpret_cast<const cs::u32x4*>(src), b = *reinterpret_cast<const cs::u32x4*>(src + 4);
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[e] = __uint_as_float(a[e]);
+      x[4 + e] = __uint_as_float(b[e]);
+    }
+    split8<PARTS>(x, part);
+  }
+}
+
+// Codes of EL elements of a row: a 32-element block, or half of one.
+template <int EL>
+struct Codes {
+  typedef typename std::conditional<EL == 32, cs::u32x4, cs::u32x2>::type V;
+  V v;
+  __device__ __forceinline__ void load(const uint8_t* base, uint32_t off) { v = *reinterpret_cast<const V*>(base + off); }
+  __device__ __forceinline__ uint32_t word(int w) const { return v[w]; }
+};
+
+// The stream and row tile of place `target` in the launch's order.  Up to 64 streams: every stream's last row tile, then every
+// stream's last but one, and so on, so that the longest sweeps start first and the launch ends on short ones; more: stream
+// by stream.  Every wave scans the streams for itself.
 struct Tile {
-  int stream, index, n_tiles, q0, rows;      // rows: of the whole stream
+  int stream, row0, q0, rows;            // first row of the tile in the stream's rows; rows of the whole stream
 };
 template <int ROWS>
 __device__ __forceinline__ bool find_tile(const Params& p, int target, Tile* t) {
@@ -82,42 +134,56 @@ __device__ __forceinline__ bool find_tile(const Params& p, int target, Tile* t) 
       n = max(0, min(p.cu_q[s + 1], static_cast<int>(p.n_q)) - a);
     }
     const int tiles = (n * p.group + ROWS - 1) / ROWS;
-    int incl = tiles;
+    int l, from_end;                     // the lane of the stream, the tile's distance from the stream's last one
+    if (p.n_streams <= 64) {
+      uint64_t live = __ballot(tiles > 0);
+      int rank = 0, left = target;
+      while (left >= __popcll(live)) {
+        if (live == 0) return false;
+        left -= __popcll(live);
+        live = __ballot(tiles > ++rank);
+      }
+      const bool mine = (live >> lane & 1) && __popcll(live & ((1ull << lane) - 1)) == left;
+      l = __ffsll(static_cast<unsigned long long>(__ballot(mine))) - 1;
+      from_end = rank;
+    } else {
+      int incl = tiles;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int up = __shfl_up(incl, d);
-      if (lane >= d) incl += up;
+      for (int d = 1; d < 64; d <<= 1) {
+        const int up = __shfl_up(incl, d);
+        if (lane >= d) incl += up;
+      }
+      const int total = __builtin_amdgcn_readlane(incl, 63);
+      if (target >= before + total) {
+        before += total;
+        continue;
+      }
+      l = __ffsll(static_cast<unsigned long long>(__ballot(before + incl > target))) - 1;
+      from_end = target - (before + __builtin_amdgcn_readlane(incl - tiles, __builtin_amdgcn_readfirstlane(l)));
     }
-    const int total = __builtin_amdgcn_readlane(incl, 63);
-    if (target < before + total) {
-      const uint64_t past = __ballot(before + incl > target);
-      const int l = __builtin_amdgcn_readfirstlane(__ffsll(static_cast<unsigned long long>(past)) - 1);
-      t->stream = s0 + l;
-      t->n_tiles = __builtin_amdgcn_readlane(tiles, l);
-      t->index = target - (before + __builtin_amdgcn_readlane(incl, l) - t->n_tiles);
-      t->q0 = __builtin_amdgcn_readlane(a, l);
-      t->rows = __builtin_amdgcn_readlane(n, l) * p.group;
-      return true;
-    }
-    before += total;
+    l = __builtin_amdgcn_readfirstlane(l);
+    t->stream = s0 + l;
+    t->row0 = (__builtin_amdgcn_readlane(tiles, l) - 1 - __builtin_amdgcn_readfirstlane(from_end)) * ROWS;
+    t->q0 = __builtin_amdgcn_readlane(a, l);
+    t->rows = __builtin_amdgcn_readlane(n, l) * p.group;
+    return true;
   }
   return false;
 }
 
-// Workgroup -> (kv head, row tile, piece).  Workgroups go round the eight XCDs, so an XCD is given a run of neighbouring
-// jobs: row tiles of the same stream and kv head meet in its L2.
+// Workgroup -> (row tile, piece, kv head), the kv head changing fastest: workgroups go round the eight XCDs, so that with four or
+// eight kv heads an XCD's L2 serves one of them.
 struct Job {
   int kvh, tile, piece, index;
 };
-__device__ __forceinline__ bool job_of(const Params& p, Job* j) {
-  const int i = static_cast<int>(blockIdx.x % 8) * p.jobs_per_xcd + static_cast<int>(blockIdx.x / 8);
-  if (static_cast<int>(blockIdx.x / 8) >= p.jobs_per_xcd || i >= p.jobs) return false;
-  j->index = i;
-  j->piece = i % p.pieces;
-  const int kt = i / p.pieces;
-  j->tile = kt % p.row_tiles;
-  j->kvh = kt / p.row_tiles;
-  return true;
+__device__ __forceinline__ Job job_of(const Params& p) {
+  Job j;
+  j.index = static_cast<int>(blockIdx.x);
+  j.kvh = j.index % p.n_kv_heads;
+  const int i = j.index / p.n_kv_heads;
+  j.piece = i % p.pieces;
+  j.tile = i / p.pieces;
+  return j;
 }
 
 // ---- a lane's query: PARTS bf16 numbers an element (1: bf16 queries, 3: fp32), elements 64 i + 32 h + 8 w + 0..7 of its row in operand
@@ -131,30 +197,10 @@ struct Query {
     for (int i = 0; i < D / 64; ++i)
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const int64_t from = at + 64 * i + 32 * h + 8 * w;
-        if (PARTS == 1) {
-          part[0][i][w] = *reinterpret_cast<const bf16x8*>(static_cast<const uint16_t*>(q) + from);
-          continue;
-        }
-        const float* src = static_cast<const float*>(q) + from;
-        const cs::u32x4 a = *reinterpret_cast<const cs::u32x4*>(src), b = *reinterpret_cast<const cs::u32x4*>(src + 4);
-        float x[8];
+        bf16x8 parts[PARTS];
+        load_parts<PARTS>(q, at + 64 * i + 32 * h + 8 * w, parts);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[e] = __uint_as_float(a[e]);
-          x[4 + e] = __uint_as_float(b[e]);
-        }
-#pragma unroll
-        for (int k = 0; k < PARTS; ++k) {
-          cs::u32x4 c;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            c[e] = pack2(x[2 * e], x[2 * e + 1]);
-            x[2 * e] -= __uint_as_float(c[e] << 16);
-            x[2 * e + 1] -= __uint_as_float(c[e] & 0xffff0000u);
-          }
-          part[k][i][w] = __builtin_bit_cast(bf16x8, c);
-        }
+        for (int k = 0; k < PARTS; ++k) part[k][i][w] = parts[k];
       }
   }
 
@@ -172,19 +218,6 @@ struct Query {
       for (int w = 0; w < 4; ++w) step(s, *reinterpret_cast<const bf16x8*>(keys + 64 * i + 32 * h + 8 * w), i, w);
     return s;
   }
-
-  // ... of codes in registers: blocks 2 i + h of the lane's key, their scales in bytes 0 and 2 of `scales`
-  __device__ __forceinline__ f32x16 scores(const cs::u32x4 (&codes)[D / 64], uint32_t scales) const {
-    f32x16 s = {};
-#pragma unroll
-    for (int i = 0; i < D / 64; ++i) {
-      const uint32_t e = (scales >> (16 * i)) & 255u;
-      const float sc = cs::kv4_scale(e == cs::kKv4NoNumber ? 1u : e);
-#pragma unroll
-      for (int w = 0; w < 4; ++w) step(s, __builtin_bit_cast(bf16x8, cs::kv4_unpack8_bf16(codes[i][w], sc)), i, w);
-    }
-    return s;
-  }
 };
 
 // ---- running softmax and sums of a lane's query over half tiles of 32 keys
@@ -193,12 +226,14 @@ struct Sums {
   static constexpr int DB = D / 32;
   f32x16 o[DB];
   float m, l;                            // reference maximum (raw score), the lane's share of the sum
+  uint32_t bad;                          // 32-column parts of the sums that a value without numbers has reached
 
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int db = 0; db < DB; ++db) o[db] = f32x16{};
     m = -INFINITY;
     l = 0.0f;
+    bad = 0;
   }
 
   // Weights of the scores of keys key0 + 8 (r / 4) + 4 h + r % 4 for a query that sees up to `pos`.
@@ -232,19 +267,10 @@ struct Sums {
         x[i] = __builtin_amdgcn_exp2f(fmaf(s[8 * st + i], c, base));
         sum += x[i];
       }
+      bf16x8 parts[PARTS];
+      split8<PARTS>(x, parts);
 #pragma unroll
-      for (int k = 0; k < PARTS; ++k) {
-        cs::u32x4 w;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          w[i] = pack2(x[2 * i], x[2 * i + 1]);
-          if (PARTS > 1) {
-            x[2 * i] -= __uint_as_float(w[i] << 16);
-            x[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
-          }
-        }
-        pf[k][st] = __builtin_bit_cast(bf16x8, w);
-      }
+      for (int k = 0; k < PARTS; ++k) pf[k][st] = parts[k];
     }
     l += sum;
   }
@@ -268,40 +294,49 @@ struct Sums {
       }
   }
 
-  // A value block without numbers (its place in LDS holds zeros) reaches the queries that see its key.
-  __device__ __forceinline__ void poison(int db, bool sees) {
+  // A value block without numbers (its place in LDS holds zeros) reaches the queries that see its key: noted, and put into
+  // the sums at the end.
+  __device__ __forceinline__ void poison(int db, bool sees) { bad |= sees ? 1u << db : 0u; }
+
+  __device__ __forceinline__ void finish() {
+    l += other_half(l);
+    if (__builtin_expect(__any(bad != 0), 0)) {
 #pragma unroll
-    for (int b = 0; b < DB; ++b)
-      if (b == db && sees) {
+      for (int db = 0; db < DB; ++db)
+        if (bad >> db & 1) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[b][r] = NAN;
-      }
+          for (int r = 0; r < 16; ++r) o[db][r] = NAN;
+        }
+    }
   }
 };
 
-// A block of 32 values -> bf16 in LDS; zeros for a block without numbers, which is reported.
-__device__ __forceinline__ bool put_values(uint16_t* dst, const cs::u32x4& code, uint32_t scale) {
+// A block of 32 elements -> bf16 in LDS.  A block without numbers becomes NaN (keys) or zeros (values, which must not meet a weight of
+// 0; it is reported).  KIND 0: keys, rows 16 bytes past a multiple of the banks' width.  Values: 1: rows 64 bytes past one, 2: 32
+// bytes; there blocks of neighbouring rows share banks, and lanes of different rows write a block's four pieces in
+// different orders (by two bits of `row`, or the second one).
+template <int KIND>
+__device__ __forceinline__ bool put_block(uint16_t* dst, const cs::u32x4& code, uint32_t scale, int row) {
   const bool none = scale == cs::kKv4NoNumber;
   const float sc = cs::kv4_scale(none ? 1u : scale);
+  cs::u32x4 c = code;
+  const int turn = KIND == 1 ? row & 3 : KIND == 2 ? (row >> 1) & 1 : 0;       // c[w] = code[w ^ turn]
+  if (KIND != 0) {
+    const bool odd = turn & 1;
+    c = cs::u32x4{odd ? c.y : c.x, odd ? c.x : c.y, odd ? c.w : c.z, odd ? c.z : c.w};
+  }
+  if (KIND == 1) {
+    const bool high = turn & 2;
+    c = cs::u32x4{high ? c.z : c.x, high ? c.w : c.y, high ? c.x : c.z, high ? c.y : c.w};
+  }
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    cs::u32x4 x = cs::kv4_unpack8_bf16(code[w], sc);
-    if (none) x = cs::u32x4{0, 0, 0, 0};
-    *reinterpret_cast<cs::u32x4*>(dst + 8 * w) = x;
+  for (int w = 0; w < 4; ++w) *reinterpret_cast<cs::u32x4*>(dst + 8 * (w ^ turn)) = cs::kv4_unpack8_bf16(c[w], sc);
+  if (__builtin_expect(none, 0)) {
+    const uint32_t x = KIND != 0 ? 0u : 0x7fc07fc0u;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) *reinterpret_cast<cs::u32x4*>(dst + 8 * w) = cs::u32x4{x, x, x, x};
   }
   return none;
-}
-
-// A block of 32 keys' elements -> bf16 in LDS; NaN for a block without numbers.
-__device__ __forceinline__ void put_keys(uint16_t* dst, const cs::u32x4& code, uint32_t scale) {
-  const bool none = scale == cs::kKv4NoNumber;
-  const float sc = cs::kv4_scale(none ? 1u : scale);
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    cs::u32x4 x = cs::kv4_unpack8_bf16(code[w], sc);
-    if (none) x = cs::u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
-    *reinterpret_cast<cs::u32x4*>(dst + 8 * w) = x;
-  }
 }
 
 __device__ __forceinline__ void store4(void* out, int64_t at, const float* x, bool bf16) {
@@ -314,42 +349,32 @@ __device__ __forceinline__ void store4(void* out, int64_t at, const float* x, bo
 
 __device__ __forceinline__ float log_sum(float m, float l, float c) { return l == 0.0f ? -INFINITY : (m * c + __builtin_amdgcn_logf(l)) * kLn2; }
 
-// Scale bytes of a cache row, from element `at` on (any alignment): block 2 i + h of the row in byte 2 i.
-template <int D>
-__device__ __forceinline__ uint32_t row_scales(const uint8_t* scales, int64_t at, int h) {
-  if (D == 128) {
-    uint32_t w;
-    __builtin_memcpy(&w, scales + at / cs::kKv4Block, 4);
-    return w >> (8 * h);
-  }
-  return scales[at / cs::kKv4Block + h];
-}
-
 // ------------------------------------------------------------------------------------------
-// Many rows: four waves of 32 rows share the tiles of a sweep.  Codes are asked for a tile ahead into registers (16 bytes a
-// lane: one block) and put into LDS as bf16, in two stages, so that a tile costs one barrier.
+// Many rows: four waves of 32 rows share the tiles of a sweep, 32 keys (head_dim 64: 64).  A thread moves one block of 32 elements a
+// tile, the first two waves keys, the others values: asked for a tile ahead into registers, put into LDS as bf16, in two
+// stages, so that a tile costs one barrier.
 template <int D, int PARTS>
-__global__ __launch_bounds__(256) void kv4_rows_kernel(Params p) {
+__global__ __launch_bounds__(256, PARTS == 1 ? 3 : D == 64 ? 2 : 1) void kv4_rows_kernel(Params p) {
   constexpr int DB = D / 32;
+  constexpr int T = 128 / DB;                              // keys of a tile
   constexpr int KROW = D + 8, VROW = D + 32;               // padded: reads of eight rows, and the transposing ones, meet no bank twice
-  constexpr int CHUNKS = kKeys * DB, MINE = 2 * CHUNKS / 256;      // blocks of a tile's keys (or values), blocks a thread moves
-  __shared__ __attribute__((aligned(16))) uint16_t s_k[2][kKeys * KROW];
-  __shared__ __attribute__((aligned(16))) uint16_t s_v[2][kKeys * VROW];
-  __shared__ uint8_t s_vs[2][CHUNKS];
+  __shared__ __attribute__((aligned(16))) uint16_t s_k[2][T * KROW];
+  __shared__ __attribute__((aligned(16))) uint16_t s_v[2][T * VROW];
+  __shared__ uint8_t s_vs[2][128];
   __shared__ int s_last[4];
   __shared__ int s_nan;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
-  Job job;
+  const Job job = job_of(p);
   Tile t;
-  if (!job_of(p, &job) || !find_tile<kRowsMany>(p, job.tile, &t)) return;
+  if (!find_tile<kRowsMany>(p, job.tile, &t)) return;
   const int kvh = job.kvh;
   const int entries = min(p.kv_len[t.stream], p.max_blocks * CS_KV_BLOCK);
   if (entries <= 0) return;
   if (tid == 0) s_nan = 0;
 
   // ---- this lane's query
-  const int row0 = (t.n_tiles - 1 - t.index) * kRowsMany + wave * 32;     // the longest sweeps first
+  const int row0 = t.row0 + wave * 32;
   const int row = min(row0 + n, t.rows - 1);
   const int tok = t.q0 + row / p.group, head = kvh * p.group + row % p.group;
   const bool live = row0 + n < t.rows;
@@ -369,44 +394,43 @@ __global__ __launch_bounds__(256) void kv4_rows_kernel(Params p) {
   wave_first = __builtin_amdgcn_readfirstlane(wave_first);
   if (lane == 0) s_last[wave] = wave_last;
   __syncthreads();
-  const int last = max(max(s_last[0], s_last[1]), max(s_last[2], s_last[3]));
-  const int all_tiles = (last + kKeys) / kKeys;            // (no entry seen: last -1, no tile)
+  const int last = __builtin_amdgcn_readfirstlane(max(max(s_last[0], s_last[1]), max(s_last[2], s_last[3])));
+  const int all_tiles = (last + T) / T;                    // (no entry seen: last -1, no tile)
   const int share = (all_tiles + p.pieces - 1) / p.pieces;
   const int kt0 = min(all_tiles, job.piece * share), kt1 = min(all_tiles, kt0 + share);
 
   // ---- tile requests
   const int32_t* ids = p.block_table + static_cast<int64_t>(t.stream) * p.max_blocks;
-  cs::u32x4 code[MINE];
-  uint32_t scale[MINE];
-  int id[MINE];
-  auto key_of = [&](int kt, int i) __attribute__((always_inline)) {        // past the frontier: the frontier's row (what lies there may be nothing)
-    const int c = tid + 256 * i;
-    return min(kt * kKeys + (c >= CHUNKS ? c - CHUNKS : c) / DB, last);
-  };
-  auto request_id = [&](int kt) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < MINE; ++i) id[i] = ids[key_of(kt, i) / CS_KV_BLOCK];
-  };
+  const bool of_v = wave >= 2;
+  const uint8_t* codes = of_v ? p.v_codes : p.k_codes;
+  const uint8_t* scales = of_v ? p.v_scales : p.k_scales;
+  const int my_row = (tid & 127) / DB, my_block = tid % DB;
+  // (a thread's place in cache block 0, in the frontier's row of it, and what a block adds: stride_slot < 2^26)
+  const int64_t head_at = static_cast<int64_t>(kvh) * p.stride_head + my_block * cs::kKv4Block;
+  const int64_t at_row = static_cast<int64_t>(my_row % CS_KV_BLOCK) * p.stride_slot + head_at;
+  const int64_t at_last = static_cast<int64_t>(max(last, 0) % CS_KV_BLOCK) * p.stride_slot + head_at;
+  const uint32_t code_step = static_cast<uint32_t>(p.stride_slot * CS_KV_BLOCK / 2), scale_step = static_cast<uint32_t>(p.stride_slot / 2);
+  const uint8_t* const my_code = codes + at_row / 2;
+  const uint8_t* const my_scale = scales + at_row / cs::kKv4Block;
+  cs::u32x4 code;
+  uint32_t scale, id;
+  // rows past the frontier are the frontier's row (what lies there may be nothing)
+  auto request_id = [&](int kt) __attribute__((always_inline)) { id = static_cast<uint32_t>(ids[min(kt * T + my_row, last) / CS_KV_BLOCK]); };
   auto request = [&](int kt) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < MINE; ++i) {
-      const int c = tid + 256 * i, of_v = c >= CHUNKS;
-      const int64_t at = (static_cast<int64_t>(id[i]) * CS_KV_BLOCK + key_of(kt, i) % CS_KV_BLOCK) * p.stride_slot +
-                         static_cast<int64_t>(kvh) * p.stride_head + (c % DB) * cs::kKv4Block;
-      code[i] = *reinterpret_cast<const cs::u32x4*>((of_v ? p.v_codes : p.k_codes) + at / 2);
-      scale[i] = (of_v ? p.v_scales : p.k_scales)[at / cs::kKv4Block];
+    const uint8_t *c = my_code, *s = my_scale;
+    if (kt * T + T - 1 > last && kt * T + my_row > last) {
+      c = codes + at_last / 2;
+      s = scales + at_last / cs::kKv4Block;
     }
+    code = *reinterpret_cast<const cs::u32x4*>(c + static_cast<uint64_t>(id) * code_step);
+    scale = s[static_cast<uint64_t>(id) * scale_step];
   };
   auto put = [&](int buf) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < MINE; ++i) {
-      const int c = tid + 256 * i, of_v = c >= CHUNKS, cc = c - (of_v ? CHUNKS : 0), r = cc / DB, b = cc % DB;
-      if (of_v) {
-        if (put_values(&s_v[buf][r * VROW + 32 * b], code[i], scale[i])) s_nan = 1;
-        s_vs[buf][cc] = static_cast<uint8_t>(scale[i]);
-      } else {
-        put_keys(&s_k[buf][r * KROW + 32 * b], code[i], scale[i]);
-      }
+    if (of_v) {
+      if (put_block<1>(&s_v[buf][my_row * VROW + 32 * my_block], code, scale, my_row)) s_nan = 1;
+      s_vs[buf][tid & 127] = static_cast<uint8_t>(scale);
+    } else {
+      put_block<0>(&s_k[buf][my_row * KROW + 32 * my_block], code, scale, my_row);
     }
   };
 
@@ -423,22 +447,17 @@ __global__ __launch_bounds__(256) void kv4_rows_kernel(Params p) {
   }
   for (int kt = kt0; kt < kt1; ++kt) {
     const int buf = (kt - kt0) & 1;
-    const int key0 = kt * kKeys;
-    if (key0 <= wave_last) {
-      const bool two = key0 + 32 <= wave_last;             // (the second half's scores beside the first half's softmax)
-      f32x16 s0 = query.scores(&s_k[buf][n * KROW], h), s1;
-      if (two) s1 = query.scores(&s_k[buf][(32 + n) * KROW], h);
+#pragma unroll
+    for (int kb = 0; kb < T / 32; ++kb) {
+      const int key0 = kt * T + 32 * kb;
+      if (key0 > wave_last) continue;
       bf16x8 pf[PARTS][2];
-      sums.weights(s0, key0, pos, key0 + 31 > wave_first, h, p.scale_log2e, pf);
-      sums.template add<VROW>(&s_v[buf][0], pf, lane);
-      if (two) {
-        sums.weights(s1, key0 + 32, pos, key0 + 63 > wave_first, h, p.scale_log2e, pf);
-        sums.template add<VROW>(&s_v[buf][32 * VROW], pf, lane);
-      }
+      sums.weights(query.scores(&s_k[buf][(32 * kb + n) * KROW], h), key0, pos, key0 + 31 > wave_first, h, p.scale_log2e, pf);
+      sums.template add<VROW>(&s_v[buf][32 * kb * VROW], pf, lane);
     }
     if (s_nan) {                                           // (a tile so far held a value block without numbers)
-      for (int c = 0; c < CHUNKS; ++c)
-        if (s_vs[buf][c] == cs::kKv4NoNumber) sums.poison(c % DB, kt * kKeys + c / DB <= pos);
+      for (int c = 0; c < 128; ++c)
+        if (s_vs[buf][c] == cs::kKv4NoNumber) sums.poison(c % DB, kt * T + c / DB <= pos);
     }
     if (kt + 1 < kt1) put(buf ^ 1);
     if (kt + 2 < kt1) request(kt + 2);
@@ -447,7 +466,7 @@ __global__ __launch_bounds__(256) void kv4_rows_kernel(Params p) {
   }
 
   // ---- results
-  sums.l += other_half(sums.l);
+  sums.finish();
   if (p.pieces > 1) {                                      // the row tile's other pieces are joined to it by a launch of its own
     const int64_t r = static_cast<int64_t>(job.index) * kRowsMany + wave * 32 + n;
     if (h == 0) *reinterpret_cast<cs::f32v2*>(p.ws_ml + 2 * r) = cs::f32v2{sums.m, sums.l};
@@ -474,35 +493,48 @@ __global__ __launch_bounds__(256) void kv4_rows_kernel(Params p) {
 }
 
 // ------------------------------------------------------------------------------------------
-// Few rows: WAVES waves hold the same 32 rows and take every WAVES-th tile of the sweep, each for itself: a wave's keys go
+// Few rows: WAVES waves hold the same 16 rows and take every WAVES-th tile of the sweep, each for itself: a wave's keys go
 // from memory into operand registers, its values through its own 32 rows of LDS.  No barrier before the end.
+// v_mfma_f32_16x16x32_bf16: lane l is query l % 16; of a 16-key cache block it holds, as an operand, key l % 16 and a quarter of
+// its elements (head_dim 128: one 32-element block, so that a wave reads a cache block in one load), and of the scores keys
+// 4 (l / 16) + 0..3.
 template <int D, int PARTS, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, D == 128 && PARTS == 3 ? 1 : 2) void kv4_keys_kernel(Params p) {
-  constexpr int DB = D / 32, KI = D / 64;
-  constexpr int VROW = D + 32;
-  constexpr int VC = kKeys * DB / 64;                      // value blocks of a tile that a lane moves (an even number)
-  constexpr int OROW = 64 + 4;                             // padded rows of the join, 64 columns at a time
-  constexpr int V_BYTES = WAVES * 32 * VROW * 2, O_BYTES = WAVES * 32 * OROW * 4;
-  __shared__ __attribute__((aligned(16))) uint8_t s_mem[V_BYTES > O_BYTES ? V_BYTES : O_BYTES];
-  __shared__ float s_m[WAVES][32], s_l[WAVES][32], s_sum[32];
+__global__ __launch_bounds__(64 * WAVES, PARTS == 1 ? 3 : 2) void kv4_keys_kernel(Params p) {
+  constexpr int DB = D / 32, EL = D / 4, SW = EL / 8;      // blocks of a row; elements of a lane's key; steps of a key's sum
+  constexpr int VROW = D + 16;                             // padded: eight rows of 32 bytes meet no bank twice
+  constexpr int VC = 32 * DB / 64;                         // value blocks of 32 keys that a lane moves
+  constexpr int OROW = D + 4;
+  constexpr int BYTES = 32 * VROW * 2 > 16 * OROW * 4 ? 32 * VROW * 2 : 16 * OROW * 4;
+  __shared__ __attribute__((aligned(16))) uint8_t s_mem[WAVES][BYTES];
+  __shared__ float s_m[WAVES][16], s_l[WAVES][16], s_sum[16];
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
-  Job job;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
+  const Job job = job_of(p);
   Tile t;
-  if (!job_of(p, &job) || !find_tile<kRowsFew>(p, job.tile, &t)) return;
+  if (!find_tile<kRowsFew>(p, job.tile, &t)) return;
   const int kvh = job.kvh;
   const int entries = min(p.kv_len[t.stream], p.max_blocks * CS_KV_BLOCK);
   if (entries <= 0) return;
-  const int row0 = (t.n_tiles - 1 - t.index) * kRowsFew;
-  const int row = min(row0 + n, t.rows - 1);
+  const int row = min(t.row0 + n, t.rows - 1);
   const int tok = t.q0 + row / p.group, head = kvh * p.group + row % p.group;
-  const bool live = row0 + n < t.rows;
+  const bool live = t.row0 + n < t.rows;
   const int pos = min(p.q_pos[tok], entries - 1);
-  Query<D, PARTS> query;
-  query.load(p.q, (static_cast<int64_t>(tok) * p.n_q_heads + head) * D, h);
+
+  // ---- the lane's query: elements EL g + 8 w + 0..7 in step w
+  bf16x8 qf[PARTS][SW];
+  {
+    const int64_t at = (static_cast<int64_t>(tok) * p.n_q_heads + head) * D + EL * g;
+#pragma unroll
+    for (int w = 0; w < SW; ++w) {
+      bf16x8 parts[PARTS];
+      load_parts<PARTS>(p.q, at + 8 * w, parts);
+#pragma unroll
+      for (int k = 0; k < PARTS; ++k) qf[k][w] = parts[k];
+    }
+  }
   int last = live ? pos : -1, first = live ? pos : 0x7fffffff;
 #pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
+  for (int d = 1; d < 16; d <<= 1) {
     last = max(last, __shfl_xor(last, d));
     first = min(first, __shfl_xor(first, d));
   }
@@ -512,43 +544,59 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 && PARTS == 3 ? 1 : 2) void kv
   const int share = (all_tiles + p.pieces - 1) / p.pieces;
   const int kt0 = min(all_tiles, job.piece * share), kt1 = min(all_tiles, kt0 + share);
 
-  // ---- a tile's blocks: 16 rows each, the same for all lanes; rows past the frontier are the frontier's
+  // ---- a tile is four cache blocks; their ids, and so the addresses of their first rows, are the same in all lanes
   const int32_t* ids = p.block_table + static_cast<int64_t>(t.stream) * p.max_blocks;
   const int last_block = max(last, 0) / CS_KV_BLOCK, last_row = max(last, 0) % CS_KV_BLOCK;
+  const uint32_t row_bytes = static_cast<uint32_t>(p.stride_slot / 2), row_scales = static_cast<uint32_t>(p.stride_slot / cs::kKv4Block);
   const int64_t head_at = static_cast<int64_t>(kvh) * p.stride_head;
-  cs::u32x4 kc[2][KI], vc[VC];
-  uint32_t ks[2];
+  const uint8_t *k_head = p.k_codes + head_at / 2, *v_head = p.v_codes + head_at / 2;
+  const uint8_t *ks_head = p.k_scales + head_at / cs::kKv4Block, *vs_head = p.v_scales + head_at / cs::kKv4Block;
+  const int v_row = lane / DB, v_block = lane % DB;        // D 128: row of a cache block; D 64: of a pair of them
+  Codes<EL> kc[4];
+  cs::u32x4 vc[2][VC];
+  uint32_t ks[4], vs[2][VC];
   int id[4];
-  uint32_t vs[VC];
   auto request_ids = [&](int kt) __attribute__((always_inline)) {
 #pragma unroll
     for (int b = 0; b < 4; ++b) id[b] = ids[min(4 * kt + b, last_block)];
   };
-  // keys and values 32 kb .. of tile kt: cache blocks 2 kb and 2 kb + 1 of its four
+  // keys and values 32 kb .. of tile kt; rows past the frontier are the frontier's row (what lies there may be nothing)
   auto request = [&](int kt, int kb) __attribute__((always_inline)) {
-    int64_t base[2];
+    uint64_t at[2], at_s[2];
     int cap[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      base[b] = static_cast<int64_t>(id[2 * kb + b]) * CS_KV_BLOCK * p.stride_slot + head_at;
+      at[b] = static_cast<uint64_t>(static_cast<uint32_t>(id[2 * kb + b])) * (CS_KV_BLOCK * row_bytes);
+      at_s[b] = static_cast<uint64_t>(static_cast<uint32_t>(id[2 * kb + b])) * (CS_KV_BLOCK * row_scales);
       cap[b] = 4 * kt + 2 * kb + b >= last_block ? last_row : CS_KV_BLOCK - 1;
     }
-    const int64_t at = (n < 16 ? base[0] : base[1]) + min(n & 15, n < 16 ? cap[0] : cap[1]) * p.stride_slot;
 #pragma unroll
-    for (int i = 0; i < KI; ++i) kc[kb][i] = *reinterpret_cast<const cs::u32x4*>(p.k_codes + (at + 64 * i + 32 * h) / 2);
-    ks[kb] = row_scales<D>(p.k_scales, at, h);
+    for (int b = 0; b < 2; ++b) {
+      const uint32_t r = min(n, cap[b]);
+      kc[2 * kb + b].load(k_head + at[b], r * row_bytes + g * (EL / 2));
+      ks[2 * kb + b] = (ks_head + at_s[b])[r * row_scales + g * EL / cs::kKv4Block];
+    }
 #pragma unroll
-    for (int i = 0; i < VC / 2; ++i) {
-      const int r = lane / DB + i * (64 / DB);             // D 128: row of cache block i; D 64: of either
-      const int64_t at_v = (r < 16 ? base[0] : base[1]) + min(r & 15, r < 16 ? cap[0] : cap[1]) * p.stride_slot + (lane % DB) * cs::kKv4Block;
-      vc[kb * (VC / 2) + i] = *reinterpret_cast<const cs::u32x4*>(p.v_codes + at_v / 2);
-      vs[kb * (VC / 2) + i] = p.v_scales[at_v / cs::kKv4Block];
+    for (int i = 0; i < VC; ++i) {
+      if constexpr (DB == 4) {
+        const uint32_t r = min(v_row, cap[i]);
+        vc[kb][i] = *reinterpret_cast<const cs::u32x4*>(v_head + at[i] + (r * row_bytes + v_block * 16));
+        vs[kb][i] = (vs_head + at_s[i])[r * row_scales + v_block];
+      } else {
+        const bool second = v_row >= CS_KV_BLOCK;
+        const uint32_t r = min(v_row % CS_KV_BLOCK, second ? cap[1] : cap[0]);
+        vc[kb][i] = *reinterpret_cast<const cs::u32x4*>(v_head + (second ? at[1] : at[0]) + (r * row_bytes + v_block * 16));
+        vs[kb][i] = (vs_head + (second ? at_s[1] : at_s[0]))[r * row_scales + v_block];
+      }
     }
   };
 
-  Sums<D, PARTS> sums;
-  sums.clear();
-  uint16_t* const v_mine = reinterpret_cast<uint16_t*>(s_mem) + wave * 32 * VROW;
+  f32x4 o[D / 16];
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) o[i] = f32x4{};
+  float m = -INFINITY, l = 0.0f;                           // reference maximum (raw score), the lane's share of the sum
+  uint32_t bad = 0;                                        // 32-column parts of the sums that a value without numbers has reached
+  uint16_t* const v_mine = reinterpret_cast<uint16_t*>(s_mem[wave]);
   if (kt0 + wave < kt1) {
     request_ids(kt0 + wave);
     request(kt0 + wave, 0);
@@ -560,84 +608,128 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 && PARTS == 3 ? 1 : 2) void kv
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       const int key0 = kt * kKeys + 32 * kb;
-      // (LDS operations of a wave keep their order: the reads of the half before are done when these writes are)
-      uint64_t none[VC / 2];
+      // ---- values to LDS (the operations of a wave on it keep their order: the reads of the half before are done by then)
+      uint64_t none[VC];
 #pragma unroll
-      for (int i = 0; i < VC / 2; ++i) {
-        const bool b = put_values(v_mine + (lane / DB + i * (64 / DB)) * VROW + 32 * (lane % DB), vc[kb * (VC / 2) + i], vs[kb * (VC / 2) + i]);
-        none[i] = __ballot(b);
+      for (int i = 0; i < VC; ++i) {
+        const int r = DB == 4 ? v_row + CS_KV_BLOCK * i : v_row;
+        none[i] = __ballot(put_block<2>(v_mine + r * VROW + 32 * v_block, vc[kb][i], vs[kb][i], v_row));
       }
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      f32x16 s = query.scores(kc[kb], ks[kb]);
-      // (a key without numbers: rare, and its column of the scores is one lane's query for all lanes)
-      const bool bad = (ks[kb] & 255u) == cs::kKv4NoNumber || (D == 128 && (ks[kb] >> 16 & 255u) == cs::kKv4NoNumber);
-      for (uint64_t left = __ballot(bad); left; left &= left - 1) {
-        const int key = (__ffsll(static_cast<unsigned long long>(left)) - 1) & 31;
+      // ---- S^T
+      f32x4 s[2];
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (8 * (r / 4) + 4 * h + r % 4 == key) s[r] = NAN;
+      for (int b = 0; b < 2; ++b) {
+        s[b] = f32x4{};
+        const uint32_t e = ks[2 * kb + b];
+        const float sc = cs::kv4_scale(e == cs::kKv4NoNumber ? 1u : e);
+#pragma unroll
+        for (int w = 0; w < SW; ++w) {
+          const bf16x8 kf = __builtin_bit_cast(bf16x8, cs::kv4_unpack8_bf16(kc[2 * kb + b].word(w), sc));
+#pragma unroll
+          for (int k = PARTS - 1; k >= 0; --k) s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[k][w], s[b], 0, 0, 0);
+        }
+        // (a key without numbers: rare)
+        for (uint64_t left = __ballot(e == cs::kKv4NoNumber); left; left &= left - 1) {
+          const int key = (__ffsll(static_cast<unsigned long long>(left)) - 1) & 15;
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (4 * g + r == key) s[b][r] = NAN;
+        }
       }
       if (more) request(kt + WAVES, kb);
-      bf16x8 pf[PARTS][2];
-      sums.weights(s, key0, pos, key0 + 31 > first, h, p.scale_log2e, pf);
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      sums.template add<VROW>(v_mine, pf, lane);
+      if (key0 + 31 > first) {
 #pragma unroll
-      for (int i = 0; i < VC / 2; ++i)
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (key0 + 16 * b + 4 * g + r > pos) s[b][r] = -INFINITY;
+      }
+      // ---- softmax
+      float top = s[0][0];
+#pragma unroll
+      for (int r = 1; r < 8; ++r) top = fmaxf(top, s[r / 4][r % 4]);
+      top = fmaxf(top, other_quarter(top));
+      top = fmaxf(top, other_half(top));
+      if (__any((top - m) * p.scale_log2e > kSlack || m == -INFINITY)) {
+        const float raised = fmaxf(m, top);
+        const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - raised) * p.scale_log2e);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) o[i] *= f;
+        l *= f;
+        m = raised;
+      }
+      const float base = m == -INFINITY ? 0.0f : -m * p.scale_log2e;
+      float x[8], sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[i] = __builtin_amdgcn_exp2f(fmaf(s[i / 4][i % 4], p.scale_log2e, base));
+        sum += x[i];
+      }
+      l += sum;
+      bf16x8 pf[PARTS];
+      split8<PARTS>(x, pf);
+      // ---- O^T: a lane's weights are of keys 4 g + 0..3 of either cache block
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      const uint16_t* v_at = v_mine + (4 * g + (n >> 2)) * VROW + 4 * (n & 3);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(v_at + 16 * i));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(v_at + 16 * i + 16 * VROW));
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int k = PARTS - 1; k >= 0; --k) o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[k], o[i], 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < VC; ++i)
         for (uint64_t left = none[i]; left; left &= left - 1) {
           const int b = __ffsll(static_cast<unsigned long long>(left)) - 1;
-          sums.poison(b % DB, key0 + b / DB + i * (64 / DB) <= pos);
+          if (key0 + b / DB + CS_KV_BLOCK * i <= pos) bad |= 1u << (b % DB);
         }
     }
   }
 
-  // ---- the waves' results, joined: 64 columns of the output at a time
-  sums.l += other_half(sums.l);
-  if (h == 0) {
-    s_m[wave][n] = sums.m;
-    s_l[wave][n] = sums.l;
+  // ---- the waves' results, joined
+  l += other_quarter(l);
+  l += other_half(l);
+  if (__builtin_expect(__any(bad != 0), 0)) {
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+      if (bad >> (i / 2) & 1) o[i] = f32x4{NAN, NAN, NAN, NAN};
+  }
+  if (g == 0) {
+    s_m[wave][n] = m;
+    s_l[wave][n] = l;
   }
   __syncthreads();
-  float m = s_m[0][n];
+  float top = s_m[0][n], sum = 0.0f;
 #pragma unroll
-  for (int w = 1; w < WAVES; ++w) m = fmaxf(m, s_m[w][n]);
-  float l = 0.0f;
-  const float f = sums.m == -INFINITY ? (sums.l == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f((sums.m - m) * p.scale_log2e);
+  for (int w = 1; w < WAVES; ++w) top = fmaxf(top, s_m[w][n]);
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) l += s_m[w][n] == -INFINITY ? s_l[w][n] : s_l[w][n] * __builtin_amdgcn_exp2f((s_m[w][n] - m) * p.scale_log2e);
-  float* const s_o = reinterpret_cast<float*>(s_mem);
+  for (int w = 0; w < WAVES; ++w) sum += s_m[w][n] == -INFINITY ? s_l[w][n] : s_l[w][n] * __builtin_amdgcn_exp2f((s_m[w][n] - top) * p.scale_log2e);
+  const float f = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - top) * p.scale_log2e);      // (sums are 0, or NaN, where m is -inf)
+  float* const s_o = reinterpret_cast<float*>(s_mem[wave]);
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(s_o + n * OROW + 16 * i + 4 * g) = o[i] * f;
   const int64_t job_row = static_cast<int64_t>(job.index) * kRowsFew;
-  if (wave == 0 && h == 0) {
-    if (p.pieces > 1) *reinterpret_cast<cs::f32v2*>(p.ws_ml + 2 * (job_row + n)) = cs::f32v2{m, l};
-    else if (p.lse && live) p.lse[static_cast<int64_t>(tok) * p.n_q_heads + head] = log_sum(m, l, p.scale_log2e);
+  if (wave == 0 && g == 0) {
+    s_sum[n] = sum;
+    if (p.pieces > 1) *reinterpret_cast<cs::f32v2*>(p.ws_ml + 2 * (job_row + n)) = cs::f32v2{top, sum};
+    else if (p.lse && live) p.lse[static_cast<int64_t>(tok) * p.n_q_heads + head] = log_sum(top, sum, p.scale_log2e);
   }
-  for (int half = 0; half < D / 64; ++half) {
-    if (half) __syncthreads();
+  __syncthreads();
+  for (int c = tid; c < 16 * D / 4; c += 64 * WAVES) {     // four columns of a row
+    const int r = c / (D / 4), d = 4 * (c % (D / 4)), rr = t.row0 + r;
+    if (rr >= t.rows) continue;
+    f32x4 y = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(s_mem[0]) + r * OROW + d);
 #pragma unroll
-    for (int db = 0; db < 2; ++db)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        f32x4 x;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = (half == 0 ? sums.o[db][4 * g + i] : sums.o[DB == 4 ? 2 + db : db][4 * g + i]) * f;
-        *reinterpret_cast<f32x4*>(s_o + (wave * 32 + n) * OROW + 32 * db + 8 * g + 4 * h) = x;
-      }
-    if (half == 0 && wave == 0 && h == 0) s_sum[n] = l;
-    __syncthreads();
-    for (int c = tid; c < 32 * 16; c += 64 * WAVES) {      // four columns of a row
-      const int r = c / 16, d = 4 * (c % 16);
-      if (row0 + r >= t.rows) continue;
-      f32x4 x = *reinterpret_cast<const f32x4*>(s_o + r * OROW + d);
-#pragma unroll
-      for (int w = 1; w < WAVES; ++w) x += *reinterpret_cast<const f32x4*>(s_o + (w * 32 + r) * OROW + d);
-      if (p.pieces > 1) {
-        *reinterpret_cast<f32x4*>(p.ws_o + (job_row + r) * D + 64 * half + d) = x;
-      } else {
-        const float sum = s_sum[r], inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        const float y[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
-        const int rr = row0 + r;
-        store4(p.out, (static_cast<int64_t>(t.q0 + rr / p.group) * p.n_q_heads + kvh * p.group + rr % p.group) * D + 64 * half + d, y, PARTS == 1);
-      }
+    for (int w = 1; w < WAVES; ++w) y += *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(s_mem[w]) + r * OROW + d);
+    if (p.pieces > 1) {
+      *reinterpret_cast<f32x4*>(p.ws_o + (job_row + r) * D + d) = y;
+    } else {
+      const float inv = s_sum[r] == 0.0f ? 0.0f : 1.0f / s_sum[r];
+      const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
+      store4(p.out, (static_cast<int64_t>(t.q0 + rr / p.group) * p.n_q_heads + kvh * p.group + rr % p.group) * D + d, z, PARTS == 1);
     }
   }
 }
@@ -651,13 +743,13 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Params p, int bf16) {
   Tile t;
   if (!find_tile<ROWS>(p, blockIdx.x, &t)) return;
   if (min(p.kv_len[t.stream], p.max_blocks * CS_KV_BLOCK) <= 0) return;
-  const int row0 = (t.n_tiles - 1 - t.index) * ROWS, d = 4 * (threadIdx.x % PER_ROW);
-  const int64_t job0 = (static_cast<int64_t>(kvh) * p.row_tiles + blockIdx.x) * p.pieces;
+  const int row0 = t.row0, d = 4 * (threadIdx.x % PER_ROW);
+  const int64_t job0 = static_cast<int64_t>(blockIdx.x) * p.pieces * p.n_kv_heads + kvh;
   for (int r = blockIdx.z * AT_ONCE + threadIdx.x / PER_ROW; r < ROWS && row0 + r < t.rows; r += AT_ONCE * gridDim.z) {
     float m = -INFINITY, l = 0.0f;
     f32x4 o = {};
     for (int k = 0; k < p.pieces; ++k) {
-      const int64_t at = (job0 + k) * ROWS + r;
+      const int64_t at = (job0 + static_cast<int64_t>(k) * p.n_kv_heads) * ROWS + r;
       const cs::f32v2 ml = *reinterpret_cast<const cs::f32v2*>(p.ws_ml + 2 * at);
       if (ml.y == 0.0f) continue;        // (a piece without entries that the row sees; its sums are 0, or were not written)
       const float top = fmaxf(m, ml.x);
@@ -706,10 +798,9 @@ Route route(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_head
 
 template <int D, int PARTS>
 int launch(const Params& p, const Route& r, hipStream_t st) {
-  const dim3 grid(static_cast<unsigned>(p.jobs_per_xcd * 8));
+  const dim3 grid(static_cast<unsigned>(r.jobs));
   if (!r.few) hipLaunchKernelGGL((kv4_rows_kernel<D, PARTS>), grid, dim3(256), 0, st, p);
-  else if (r.waves == 8 && !(D == 128 && PARTS == 3))      // (whose registers a wave a SIMD takes)
-    hipLaunchKernelGGL((kv4_keys_kernel<D, D == 128 ? 1 : PARTS, 8>), grid, dim3(512), 0, st, p);
+  else if (r.waves == 8) hipLaunchKernelGGL((kv4_keys_kernel<D, PARTS, 8>), grid, dim3(512), 0, st, p);
   else hipLaunchKernelGGL((kv4_keys_kernel<D, PARTS, 4>), grid, dim3(256), 0, st, p);
   if (r.pieces > 1) {
     const dim3 all(static_cast<unsigned>(r.row_tiles), static_cast<unsigned>(p.n_kv_heads), r.few ? 2 : 8);
@@ -739,14 +830,14 @@ extern "C" int cs_kv4_window_attn(const void* q, const uint8_t* k_codes_layer, c
   if (!(softmax_scale > 0.0f && softmax_scale <= 3.0e38f)) return CS_EINVAL;
   if (dtype != CS_F32 && dtype != CS_BF16) return CS_EUNSUPPORTED;
   if ((head_dim != 64 && head_dim != 128) || block_size != CS_KV_BLOCK || n_q_heads / n_kv_heads > 16 || n_kv_heads > 65535) return CS_EUNSUPPORTED;
-  if (!cs::kv4_strides(stride_slot, stride_head, 0)) return CS_EUNSUPPORTED;
+  if (!cs::kv4_strides(stride_slot, stride_head, 0) || stride_slot >= (1 << 26)) return CS_EUNSUPPORTED;
   if (n_q > 0x7fffffffll / 16 || max_blocks > 0x7fffffff / CS_KV_BLOCK - kKeys) return CS_EUNSUPPORTED;
   if (n_q == 0 || n_streams == 0) return CS_OK;
   if (!q || !k_codes_layer || !k_scales_layer || !v_codes_layer || !v_scales_layer || !cu_q || !q_pos || !kv_len || !block_table || !out || max_blocks < 1)
     return CS_EINVAL;
   if (!cs::aligned16(q) || !cs::aligned16(out) || !cs::aligned16(k_codes_layer) || !cs::aligned16(v_codes_layer)) return CS_EUNSUPPORTED;
   const Route r = route(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, max_blocks);
-  if (r.jobs > 0x7fffffffll - 64) return CS_EUNSUPPORTED;
+  if (r.jobs > 0x7fffffffll) return CS_EUNSUPPORTED;
   if (r.total && (!workspace || workspace_bytes < r.total || !cs::aligned16(workspace))) return CS_EWORKSPACE;
 
   Params p;
@@ -771,10 +862,7 @@ extern "C" int cs_kv4_window_attn(const void* q, const uint8_t* k_codes_layer, c
   p.n_q_heads = n_q_heads;
   p.n_kv_heads = n_kv_heads;
   p.group = n_q_heads / n_kv_heads;
-  p.row_tiles = static_cast<int32_t>(r.row_tiles);
   p.pieces = static_cast<int32_t>(r.pieces);
-  p.jobs = static_cast<int32_t>(r.jobs);
-  p.jobs_per_xcd = static_cast<int32_t>((r.jobs + 7) / 8);
   p.scale_log2e = softmax_scale * 1.4426950408889634f;
   hipStream_t st = cs::as_stream(stream);
   if (head_dim == 128) return dtype == CS_BF16 ? launch<128, 1>(p, r, st) : launch<128, 3>(p, r, st);
