@@ -412,41 +412,33 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 3 : D == 64 ? 2 : 1) void kv4_row
   const uint32_t code_step = static_cast<uint32_t>(p.stride_slot * CS_KV_BLOCK / 2), scale_step = static_cast<uint32_t>(p.stride_slot / 2);
   const uint8_t* const my_code = codes + at_row / 2;
   const uint8_t* const my_scale = scales + at_row / cs::kKv4Block;
-  cs::u32x4 code;
-  uint32_t scale, id;
+  // Two tiles are under way while one is computed on: a tile of 32 keys takes less time than its codes.
+  cs::u32x4 code[2];
+  uint32_t scale[2], id;
   // rows past the frontier are the frontier's row (what lies there may be nothing)
   auto request_id = [&](int kt) __attribute__((always_inline)) { id = static_cast<uint32_t>(ids[min(kt * T + my_row, last) / CS_KV_BLOCK]); };
-  auto request = [&](int kt) __attribute__((always_inline)) {
+  auto request = [&](int kt, int at) __attribute__((always_inline)) {
     const uint8_t *c = my_code, *s = my_scale;
     if (kt * T + T - 1 > last && kt * T + my_row > last) {
       c = codes + at_last / 2;
       s = scales + at_last / cs::kKv4Block;
     }
-    code = *reinterpret_cast<const cs::u32x4*>(c + static_cast<uint64_t>(id) * code_step);
-    scale = s[static_cast<uint64_t>(id) * scale_step];
+    code[at] = *reinterpret_cast<const cs::u32x4*>(c + static_cast<uint64_t>(id) * code_step);
+    scale[at] = s[static_cast<uint64_t>(id) * scale_step];
   };
-  auto put = [&](int buf) __attribute__((always_inline)) {
+  auto put = [&](int buf) __attribute__((always_inline)) {       // tile kt0 + k: stage k & 1 of the registers and of LDS
     if (of_v) {
-      if (put_block<1>(&s_v[buf][my_row * VROW + 32 * my_block], code, scale, my_row)) s_nan = 1;
-      s_vs[buf][tid & 127] = static_cast<uint8_t>(scale);
+      if (put_block<1>(&s_v[buf][my_row * VROW + 32 * my_block], code[buf], scale[buf], my_row)) s_nan = 1;
+      s_vs[buf][tid & 127] = static_cast<uint8_t>(scale[buf]);
     } else {
-      put_block<0>(&s_k[buf][my_row * KROW + 32 * my_block], code, scale, my_row);
+      put_block<0>(&s_k[buf][my_row * KROW + 32 * my_block], code[buf], scale[buf], my_row);
     }
   };
 
   Sums<D, PARTS> sums;
   sums.clear();
-  if (kt0 < kt1) {
-    request_id(kt0);
-    request(kt0);
-    if (kt0 + 1 < kt1) request_id(kt0 + 1);
-    put(0);
-    if (kt0 + 1 < kt1) request(kt0 + 1);
-    if (kt0 + 2 < kt1) request_id(kt0 + 2);
-    __syncthreads();
-  }
-  for (int kt = kt0; kt < kt1; ++kt) {
-    const int buf = (kt - kt0) & 1;
+  auto tile = [&](int kt, auto stage) __attribute__((always_inline)) {
+    constexpr int buf = decltype(stage)::value;
 #pragma unroll
     for (int kb = 0; kb < T / 32; ++kb) {
       const int key0 = kt * T + 32 * kb;
@@ -460,9 +452,26 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 3 : D == 64 ? 2 : 1) void kv4_row
         if (s_vs[buf][c] == cs::kKv4NoNumber) sums.poison(c % DB, kt * T + c / DB <= pos);
     }
     if (kt + 1 < kt1) put(buf ^ 1);
-    if (kt + 2 < kt1) request(kt + 2);
-    if (kt + 3 < kt1) request_id(kt + 3);
+    if (kt + 3 < kt1) request(kt + 3, buf ^ 1);
+    if (kt + 4 < kt1) request_id(kt + 4);
     __syncthreads();
+  };
+  if (kt0 < kt1) {
+    request_id(kt0);
+    request(kt0, 0);
+    if (kt0 + 1 < kt1) {
+      request_id(kt0 + 1);
+      request(kt0 + 1, 1);
+    }
+    if (kt0 + 2 < kt1) request_id(kt0 + 2);
+    put(0);
+    if (kt0 + 2 < kt1) request(kt0 + 2, 0);
+    if (kt0 + 3 < kt1) request_id(kt0 + 3);
+    __syncthreads();
+  }
+  for (int kt = kt0; kt < kt1; kt += 2) {
+    tile(kt, std::integral_constant<int, 0>());
+    if (kt + 1 < kt1) tile(kt + 1, std::integral_constant<int, 1>());
   }
 
   // ---- results
