@@ -39,6 +39,7 @@ struct Params {
 };
 
 constexpr int kStep = 32;                // query rows of a step
+constexpr int kGroups = 1024, kLeast = 4;      // workgroups wanted, steps that a share of a stream's rows has at least
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 constexpr int keys_per_wave(int cache) { return cache == CS_F32 ? 32 : 64; }
@@ -143,11 +144,12 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
     }
     if (tid < kStep) {
       const int r = step * kStep + tid;
-      next_pos = -1;                                       // rows past the last: see nothing
+      next_pos = -1;                                       // rows past the last, like those of a negative position: see nothing
+      next_lse = 0.0f;
       if (r < rows) {
         const int tok = q0 + r / p.group;
         next_pos = min(p.q_pos[tok], entries - 1);
-        if (!STATS) next_lse = p.lse[static_cast<int64_t>(tok) * p.n_q_heads + kvh * p.group + r % p.group] * kLog2e;
+        if (!STATS && next_pos >= 0) next_lse = p.lse[static_cast<int64_t>(tok) * p.n_q_heads + kvh * p.group + r % p.group] * kLog2e;
       }
     }
   };
@@ -220,9 +222,18 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             s[kb][r] *= p.scale_log2e;
-            if (masked && key0 + 32 * kb + 8 * (r / 4) + 4 * h + r % 4 > my_pos) s[kb][r] = -INFINITY;
-            m = fmaxf(m, s[kb][r]);
           }
+        if (masked) {
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (key0 + 32 * kb + 8 * (r / 4) + 4 * h + r % 4 > my_pos) s[kb][r] = -INFINITY;
+        }
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) m = fmaxf(m, s[kb][r]);
         m = fmaxf(m, __shfl_xor(m, 32));
         const float base = m == -INFINITY ? 0.0f : m;
 #pragma unroll
@@ -235,23 +246,28 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
           s_l[buf][wave][n] = l;
         }
       } else {
+        if (masked) {                                      // weights of keys that a row does not see: exp2 of -inf
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-          const int key = key0 + 32 * kb + n;
-          float sum = 0.0f;
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {                    // rows 8 g + 4 h + 0..3
-            const cs::u32x4 lse = *reinterpret_cast<const cs::u32x4*>(&s_lse[buf][8 * g + 4 * h]);
+          for (int g = 0; g < 4; ++g) {
             const cs::u32x4 pos = *reinterpret_cast<const cs::u32x4*>(&s_pos[buf][8 * g + 4 * h]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float w = __builtin_amdgcn_exp2f(fmaf(s[kb][4 * g + i], p.scale_log2e, -__uint_as_float(lse[i])));
-              if (masked && key > static_cast<int>(pos[i])) w = 0.0f;
-              sum += w;
-            }
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (key0 + 32 * kb + n > static_cast<int>(pos[i])) s[kb][4 * g + i] = -INFINITY;
           }
-          acc[kb] += sum;
         }
+        float sum[KB] = {};
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {                      // rows 8 g + 4 h + 0..3
+          const cs::u32x4 lse = *reinterpret_cast<const cs::u32x4*>(&s_lse[buf][8 * g + 4 * h]);
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[kb] += __builtin_amdgcn_exp2f(fmaf(s[kb][4 * g + i], p.scale_log2e, -__uint_as_float(lse[i])));
+        }
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) acc[kb] += sum[kb];
       }
     } else if (STATS && h == 0) {
       s_m[buf][wave][n] = -INFINITY;
@@ -274,12 +290,13 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
   }
 }
 
-// log-sum-exp of every query row from its key ranges' maxima and sums.
+// log-sum-exp of every query row from its key ranges' maxima and sums: a wave a row, ranges dealt to its lanes.
 __global__ __launch_bounds__(256) void attn_weights_join_kernel(Params p, int tile) {
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  const int lane = threadIdx.x & 63;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
   if (i >= p.n_q * p.n_q_heads) return;
   const int tok = static_cast<int>(i / p.n_q_heads);
-  int lo = 0, hi = p.n_streams;                            // the last stream that starts at or before the token and is not empty
+  int lo = 0, hi = p.n_streams;                            // the last stream that starts at or before the token
   while (hi - lo > 1) {
     const int mid = (lo + hi) / 2;
     if (p.cu_q[mid] <= tok) lo = mid;
@@ -289,13 +306,22 @@ __global__ __launch_bounds__(256) void attn_weights_join_kernel(Params p, int ti
   const int pos = min(p.q_pos[tok], stream_entries(p, lo) - 1);
   if (pos < 0) return;
   float m = -INFINITY, l = 0.0f;
-  const cs::f32v2* part = p.ws_stat + i * p.key_tiles;
-  for (int kt = 0; kt <= pos / tile; ++kt) {
-    const float pm = part[kt].x, pl = part[kt].y, top = fmaxf(m, pm);
-    l = (m == -INFINITY ? 0.0f : l * __builtin_amdgcn_exp2f(m - top)) + (pm == -INFINITY ? pl : pl * __builtin_amdgcn_exp2f(pm - top));
+  auto add = [&](float pm, float pl) __attribute__((always_inline)) {
+    const float top = fmaxf(m, pm);
+    l = (m == -INFINITY ? l : l * __builtin_amdgcn_exp2f(m - top)) + (pm == -INFINITY ? pl : pl * __builtin_amdgcn_exp2f(pm - top));
     m = top;
+  };
+  const cs::f32v2* part = p.ws_stat + i * p.key_tiles;
+  for (int kt = lane; kt <= pos / tile; kt += 64) {
+    const cs::f32v2 x = part[kt];
+    add(x.x, x.y);
   }
-  p.ws_lse[i] = ((m == -INFINITY ? 0.0f : m) + __builtin_amdgcn_logf(l)) * kLn2;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const float pm = __shfl_xor(m, d), pl = __shfl_xor(l, d);
+    add(pm, pl);
+  }
+  if (lane == 0) p.ws_lse[i] = ((m == -INFINITY ? 0.0f : m) + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // Partial sums of shares and kv heads, added in order to what earlier calls left.
@@ -322,8 +348,8 @@ Layout layout(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_he
   // Shares of a stream's rows: until about four workgroups a CU are under way, but at least four steps of rows each.
   const int64_t jobs = static_cast<int64_t>(w.key_tiles) * n_streams * n_kv_heads;
   const int64_t steps = (n_q * (n_q_heads / n_kv_heads) / (n_streams > 0 ? n_streams : 1) + kStep - 1) / kStep;
-  int64_t c = jobs > 0 ? 1024 / jobs : 1;
-  if (c > steps / 4) c = steps / 4;
+  int64_t c = jobs > 0 ? kGroups / jobs : 1;
+  if (c > steps / kLeast) c = steps / kLeast;
   w.chunks = static_cast<int>(c < 1 ? 1 : c);
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   w.lse = 0;
@@ -341,7 +367,7 @@ int launch(Params p, const Layout& w, bool have_lse, hipStream_t st) {
   const int64_t all = static_cast<int64_t>(p.max_blocks) * CS_KV_BLOCK * p.n_streams;
   if (!have_lse) {
     hipLaunchKernelGGL((attn_weights_kernel<D, CACHE, QP, true>), grid, dim3(256), 0, st, p);
-    hipLaunchKernelGGL(attn_weights_join_kernel, dim3(static_cast<unsigned>((p.n_q * p.n_q_heads + 255) / 256)), dim3(256), 0, st, p, keys_per_tile(CACHE));
+    hipLaunchKernelGGL(attn_weights_join_kernel, dim3(static_cast<unsigned>((p.n_q * p.n_q_heads + 3) / 4)), dim3(256), 0, st, p, keys_per_tile(CACHE));
     p.lse = p.ws_lse;
   }
   hipLaunchKernelGGL((attn_weights_kernel<D, CACHE, QP, false>), grid, dim3(256), 0, st, p);

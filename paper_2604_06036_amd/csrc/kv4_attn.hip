@@ -794,7 +794,7 @@ Route route(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_head
   const int64_t jobs = r.row_tiles * n_kv_heads, tiles = (static_cast<int64_t>(max_blocks) * CS_KV_BLOCK + kKeys - 1) / kKeys;
   r.waves = 4;
   const int64_t least = r.few ? 8 : 6;                     // tiles that make a piece worth its share of the join
-  r.pieces = (r.few ? 1024 : 512) / jobs;
+  r.pieces = (r.few ? 1024 : 768) / jobs;
   if (r.pieces > tiles / least) r.pieces = tiles / least;
   if (r.pieces > 64) r.pieces = 64;
   if (r.pieces < 1) r.pieces = 1;

@@ -13,6 +13,7 @@
 namespace {
 
 constexpr int kPairs = 8;                // pairs a lane owns
+constexpr int kRopeGroups = 4096;        // workgroups wanted
 
 template <bool kBf16>
 struct Eight;
@@ -223,90 +224,111 @@ struct Kv4RerotateParams {
   const int32_t* __restrict__ src_slot;
   const int32_t* __restrict__ dst_slot;        // nullptr: in place, keys only
   int64_t n_rows, stride_layer, stride_slot, stride_head;
-  int32_t n_layers, n_kv_heads, head_dim, lanes_per_head, layers_per_block;
+  int32_t n_layers, n_kv_heads, head_dim, lanes_per_head, layers_per_block, rows_per_block;
 };
 
-// A lane owns 32 pairs of a row and head, two blocks, in every layer of its share: 16-byte loads, and a block's largest
-// magnitude is the lane's own.
+// A workgroup evaluates the angles of its rows once, into LDS (all heads and layers of a row turn by them).  A lane owns 32 pairs of
+// a row and head, two blocks, in every layer of its share: 16-byte loads, and a block's largest magnitude is the lane's own.
+constexpr int kAngleRows = 4096;         // (row, pair) places in LDS
+constexpr int kRerotateGroups = 512;    // workgroups wanted
+
 template <int kStyle>
 __global__ __launch_bounds__(256) void kv4_rerotate_kernel(Kv4RerotateParams p) {
   constexpr int N = cs::kKv4Block;
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+  extern __shared__ __attribute__((aligned(16))) float s_angle[];       // [rows][2 * pairs + 4]: cosine, sine
+  const int half = p.head_dim / 2, pitch = 2 * half + 4, tid = threadIdx.x;
+  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * p.rows_per_block;
+  const int rows = static_cast<int>(min(static_cast<int64_t>(p.rows_per_block), p.n_rows - row0));
+  for (int i = tid; i < rows * half; i += 256) {
+    const int r = i / half, c = i - r * half;
+    float cn, sn;
+    cs::rope_row<1>(p.rope, row0 + r, c, &cn, &sn);
+    *reinterpret_cast<cs::f32v2*>(s_angle + r * pitch + 2 * c) = cs::f32v2{cn, sn};
+  }
+  __syncthreads();
   const int units_per_row = p.n_kv_heads * p.lanes_per_head;
-  const int64_t row = unit / units_per_row;
-  if (row >= p.n_rows) return;
-  const int rem = static_cast<int>(unit - row * units_per_row);
-  const int head = rem / p.lanes_per_head;
-  const int j = rem - head * p.lanes_per_head;
-  const int src = p.src_slot[row];
-  const int dst = p.dst_slot ? p.dst_slot[row] : src;
-  if (src < 0 || dst < 0) return;
-  float cn[N], sn[N];
-  cs::rope_row<N>(p.rope, row, j * N, cn, sn);
-
-  const int off_a = kStyle == CS_ROPE_HALF_SPLIT ? j * N : 2 * j * N;
-  const int off_b = kStyle == CS_ROPE_HALF_SPLIT ? p.head_dim / 2 + j * N : 2 * j * N + N;
-  const int64_t from = static_cast<int64_t>(src) * p.stride_slot + static_cast<int64_t>(head) * p.stride_head;
-  const int64_t to = static_cast<int64_t>(dst) * p.stride_slot + static_cast<int64_t>(head) * p.stride_head;
   const int l_begin = blockIdx.y * p.layers_per_block, l_end = min(p.n_layers, l_begin + p.layers_per_block);
-  for (int l = l_begin; l < l_end; ++l) {
-    const int64_t s = static_cast<int64_t>(l) * p.stride_layer + from, d = static_cast<int64_t>(l) * p.stride_layer + to;
-    const cs::u32x4 wa = *reinterpret_cast<const cs::u32x4*>(p.k_codes + (s + off_a) / 2);
-    const cs::u32x4 wb = *reinterpret_cast<const cs::u32x4*>(p.k_codes + (s + off_b) / 2);
-    const uint32_t ea = p.k_scales[(s + off_a) / N], eb = p.k_scales[(s + off_b) / N];
-    cs::u32x4 va, vb;
-    uint8_t fa = 0, fb = 0;
-    if (p.dst_slot) {
-      va = *reinterpret_cast<const cs::u32x4*>(p.v_codes + (s + off_a) / 2);
-      vb = *reinterpret_cast<const cs::u32x4*>(p.v_codes + (s + off_b) / 2);
-      fa = p.v_scales[(s + off_a) / N];
-      fb = p.v_scales[(s + off_b) / N];
-    }
-    float a[N], b[N];
+  for (int unit = tid; unit < rows * units_per_row; unit += 256) {
+    const int r = unit / units_per_row;
+    const int rem = unit - r * units_per_row;
+    const int head = rem / p.lanes_per_head;
+    const int j = rem - head * p.lanes_per_head;
+    const int src = p.src_slot[row0 + r];
+    const int dst = p.dst_slot ? p.dst_slot[row0 + r] : src;
+    if (src < 0 || dst < 0) continue;
+    float cn[N], sn[N];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      cs::kv4_unpack8(wa[i], cs::kv4_scale(ea), a + 8 * i);
-      cs::kv4_unpack8(wb[i], cs::kv4_scale(eb), b + 8 * i);
+    for (int i = 0; i < N / 2; ++i) {
+      const cs::u32x4 v = *reinterpret_cast<const cs::u32x4*>(s_angle + r * pitch + 2 * j * N + 4 * i);
+      cn[2 * i] = __uint_as_float(v.x);
+      sn[2 * i] = __uint_as_float(v.y);
+      cn[2 * i + 1] = __uint_as_float(v.z);
+      sn[2 * i + 1] = __uint_as_float(v.w);
     }
-    if (ea == cs::kKv4NoNumber || eb == cs::kKv4NoNumber) {
+
+    const int off_a = kStyle == CS_ROPE_HALF_SPLIT ? j * N : 2 * j * N;
+    const int off_b = kStyle == CS_ROPE_HALF_SPLIT ? p.head_dim / 2 + j * N : 2 * j * N + N;
+    const int64_t from = static_cast<int64_t>(src) * p.stride_slot + static_cast<int64_t>(head) * p.stride_head;
+    const int64_t to = static_cast<int64_t>(dst) * p.stride_slot + static_cast<int64_t>(head) * p.stride_head;
+    for (int l = l_begin; l < l_end; ++l) {
+      const int64_t s = static_cast<int64_t>(l) * p.stride_layer + from, d = static_cast<int64_t>(l) * p.stride_layer + to;
+      const cs::u32x4 wa = *reinterpret_cast<const cs::u32x4*>(p.k_codes + (s + off_a) / 2);
+      const cs::u32x4 wb = *reinterpret_cast<const cs::u32x4*>(p.k_codes + (s + off_b) / 2);
+      const uint32_t ea = p.k_scales[(s + off_a) / N], eb = p.k_scales[(s + off_b) / N];
+      cs::u32x4 va, vb;
+      uint8_t fa = 0, fb = 0;
+      if (p.dst_slot) {
+        va = *reinterpret_cast<const cs::u32x4*>(p.v_codes + (s + off_a) / 2);
+        vb = *reinterpret_cast<const cs::u32x4*>(p.v_codes + (s + off_b) / 2);
+        fa = p.v_scales[(s + off_a) / N];
+        fb = p.v_scales[(s + off_b) / N];
+      }
+      float a[N], b[N];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        cs::kv4_unpack8(wa[i], cs::kv4_scale(ea), a + 8 * i);
+        cs::kv4_unpack8(wb[i], cs::kv4_scale(eb), b + 8 * i);
+      }
+      if (ea == cs::kKv4NoNumber || eb == cs::kKv4NoNumber) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          if (ea == cs::kKv4NoNumber) a[i] = NAN;
+          if (eb == cs::kKv4NoNumber) b[i] = NAN;
+        }
+      }
+      uint32_t ma = 0, mb = 0;
+      if (kStyle == CS_ROPE_HALF_SPLIT) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) cs::rope_turn(a[i], b[i], cn[i], sn[i], &a[i], &b[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+          cs::rope_turn(a[2 * i], a[2 * i + 1], cn[i], sn[i], &a[2 * i], &a[2 * i + 1]);
+          cs::rope_turn(b[2 * i], b[2 * i + 1], cn[N / 2 + i], sn[N / 2 + i], &b[2 * i], &b[2 * i + 1]);
+        }
+      }
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        if (ea == cs::kKv4NoNumber) a[i] = NAN;
-        if (eb == cs::kKv4NoNumber) b[i] = NAN;
+        ma = max(ma, cs::abs_bits(a[i]));
+        mb = max(mb, cs::abs_bits(b[i]));
       }
-    }
-    uint32_t ma = 0, mb = 0;
-    if (kStyle == CS_ROPE_HALF_SPLIT) {
+      const uint32_t na = cs::kv4_scale_byte(ma), nb = cs::kv4_scale_byte(mb);
+      cs::u32x4 oa, ob;
 #pragma unroll
-      for (int i = 0; i < N; ++i) cs::rope_turn(a[i], b[i], cn[i], sn[i], &a[i], &b[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < N / 2; ++i) {
-        cs::rope_turn(a[2 * i], a[2 * i + 1], cn[i], sn[i], &a[2 * i], &a[2 * i + 1]);
-        cs::rope_turn(b[2 * i], b[2 * i + 1], cn[N / 2 + i], sn[N / 2 + i], &b[2 * i], &b[2 * i + 1]);
+      for (int i = 0; i < 4; ++i) {
+        oa[i] = cs::kv4_pack8(a + 8 * i, cs::kv4_scale(na));
+        ob[i] = cs::kv4_pack8(b + 8 * i, cs::kv4_scale(nb));
       }
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      ma = max(ma, cs::abs_bits(a[i]));
-      mb = max(mb, cs::abs_bits(b[i]));
-    }
-    const uint32_t na = cs::kv4_scale_byte(ma), nb = cs::kv4_scale_byte(mb);
-    cs::u32x4 oa, ob;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      oa[i] = cs::kv4_pack8(a + 8 * i, cs::kv4_scale(na));
-      ob[i] = cs::kv4_pack8(b + 8 * i, cs::kv4_scale(nb));
-    }
-    *reinterpret_cast<cs::u32x4*>(p.k_codes + (d + off_a) / 2) = oa;
-    *reinterpret_cast<cs::u32x4*>(p.k_codes + (d + off_b) / 2) = ob;
-    p.k_scales[(d + off_a) / N] = static_cast<uint8_t>(na);
-    p.k_scales[(d + off_b) / N] = static_cast<uint8_t>(nb);
-    if (p.dst_slot) {
-      *reinterpret_cast<cs::u32x4*>(p.v_codes + (d + off_a) / 2) = va;
-      *reinterpret_cast<cs::u32x4*>(p.v_codes + (d + off_b) / 2) = vb;
-      p.v_scales[(d + off_a) / N] = fa;
-      p.v_scales[(d + off_b) / N] = fb;
+      *reinterpret_cast<cs::u32x4*>(p.k_codes + (d + off_a) / 2) = oa;
+      *reinterpret_cast<cs::u32x4*>(p.k_codes + (d + off_b) / 2) = ob;
+      p.k_scales[(d + off_a) / N] = static_cast<uint8_t>(na);
+      p.k_scales[(d + off_b) / N] = static_cast<uint8_t>(nb);
+      if (p.dst_slot) {
+        *reinterpret_cast<cs::u32x4*>(p.v_codes + (d + off_a) / 2) = va;
+        *reinterpret_cast<cs::u32x4*>(p.v_codes + (d + off_b) / 2) = vb;
+        p.v_scales[(d + off_a) / N] = fa;
+        p.v_scales[(d + off_b) / N] = fb;
+      }
     }
   }
 }
@@ -378,7 +400,7 @@ extern "C" int cs_rope_refresh_scatter(const void* q, void* q_out, const void* k
   if (blocks_x > 0x7fffffffll) return CS_EUNSUPPORTED;
   // Heads a thread turns with one evaluation of its angles: all of them where the tokens alone fill the card, fewer below.
   const int heads = n_q_heads + 2 * n_kv_heads;
-  const int64_t shares = blocks_x >= 1024 ? 1 : (1024 + blocks_x - 1) / blocks_x;
+  const int64_t shares = blocks_x >= kRopeGroups ? 1 : (kRopeGroups + blocks_x - 1) / blocks_x;
   p.heads_per_thread = static_cast<int32_t>(shares >= heads ? 1 : (heads + shares - 1) / shares);
   const dim3 grid(static_cast<unsigned>(blocks_x), static_cast<unsigned>((heads + p.heads_per_thread - 1) / p.heads_per_thread));
   if (grid.y > 65535u) return CS_EUNSUPPORTED;
@@ -468,15 +490,18 @@ extern "C" int cs_kv4_rerotate(uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_c
   p.n_kv_heads = n_kv_heads;
   p.head_dim = head_dim;
   p.lanes_per_head = head_dim / 64;
-  const int64_t blocks_x = (n_rows * n_kv_heads * p.lanes_per_head + 255) / 256;
+  const int units = n_kv_heads * p.lanes_per_head, places = kAngleRows / (head_dim / 2);
+  p.rows_per_block = units >= 256 ? 1 : 256 / units < places ? 256 / units : places;
+  const int64_t blocks_x = (n_rows + p.rows_per_block - 1) / p.rows_per_block;
   if (blocks_x > 0x7fffffffll) return CS_EUNSUPPORTED;
-  // Layers a thread sweeps with one evaluation of its 32 angles: all of them where the rows alone fill the card.
-  const int64_t shares = blocks_x >= 1024 ? 1 : (1024 + blocks_x - 1) / blocks_x;
+  // Layers of a workgroup: all of them where the rows alone fill the card.
+  const int64_t shares = blocks_x >= kRerotateGroups ? 1 : (kRerotateGroups + blocks_x - 1) / blocks_x;
   p.layers_per_block = static_cast<int32_t>(shares >= n_layers ? 1 : (n_layers + shares - 1) / shares);
   const int64_t blocks_y = (n_layers + p.layers_per_block - 1) / p.layers_per_block;
   if (blocks_y > 65535) return CS_EUNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(blocks_x), static_cast<unsigned>(blocks_y));
-  if (rope_style == CS_ROPE_HALF_SPLIT) hipLaunchKernelGGL(kv4_rerotate_kernel<CS_ROPE_HALF_SPLIT>, grid, dim3(256), 0, cs::as_stream(stream), p);
-  else hipLaunchKernelGGL(kv4_rerotate_kernel<CS_ROPE_INTERLEAVED>, grid, dim3(256), 0, cs::as_stream(stream), p);
+  const size_t lds = static_cast<size_t>(p.rows_per_block) * (head_dim + 4) * sizeof(float);
+  if (rope_style == CS_ROPE_HALF_SPLIT) hipLaunchKernelGGL(kv4_rerotate_kernel<CS_ROPE_HALF_SPLIT>, grid, dim3(256), lds, cs::as_stream(stream), p);
+  else hipLaunchKernelGGL(kv4_rerotate_kernel<CS_ROPE_INTERLEAVED>, grid, dim3(256), lds, cs::as_stream(stream), p);
   return cs::note_hip(hipGetLastError());
 }

@@ -2,8 +2,10 @@
 //
 // Per stream: the first n_first and last n_last entries, then those of the largest accumulated weight, ties to the lowest
 // index, NaN last, up to the budget; kept in their order.  One workgroup a stream: weights become unsigned integers of the same
-// order, four passes of 256 LDS counters find the smallest kept one and how many of its equals stay, and a pass in index order
-// places what is kept by counting across lanes and waves.  All of it is integer work: bit exact, the same from run to run.
+// order, held in registers (up to 32 a thread), three passes of LDS counters over 11, 11 and 10 bits find the smallest kept one and
+// how many of its equals stay, and one count of the larger and of the equal ones before every entry places what is kept.
+// (11 bits hold the exponent and two more, so that sums of softmax weights, within a few powers of two of each other, spread over
+// enough counters.)  All of it is integer work: bit exact, the same from run to run.  Latency bounds it: MEASURED
 #include "common.h"
 
 namespace {
@@ -13,7 +15,7 @@ struct Params {
   const int32_t* __restrict__ kv_len;
   const int32_t* __restrict__ bt_old;
   const int32_t* __restrict__ bt_new;
-  int32_t* __restrict__ kept;
+  int32_t* kept;                         // (written, and read back by other threads of the workgroup)
   int32_t* __restrict__ src_slot;
   int32_t* __restrict__ dst_slot;
   int32_t* __restrict__ delta;
@@ -33,109 +35,187 @@ __device__ __forceinline__ uint32_t rank_of(float w, bool fixed) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
+constexpr int kWaves = kThreads / 64, kBins = 2048;
+
+// Entries a thread holds; HELD 0: any number, read anew in every pass.
+template <int HELD>
 __global__ __launch_bounds__(kThreads) void plan_evict_kernel(Params p) {
-  __shared__ int s_hist[256];
+  constexpr int ROUNDS = HELD ? HELD : 32;                 // entries of a thread that are placed at once
+  __shared__ int s_bins[kBins];
+  __shared__ int s_wave[kWaves];
   __shared__ int s_digit, s_left;
-  __shared__ int s_wave[2][kThreads / 64];
+  __shared__ int s_above[ROUNDS * kWaves], s_equal[ROUNDS * kWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, stream = blockIdx.x;
   const int row_old = p.max_blocks_old * CS_KV_BLOCK;
   const int n = max(0, min(p.kv_len[stream], row_old)), keep = min(n, p.budget);
   const float* weight = p.weight + static_cast<int64_t>(stream) * row_old;
   const int first = p.n_first, last = max(0, n - min(p.n_last, n));
-  auto rank = [&](int j) __attribute__((always_inline)) { return rank_of(weight[j], j < first || j >= last); };
+  const int rounds = (n + kThreads - 1) / kThreads;
+  float held[HELD ? HELD : 1];
+  if (HELD) {
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      const int j = i * kThreads + tid;
+      held[i] = j < n ? weight[j] : 0.0f;
+    }
+  }
+  auto rank = [&](int i, int j) __attribute__((always_inline)) { return rank_of(HELD ? held[HELD ? i : 0] : weight[j], j < first || j >= last); };
 
   // ---- the smallest rank that stays, and how many entries of that rank
   uint32_t prefix = 0, mask = 0;
   int left = keep;                       // entries still to find among those that share the prefix
   if (keep < n && keep > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) s_hist[tid] = 0;
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+      s_bins[tid] = 0;
+      s_bins[kThreads + tid] = 0;
       __syncthreads();
-      for (int j = tid; j < n; j += kThreads) {
-        const uint32_t r = rank(j);
-        if ((r & mask) == prefix) atomicAdd(&s_hist[(r >> shift) & 255u], 1);
+      auto count = [&](int i) __attribute__((always_inline)) {
+        const int j = i * kThreads + tid;
+        if (j >= n) return;
+        const uint32_t r = rank(i, j);
+        if ((r & mask) == prefix) atomicAdd(&s_bins[(r >> shift) & ((1u << bits) - 1)], 1);
+      };
+      if (HELD) {
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+          if (i < rounds) count(i);
+      } else {
+        for (int i = 0; i < rounds; ++i) count(i);
       }
       __syncthreads();
-      if (tid < 64) {                    // from the largest digit down: the digit at which `left` is reached
-        int c[4], sum = 0;
+      // from the largest digit down, two digits a thread: the one at which `left` is reached
+      const int d = kBins - 1 - 2 * tid, c0 = s_bins[d], c1 = s_bins[d - 1];
+      int incl = c0 + c1;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          c[i] = s_hist[255 - 4 * tid - i];
-          sum += c[i];
-        }
-        int incl = sum;
+      for (int k = 1; k < 64; k <<= 1) {
+        const int up = __shfl_up(incl, k);
+        if (lane >= k) incl += up;
+      }
+      if (lane == 63) s_wave[wave] = incl;
+      __syncthreads();
+      int before = incl - c0 - c1;
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-          const int up = __shfl_up(incl, d);
-          if (tid >= d) incl += up;
-        }
-        int before = incl - sum;
-        if (before < left && left <= incl) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (before < left && left <= before + c[i]) {
-              s_digit = 255 - 4 * tid - i;
-              s_left = left - before;
-            }
-            before += c[i];
-          }
-        }
+      for (int w = 0; w < kWaves; ++w) before += w < wave ? s_wave[w] : 0;
+      if (before < left && left <= before + c0 + c1) {     // (one thread)
+        const bool second = left > before + c0;
+        s_digit = second ? d - 1 : d;
+        s_left = left - before - (second ? c0 : 0);
       }
       __syncthreads();
       prefix |= static_cast<uint32_t>(s_digit) << shift;
-      mask |= 255u << shift;
+      mask |= ((1u << bits) - 1) << shift;
       left = s_left;
-      __syncthreads();
     }
   }
 
-  // ---- lists, in index order
+  // ---- lists, in index order: before an entry stay the larger ones before it, and of its equals no more than `left`
   const int64_t list = static_cast<int64_t>(stream) * p.budget;
   const int32_t* ids_old = p.bt_old + static_cast<int64_t>(stream) * p.max_blocks_old;
   const int32_t* ids_new = p.bt_new + static_cast<int64_t>(stream) * p.max_blocks_new;
   float* weight_new = p.weight_new ? p.weight_new + static_cast<int64_t>(stream) * p.max_blocks_new * CS_KV_BLOCK : nullptr;
-  int at0 = 0, equal0 = 0;               // kept entries and entries of the smallest rank before this round
-  for (int j0 = 0; j0 < n && keep > 0; j0 += kThreads) {
-    const int j = j0 + tid;
-    const uint32_t r = j < n ? rank(j) : 0u;
-    const bool above = j < n && (keep == n || r > prefix), equal = j < n && keep < n && r == prefix;
-    const uint64_t lower = (1ull << lane) - 1, eq = __ballot(equal);
-    if (lane == 0) s_wave[0][wave] = __popcll(eq);
-    __syncthreads();
-    int eq_before = equal0, eq_all = equal0;
+  const bool all = keep == n;
+  int above0 = 0, equal0 = 0;            // before this lot of entries
+  for (int i0 = 0; i0 < rounds && keep > 0; i0 += ROUNDS) {
+    auto marks = [&](int i, uint64_t* above, uint64_t* equal) __attribute__((always_inline)) {
+      const int j = (i0 + i) * kThreads + tid;
+      const uint32_t r = j < n ? rank(i, j) : 0u;
+      *above = __ballot(j < n && (all || r > prefix));
+      *equal = __ballot(j < n && !all && r == prefix);
+    };
 #pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) {
-      const int c = s_wave[0][w];
-      if (w < wave) eq_before += c;
-      eq_all += c;
+    for (int i = 0; i < ROUNDS; ++i) {
+      uint64_t a = 0, e = 0;
+      if (i0 + i < rounds) marks(i, &a, &e);
+      if (lane == 0) {
+        s_above[i * kWaves + wave] = __popcll(a);
+        s_equal[i * kWaves + wave] = __popcll(e);
+      }
     }
-    const bool stays = above || (equal && eq_before + __popcll(eq & lower) < left);
-    const uint64_t st = __ballot(stays);
-    if (lane == 0) s_wave[1][wave] = __popcll(st);
     __syncthreads();
-    int at = at0, all = at0;
+    // exclusive sums over (round, wave), by the first wave, ROUNDS * kWaves / 64 neighbours a lane
+    constexpr int PER = (ROUNDS * kWaves + 63) / 64;
+    if (wave == 0) {
+      int ca[PER], ce[PER], sa = 0, se = 0;
 #pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) {
-      const int c = s_wave[1][w];
-      if (w < wave) at += c;
-      all += c;
+      for (int k = 0; k < PER; ++k) {
+        const int x = lane * PER + k;
+        ca[k] = x < ROUNDS * kWaves ? s_above[x] : 0;
+        ce[k] = x < ROUNDS * kWaves ? s_equal[x] : 0;
+        sa += ca[k];
+        se += ce[k];
+      }
+      int ia = sa, ie = se;
+#pragma unroll
+      for (int k = 1; k < 64; k <<= 1) {
+        const int ua = __shfl_up(ia, k), ue = __shfl_up(ie, k);
+        if (lane >= k) {
+          ia += ua;
+          ie += ue;
+        }
+      }
+      ia += above0 - sa;
+      ie += equal0 - se;
+#pragma unroll
+      for (int k = 0; k < PER; ++k) {
+        const int x = lane * PER + k;
+        if (x < ROUNDS * kWaves) {
+          s_above[x] = ia;
+          s_equal[x] = ie;
+        }
+        ia += ca[k];
+        ie += ce[k];
+      }
+      if (lane == 63) {
+        s_digit = ia;
+        s_left = ie;
+      }
     }
-    at += __popcll(st & lower);
-    if (stays) {
-      p.kept[list + at] = j;
-      p.src_slot[list + at] = ids_old[j / CS_KV_BLOCK] * CS_KV_BLOCK + j % CS_KV_BLOCK;
-      p.dst_slot[list + at] = ids_new[at / CS_KV_BLOCK] * CS_KV_BLOCK + at % CS_KV_BLOCK;
-      p.delta[list + at] = p.renumber ? at - j : 0;
-      if (weight_new) weight_new[at] = weight[j];
+    __syncthreads();
+    const uint64_t lower = (1ull << lane) - 1;
+#pragma unroll
+    for (int i = 0; i < ROUNDS; ++i) {
+      if (i0 + i >= rounds) break;
+      uint64_t a, e;
+      marks(i, &a, &e);
+      const int before = s_equal[i * kWaves + wave] + __popcll(e & lower);
+      const bool stays = (a >> lane & 1) || ((e >> lane & 1) && before < left);
+      if (stays) {
+        const int j = (i0 + i) * kThreads + tid;
+        const int at = s_above[i * kWaves + wave] + __popcll(a & lower) + min(before, left);
+        p.kept[list + at] = j;
+        if (weight_new) weight_new[at] = HELD ? held[HELD ? i : 0] : weight[j];
+      }
     }
-    at0 = all;
-    equal0 = eq_all;
+    above0 = s_digit;
+    equal0 = s_left;
+    if (!HELD) __syncthreads();
   }
-  for (int i = keep + tid; i < p.budget; i += kThreads) {
-    p.kept[list + i] = -1;
-    p.src_slot[list + i] = -1;
-    p.dst_slot[list + i] = -1;
-    p.delta[list + i] = 0;
+  // slots of what is kept, in its order: four entries of a thread at once
+  __syncthreads();
+  for (int i0 = 0; i0 < p.budget; i0 += 4 * kThreads) {
+    int j[4], id_old[4], id_new[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int i = i0 + k * kThreads + tid;
+      j[k] = i < keep ? p.kept[list + i] : -1;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      id_old[k] = j[k] < 0 ? 0 : ids_old[j[k] / CS_KV_BLOCK];
+      id_new[k] = j[k] < 0 ? 0 : ids_new[(i0 + k * kThreads + tid) / CS_KV_BLOCK];
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int i = i0 + k * kThreads + tid;
+      if (i >= p.budget) break;
+      const bool none = j[k] < 0;
+      if (none) p.kept[list + i] = -1;
+      p.src_slot[list + i] = none ? -1 : id_old[k] * CS_KV_BLOCK + j[k] % CS_KV_BLOCK;
+      p.dst_slot[list + i] = none ? -1 : id_new[k] * CS_KV_BLOCK + i % CS_KV_BLOCK;
+      p.delta[list + i] = none || !p.renumber ? 0 : i - j[k];
+    }
   }
   if (tid == 0) p.kv_len_new[stream] = keep;
 }
@@ -169,6 +249,13 @@ extern "C" int cs_plan_evict(const float* weight, const int32_t* kv_len, const i
   p.n_first = n_first;
   p.n_last = n_last;
   p.renumber = renumber;
-  hipLaunchKernelGGL(plan_evict_kernel, dim3(static_cast<unsigned>(n_streams)), dim3(kThreads), 0, cs::as_stream(stream), p);
+  const dim3 grid(static_cast<unsigned>(n_streams));
+  hipStream_t st = cs::as_stream(stream);
+  const int entries = max_blocks_old * CS_KV_BLOCK;        // of the widest row there may be
+  if (entries <= kThreads) hipLaunchKernelGGL(plan_evict_kernel<1>, grid, dim3(kThreads), 0, st, p);
+  else if (entries <= 4 * kThreads) hipLaunchKernelGGL(plan_evict_kernel<4>, grid, dim3(kThreads), 0, st, p);
+  else if (entries <= 16 * kThreads) hipLaunchKernelGGL(plan_evict_kernel<16>, grid, dim3(kThreads), 0, st, p);
+  else if (entries <= 32 * kThreads) hipLaunchKernelGGL(plan_evict_kernel<32>, grid, dim3(kThreads), 0, st, p);
+  else hipLaunchKernelGGL(plan_evict_kernel<0>, grid, dim3(kThreads), 0, st, p);
   return cs::note_hip(hipGetLastError());
 }
