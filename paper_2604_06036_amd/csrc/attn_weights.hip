@@ -34,11 +34,13 @@ struct Params {
   cs::f32v2* ws_stat;                    // [n_q][n_q_heads][key_tiles]: maximum (log2 units), sum
   float* ws_part;                        // [chunks][n_kv_heads][n_streams][max_blocks * 16]
   int64_t n_q, stride_slot, stride_head;
-  int32_t max_blocks, n_streams, n_q_heads, n_kv_heads, group, key_tiles, chunks;
+  int32_t max_blocks, n_streams, n_q_heads, n_kv_heads, group, key_tiles, chunks, shares_per_xcd;
+  uint32_t group_inv;                    // 2^32 / group, rounded up (group 1: 0): rows below 2^28 are divided by a high product
   float scale_log2e, decay;
 };
 
 constexpr int kStep = 32;                // query rows of a step
+constexpr int kListed = 2048;            // steps of a stream that a workgroup sorts out
 constexpr int kGroups = 1024, kLeast = 4;      // workgroups wanted, steps that a share of a stream's rows has at least
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -62,14 +64,7 @@ __device__ __forceinline__ cs::u32x4 next_part(float* x) {
   return w;
 }
 
-__device__ __forceinline__ void load8(const float* p, float* x) {
-  const cs::u32x4 a = *reinterpret_cast<const cs::u32x4*>(p), b = *reinterpret_cast<const cs::u32x4*>(p + 4);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[i] = __uint_as_float(a[i]);
-    x[4 + i] = __uint_as_float(b[i]);
-  }
-}
+__device__ __forceinline__ int token_of(const Params& p, int row) { return p.group_inv ? static_cast<int>(__umulhi(static_cast<uint32_t>(row), p.group_inv)) : row; }
 
 __device__ __forceinline__ int stream_entries(const Params& p, int s) { return min(p.kv_len[s], p.max_blocks * CS_KV_BLOCK); }
 
@@ -83,79 +78,114 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
   __shared__ __attribute__((aligned(16))) float s_lse[2][kStep];
   __shared__ __attribute__((aligned(16))) int s_pos[2][kStep];
   __shared__ float s_m[2][4][kStep], s_l[2][4][kStep];
+  __shared__ uint16_t s_list[kListed];
+  __shared__ int s_count[4];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, h = lane >> 5;
   // ---- which keys, which rows
-  int job = blockIdx.x;
-  const int chunk = job % p.chunks;
-  job /= p.chunks;
-  const int kt = job % p.key_tiles;
-  job /= p.key_tiles;
-  const int kvh = job % p.n_kv_heads, stream = job / p.n_kv_heads;
+  // (workgroups go round the eight XCDs: where there are enough, the key tiles that read the same rows follow each other on one)
+  int kt, share_of;
+  if (p.shares_per_xcd) {
+    const int turn = static_cast<int>(blockIdx.x / 8);
+    kt = turn % p.key_tiles;
+    share_of = turn / p.key_tiles * 8 + static_cast<int>(blockIdx.x % 8);
+  } else {
+    kt = static_cast<int>(blockIdx.x) % p.key_tiles;
+    share_of = static_cast<int>(blockIdx.x) / p.key_tiles;
+  }
+  const int chunk = share_of % p.chunks, kvh = share_of / p.chunks % p.n_kv_heads, stream = share_of / p.chunks / p.n_kv_heads;
+  if (stream >= p.n_streams) return;
   const int entries = stream_entries(p, stream);
   if (kt * TILE >= entries) return;
   const int q0 = p.cu_q[stream];
   const int rows = max(0, min(p.cu_q[stream + 1], static_cast<int>(p.n_q)) - q0) * p.group;
-  const int steps = (rows + kStep - 1) / kStep, share = (steps + p.chunks - 1) / p.chunks;
-  const int step_begin = chunk * share, step_end = min(steps, step_begin + share);
+  const int steps = (rows + kStep - 1) / kStep;
   const int tile0 = kt * TILE, key0 = tile0 + wave * 32 * KB;
 
-  // ---- keys: operand layout, lane n is a key, 8 h + 0..7 its elements of a step
-  bf16x8 kf[KP][KB][STEPS];
+  // ---- keys, as they lie in the cache: lane n is a key, of whose elements it takes 64 i + 32 h + 0..31 (one 4-bit block); asked for
+  // before the steps are looked over
+  constexpr int RAW = CACHE == CS_KV4 ? 1 : CACHE == CS_BF16 ? 4 : 8;       // 16-byte vectors of 32 elements
+  cs::u32x4 k_raw[KB][D / 64][RAW];
+  uint32_t k_scale[KB];
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb) {
     const int key = min(key0 + 32 * kb + n, entries - 1);
     const int64_t at = (static_cast<int64_t>(p.block_table[static_cast<int64_t>(stream) * p.max_blocks + key / CS_KV_BLOCK]) * CS_KV_BLOCK + key % CS_KV_BLOCK) * p.stride_slot +
-                       static_cast<int64_t>(kvh) * p.stride_head + 8 * h;
+                       static_cast<int64_t>(kvh) * p.stride_head;
+    constexpr int BITS = CACHE == CS_KV4 ? 4 : CACHE == CS_BF16 ? 16 : 32;
+    const char* src = static_cast<const char*>(p.k) + at * BITS / 8 + 4 * BITS * h;
 #pragma unroll
-    for (int st = 0; st < STEPS; ++st) {
-      if (CACHE == CS_KV4) {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(p.k) + (at + 16 * st) / 2);
-        const uint32_t e = p.k_scales[(at + 16 * st) / cs::kKv4Block];
-        cs::u32x4 x = cs::kv4_unpack8_bf16(w, cs::kv4_scale(e));
-        if (e == cs::kKv4NoNumber) x = cs::u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
-        kf[0][kb][st] = __builtin_bit_cast(bf16x8, x);
-      } else if (CACHE == CS_BF16) {
-        kf[0][kb][st] = *reinterpret_cast<const bf16x8*>(static_cast<const uint16_t*>(p.k) + at + 16 * st);
-      } else {
-        float x[8];
-        load8(static_cast<const float*>(p.k) + at + 16 * st, x);
+    for (int i = 0; i < D / 64; ++i)
 #pragma unroll
-        for (int part = 0; part < KP; ++part) kf[part][kb][st] = __builtin_bit_cast(bf16x8, next_part(x));
-      }
+      for (int w = 0; w < RAW; ++w) k_raw[kb][i][w] = *reinterpret_cast<const cs::u32x4*>(src + 8 * BITS * i + 16 * w);
+    k_scale[kb] = 0;
+    if (CACHE == CS_KV4) {
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) k_scale[kb] |= static_cast<uint32_t>(p.k_scales[at / cs::kKv4Block + 2 * i + h]) << (8 * i);
     }
   }
 
-  // ---- query rows: asked for a step ahead
-  cs::u32x4 raw[CHUNKS][QP == 1 ? 1 : 2];
-  int next_pos = -1;
-  float next_lse = 0.0f;
-  auto request = [&](int step) __attribute__((always_inline)) {
+  // ---- the steps with a row that sees a key of the tile; shares are of those (of more steps than the list holds: of all)
+  const bool listed = steps <= kListed;
+  int n_active = steps;
+  if (listed) {
+    n_active = 0;
+    for (int s0 = 0; s0 < steps; s0 += 256) {
+      const int st = s0 + tid;
+      bool active = false;
+      if (st < steps) {
+        const int t0 = token_of(p, st * kStep), t1 = token_of(p, min(st * kStep + kStep, rows) - 1);
+        for (int t = t0; t <= t1; ++t) active |= p.q_pos[q0 + t] >= tile0;
+      }
+      const uint64_t in_wave = __ballot(active);
+      if (lane == 0) s_count[wave] = __popcll(in_wave);
+      __syncthreads();
+      int before = n_active, all = n_active;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        before += w < wave ? s_count[w] : 0;
+        all += s_count[w];
+      }
+      if (active) s_list[before + __popcll(in_wave & ((1ull << lane) - 1))] = static_cast<uint16_t>(st);
+      n_active = all;
+      __syncthreads();
+    }
+  }
+  const int share = (n_active + p.chunks - 1) / p.chunks;
+  const int step_begin = chunk * share, step_end = min(n_active, step_begin + share);
+  auto step_at = [&](int i) __attribute__((always_inline)) { return listed ? static_cast<int>(s_list[i]) : i; };
+
+  // ---- query rows: asked for two steps ahead
+  constexpr int QB = QP == 1 ? 2 : 4;                      // bytes of an element
+  const char* const q_base = static_cast<const char*>(p.q) + (static_cast<int64_t>(q0) * p.n_q_heads + kvh * p.group) * (D * QB);
+  const float* const lse_base = STATS ? nullptr : p.lse + static_cast<int64_t>(q0) * p.n_q_heads + kvh * p.group;
+  const uint32_t tok_bytes = static_cast<uint32_t>(p.n_q_heads) * (D * QB);
+  cs::u32x4 raw[2][CHUNKS][QP == 1 ? 1 : 2];
+  int next_pos[2] = {-1, -1};
+  float next_lse[2] = {0.0f, 0.0f};
+  auto request = [&](int index, int at) __attribute__((always_inline)) {
+    const int step = step_at(index);
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i) {
-      const int c = tid + 256 * i, r = min(step * kStep + c / (D / 8), rows - 1);
-      const int64_t at = (static_cast<int64_t>(q0 + r / p.group) * p.n_q_heads + kvh * p.group + r % p.group) * D + 8 * (c % (D / 8));
-      if (QP == 1) {
-        raw[i][0] = *reinterpret_cast<const cs::u32x4*>(static_cast<const uint16_t*>(p.q) + at);
-      } else {
-        raw[i][0] = *reinterpret_cast<const cs::u32x4*>(static_cast<const float*>(p.q) + at);
-        raw[i][QP == 1 ? 0 : 1] = *reinterpret_cast<const cs::u32x4*>(static_cast<const float*>(p.q) + at + 4);
-      }
+      const int c = tid + 256 * i, r = min(step * kStep + c / (D / 8), rows - 1), tok = token_of(p, r);
+      const char* src = q_base + static_cast<uint64_t>(tok) * tok_bytes + ((r - tok * p.group) * D + 8 * (c % (D / 8))) * QB;
+      raw[at][i][0] = *reinterpret_cast<const cs::u32x4*>(src);
+      if (QP != 1) raw[at][i][QP == 1 ? 0 : 1] = *reinterpret_cast<const cs::u32x4*>(src + 16);
     }
     if (tid < kStep) {
       const int r = step * kStep + tid;
-      next_pos = -1;                                       // rows past the last, like those of a negative position: see nothing
-      next_lse = 0.0f;
+      next_pos[at] = -1;                                   // rows past the last, like those of a negative position: see nothing
+      next_lse[at] = 0.0f;
       if (r < rows) {
-        const int tok = q0 + r / p.group;
-        next_pos = min(p.q_pos[tok], entries - 1);
-        if (!STATS && next_pos >= 0) next_lse = p.lse[static_cast<int64_t>(tok) * p.n_q_heads + kvh * p.group + r % p.group] * kLog2e;
+        const int tok = token_of(p, r);
+        next_pos[at] = min(p.q_pos[q0 + tok], entries - 1);
+        if (!STATS && next_pos[at] >= 0) next_lse[at] = lse_base[static_cast<int64_t>(tok) * p.n_q_heads + (r - tok * p.group)] * kLog2e;
       }
     }
   };
   // (STATS) a step's maxima and sums of the four waves joined, left for the launch that joins key ranges
-  auto join = [&](int step, int buf) __attribute__((always_inline)) {
-    const int r = step * kStep + tid;
+  auto join = [&](int index, int buf) __attribute__((always_inline)) {
+    const int r = step_at(index) * kStep + tid;
     if (tid < kStep && r < rows) {
       float m = s_m[buf][0][tid];
 #pragma unroll
@@ -163,35 +193,72 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
       float l = 0.0f;
 #pragma unroll
       for (int w = 0; w < 4; ++w) l += m == -INFINITY ? s_l[buf][w][tid] : s_l[buf][w][tid] * __builtin_amdgcn_exp2f(s_m[buf][w][tid] - m);
-      p.ws_stat[(static_cast<int64_t>(q0 + r / p.group) * p.n_q_heads + kvh * p.group + r % p.group) * p.key_tiles + kt] = cs::f32v2{m, l};
+      const int tok = token_of(p, r);
+      p.ws_stat[(static_cast<int64_t>(q0 + tok) * p.n_q_heads + kvh * p.group + (r - tok * p.group)) * p.key_tiles + kt] = cs::f32v2{m, l};
+    }
+  };
+
+  // ---- keys as operands: elements 64 i + 32 h + 8 w + 0..7 in step 4 i + w
+  bf16x8 kf[KP][KB][STEPS];
+  auto unpack = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          if (CACHE == CS_KV4) {
+            const uint32_t e = k_scale[kb] >> (8 * i) & 255u;
+            kf[0][kb][4 * i + w] = __builtin_bit_cast(bf16x8, cs::kv4_unpack8_bf16(k_raw[kb][i][0][w], cs::kv4_scale(e)));
+          } else if (CACHE == CS_BF16) {
+            kf[0][kb][4 * i + w] = __builtin_bit_cast(bf16x8, k_raw[kb][i][RAW == 4 ? w : 0]);
+          } else {
+            float x[8];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              x[c] = __uint_as_float(k_raw[kb][i][RAW == 8 ? 2 * w : 0][c]);
+              x[4 + c] = __uint_as_float(k_raw[kb][i][RAW == 8 ? 2 * w + 1 : 0][c]);
+            }
+#pragma unroll
+            for (int part = 0; part < KP; ++part) kf[part][kb][4 * i + w] = __builtin_bit_cast(bf16x8, next_part(x));
+          }
+        }
+    if (CACHE == CS_KV4) {                                 // (blocks without numbers: rare)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i)
+          if (__builtin_expect((k_scale[kb] >> (8 * i) & 255u) == cs::kKv4NoNumber, 0)) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) kf[0][kb][4 * i + w] = __builtin_bit_cast(bf16x8, cs::u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u});
+          }
     }
   };
 
   float acc[KB] = {};
-  if (step_begin < step_end) request(step_begin);
-  for (int step = step_begin; step < step_end; ++step) {
-    const int buf = (step - step_begin) & 1;
+  auto do_step = [&](int step, auto stage) __attribute__((always_inline)) {
+    constexpr int buf = decltype(stage)::value;
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i) {
       const int c = tid + 256 * i, at = (c / (D / 8)) * QROW + 8 * (c % (D / 8));
       if (QP == 1) {
-        *reinterpret_cast<cs::u32x4*>(&s_q[buf][0][at]) = raw[i][0];
+        *reinterpret_cast<cs::u32x4*>(&s_q[buf][0][at]) = raw[buf][i][0];
       } else {
         float x[8];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          x[e] = __uint_as_float(raw[i][0][e]);
-          x[4 + e] = __uint_as_float(raw[i][QP == 1 ? 0 : 1][e]);
+          x[e] = __uint_as_float(raw[buf][i][0][e]);
+          x[4 + e] = __uint_as_float(raw[buf][i][QP == 1 ? 0 : 1][e]);
         }
 #pragma unroll
         for (int part = 0; part < QP; ++part) *reinterpret_cast<cs::u32x4*>(&s_q[buf][part][at]) = next_part(x);
       }
     }
     if (tid < kStep) {
-      s_pos[buf][tid] = next_pos;
-      if (!STATS) s_lse[buf][tid] = next_lse;
+      s_pos[buf][tid] = next_pos[buf];
+      if (!STATS) s_lse[buf][tid] = next_lse[buf];
     }
-    if (step + 1 < step_end) request(step + 1);
+    if (step + 2 < step_end) request(step + 2, buf);
     __syncthreads();
     if (STATS && step > step_begin) join(step - 1, buf ^ 1);
 
@@ -204,7 +271,7 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
       for (int st = 0; st < STEPS; ++st) {
         bf16x8 qf[QP];
 #pragma unroll
-        for (int part = 0; part < QP; ++part) qf[part] = *reinterpret_cast<const bf16x8*>(&s_q[buf][part][n * QROW + 16 * st + 8 * h]);
+        for (int part = 0; part < QP; ++part) qf[part] = *reinterpret_cast<const bf16x8*>(&s_q[buf][part][n * QROW + 64 * (st / 4) + 32 * h + 8 * (st % 4)]);
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -273,6 +340,13 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
       s_m[buf][wave][n] = -INFINITY;
       s_l[buf][wave][n] = 0.0f;
     }
+  };
+  if (step_begin < step_end) request(step_begin, 0);
+  if (step_begin + 1 < step_end) request(step_begin + 1, 1);
+  unpack();
+  for (int step = step_begin; step < step_end; step += 2) {
+    do_step(step, std::integral_constant<int, 0>());
+    if (step + 1 < step_end) do_step(step + 1, std::integral_constant<int, 1>());
   }
   if (STATS) {
     if (step_begin < step_end) {
@@ -361,7 +435,9 @@ Layout layout(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_he
 
 template <int D, int CACHE, int QP>
 int launch(Params p, const Layout& w, bool have_lse, hipStream_t st) {
-  const int64_t jobs = static_cast<int64_t>(p.n_streams) * p.n_kv_heads * w.key_tiles * w.chunks;
+  const int64_t shares = static_cast<int64_t>(p.n_streams) * p.n_kv_heads * w.chunks;
+  p.shares_per_xcd = shares >= 64;       // (few shares would load the XCDs unevenly)
+  const int64_t jobs = (p.shares_per_xcd ? (shares + 7) / 8 * 8 : shares) * w.key_tiles;
   if (jobs > 0x7fffffffll) return CS_EUNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(jobs));
   const int64_t all = static_cast<int64_t>(p.max_blocks) * CS_KV_BLOCK * p.n_streams;
@@ -400,7 +476,7 @@ extern "C" int cs_attn_weights(const void* q, const float* lse, const void* k_ca
   if ((head_dim != 64 && head_dim != 128) || block_size != CS_KV_BLOCK || n_q_heads / n_kv_heads > 16) return CS_EUNSUPPORTED;
   const int unit = cache_dtype == CS_KV4 ? cs::kKv4Block : cache_dtype == CS_BF16 ? 8 : 4;
   if (stride_slot % unit || stride_head % unit) return CS_EUNSUPPORTED;
-  if (n_q > 0x7fffffffll / n_q_heads || max_blocks > 0x7fffffff / CS_KV_BLOCK) return CS_EUNSUPPORTED;
+  if (n_q > 0x7fffffffll / n_q_heads || n_q * (n_q_heads / n_kv_heads) >= (1 << 28) || max_blocks > 0x7fffffff / CS_KV_BLOCK) return CS_EUNSUPPORTED;
   if (static_cast<int64_t>(max_blocks) * CS_KV_BLOCK * n_streams > 0x7fffffffll * 255) return CS_EUNSUPPORTED;
   if (n_streams == 0) return CS_OK;
   if (!kv_len || !weight_out || max_blocks < 1) return CS_EINVAL;
@@ -445,6 +521,7 @@ extern "C" int cs_attn_weights(const void* q, const float* lse, const void* k_ca
   p.n_q_heads = n_q_heads;
   p.n_kv_heads = n_kv_heads;
   p.group = n_q_heads / n_kv_heads;
+  p.group_inv = p.group == 1 ? 0u : static_cast<uint32_t>(((1ull << 32) + p.group - 1) / p.group);
   p.key_tiles = w.key_tiles;
   p.chunks = w.chunks;
   p.scale_log2e = softmax_scale * kLog2e;

@@ -51,15 +51,19 @@ __global__ __launch_bounds__(kThreads) void plan_evict_kernel(Params p) {
   const float* weight = p.weight + static_cast<int64_t>(stream) * row_old;
   const int first = p.n_first, last = max(0, n - min(p.n_last, n));
   const int rounds = (n + kThreads - 1) / kThreads;
-  float held[HELD ? HELD : 1];
+  auto rank_at = [&](int j) __attribute__((always_inline)) { return rank_of(weight[j], j < first || j >= last); };
+  uint32_t held[HELD ? HELD : 1];
   if (HELD) {
+    float w[HELD ? HELD : 1];
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) w[i] = i * kThreads + tid < n ? weight[i * kThreads + tid] : 0.0f;
 #pragma unroll
     for (int i = 0; i < HELD; ++i) {
       const int j = i * kThreads + tid;
-      held[i] = j < n ? weight[j] : 0.0f;
+      held[i] = rank_of(w[i], j < first || j >= last);
     }
   }
-  auto rank = [&](int i, int j) __attribute__((always_inline)) { return rank_of(HELD ? held[HELD ? i : 0] : weight[j], j < first || j >= last); };
+  auto rank = [&](int i, int j) __attribute__((always_inline)) { return HELD ? held[HELD ? i : 0] : rank_at(j); };
 
   // ---- the smallest rank that stays, and how many entries of that rank
   uint32_t prefix = 0, mask = 0;
@@ -185,7 +189,6 @@ __global__ __launch_bounds__(kThreads) void plan_evict_kernel(Params p) {
         const int j = (i0 + i) * kThreads + tid;
         const int at = s_above[i * kWaves + wave] + __popcll(a & lower) + min(before, left);
         p.kept[list + at] = j;
-        if (weight_new) weight_new[at] = HELD ? held[HELD ? i : 0] : weight[j];
       }
     }
     above0 = s_digit;
@@ -196,6 +199,7 @@ __global__ __launch_bounds__(kThreads) void plan_evict_kernel(Params p) {
   __syncthreads();
   for (int i0 = 0; i0 < p.budget; i0 += 4 * kThreads) {
     int j[4], id_old[4], id_new[4];
+    float w[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int i = i0 + k * kThreads + tid;
@@ -205,6 +209,7 @@ __global__ __launch_bounds__(kThreads) void plan_evict_kernel(Params p) {
     for (int k = 0; k < 4; ++k) {
       id_old[k] = j[k] < 0 ? 0 : ids_old[j[k] / CS_KV_BLOCK];
       id_new[k] = j[k] < 0 ? 0 : ids_new[(i0 + k * kThreads + tid) / CS_KV_BLOCK];
+      w[k] = j[k] < 0 ? 0.0f : weight[j[k]];
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -215,6 +220,7 @@ __global__ __launch_bounds__(kThreads) void plan_evict_kernel(Params p) {
       p.src_slot[list + i] = none ? -1 : id_old[k] * CS_KV_BLOCK + j[k] % CS_KV_BLOCK;
       p.dst_slot[list + i] = none ? -1 : id_new[k] * CS_KV_BLOCK + i % CS_KV_BLOCK;
       p.delta[list + i] = none || !p.renumber ? 0 : i - j[k];
+      if (weight_new && !none) weight_new[i] = w[k];
     }
   }
   if (tid == 0) p.kv_len_new[stream] = keep;
