@@ -74,12 +74,16 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
   constexpr int TILE = keys_per_tile(CACHE);
   constexpr int QROW = D + 8;                              // padded LDS row
   constexpr int CHUNKS = kStep * D / 8 / 256;              // 8-element pieces of a step's rows a thread moves (D 64: 1, D 128: 2)
-  __shared__ __attribute__((aligned(16))) uint16_t s_q[2][QP][kStep * QROW];
+  constexpr int EB = CACHE == CS_BF16 ? 2 : 4;             // bytes of a key's element (caches that are not of 4 bits)
+  constexpr int KROW = D * EB + 16;                        // padded LDS row of a key on its way, bytes
+  constexpr int Q_BYTES = 2 * QP * kStep * QROW * 2, K_BYTES = CACHE == CS_KV4 ? 0 : 4 * 32 * KROW;
+  __shared__ __attribute__((aligned(16))) char s_mem[Q_BYTES > K_BYTES ? Q_BYTES : K_BYTES];
+  uint16_t (*const s_q)[QP][kStep * QROW] = reinterpret_cast<uint16_t (*)[QP][kStep * QROW]>(s_mem);
   __shared__ __attribute__((aligned(16))) float s_lse[2][kStep];
   __shared__ __attribute__((aligned(16))) int s_pos[2][kStep];
   __shared__ float s_m[2][4][kStep], s_l[2][4][kStep];
   __shared__ uint16_t s_list[kListed];
-  __shared__ int s_count[4];
+  __shared__ uint32_t s_bits[kListed / 32];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, h = lane >> 5;
   // ---- which keys, which rows
@@ -102,26 +106,32 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
   const int steps = (rows + kStep - 1) / kStep;
   const int tile0 = kt * TILE, key0 = tile0 + wave * 32 * KB;
 
-  // ---- keys, as they lie in the cache: lane n is a key, of whose elements it takes 64 i + 32 h + 0..31 (one 4-bit block); asked for
-  // before the steps are looked over
-  constexpr int RAW = CACHE == CS_KV4 ? 1 : CACHE == CS_BF16 ? 4 : 8;       // 16-byte vectors of 32 elements
-  cs::u32x4 k_raw[KB][D / 64][RAW];
+  // ---- keys, asked for before the steps are looked over.  4-bit: lane n is a key, of whose elements it takes 64 i + 32 h + 0..31, one
+  // block.  Others: whole rows by neighbouring lanes, to change places in LDS (16 bytes of each of 32 rows a load would cost the
+  // address unit four times as much).
+  const int32_t* ids = p.block_table + static_cast<int64_t>(stream) * p.max_blocks;
+  constexpr int LANES = D * EB / 16, ROWS = 64 / LANES;    // lanes of a row, rows of a load
+  constexpr int RAW = CACHE == CS_KV4 ? D / 64 : 32 / ROWS;
+  cs::u32x4 k_raw[KB][RAW];
   uint32_t k_scale[KB];
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb) {
-    const int key = min(key0 + 32 * kb + n, entries - 1);
-    const int64_t at = (static_cast<int64_t>(p.block_table[static_cast<int64_t>(stream) * p.max_blocks + key / CS_KV_BLOCK]) * CS_KV_BLOCK + key % CS_KV_BLOCK) * p.stride_slot +
-                       static_cast<int64_t>(kvh) * p.stride_head;
-    constexpr int BITS = CACHE == CS_KV4 ? 4 : CACHE == CS_BF16 ? 16 : 32;
-    const char* src = static_cast<const char*>(p.k) + at * BITS / 8 + 4 * BITS * h;
-#pragma unroll
-    for (int i = 0; i < D / 64; ++i)
-#pragma unroll
-      for (int w = 0; w < RAW; ++w) k_raw[kb][i][w] = *reinterpret_cast<const cs::u32x4*>(src + 8 * BITS * i + 16 * w);
     k_scale[kb] = 0;
     if (CACHE == CS_KV4) {
+      const int key = min(key0 + 32 * kb + n, entries - 1);
+      const int64_t at = (static_cast<int64_t>(ids[key / CS_KV_BLOCK]) * CS_KV_BLOCK + key % CS_KV_BLOCK) * p.stride_slot + static_cast<int64_t>(kvh) * p.stride_head;
 #pragma unroll
-      for (int i = 0; i < D / 64; ++i) k_scale[kb] |= static_cast<uint32_t>(p.k_scales[at / cs::kKv4Block + 2 * i + h]) << (8 * i);
+      for (int i = 0; i < D / 64; ++i) {
+        k_raw[kb][i] = *reinterpret_cast<const cs::u32x4*>(static_cast<const char*>(p.k) + at / 2 + 32 * i + 16 * h);
+        k_scale[kb] |= static_cast<uint32_t>(p.k_scales[at / cs::kKv4Block + 2 * i + h]) << (8 * i);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < RAW; ++j) {
+        const int key = min(key0 + 32 * kb + ROWS * j + lane / LANES, entries - 1);
+        const int64_t at = (static_cast<int64_t>(ids[key / CS_KV_BLOCK]) * CS_KV_BLOCK + key % CS_KV_BLOCK) * p.stride_slot + static_cast<int64_t>(kvh) * p.stride_head;
+        k_raw[kb][j] = *reinterpret_cast<const cs::u32x4*>(static_cast<const char*>(p.k) + at * EB + 16 * (lane % LANES));
+      }
     }
   }
 
@@ -129,40 +139,39 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
   const bool listed = steps <= kListed;
   int n_active = steps;
   if (listed) {
-    n_active = 0;
-    for (int s0 = 0; s0 < steps; s0 += 256) {
-      const int st = s0 + tid;
-      bool active = false;
-      if (st < steps) {
-        const int t0 = token_of(p, st * kStep), t1 = token_of(p, min(st * kStep + kStep, rows) - 1);
-        for (int t = t0; t <= t1; ++t) active |= p.q_pos[q0 + t] >= tile0;
+    if (tid < kListed / 32) s_bits[tid] = 0;
+    __syncthreads();
+    for (int t = tid; t * p.group < rows; t += 256) {      // a token's rows lie in one step, or two
+      if (p.q_pos[q0 + t] >= tile0) {
+        const int s0 = t * p.group / kStep, s1 = (t * p.group + p.group - 1) / kStep;
+        atomicOr(&s_bits[s0 / 32], 1u << (s0 % 32));
+        if (s1 != s0) atomicOr(&s_bits[s1 / 32], 1u << (s1 % 32));
       }
-      const uint64_t in_wave = __ballot(active);
-      if (lane == 0) s_count[wave] = __popcll(in_wave);
-      __syncthreads();
-      int before = n_active, all = n_active;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        before += w < wave ? s_count[w] : 0;
-        all += s_count[w];
-      }
-      if (active) s_list[before + __popcll(in_wave & ((1ull << lane) - 1))] = static_cast<uint16_t>(st);
-      n_active = all;
-      __syncthreads();
     }
+    __syncthreads();
+    n_active = 0;
+    for (int s0 = 0; s0 < steps; s0 += 64) {               // (every wave writes the same list)
+      const int st = s0 + lane;
+      const uint64_t in = static_cast<uint64_t>(s_bits[s0 / 32 + 1]) << 32 | s_bits[s0 / 32];
+      if (in >> lane & 1) s_list[n_active + __popcll(in & ((1ull << lane) - 1))] = static_cast<uint16_t>(st);
+      n_active += __popcll(in);
+    }
+    n_active = __builtin_amdgcn_readfirstlane(n_active);
+    __syncthreads();
   }
   const int share = (n_active + p.chunks - 1) / p.chunks;
   const int step_begin = chunk * share, step_end = min(n_active, step_begin + share);
   auto step_at = [&](int i) __attribute__((always_inline)) { return listed ? static_cast<int>(s_list[i]) : i; };
 
-  // ---- query rows: asked for two steps ahead
+  // ---- query rows: asked for AHEAD steps ahead (a step takes a fraction of their latency)
+  constexpr int AHEAD = QP == 1 ? 4 : 2;
   constexpr int QB = QP == 1 ? 2 : 4;                      // bytes of an element
   const char* const q_base = static_cast<const char*>(p.q) + (static_cast<int64_t>(q0) * p.n_q_heads + kvh * p.group) * (D * QB);
   const float* const lse_base = STATS ? nullptr : p.lse + static_cast<int64_t>(q0) * p.n_q_heads + kvh * p.group;
   const uint32_t tok_bytes = static_cast<uint32_t>(p.n_q_heads) * (D * QB);
-  cs::u32x4 raw[2][CHUNKS][QP == 1 ? 1 : 2];
-  int next_pos[2] = {-1, -1};
-  float next_lse[2] = {0.0f, 0.0f};
+  cs::u32x4 raw[AHEAD][CHUNKS][QP == 1 ? 1 : 2];
+  int next_pos[AHEAD];
+  float next_lse[AHEAD];
   auto request = [&](int index, int at) __attribute__((always_inline)) {
     const int step = step_at(index);
 #pragma unroll
@@ -172,15 +181,10 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
       raw[at][i][0] = *reinterpret_cast<const cs::u32x4*>(src);
       if (QP != 1) raw[at][i][QP == 1 ? 0 : 1] = *reinterpret_cast<const cs::u32x4*>(src + 16);
     }
-    if (tid < kStep) {
-      const int r = step * kStep + tid;
-      next_pos[at] = -1;                                   // rows past the last, like those of a negative position: see nothing
-      next_lse[at] = 0.0f;
-      if (r < rows) {
-        const int tok = token_of(p, r);
-        next_pos[at] = min(p.q_pos[q0 + tok], entries - 1);
-        if (!STATS && next_pos[at] >= 0) next_lse[at] = lse_base[static_cast<int64_t>(tok) * p.n_q_heads + (r - tok * p.group)] * kLog2e;
-      }
+    if (tid < kStep) {                                     // (used as they come when the step's turn is there: no wait in between)
+      const int r = min(step * kStep + tid, rows - 1), tok = token_of(p, r);
+      next_pos[at] = p.q_pos[q0 + tok];
+      if (!STATS) next_lse[at] = lse_base[static_cast<int64_t>(tok) * p.n_q_heads + (r - tok * p.group)];
     }
   };
   // (STATS) a step's maxima and sums of the four waves joined, left for the launch that joins key ranges
@@ -202,27 +206,39 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
   bf16x8 kf[KP][KB][STEPS];
   auto unpack = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
+    for (int kb = 0; kb < KB; ++kb) {
+      char* const mine = s_mem + wave * 32 * KROW;         // (a wave's own; its LDS operations keep their order)
+      if (CACHE != CS_KV4) {
+#pragma unroll
+        for (int j = 0; j < RAW; ++j)
+          *reinterpret_cast<cs::u32x4*>(mine + (ROWS * j + lane / LANES) * KROW + 16 * (lane % LANES)) = k_raw[kb][j];
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      }
 #pragma unroll
       for (int i = 0; i < D / 64; ++i)
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
+          const char* at = mine + n * KROW + (64 * i + 32 * h + 8 * w) * EB;
           if (CACHE == CS_KV4) {
             const uint32_t e = k_scale[kb] >> (8 * i) & 255u;
-            kf[0][kb][4 * i + w] = __builtin_bit_cast(bf16x8, cs::kv4_unpack8_bf16(k_raw[kb][i][0][w], cs::kv4_scale(e)));
+            kf[0][kb][4 * i + w] = __builtin_bit_cast(bf16x8, cs::kv4_unpack8_bf16(k_raw[kb][CACHE == CS_KV4 ? i : 0][w], cs::kv4_scale(e)));
           } else if (CACHE == CS_BF16) {
-            kf[0][kb][4 * i + w] = __builtin_bit_cast(bf16x8, k_raw[kb][i][RAW == 4 ? w : 0]);
+            kf[0][kb][4 * i + w] = *reinterpret_cast<const bf16x8*>(at);
           } else {
+            const cs::u32x4 lo = *reinterpret_cast<const cs::u32x4*>(at), hi = *reinterpret_cast<const cs::u32x4*>(at + 16);
             float x[8];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-              x[c] = __uint_as_float(k_raw[kb][i][RAW == 8 ? 2 * w : 0][c]);
-              x[4 + c] = __uint_as_float(k_raw[kb][i][RAW == 8 ? 2 * w + 1 : 0][c]);
+              x[c] = __uint_as_float(lo[c]);
+              x[4 + c] = __uint_as_float(hi[c]);
             }
 #pragma unroll
             for (int part = 0; part < KP; ++part) kf[part][kb][4 * i + w] = __builtin_bit_cast(bf16x8, next_part(x));
           }
         }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    }
     if (CACHE == CS_KV4) {                                 // (blocks without numbers: rare)
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
@@ -237,28 +253,30 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
 
   float acc[KB] = {};
   auto do_step = [&](int step, auto stage) __attribute__((always_inline)) {
-    constexpr int buf = decltype(stage)::value;
+    constexpr int at_stage = decltype(stage)::value, buf = at_stage & 1;
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i) {
       const int c = tid + 256 * i, at = (c / (D / 8)) * QROW + 8 * (c % (D / 8));
       if (QP == 1) {
-        *reinterpret_cast<cs::u32x4*>(&s_q[buf][0][at]) = raw[buf][i][0];
+        *reinterpret_cast<cs::u32x4*>(&s_q[buf][0][at]) = raw[at_stage][i][0];
       } else {
         float x[8];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          x[e] = __uint_as_float(raw[buf][i][0][e]);
-          x[4 + e] = __uint_as_float(raw[buf][i][QP == 1 ? 0 : 1][e]);
+          x[e] = __uint_as_float(raw[at_stage][i][0][e]);
+          x[4 + e] = __uint_as_float(raw[at_stage][i][QP == 1 ? 0 : 1][e]);
         }
 #pragma unroll
         for (int part = 0; part < QP; ++part) *reinterpret_cast<cs::u32x4*>(&s_q[buf][part][at]) = next_part(x);
       }
     }
     if (tid < kStep) {
-      s_pos[buf][tid] = next_pos[buf];
-      if (!STATS) s_lse[buf][tid] = next_lse[buf];
+      // rows past the last, like those of a negative position, see nothing
+      const int pos = step_at(step) * kStep + tid < rows ? min(next_pos[at_stage], entries - 1) : -1;
+      s_pos[buf][tid] = pos;
+      if (!STATS) s_lse[buf][tid] = pos >= 0 ? next_lse[at_stage] * kLog2e : 0.0f;
     }
-    if (step + 2 < step_end) request(step + 2, buf);
+    if (step + AHEAD < step_end) request(step + AHEAD, at_stage);
     __syncthreads();
     if (STATS && step > step_begin) join(step - 1, buf ^ 1);
 
@@ -341,12 +359,18 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
       s_l[buf][wave][n] = 0.0f;
     }
   };
-  if (step_begin < step_end) request(step_begin, 0);
-  if (step_begin + 1 < step_end) request(step_begin + 1, 1);
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (step_begin + i < step_end) request(step_begin + i, i);
   unpack();
-  for (int step = step_begin; step < step_end; step += 2) {
+  if (CACHE != CS_KV4) __syncthreads();                    // (what the keys passed through becomes the rows')
+  for (int step = step_begin; step < step_end; step += AHEAD) {
     do_step(step, std::integral_constant<int, 0>());
     if (step + 1 < step_end) do_step(step + 1, std::integral_constant<int, 1>());
+    if constexpr (AHEAD == 4) {
+      if (step + 2 < step_end) do_step(step + 2, std::integral_constant<int, 2>());
+      if (step + 3 < step_end) do_step(step + 3, std::integral_constant<int, 3>());
+    }
   }
   if (STATS) {
     if (step_begin < step_end) {

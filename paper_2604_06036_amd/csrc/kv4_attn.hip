@@ -414,17 +414,25 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 3 : D == 64 ? 2 : 1) void kv4_row
   const uint8_t* const my_scale = scales + at_row / cs::kKv4Block;
   // Two tiles are under way while one is computed on: a tile of 32 keys takes less time than its codes.
   cs::u32x4 code[2];
-  uint32_t scale[2], id;
+  uint32_t scale[2];
+  // A wave's rows lie in one cache block (head_dim 64: two): its id is the same in all lanes, and a scalar load keeps out of the
+  // queue of vector loads, in which waiting for it would be waiting for the codes asked for before.
+  const int last_block = max(last, 0) / CS_KV_BLOCK, first_block = (wave & 1) * (T / CS_KV_BLOCK / 2);
+  int id[2];
+  auto request_id = [&](int kt) __attribute__((always_inline)) {
+#pragma unroll
+    for (int b = 0; b < T / CS_KV_BLOCK / 2; ++b) id[b] = ids[min(kt * (T / CS_KV_BLOCK) + first_block + b, last_block)];
+  };
   // rows past the frontier are the frontier's row (what lies there may be nothing)
-  auto request_id = [&](int kt) __attribute__((always_inline)) { id = static_cast<uint32_t>(ids[min(kt * T + my_row, last) / CS_KV_BLOCK]); };
   auto request = [&](int kt, int at) __attribute__((always_inline)) {
     const uint8_t *c = my_code, *s = my_scale;
     if (kt * T + T - 1 > last && kt * T + my_row > last) {
       c = codes + at_last / 2;
       s = scales + at_last / cs::kKv4Block;
     }
-    code[at] = *reinterpret_cast<const cs::u32x4*>(c + static_cast<uint64_t>(id) * code_step);
-    scale[at] = s[static_cast<uint64_t>(id) * scale_step];
+    const uint32_t block = static_cast<uint32_t>(T == 64 && lane >= 32 ? id[T == 64 ? 1 : 0] : id[0]);
+    code[at] = *reinterpret_cast<const cs::u32x4*>(c + static_cast<uint64_t>(block) * code_step);
+    scale[at] = s[static_cast<uint64_t>(block) * scale_step];
   };
   auto put = [&](int buf) __attribute__((always_inline)) {       // tile kt0 + k: stage k & 1 of the registers and of LDS
     if (of_v) {
