@@ -40,8 +40,8 @@ struct Params {
 };
 
 constexpr int kStep = 32;                // query rows of a step
-constexpr int kListed = 2048;            // steps of a stream that a workgroup sorts out
-constexpr int kGroups = 1024, kLeast = 4;      // workgroups wanted, steps that a share of a stream's rows has at least
+constexpr int kListed = 2048, kFewSteps = 8;   // steps of a stream that a workgroup sorts out; of a share, that it does not
+constexpr int kGroups = 1536, kLeast = 4;      // workgroups wanted, steps that a share of a stream's rows has at least
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 constexpr int keys_per_wave(int cache) { return cache == CS_F32 ? 32 : 64; }
@@ -99,10 +99,9 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
   }
   const int chunk = share_of % p.chunks, kvh = share_of / p.chunks % p.n_kv_heads, stream = share_of / p.chunks / p.n_kv_heads;
   if (stream >= p.n_streams) return;
-  const int entries = stream_entries(p, stream);
-  if (kt * TILE >= entries) return;
-  const int q0 = p.cu_q[stream];
+  const int entries = stream_entries(p, stream), q0 = p.cu_q[stream];
   const int rows = max(0, min(p.cu_q[stream + 1], static_cast<int>(p.n_q)) - q0) * p.group;
+  if (kt * TILE >= entries) return;
   const int steps = (rows + kStep - 1) / kStep;
   const int tile0 = kt * TILE, key0 = tile0 + wave * 32 * KB;
 
@@ -135,8 +134,9 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
     }
   }
 
-  // ---- the steps with a row that sees a key of the tile; shares are of those (of more steps than the list holds: of all)
-  const bool listed = steps <= kListed;
+  // ---- the steps with a row that sees a key of the tile; shares are of those.  Of all steps where they are more than the list holds, or
+  // so few that sorting them out (2 us) takes longer than passing over what sees nothing.
+  const bool listed = steps <= kListed && steps > kFewSteps * p.chunks;
   int n_active = steps;
   if (listed) {
     if (tid < kListed / 32) s_bits[tid] = 0;
