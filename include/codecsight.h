@@ -604,7 +604,8 @@ int cs_kv4_rerotate(uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_codes, uint8
  *                    not be initialised.  Two calls that overlap in time must not share a workspace.
  * Errors: CS_EINVAL (null pointer, negative size, n_q_heads not a multiple of n_kv_heads, softmax_scale not a positive
  *         finite number), CS_EUNSUPPORTED (head_dim not in {64,128}, block_size != 16, n_q_heads/n_kv_heads > 16, strides not
- *         multiples of 32, alignment, unknown dtype, n_q >= 2^27, n_kv_heads > 65,535), CS_EWORKSPACE, CS_EHIP.
+ *         multiples of 32, stride_slot >= 2^26, alignment, unknown dtype, n_q >= 2^27, n_kv_heads > 65,535), CS_EWORKSPACE,
+ *         CS_EHIP.
  *         n_q == 0 or n_streams == 0 returns CS_OK.
  * ------------------------------------------------------------------------------------------ */
 size_t cs_kv4_window_attn_workspace(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads,
@@ -633,8 +634,9 @@ int cs_kv4_window_attn(const void* q, const uint8_t* k_codes_layer, const uint8_
  *  decay              0 .. 1: 1 sums up, less lets earlier steps fade, 0 starts anew
  *  workspace          cs_attn_weights_workspace() bytes, 16-byte aligned, contents need not be initialised.  Two calls that
  *                     overlap in time must not share a workspace.
- * Errors: as cs_kv4_window_attn; CS_EINVAL also for a decay outside 0 .. 1, CS_EUNSUPPORTED for a cache_dtype that is neither
- *         dtype nor CS_KV4.  n_streams == 0 returns CS_OK; n_q == 0 only lets weights fade.
+ * Errors: as cs_kv4_window_attn (strides: multiples of 16 bytes, of 32 elements for a 4-bit cache); CS_EINVAL also for a decay
+ *         outside 0 .. 1, CS_EUNSUPPORTED for a cache_dtype that is neither dtype nor CS_KV4, and for 2^28 rows of a kv head
+ *         (n_q * n_q_heads / n_kv_heads).  n_streams == 0 returns CS_OK; n_q == 0 only lets weights fade.
  * ------------------------------------------------------------------------------------------ */
 size_t cs_attn_weights_workspace(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                                  int32_t max_blocks);

@@ -421,6 +421,132 @@ class DeviceStep:
 DevicePlannedStep = DeviceStep     # former name of the device-planned step
 
 
+class Kv4Step(DeviceStep):
+    """A step whose window cache is held in 4 bits (a quarter of the 16-bit pool) and whose fresh queries and keys arrive as the
+    projections leave them, not yet rotated.
+
+    Scoring and planning are DeviceStep's.  The reused keys' position correction is cs_kv4_rerotate; a layer is two calls:
+    cs_rope_refresh_scatter (rotary embedding, refresh write) and cs_kv4_window_attn.  `positions` are the executed tokens' rotary
+    positions, int32 [q_cap] or, with `axis_of_pair` (uint8 [head_dim/2]), [q_cap][3] as (time, height, width); the model knows
+    them, and may overwrite the tensor between steps.  With axes, time counts frames and a slide shifts it by the stride;
+    without, positions are dense (frame slot * tokens_per_frame + token id) and the plan's shifts apply.
+
+    `weigh`: every step also sums the attention weight that each window entry received, over layers, queries and heads, into
+    `weight` [n_streams][max_blocks * 16]; `evict` cuts the windows to a budget by it."""
+
+    def __init__(self, data: StepData, positions, axis_of_pair=None, reuse_cap: Optional[int] = None, q_cap: Optional[int] = None,
+                 weigh: bool = False):
+        import torch
+        super().__init__(data, reuse_cap=reuse_cap, q_cap=q_cap, overlap=False, own_rows=False)
+        cs, w, dev = self.cs, data.workload, self.dev
+        to = lambda a: (a if isinstance(a, torch.Tensor) else torch.from_numpy(np.ascontiguousarray(a))).to(dev)
+        self.positions = to(positions)
+        self.axis_of_pair = None if axis_of_pair is None else to(axis_of_pair)
+        width = 1 if axis_of_pair is None else 3
+        if self.positions.dtype != torch.int32 or self.positions.numel() < width * self.q_cap:
+            raise ValueError(f"positions: int32 of {width} x {self.q_cap} executed rows expected")
+        if self.axis_of_pair is not None:
+            # one shift for all reused rows: whole frames along time
+            self.delta3 = torch.zeros((max(1, self.reuse_cap), 3), dtype=torch.int32, device=dev)
+            self.delta3[:, 0] = -w.stride
+        # the cached windows in 4 bits, head by head: attention reads one kv head's 16 rows of a block as a kilobyte
+        n_layers, n_slots = int(self.k_pool.shape[0]), int(self.k_pool.shape[1])
+        shape = lambda width: (n_layers, w.n_kv_heads, n_slots, width)
+        pool = lambda width: torch.zeros(shape(width), dtype=torch.uint8, device=dev).transpose(1, 2)
+        self.k_codes, self.v_codes = pool(w.head_dim // 2), pool(w.head_dim // 2)
+        self.k_scales, self.v_scales = pool(w.head_dim // 32), pool(w.head_dim // 32)
+        self.stride_layer, self.stride_slot, self.stride_head = (2 * self.k_codes.stride(i) for i in range(3))
+        every = torch.arange(n_slots, dtype=torch.int32, device=dev)
+        row = w.n_kv_heads * w.head_dim
+        for layer in range(n_layers):
+            k, v = self.k_pool[layer].contiguous(), self.v_pool[layer].contiguous()
+            cs.cs_rope_refresh_scatter(None, None, k, v, every, None, None, self.k_codes[layer], self.v_codes[layer], self.k_scales[layer],
+                                       self.v_scales[layer], n_slots, 0, w.n_kv_heads, w.head_dim, 0, row, row, self.stride_slot,
+                                       self.stride_head, w.rope_base, cs.CS_ROPE_HALF_SPLIT, self.dtype, cs.CS_KV4)
+        self.k_pool = self.v_pool = None
+        self.q_turned = torch.empty_like(self.q[0])
+        self.lse = torch.empty((self.n_q, w.n_q_heads), dtype=torch.float32, device=dev)
+        attn = (self.n_q, w.n_streams, w.n_q_heads, w.n_kv_heads, w.head_dim, self.max_blocks)
+        self.ws_d_bytes = cs.cs_kv4_window_attn_workspace(*attn)
+        self.ws_d = torch.empty((max(16, self.ws_d_bytes),), dtype=torch.uint8, device=dev)
+        self.weight = None
+        if weigh:
+            self.weight = torch.zeros((w.n_streams, self.max_blocks * cs.CS_KV_BLOCK), dtype=torch.float32, device=dev)
+            self.ws_w_bytes = cs.cs_attn_weights_workspace(*attn)
+            self.ws_w = torch.empty((max(16, self.ws_w_bytes),), dtype=torch.uint8, device=dev)
+
+    def rerotate(self, in_place: bool = False, layers=None):
+        w, cs = self.data.workload, self.cs
+        if self.reuse_cap == 0:
+            return
+        l0, l1 = layers if layers is not None else (0, w.n_layers)
+        self._move(self.src_slot, None if in_place else self.dst_slot, self.delta if self.axis_of_pair is None else self.delta3,
+                   self.axis_of_pair, int(self.src_slot.shape[0]), l0, l1)
+
+    def _move(self, src_slot, dst_slot, delta, axis_of_pair, n_rows, l0, l1):
+        w, cs = self.data.workload, self.cs
+        cs.cs_kv4_rerotate(self.k_codes[l0:l1], self.k_scales[l0:l1], self.v_codes[l0:l1], self.v_scales[l0:l1], src_slot, dst_slot, delta,
+                           axis_of_pair, n_rows, l1 - l0, w.n_kv_heads, w.head_dim, self.stride_layer, self.stride_slot, self.stride_head,
+                           w.rope_base, cs.CS_ROPE_HALF_SPLIT)
+
+    def refresh_scatter(self, layer: int):
+        """Queries of the layer rotated (into q_turned), keys rotated and written, values written."""
+        w, cs = self.data.workload, self.cs
+        q, k, v = self.q[layer], self.k_new[layer], self.v_new[layer]
+        cs.cs_rope_refresh_scatter(q, self.q_turned, k, v, self.q_slot, self.positions, self.axis_of_pair, self.k_codes[layer],
+                                   self.v_codes[layer], self.k_scales[layer], self.v_scales[layer], self.n_q, w.n_q_heads, w.n_kv_heads,
+                                   w.head_dim, q.stride(0), k.stride(0), v.stride(0), self.stride_slot, self.stride_head, w.rope_base,
+                                   cs.CS_ROPE_HALF_SPLIT, self.dtype, cs.CS_KV4)
+
+    def attention(self, layer: int, reuse_plan: bool = False):
+        """Attention of one layer over q_turned (there is no plan to reuse)."""
+        w, cs = self.data.workload, self.cs
+        cs.cs_kv4_window_attn(self.q_turned, self.k_codes[layer], self.k_scales[layer], self.v_codes[layer], self.v_scales[layer], self.cu_q,
+                              self.q_pos, self.kv_len, self.block_table, self.max_blocks, cs.CS_KV_BLOCK, self.out[layer], self.lse, self.n_q,
+                              w.n_streams, w.n_q_heads, w.n_kv_heads, w.head_dim, self.stride_slot, self.stride_head,
+                              self.data.softmax_scale, self.dtype, self.ws_d, self.ws_d_bytes)
+
+    def add_weights(self, layer: int):
+        """The layer's attention weights added to `weight` (layer 0 starts anew)."""
+        w, cs = self.data.workload, self.cs
+        cs.cs_attn_weights(self.q_turned, self.lse, self.k_codes[layer], self.k_scales[layer], self.cu_q, self.q_pos, self.kv_len,
+                           self.block_table, self.max_blocks, cs.CS_KV_BLOCK, self.weight, self.weight, 0.0 if layer == 0 else 1.0, self.n_q,
+                           w.n_streams, w.n_q_heads, w.n_kv_heads, w.head_dim, self.stride_slot, self.stride_head, self.data.softmax_scale,
+                           self.dtype, cs.CS_KV4, self.ws_w, self.ws_w_bytes)
+
+    def refresh_and_attention(self, layer: int, reuse_plan: bool = False, own_rows: bool = False):
+        self.refresh_scatter(layer)
+        self.attention(layer)
+        if self.weight is not None:
+            self.add_weights(layer)
+
+    def attention_status(self) -> int:
+        return 0                        # (no launch-wide barrier)
+
+    def run(self):
+        self.prepare()
+        self.rerotate()
+        for layer in range(self.data.workload.n_layers):
+            self.refresh_and_attention(layer)
+
+    def evict(self, budget: int, block_table, n_first: int = 4, n_last: int = 64):
+        """The windows cut to `budget` entries by `weight`, moved to the blocks of `block_table` (int32 [n_streams][..], on the device, none
+        of them the windows' own).  Kept entries keep their rotary positions.  Returns kept [n_streams][budget] (old indices, -1 past
+        a stream's own), the new lengths, and the kept entries' weights."""
+        import torch
+        if self.weight is None:
+            raise ValueError("evict: the step was built without weigh=True")
+        w, cs, dev = self.data.workload, self.cs, self.dev
+        i32 = lambda *shape: torch.empty(shape, dtype=torch.int32, device=dev)
+        n, columns = w.n_streams, int(block_table.shape[1])
+        kept, src, dst, delta, kv_len = i32(n, budget), i32(n, budget), i32(n, budget), i32(n, budget), i32(n)
+        weight = torch.zeros((n, columns * cs.CS_KV_BLOCK), dtype=torch.float32, device=dev)
+        cs.cs_plan_evict(self.weight, self.kv_len, self.block_table, self.max_blocks, block_table, columns, n, budget, n_first, n_last, False, kept,
+                         src, dst, delta, kv_len, weight)
+        self._move(src, dst, delta, None, n * budget, 0, w.n_layers)
+        return kept, kv_len, weight
+
+
 @dataclass
 class FrontEndData:
     """Inputs of a slide step that starts from decoder output: coding blocks, a motion field and

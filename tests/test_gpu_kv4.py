@@ -622,3 +622,110 @@ def test_calls_in_a_graph_and_on_a_stream_of_their_own(cs):
         run()
         torch.cuda.synchronize()
         assert all(torch.equal(a, c) for a, c in zip(results, want))
+
+
+# ------------------------------------------------------------------------------------------ a step over a 4-bit cache
+
+@pytest.mark.parametrize("axes", ["one", "sections"])
+def test_step_over_a_4bit_cache(cs, axes):
+    """engine.Kv4Step (scoring, plan, position correction, rotary embedding with the write, attention, weights; then an eviction)
+    against the oracles, twice eagerly and replayed from a graph."""
+    from dataclasses import replace
+
+    from paper_2604_06036_amd import engine, synth
+    from tests import helpers as hp
+    say("Kv4Step", axes)
+    w = replace(synth.CFG2, n_streams=2, n_layers=2, n_q_heads=8, n_kv_heads=2, head_dim=64)
+    data = engine.assemble_step(w, engine.hip_scorer, device="cpu")
+    n_q, cap = data.info["n_q"], data.info["n_q"] + 37
+    rng = np.random.default_rng(5)
+    axis = AXES[axes](32)
+    pos = rng.integers(0, 2500, (cap, 3) if axis is not None else (cap,)).astype(np.int32)
+    plan = hp.OraclePlan(data)
+    pools = [ko.quantise(t.float().numpy()) for t in (data.k_pool, data.v_pool)]
+    step = engine.Kv4Step(data, pos, axis, reuse_cap=data.info["n_reuse"] + 11, q_cap=cap, weigh=True)
+    codes = [t.clone() for t in (step.k_codes, step.k_scales, step.v_codes, step.v_scales)]
+    for (c, s), got_c, got_s in ((pools[0], step.k_codes, step.k_scales), (pools[1], step.v_codes, step.v_scales)):
+        assert np.array_equal(got_s.cpu().numpy(), s) and np.array_equal(ko.values(got_c.cpu().numpy(), s), ko.values(c, s))
+    step.run()
+    torch.cuda.synchronize()
+    assert step.scoring_status() == 0
+    hp.assert_device_plan(step, plan)
+    # reused rows corrected, executed rows turned and written, then attention over them
+    delta = plan.delta if axis is None else np.tile(np.array([-w.stride, 0, 0], np.int32), (len(plan.delta), 1))
+    u, total = U, [np.zeros(int(n)) for n in plan.kv_len]
+    slack = [np.zeros(int(n)) for n in plan.kv_len]
+    for l in range(2):
+        k, v = (ko.values(c[l], s[l]) for c, s in pools)
+        k[plan.dst_slot] = ko.values(*ko.quantise(ko.rope_single(k[plan.src_slot].astype(np.float32), delta, axis, w.rope_base, 0)))
+        v[plan.dst_slot] = v[plan.src_slot]
+        k[plan.q_slot] = ko.values(*ko.quantise(ko.rope_single(data.k_new[l].float().numpy(), pos[:n_q], axis, w.rope_base, 0)))
+        v[plan.q_slot] = ko.values(*ko.quantise(data.v_new[l].double().numpy()))
+        q = single(ko.rope_single(data.q[l].float().numpy(), pos[:n_q], axis, w.rope_base, 0), torch.bfloat16)[0]
+        for s in range(2):
+            rows = slice(int(plan.cu_q[s]), int(plan.cu_q[s + 1]))
+            n = int(plan.kv_len[s])
+            slots = np.array([plan.block_table[s, j // 16] * 16 + j % 16 for j in range(n)])
+            out, lse, p = ko.attention(q[rows], k[slots], v[slots], plan.q_pos[rows], data.softmax_scale)
+            mass = np.einsum("thj,jhc->thc", p, np.abs(np.repeat(v[slots], 4, 1)))
+            score = data.softmax_scale * max(float((np.abs(q[rows][:, h]) @ np.abs(k[slots][:, h // 4]).T).max()) for h in range(8))
+            e = (64 / 8 + 8) * u * score + 4 * u * 2 * score
+            got = step.out[l][rows].double().cpu().numpy()
+            assert np.all(np.abs(got - out) <= (2 * e + 2 * B + (8 + n / 8) * u) * mass + B * np.abs(out))
+            total[s] += p.sum((0, 1))
+            slack[s] += (2 * e + 16 * u) * p.sum((0, 1)) + (len(q[rows]) / 2 + 80) * u * p.sum((0, 1))
+    for s in range(2):
+        n = int(plan.kv_len[s])
+        assert np.all(np.abs(step.weight[s, :n].double().cpu().numpy() - total[s]) <= slack[s] + 1e-30)
+    # once more, and from a graph, from the same cached windows
+    first = step.out.clone()
+    weight = step.weight.clone()
+
+    def restore():
+        for t, c in zip((step.k_codes, step.k_scales, step.v_codes, step.v_scales), codes):
+            t.copy_(c)
+
+    restore()
+    step.run()
+    torch.cuda.synchronize()
+    assert torch.equal(step.out, first) and torch.equal(step.weight, weight)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step.run()
+    for _ in range(3):
+        restore()
+        step.out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(step.out, first) and torch.equal(step.weight, weight)
+    # the windows cut to half, into the blocks of the window before
+    budget = int(plan.kv_len.max()) // 2
+    table = step.bt_old[:, :-(-budget // 16)].contiguous()
+    before = [step.k_codes.cpu().numpy(), step.v_codes.cpu().numpy(), step.k_scales.cpu().numpy(), step.v_scales.cpu().numpy()]
+    kept, kv_new, w_new = step.evict(budget, table, n_first=2, n_last=16)
+    torch.cuda.synchronize()
+    after = [step.k_codes.cpu().numpy(), step.v_codes.cpu().numpy(), step.k_scales.cpu().numpy(), step.v_scales.cpu().numpy()]
+    for s in range(2):
+        n = int(plan.kv_len[s])
+        want = np.array(ko.evict(weight[s].cpu().numpy(), n, budget, 2, 16))
+        assert int(kv_new[s]) == len(want) and kept[s, :len(want)].tolist() == want.tolist()
+        assert np.array_equal(w_new[s, :len(want)].cpu().numpy(), weight[s].cpu().numpy()[want])
+        t = table.cpu().numpy()
+        src = plan.block_table[s, want // 16] * 16 + want % 16
+        dst = t[s, np.arange(len(want)) // 16] * 16 + np.arange(len(want)) % 16
+        for i in range(2):
+            assert np.array_equal(ko.values(after[i][:, dst], after[i + 2][:, dst]), ko.values(before[i][:, src], before[i + 2][:, src]))
+
+
+def test_step_over_a_4bit_cache_refuses_what_does_not_fit(cs):
+    from paper_2604_06036_amd import engine, synth
+    say("Kv4Step refusals")
+    w = synth.small_variant(synth.CFG1, n_layers=1)
+    data = engine.assemble_step(w, engine.hip_scorer, device="cpu")
+    with pytest.raises(ValueError, match="positions"):
+        engine.Kv4Step(data, np.zeros(data.info["n_q"] - 1, np.int32))
+    with pytest.raises(ValueError, match="positions"):
+        engine.Kv4Step(data, np.zeros(data.info["n_q"], np.int32), AXES["sections"](64))
+    step = engine.Kv4Step(data, np.zeros(data.info["n_q"], np.int32))
+    with pytest.raises(ValueError, match="weigh"):
+        step.evict(100, step.bt_old)
