@@ -212,10 +212,12 @@ struct Query {
   // S^T of 32 keys in LDS: `keys` is the lane's row
   __device__ __forceinline__ f32x16 scores(const uint16_t* keys, int h) const {
     f32x16 s = {};
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int i = 0; i < D / 64; ++i)
 #pragma unroll
       for (int w = 0; w < 4; ++w) step(s, *reinterpret_cast<const bf16x8*>(keys + 64 * i + 32 * h + 8 * w), i, w);
+    __builtin_amdgcn_s_setprio(0);
     return s;
   }
 };
@@ -447,18 +449,22 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 3 : D == 64 ? 2 : 1) void kv4_row
   sums.clear();
   auto tile = [&](int kt, auto stage) __attribute__((always_inline)) {
     constexpr int buf = decltype(stage)::value;
+    const int nan = s_nan;                                 // (read ahead of the products)
 #pragma unroll
     for (int kb = 0; kb < T / 32; ++kb) {
       const int key0 = kt * T + 32 * kb;
       if (key0 > wave_last) continue;
       bf16x8 pf[PARTS][2];
       sums.weights(query.scores(&s_k[buf][(32 * kb + n) * KROW], h), key0, pos, key0 + 31 > wave_first, h, p.scale_log2e, pf);
+      __builtin_amdgcn_s_setprio(1);                       // (products before other waves' vector work: 2-3 % for these and the scores)
       sums.template add<VROW>(&s_v[buf][32 * kb * VROW], pf, lane);
+      __builtin_amdgcn_s_setprio(0);
     }
-    if (s_nan) {                                           // (a tile so far held a value block without numbers)
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane(nan), 0)) {      // (a tile so far held a value block without numbers)
       for (int c = 0; c < 128; ++c)
         if (s_vs[buf][c] == cs::kKv4NoNumber) sums.poison(c % DB, kt * T + c / DB <= pos);
     }
+    // (requests past the end made the last tile's instead, so that a wait for one is not a wait for all, were level or 2 % slower)
     if (kt + 1 < kt1) put(buf ^ 1);
     if (kt + 3 < kt1) request(kt + 3, buf ^ 1);
     if (kt + 4 < kt1) request_id(kt + 4);
