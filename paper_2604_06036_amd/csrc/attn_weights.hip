@@ -430,7 +430,14 @@ __global__ __launch_bounds__(256) void attn_weights_sum_kernel(Params p) {
   const int stream = static_cast<int>(i / row);
   if (i - stream * row >= stream_entries(p, stream)) return;
   float sum = 0.0f;
-  for (int c = 0; c < p.chunks * p.n_kv_heads; ++c) sum += p.ws_part[c * all + i];
+  const int parts = p.chunks * p.n_kv_heads;
+  for (int c0 = 0; c0 < parts; c0 += 8) {                  // (eight under way at once, added in order)
+    float x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = c0 + k < parts ? p.ws_part[(c0 + k) * all + i] : 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += x[k];
+  }
   if (p.weight_in && p.decay != 0.0f) sum = fmaf(p.decay, p.weight_in[i], sum);
   p.weight_out[i] = sum;
 }

@@ -1,11 +1,14 @@
 // Which cache entries stay when a window is cut to a budget, and the row lists of the repacking, gfx950.
 //
 // Per stream: the first n_first and last n_last entries, then those of the largest accumulated weight, ties to the lowest
-// index, NaN last, up to the budget; kept in their order.  One workgroup a stream: weights become unsigned integers of the same
-// order, held in registers (up to 32 a thread), three passes of LDS counters over 11, 11 and 10 bits find the smallest kept one and
-// how many of its equals stay, and one count of the larger and of the equal ones before every entry places what is kept.
-// (11 bits hold the exponent and two more, so that sums of softmax weights, within a few powers of two of each other, spread over
-// enough counters.)  All of it is integer work: bit exact, the same from run to run.  Latency bounds it: MEASURED
+// index, NaN last, up to the budget; kept in their order.  One workgroup a stream, a run of neighbouring entries a wave: weights
+// become unsigned integers of the same order, held in registers (up to 24 a thread), three passes of LDS counters over 11, 11 and
+// 10 bits find the smallest kept one and how many of its equals stay, and every wave counts the larger and the equal ones
+// before its own and places what it keeps.  (11 bits hold the exponent and two more, so that sums of softmax weights, within a few
+// powers of two of each other, spread over enough counters.)  What is kept passes through a list in LDS, so that the lists in memory
+// are written in whole lines: a quarter of a wave's lanes storing to five of them took a third of the time.
+// All of it is integer work: bit exact, the same from run to run.  A chain of about ten barriers and one trip to memory bounds it:
+// MEASURED
 #include "common.h"
 
 namespace {
@@ -15,7 +18,7 @@ struct Params {
   const int32_t* __restrict__ kv_len;
   const int32_t* __restrict__ bt_old;
   const int32_t* __restrict__ bt_new;
-  int32_t* kept;                         // (written, and read back by other threads of the workgroup)
+  int32_t* __restrict__ kept;
   int32_t* __restrict__ src_slot;
   int32_t* __restrict__ dst_slot;
   int32_t* __restrict__ delta;
@@ -40,30 +43,40 @@ constexpr int kWaves = kThreads / 64, kBins = 2048;
 // Entries a thread holds; HELD 0: any number, read anew in every pass.
 template <int HELD>
 __global__ __launch_bounds__(kThreads) void plan_evict_kernel(Params p) {
-  constexpr int ROUNDS = HELD ? HELD : 32;                 // entries of a thread that are placed at once
-  __shared__ int s_bins[kBins];
-  __shared__ int s_wave[kWaves];
+  // counters of the passes, then the list of what is kept
+  __shared__ __attribute__((aligned(16))) char s_mem[kBins * 4 > HELD * kThreads * 2 ? kBins * 4 : HELD * kThreads * 2];
+  int* const s_bins = reinterpret_cast<int*>(s_mem);
+  uint16_t* const s_list = reinterpret_cast<uint16_t*>(s_mem);
+  __shared__ int s_wave[kWaves], s_above[kWaves], s_equal[kWaves];
   __shared__ int s_digit, s_left;
-  __shared__ int s_above[ROUNDS * kWaves], s_equal[ROUNDS * kWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, stream = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), stream = blockIdx.x;
   const int row_old = p.max_blocks_old * CS_KV_BLOCK;
   const int n = max(0, min(p.kv_len[stream], row_old)), keep = min(n, p.budget);
   const float* weight = p.weight + static_cast<int64_t>(stream) * row_old;
   const int first = p.n_first, last = max(0, n - min(p.n_last, n));
-  const int rounds = (n + kThreads - 1) / kThreads;
+  const int rounds = (n + kThreads - 1) / kThreads;        // of 64 entries a wave
+  const int j0 = wave * rounds * 64 + lane;                // entry i of a thread: j0 + 64 i
+  const int32_t* ids_old = p.bt_old + static_cast<int64_t>(stream) * p.max_blocks_old;
+  const int32_t* ids_new = p.bt_new + static_cast<int64_t>(stream) * p.max_blocks_new;
   auto rank_at = [&](int j) __attribute__((always_inline)) { return rank_of(weight[j], j < first || j >= last); };
   uint32_t held[HELD ? HELD : 1];
   if (HELD) {
     float w[HELD ? HELD : 1];
 #pragma unroll
-    for (int i = 0; i < HELD; ++i) w[i] = i * kThreads + tid < n ? weight[i * kThreads + tid] : 0.0f;
+    for (int i = 0; i < HELD; ++i) w[i] = i < rounds && j0 + 64 * i < n ? weight[j0 + 64 * i] : 0.0f;
 #pragma unroll
-    for (int i = 0; i < HELD; ++i) {
-      const int j = i * kThreads + tid;
-      held[i] = rank_of(w[i], j < first || j >= last);
-    }
+    for (int i = 0; i < HELD; ++i) held[i] = rank_of(w[i], j0 + 64 * i < first || j0 + 64 * i >= last);
   }
-  auto rank = [&](int i, int j) __attribute__((always_inline)) { return HELD ? held[HELD ? i : 0] : rank_at(j); };
+  auto rank = [&](int i) __attribute__((always_inline)) { return HELD ? held[HELD ? i : 0] : rank_at(j0 + 64 * i); };
+  auto each = [&](auto f) __attribute__((always_inline)) {
+    if (HELD) {
+#pragma unroll
+      for (int i = 0; i < HELD; ++i)
+        if (i < rounds) f(i);
+    } else {
+      for (int i = 0; i < rounds; ++i) f(i);
+    }
+  };
 
   // ---- the smallest rank that stays, and how many entries of that rank
   uint32_t prefix = 0, mask = 0;
@@ -75,19 +88,11 @@ __global__ __launch_bounds__(kThreads) void plan_evict_kernel(Params p) {
       s_bins[tid] = 0;
       s_bins[kThreads + tid] = 0;
       __syncthreads();
-      auto count = [&](int i) __attribute__((always_inline)) {
-        const int j = i * kThreads + tid;
-        if (j >= n) return;
-        const uint32_t r = rank(i, j);
+      each([&](int i) __attribute__((always_inline)) {
+        if (j0 + 64 * i >= n) return;
+        const uint32_t r = rank(i);
         if ((r & mask) == prefix) atomicAdd(&s_bins[(r >> shift) & ((1u << bits) - 1)], 1);
-      };
-      if (HELD) {
-#pragma unroll
-        for (int i = 0; i < HELD; ++i)
-          if (i < rounds) count(i);
-      } else {
-        for (int i = 0; i < rounds; ++i) count(i);
-      }
+      });
       __syncthreads();
       // from the largest digit down, two digits a thread: the one at which `left` is reached
       const int d = kBins - 1 - 2 * tid, c0 = s_bins[d], c1 = s_bins[d - 1];
@@ -101,7 +106,7 @@ __global__ __launch_bounds__(kThreads) void plan_evict_kernel(Params p) {
       __syncthreads();
       int before = incl - c0 - c1;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) before += w < wave ? s_wave[w] : 0;
+      for (int k = 0; k < kWaves; ++k) before += k < wave ? s_wave[k] : 0;
       if (before < left && left <= before + c0 + c1) {     // (one thread)
         const bool second = left > before + c0;
         s_digit = second ? d - 1 : d;
@@ -115,113 +120,77 @@ __global__ __launch_bounds__(kThreads) void plan_evict_kernel(Params p) {
   }
 
   // ---- lists, in index order: before an entry stay the larger ones before it, and of its equals no more than `left`
-  const int64_t list = static_cast<int64_t>(stream) * p.budget;
-  const int32_t* ids_old = p.bt_old + static_cast<int64_t>(stream) * p.max_blocks_old;
-  const int32_t* ids_new = p.bt_new + static_cast<int64_t>(stream) * p.max_blocks_new;
-  float* weight_new = p.weight_new ? p.weight_new + static_cast<int64_t>(stream) * p.max_blocks_new * CS_KV_BLOCK : nullptr;
   const bool all = keep == n;
-  int above0 = 0, equal0 = 0;            // before this lot of entries
-  for (int i0 = 0; i0 < rounds && keep > 0; i0 += ROUNDS) {
-    auto marks = [&](int i, uint64_t* above, uint64_t* equal) __attribute__((always_inline)) {
-      const int j = (i0 + i) * kThreads + tid;
-      const uint32_t r = j < n ? rank(i, j) : 0u;
-      *above = __ballot(j < n && (all || r > prefix));
-      *equal = __ballot(j < n && !all && r == prefix);
-    };
+  auto marks = [&](int i, uint64_t* above, uint64_t* equal) __attribute__((always_inline)) {
+    const bool there = j0 + 64 * i < n;
+    const uint32_t r = there ? rank(i) : 0u;
+    *above = __ballot(there && (all || r > prefix));
+    *equal = __ballot(there && !all && r == prefix);
+  };
+  int above = 0, equal = 0;
+  each([&](int i) __attribute__((always_inline)) {
+    uint64_t a, e;
+    marks(i, &a, &e);
+    above += __popcll(a);
+    equal += __popcll(e);
+  });
+  if (lane == 0) {
+    s_above[wave] = above;
+    s_equal[wave] = equal;
+  }
+  __syncthreads();                       // (the counters have been read, too)
+  above = equal = 0;
 #pragma unroll
-    for (int i = 0; i < ROUNDS; ++i) {
-      uint64_t a = 0, e = 0;
-      if (i0 + i < rounds) marks(i, &a, &e);
-      if (lane == 0) {
-        s_above[i * kWaves + wave] = __popcll(a);
-        s_equal[i * kWaves + wave] = __popcll(e);
-      }
-    }
-    __syncthreads();
-    // exclusive sums over (round, wave), by the first wave, ROUNDS * kWaves / 64 neighbours a lane
-    constexpr int PER = (ROUNDS * kWaves + 63) / 64;
-    if (wave == 0) {
-      int ca[PER], ce[PER], sa = 0, se = 0;
-#pragma unroll
-      for (int k = 0; k < PER; ++k) {
-        const int x = lane * PER + k;
-        ca[k] = x < ROUNDS * kWaves ? s_above[x] : 0;
-        ce[k] = x < ROUNDS * kWaves ? s_equal[x] : 0;
-        sa += ca[k];
-        se += ce[k];
-      }
-      int ia = sa, ie = se;
-#pragma unroll
-      for (int k = 1; k < 64; k <<= 1) {
-        const int ua = __shfl_up(ia, k), ue = __shfl_up(ie, k);
-        if (lane >= k) {
-          ia += ua;
-          ie += ue;
-        }
-      }
-      ia += above0 - sa;
-      ie += equal0 - se;
-#pragma unroll
-      for (int k = 0; k < PER; ++k) {
-        const int x = lane * PER + k;
-        if (x < ROUNDS * kWaves) {
-          s_above[x] = ia;
-          s_equal[x] = ie;
-        }
-        ia += ca[k];
-        ie += ce[k];
-      }
-      if (lane == 63) {
-        s_digit = ia;
-        s_left = ie;
-      }
-    }
-    __syncthreads();
-    const uint64_t lower = (1ull << lane) - 1;
-#pragma unroll
-    for (int i = 0; i < ROUNDS; ++i) {
-      if (i0 + i >= rounds) break;
+  for (int k = 0; k < kWaves; ++k) {
+    above += k < wave ? s_above[k] : 0;
+    equal += k < wave ? s_equal[k] : 0;
+  }
+  const int64_t list = static_cast<int64_t>(stream) * p.budget;
+  float* weight_new = p.weight_new ? p.weight_new + static_cast<int64_t>(stream) * p.max_blocks_new * CS_KV_BLOCK : nullptr;
+  auto put = [&](int at, int j, int old_id, int new_id, float x) __attribute__((always_inline)) {
+    p.kept[list + at] = j;
+    p.src_slot[list + at] = old_id * CS_KV_BLOCK + j % CS_KV_BLOCK;
+    p.dst_slot[list + at] = new_id * CS_KV_BLOCK + at % CS_KV_BLOCK;
+    p.delta[list + at] = p.renumber ? at - j : 0;
+    if (weight_new) weight_new[at] = x;
+  };
+  const uint64_t lower = (1ull << lane) - 1;
+  if (keep > 0)
+    each([&](int i) __attribute__((always_inline)) {
       uint64_t a, e;
       marks(i, &a, &e);
-      const int before = s_equal[i * kWaves + wave] + __popcll(e & lower);
-      const bool stays = (a >> lane & 1) || ((e >> lane & 1) && before < left);
-      if (stays) {
-        const int j = (i0 + i) * kThreads + tid;
-        const int at = s_above[i * kWaves + wave] + __popcll(a & lower) + min(before, left);
-        p.kept[list + at] = j;
+      const int before = equal + __popcll(e & lower), j = j0 + 64 * i;
+      if ((a >> lane & 1) || ((e >> lane & 1) && before < left)) {
+        const int at = above + __popcll(a & lower) + min(before, left);
+        if (HELD) s_list[at] = static_cast<uint16_t>(j);
+        else put(at, j, ids_old[j / CS_KV_BLOCK], ids_new[at / CS_KV_BLOCK], weight[j]);
       }
+      above += __popcll(a);
+      equal += __popcll(e);
+    });
+  if (HELD) {                            // four entries of a thread at once
+    __syncthreads();
+    for (int i0 = tid; i0 < keep; i0 += 4 * kThreads) {
+      int j[4], id_old[4], id_new[4];
+      float x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = min(i0 + k * kThreads, keep - 1);
+        j[k] = s_list[i];
+        id_old[k] = ids_old[j[k] / CS_KV_BLOCK];
+        id_new[k] = ids_new[i / CS_KV_BLOCK];
+        x[k] = weight_new ? weight[j[k]] : 0.0f;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (i0 + k * kThreads < keep) put(i0 + k * kThreads, j[k], id_old[k], id_new[k], x[k]);
     }
-    above0 = s_digit;
-    equal0 = s_left;
-    if (!HELD) __syncthreads();
   }
-  // slots of what is kept, in its order: four entries of a thread at once
-  __syncthreads();
-  for (int i0 = 0; i0 < p.budget; i0 += 4 * kThreads) {
-    int j[4], id_old[4], id_new[4];
-    float w[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int i = i0 + k * kThreads + tid;
-      j[k] = i < keep ? p.kept[list + i] : -1;
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      id_old[k] = j[k] < 0 ? 0 : ids_old[j[k] / CS_KV_BLOCK];
-      id_new[k] = j[k] < 0 ? 0 : ids_new[(i0 + k * kThreads + tid) / CS_KV_BLOCK];
-      w[k] = j[k] < 0 ? 0.0f : weight[j[k]];
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int i = i0 + k * kThreads + tid;
-      if (i >= p.budget) break;
-      const bool none = j[k] < 0;
-      if (none) p.kept[list + i] = -1;
-      p.src_slot[list + i] = none ? -1 : id_old[k] * CS_KV_BLOCK + j[k] % CS_KV_BLOCK;
-      p.dst_slot[list + i] = none ? -1 : id_new[k] * CS_KV_BLOCK + i % CS_KV_BLOCK;
-      p.delta[list + i] = none || !p.renumber ? 0 : i - j[k];
-      if (weight_new && !none) weight_new[i] = w[k];
-    }
+  for (int i = keep + tid; i < p.budget; i += kThreads) {
+    p.kept[list + i] = -1;
+    p.src_slot[list + i] = -1;
+    p.dst_slot[list + i] = -1;
+    p.delta[list + i] = 0;
   }
   if (tid == 0) p.kv_len_new[stream] = keep;
 }
@@ -260,8 +229,8 @@ extern "C" int cs_plan_evict(const float* weight, const int32_t* kv_len, const i
   const int entries = max_blocks_old * CS_KV_BLOCK;        // of the widest row there may be
   if (entries <= kThreads) hipLaunchKernelGGL(plan_evict_kernel<1>, grid, dim3(kThreads), 0, st, p);
   else if (entries <= 4 * kThreads) hipLaunchKernelGGL(plan_evict_kernel<4>, grid, dim3(kThreads), 0, st, p);
-  else if (entries <= 16 * kThreads) hipLaunchKernelGGL(plan_evict_kernel<16>, grid, dim3(kThreads), 0, st, p);
-  else if (entries <= 32 * kThreads) hipLaunchKernelGGL(plan_evict_kernel<32>, grid, dim3(kThreads), 0, st, p);
+  else if (entries <= 12 * kThreads) hipLaunchKernelGGL(plan_evict_kernel<12>, grid, dim3(kThreads), 0, st, p);
+  else if (entries <= 24 * kThreads) hipLaunchKernelGGL(plan_evict_kernel<24>, grid, dim3(kThreads), 0, st, p);
   else hipLaunchKernelGGL(plan_evict_kernel<0>, grid, dim3(kThreads), 0, st, p);
   return cs::note_hip(hipGetLastError());
 }

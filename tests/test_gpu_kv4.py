@@ -520,7 +520,8 @@ def test_attn_weights_sum_to_the_number_of_rows(cs):
 
 @pytest.mark.parametrize("kv,budget,first,last", [
     ([1], 1, 0, 0), ([5, 0, 33, 16], 7, 1, 2), ([919], 460, 4, 64), ([3000, 1024, 1025, 1, 2048], 1000, 0, 0), ([300, 20], 16, 10, 10), ([300], 8, 20, 20),
-    ([64, 10], 64, 3, 3), ([17000, 16383], 4096, 4, 64), ([100] * 70, 31, 0, 1)])
+    ([64, 10], 64, 3, 3), ([17000, 16383], 4096, 4, 64), ([100] * 70, 31, 0, 1),
+    ([9000, 50, 4097], 3001, 3, 9), ([30001, 24577, 2], 7000, 4, 64), ([40000], 33000, 0, 0)])
 @pytest.mark.parametrize("values", ["spread", "ties", "odd"])
 def test_plan_evict(cs, kv, budget, first, last, values):
     say("evict", kv[:5], budget, first, last, values)
