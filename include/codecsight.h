@@ -604,7 +604,7 @@ int cs_kv4_rerotate(uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_codes, uint8
  *                    not be initialised.  Two calls that overlap in time must not share a workspace.
  * Errors: CS_EINVAL (null pointer, negative size, n_q_heads not a multiple of n_kv_heads, softmax_scale not a positive
  *         finite number), CS_EUNSUPPORTED (head_dim not in {64,128}, block_size != 16, n_q_heads/n_kv_heads > 16, strides not
- *         multiples of 32, stride_slot >= 2^26, alignment, unknown dtype, n_q >= 2^27, n_kv_heads > 65,535), CS_EWORKSPACE,
+ *         multiples of 32, stride_slot >= 2^26, alignment, unknown dtype, n_q >= 2^26, n_kv_heads > 65,535), CS_EWORKSPACE,
  *         CS_EHIP.
  *         n_q == 0 or n_streams == 0 returns CS_OK.
  * ------------------------------------------------------------------------------------------ */
@@ -632,8 +632,9 @@ int cs_kv4_window_attn(const void* q, const uint8_t* k_codes_layer, const uint8_
  *  weight_in     in   float [n_streams][max_blocks * 16], or NULL (zeros); not read with decay == 0
  *  weight_out    out  the same layout, may be weight_in
  *  decay              0 .. 1: 1 sums up, less lets earlier steps fade, 0 starts anew
- *  workspace          cs_attn_weights_workspace() bytes, 16-byte aligned, contents need not be initialised.  Two calls that
- *                     overlap in time must not share a workspace.
+ *  workspace          cs_attn_weights_workspace() bytes, 16-byte aligned, contents need not be initialised (8 bytes a query row
+ *                     and 128 entries of max_blocks * 16 for calls without lse, and the partial sums).  Two calls that overlap in
+ *                     time must not share a workspace.
  * Errors: as cs_kv4_window_attn (strides: multiples of 16 bytes, of 32 elements for a 4-bit cache); CS_EINVAL also for a decay
  *         outside 0 .. 1, CS_EUNSUPPORTED for a cache_dtype that is neither dtype nor CS_KV4, and for 2^28 rows of a kv head
  *         (n_q * n_q_heads / n_kv_heads).  n_streams == 0 returns CS_OK; n_q == 0 only lets weights fade.
@@ -667,7 +668,7 @@ int cs_attn_weights(const void* q, const float* lse, const void* k_cache_layer, 
  *  weight_new       out  float [n_streams][max_blocks_new * 16] or NULL: the kept entries' weights; places past m are left
  * Bit exact.
  * Errors: CS_EINVAL (null pointer, negative size, budget < 1, a block table without columns, a new table too narrow for what
- *         may stay), CS_EUNSUPPORTED (tables of 2^27 columns), CS_EHIP.  n_streams == 0 returns CS_OK.
+ *         may stay), CS_EUNSUPPORTED (tables of 2^27 columns, budget > 2^30), CS_EHIP.  n_streams == 0 returns CS_OK.
  * ------------------------------------------------------------------------------------------ */
 int cs_plan_evict(const float* weight, const int32_t* kv_len, const int32_t* block_table_old, int32_t max_blocks_old,
                   const int32_t* block_table_new, int32_t max_blocks_new, int32_t n_streams, int32_t budget,

@@ -360,6 +360,12 @@ def cs_attn_status(workspace) -> int:
     return int(flat[CS_ATTN_STATUS_OFFSET:CS_ATTN_STATUS_OFFSET + 4].view(torch.int32).item())
 
 
+def _here(fn: str, t: Optional[torch.Tensor]):
+    """The work goes to the current device's stream: a call on another device's tensors is refused."""
+    if t is not None and t.is_cuda and t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{fn}: tensors on device {t.get_device()}, the current device is {torch.cuda.current_device()}")
+
+
 def _span(t: Optional[torch.Tensor], rows: int, stride: int, row: int) -> bool:
     """Whether the memory from t's first element on holds `rows` rows of `row` elements, `stride` apart."""
     if t is None or rows < 1:
@@ -371,6 +377,7 @@ def cs_rope_refresh_scatter(q, q_out, k_new, v_new, slot, pos, axis_of_pair, k_c
                             v_scales_layer, n_tok, n_q_heads, n_kv_heads, head_dim, stride_q, stride_k, stride_v, stride_slot,
                             stride_head, rope_base, rope_style, dtype, cache_dtype):
     fn = "cs_rope_refresh_scatter"
+    _here(fn, pos if k_cache_layer is None else k_cache_layer)
     _need(fn, slot, n_tok, "slot")
     _need(fn, pos, n_tok if axis_of_pair is None else 3 * n_tok, "pos"); _need(fn, axis_of_pair, head_dim // 2, "axis_of_pair")
     for t, stride, heads, what in ((q, stride_q, n_q_heads, "q"), (k_new, stride_k, n_kv_heads, "k_new"), (v_new, stride_v, n_kv_heads, "v_new")):
@@ -387,6 +394,7 @@ def cs_rope_refresh_scatter(q, q_out, k_new, v_new, slot, pos, axis_of_pair, k_c
 def cs_kv4_gather(k_codes, k_scales, v_codes, v_scales, slot, n_rows, n_layers, n_kv_heads, head_dim, stride_layer, stride_slot,
                   stride_head, k_out, v_out, dtype):
     fn = "cs_kv4_gather"
+    _here(fn, slot)
     _need(fn, slot, n_rows, "slot")
     for t, what in ((k_out, "k_out"), (v_out, "v_out")):
         _need(fn, t, n_layers * n_rows * n_kv_heads * head_dim, what)
@@ -397,6 +405,7 @@ def cs_kv4_gather(k_codes, k_scales, v_codes, v_scales, slot, n_rows, n_layers, 
 def cs_kv4_rerotate(k_codes, k_scales, v_codes, v_scales, src_slot, dst_slot, delta, axis_of_pair, n_rows, n_layers, n_kv_heads,
                     head_dim, stride_layer, stride_slot, stride_head, rope_base, rope_style):
     fn = "cs_kv4_rerotate"
+    _here(fn, k_codes)
     _need(fn, src_slot, n_rows, "src_slot"); _need(fn, dst_slot, n_rows, "dst_slot")
     _need(fn, delta, n_rows if axis_of_pair is None else 3 * n_rows, "delta"); _need(fn, axis_of_pair, head_dim // 2, "axis_of_pair")
     _check(fn, lib().cs_kv4_rerotate(_ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales), _ptr(src_slot), _ptr(dst_slot), _ptr(delta),
@@ -414,6 +423,7 @@ def cs_kv4_window_attn(q, k_codes_layer, k_scales_layer, v_codes_layer, v_scales
     if workspace_bytes is None:
         workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     fn = "cs_kv4_window_attn"
+    _here(fn, out)
     _need(fn, q, n_q * n_q_heads * head_dim, "q"); _need(fn, out, n_q * n_q_heads * head_dim, "out"); _need(fn, lse, n_q * n_q_heads, "lse")
     _need(fn, cu_q, n_streams + 1, "cu_q"); _need(fn, q_pos, n_q, "q_pos"); _need(fn, kv_len, n_streams, "kv_len")
     _need(fn, block_table, n_streams * max_blocks, "block_table")
@@ -435,6 +445,7 @@ def cs_attn_weights(q, lse, k_cache_layer, k_scales_layer, cu_q, q_pos, kv_len, 
     if workspace_bytes is None:
         workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     fn = "cs_attn_weights"
+    _here(fn, weight_out)
     _need(fn, q, n_q * n_q_heads * head_dim, "q"); _need(fn, lse, n_q * n_q_heads, "lse")
     _need(fn, cu_q, n_streams + 1, "cu_q"); _need(fn, q_pos, n_q, "q_pos"); _need(fn, kv_len, n_streams, "kv_len")
     _need(fn, block_table, n_streams * max_blocks, "block_table")
@@ -451,6 +462,7 @@ def cs_attn_weights(q, lse, k_cache_layer, k_scales_layer, cu_q, q_pos, kv_len, 
 def cs_plan_evict(weight, kv_len, block_table_old, max_blocks_old, block_table_new, max_blocks_new, n_streams, budget, n_first, n_last,
                   renumber, kept, src_slot, dst_slot, delta, kv_len_new, weight_new):
     fn = "cs_plan_evict"
+    _here(fn, kept)
     _need(fn, weight, n_streams * max_blocks_old * CS_KV_BLOCK, "weight"); _need(fn, kv_len, n_streams, "kv_len")
     _need(fn, block_table_old, n_streams * max_blocks_old, "block_table_old")
     _need(fn, block_table_new, n_streams * max_blocks_new, "block_table_new")

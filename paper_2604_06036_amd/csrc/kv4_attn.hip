@@ -854,7 +854,7 @@ extern "C" int cs_kv4_window_attn(const void* q, const uint8_t* k_codes_layer, c
   if (dtype != CS_F32 && dtype != CS_BF16) return CS_EUNSUPPORTED;
   if ((head_dim != 64 && head_dim != 128) || block_size != CS_KV_BLOCK || n_q_heads / n_kv_heads > 16 || n_kv_heads > 65535) return CS_EUNSUPPORTED;
   if (!cs::kv4_strides(stride_slot, stride_head, 0) || stride_slot >= (1 << 26)) return CS_EUNSUPPORTED;
-  if (n_q > 0x7fffffffll / 16 || max_blocks > 0x7fffffff / CS_KV_BLOCK - kKeys) return CS_EUNSUPPORTED;
+  if (n_q >= (1 << 26) || max_blocks > 0x7fffffff / CS_KV_BLOCK - kKeys) return CS_EUNSUPPORTED;
   if (n_q == 0 || n_streams == 0) return CS_OK;
   if (!q || !k_codes_layer || !k_scales_layer || !v_codes_layer || !v_scales_layer || !cu_q || !q_pos || !kv_len || !block_table || !out || max_blocks < 1)
     return CS_EINVAL;

@@ -404,6 +404,8 @@ SHAPES = [
     (28, 4, 128, [2500, 300], [1, 2], "tail", "head"),
     (4, 1, 128, [5000], [3], "any", "slot"),
     (12, 3, 64, [3000, 1], [5, 1], "any", "head"),
+    (16, 4, 64, [2439, 800], [60, 45], "any", "slot"),                      # many rows, sweeps in pieces
+    (8, 2, 64, [30 + 3 * i for i in range(66)], [20] * 66, "sorted", "head"),    # more streams than lanes, many rows
 ]
 
 
@@ -466,6 +468,46 @@ def test_kv4_attention_equals_attention_over_the_gathered_rows(cs):
     torch.cuda.synchronize()
     b.check(out, None)
     b.check(other, None)
+
+
+@pytest.mark.parametrize("n_q", [1, 40])
+def test_kv4_pools_past_32_bits(cs, n_q):
+    """Rows 4 KiB apart, blocks in the last of 4.5 GB of codes: write, move, read back, attention, weights."""
+    say("4-bit pool of 4.5 GB, queries:", n_q)
+    n_slots, stride, d, kv = 1100000, 8192, 128, 300
+    rng = np.random.default_rng(11)
+    codes = [torch.zeros((n_slots * stride // 2,), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    scales = [torch.zeros((n_slots * stride // 32,), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    blocks = n_slots // 16 - 1 - rng.permutation(40)[:19].astype(np.int32)
+    table = blocks[None].astype(np.int32)
+    slots = (blocks[np.arange(kv) // 16] * 16 + np.arange(kv) % 16).astype(np.int32)
+    assert int(slots.min()) * (stride // 2) > 1 << 32
+    k, v = (rng.normal(size=(kv, 1, d)).astype(np.float32) for _ in range(2))
+    cs.cs_rope_refresh_scatter(None, None, dev(k), dev(v), dev(slots), None, None, codes[0], codes[1], scales[0], scales[1], kv, 0, 1, d, 0, d, d, stride, d, 1e6, 0,
+                               cs.CS_F32, cs.CS_KV4)
+    low = np.arange(kv, dtype=np.int32)
+    cs.cs_kv4_rerotate(codes[0], scales[0], codes[1], scales[1], dev(slots), dev(low), dev(np.zeros(kv, np.int32)), None, kv, 1, 1, d, 0, stride, d, 1e6, 0)
+    got = [[torch.zeros((1, kv, 1, d), device=DEV) for _ in range(2)] for _ in range(2)]
+    for at, out in ((slots, got[0]), (low, got[1])):
+        cs.cs_kv4_gather(codes[0], scales[0], codes[1], scales[1], dev(at), kv, 1, 1, d, 0, stride, d, *out, cs.CS_F32)
+    kq, vq = ko.values(*ko.quantise(k)), ko.values(*ko.quantise(v))
+    for out in got:
+        assert np.array_equal(out[0][0].double().cpu().numpy(), kq) and np.array_equal(out[1][0].double().cpu().numpy(), vq)
+    q64, q = single(rng.normal(size=(n_q, 4, d)), torch.bfloat16)
+    pos = np.arange(kv - n_q, kv).astype(np.int32)
+    out, lse = torch.zeros_like(q), torch.zeros((n_q, 4), device=DEV)
+    i32 = lambda *x: dev(np.array(x, np.int32))
+    nbytes = max(cs.cs_kv4_window_attn_workspace(n_q, 1, 4, 1, d, 19), cs.cs_attn_weights_workspace(n_q, 1, 4, 1, d, 19))
+    ws = torch.zeros((nbytes,), dtype=torch.uint8, device=DEV)
+    cs.cs_kv4_window_attn(q, codes[0], scales[0], codes[1], scales[1], i32(0, n_q), dev(pos), i32(kv), dev(table), 19, 16, out, lse, n_q, 1, 4, 1, d, stride, d, d ** -0.5,
+                          cs.CS_BF16, ws)
+    want, stat, p = ko.attention(q64, kq, vq, pos, d ** -0.5)
+    mass = np.einsum("thj,jhc->thc", p, np.abs(np.repeat(vq, 4, 1)))
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= 3 * B * mass + B * np.abs(want))
+    w = torch.zeros((1, 19 * 16), device=DEV)
+    cs.cs_attn_weights(q, lse, codes[0], scales[0], i32(0, n_q), dev(pos), i32(kv), dev(table), 19, 16, None, w, 1.0, n_q, 1, 4, 1, d, stride, d, d ** -0.5, cs.CS_BF16, cs.CS_KV4, ws)
+    # (sums |q k| scale below 40, on either side of the statistics: 2 (d/8 + 8) u 40)
+    assert np.all(np.abs(w[0, :kv].double().cpu().numpy() - p.sum((0, 1))) <= 80 * (d / 8 + 8) * U * p.sum((0, 1)) + 1e-30)
 
 
 CACHES = [("bf16", "kv4"), ("f32", "kv4"), ("bf16", "bf16"), ("f32", "f32")]

@@ -35,15 +35,15 @@ REFUSED = [
                                      dict(out=None), dict(mb=0), dict(mb=-1), dict(n=-1), dict(s=-1), dict(hq=5), dict(hkv=0), dict(hq=0), dict(scale=0.0), dict(scale=-1.0),
                                      dict(scale=NAN), dict(scale=INF), dict(ss=-32)]),
     ("cs_kv4_window_attn", ATTN, U, [dict(d=32), dict(d=96), dict(d=256), dict(bs=32), dict(hq=34), dict(dt=cs.CS_KV4), dict(ss=40), dict(sh=8), dict(q=A + 8), dict(out=A + 8),
-                                     dict(kc=A + 8), dict(vc=A + 8), dict(n=1 << 27), dict(hkv=70000, hq=70000), dict(mb=1 << 27)]),
+                                     dict(kc=A + 8), dict(vc=A + 8), dict(n=1 << 26), dict(ss=1 << 26), dict(hkv=70000, hq=70000), dict(mb=1 << 27)]),
     ("cs_attn_weights", WEIGHTS, I, [dict(q=None), dict(kc=None), dict(ks=None), dict(cu=None), dict(pos=None), dict(kv=None), dict(bt=None), dict(wo=None), dict(mb=0), dict(n=-1),
                                      dict(s=-1), dict(hq=5), dict(scale=0.0), dict(scale=NAN), dict(decay=-0.1), dict(decay=1.1), dict(decay=NAN)]),
     ("cs_attn_weights", WEIGHTS, U, [dict(d=32), dict(bs=8), dict(hq=34), dict(dt=cs.CS_KV4), dict(cdt=cs.CS_F32), dict(cdt=5), dict(ss=40), dict(ss=132, cdt=cs.CS_BF16), dict(q=A + 8),
-                                     dict(kc=A + 8), dict(mb=1 << 27), dict(n=1 << 31)]),
+                                     dict(kc=A + 8), dict(mb=1 << 27), dict(n=1 << 31), dict(n=1 << 28, hq=2)]),
     ("cs_attn_weights", WEIGHTS, W, [dict(ws=None), dict(ws=A + 8), dict(wsb=16)]),
     ("cs_plan_evict", EVICT, I, [dict(w=None), dict(kv=None), dict(bo=None), dict(bn=None), dict(kept=None), dict(src=None), dict(dst=None), dict(delta=None), dict(kvn=None), dict(s=-1),
                                  dict(budget=0), dict(first=-1), dict(last=-1), dict(mbo=0), dict(mbn=0), dict(budget=65), dict(mbn=3)]),
-    ("cs_plan_evict", EVICT, U, [dict(mbo=1 << 27), dict(mbn=1 << 27)]),
+    ("cs_plan_evict", EVICT, U, [dict(mbo=1 << 27), dict(mbn=1 << 27), dict(budget=(1 << 30) + 1, mbn=8)]),
 ]
 
 
