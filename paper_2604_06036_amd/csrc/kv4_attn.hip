@@ -758,40 +758,73 @@ __global__ __launch_bounds__(64 * WAVES, PARTS == 1 ? 3 : 2) void kv4_keys_kerne
 }
 
 // ------------------------------------------------------------------------------------------
-// The pieces of a row tile's sweep, joined: a thread four columns of a row.
-template <int D, int ROWS>
+// The pieces of a row tile's sweep, joined: a thread four columns of a row.  SLICED: the workgroup's eight (head_dim 64: sixteen) groups
+// of lanes that make a row share the pieces of one row, and meet in LDS.
+template <int D, int ROWS, bool SLICED>
 __global__ __launch_bounds__(256) void kv4_join_kernel(Params p, int bf16) {
-  constexpr int PER_ROW = D / 4, AT_ONCE = 256 / PER_ROW;
-  const int kvh = blockIdx.y;
+  constexpr int PER_ROW = D / 4, GROUPS = 256 / PER_ROW;
+  __shared__ __attribute__((aligned(16))) float s_o[SLICED ? GROUPS : 1][D];
+  __shared__ float s_m[GROUPS], s_l[GROUPS];
+  const int kvh = blockIdx.y, grp = threadIdx.x / PER_ROW, d = 4 * (threadIdx.x % PER_ROW);
   Tile t;
   if (!find_tile<ROWS>(p, blockIdx.x, &t)) return;
   if (min(p.kv_len[t.stream], p.max_blocks * CS_KV_BLOCK) <= 0) return;
-  const int row0 = t.row0, d = 4 * (threadIdx.x % PER_ROW);
+  const int r = SLICED ? static_cast<int>(blockIdx.z) : static_cast<int>(blockIdx.z) * GROUPS + grp;
+  const bool live = r < ROWS && t.row0 + r < t.rows;
+  if (SLICED && !live) return;
   const int64_t job0 = static_cast<int64_t>(blockIdx.x) * p.pieces * p.n_kv_heads + kvh;
-  for (int r = blockIdx.z * AT_ONCE + threadIdx.x / PER_ROW; r < ROWS && row0 + r < t.rows; r += AT_ONCE * gridDim.z) {
-    float m = -INFINITY, l = 0.0f;
-    f32x4 o = {};
-    for (int k = 0; k < p.pieces; ++k) {
-      const int64_t at = (job0 + static_cast<int64_t>(k) * p.n_kv_heads) * ROWS + r;
-      const cs::f32v2 ml = *reinterpret_cast<const cs::f32v2*>(p.ws_ml + 2 * at);
-      if (ml.y == 0.0f) continue;        // (a piece without entries that the row sees; its sums are 0, or were not written)
-      const float top = fmaxf(m, ml.x);
-      const float fo = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - top) * p.scale_log2e);      // (sums are 0 there)
-      const float fn = ml.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((ml.x - top) * p.scale_log2e);
-      const f32x4 x = *reinterpret_cast<const f32x4*>(p.ws_o + at * D + d);
-      o = o * fo + x * fn;
-      l = l * fo + ml.y * fn;
-      m = top;
+  float m = -INFINITY, l = 0.0f;
+  f32x4 o = {};
+  auto add = [&](float pm, float pl, const f32x4& x) __attribute__((always_inline)) {
+    const float top = fmaxf(m, pm);
+    const float fo = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - top) * p.scale_log2e);      // (sums are 0 there)
+    const float fn = pm == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((pm - top) * p.scale_log2e);
+    o = o * fo + x * fn;
+    l = l * fo + pl * fn;
+    m = top;
+  };
+  constexpr int STEP = SLICED ? GROUPS : 1;
+  if (live)
+    for (int k0 = SLICED ? grp : 0; k0 < p.pieces; k0 += 4 * STEP) {       // (four under way at once)
+      cs::f32v2 ml[4];
+      f32x4 x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int64_t at = (job0 + static_cast<int64_t>(min(k0 + k * STEP, p.pieces - 1)) * p.n_kv_heads) * ROWS + r;
+        ml[k] = *reinterpret_cast<const cs::f32v2*>(p.ws_ml + 2 * at);
+        x[k] = *reinterpret_cast<const f32x4*>(p.ws_o + at * D + d);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k0 + k * STEP < p.pieces && ml[k].y != 0.0f) add(ml[k].x, ml[k].y, x[k]);      // (0: a piece without entries that the row sees)
     }
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    const int row = row0 + r, tok = t.q0 + row / p.group, head = kvh * p.group + row % p.group;
-    const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-    store4(p.out, (static_cast<int64_t>(tok) * p.n_q_heads + head) * D + d, y, bf16);
-    if (p.lse && d == 0) p.lse[static_cast<int64_t>(tok) * p.n_q_heads + head] = log_sum(m, l, p.scale_log2e);
+  if (SLICED) {
+    *reinterpret_cast<f32x4*>(&s_o[SLICED ? grp : 0][d]) = o;
+    if (d == 0) {
+      s_m[grp] = m;
+      s_l[grp] = l;
+    }
+    __syncthreads();
+    if (grp != 0) return;
+    for (int g = 1; g < GROUPS; ++g)
+      if (s_l[g] != 0.0f) add(s_m[g], s_l[g], *reinterpret_cast<const f32x4*>(&s_o[SLICED ? g : 0][d]));
   }
+  if (!live) return;
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const int row = t.row0 + r, tok = t.q0 + row / p.group, head = kvh * p.group + row % p.group;
+  const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+  store4(p.out, (static_cast<int64_t>(tok) * p.n_q_heads + head) * D + d, y, bf16);
+  if (p.lse && d == 0) p.lse[static_cast<int64_t>(tok) * p.n_q_heads + head] = log_sum(m, l, p.scale_log2e);
 }
 
 // ---- which kernel, how many pieces
+// Tiles that make a piece worth its share of the join, of the keys and the rows kernel.  4 kv heads of 7 query heads, head_dim 128: one
+// token over 919 entries takes 9.9 us uncut (8), 13.3 us in pieces (6), over 1,500 13.2 us at 8 and 11.8 at 16, over 17,630 15.1 and 17.1;
+// 424 tokens over 919 take 30.5 us at 6, 28.8 at 4, 31.4 at 3.
+constexpr int kLeastFew = 8, kLeastMany = 4;
+// Pieces above which a workgroup shares a row's.  64 tokens over 17,630 entries (51 pieces): 45.6 us, 61 us with one thread walking
+// all pieces of its columns; 16 tokens 25.7 and 45 us.
+constexpr int kSliced = 8;
 struct Route {
   bool few;
   int rows, waves;
@@ -807,7 +840,7 @@ Route route(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_head
   r.row_tiles = n_q * group / r.rows + busy;               // no less than the row tiles there are, whatever cu_q says
   const int64_t jobs = r.row_tiles * n_kv_heads, tiles = (static_cast<int64_t>(max_blocks) * CS_KV_BLOCK + kKeys - 1) / kKeys;
   r.waves = 4;
-  const int64_t least = r.few ? 8 : 6;                     // tiles that make a piece worth its share of the join
+  const int64_t least = r.few ? kLeastFew : kLeastMany;
   r.pieces = (r.few ? 1024 : 768) / jobs;
   if (r.pieces > tiles / least) r.pieces = tiles / least;
   if (r.pieces > 64) r.pieces = 64;
@@ -826,9 +859,13 @@ int launch(const Params& p, const Route& r, hipStream_t st) {
   else if (r.waves == 8) hipLaunchKernelGGL((kv4_keys_kernel<D, PARTS, 8>), grid, dim3(512), 0, st, p);
   else hipLaunchKernelGGL((kv4_keys_kernel<D, PARTS, 4>), grid, dim3(256), 0, st, p);
   if (r.pieces > 1) {
-    const dim3 all(static_cast<unsigned>(r.row_tiles), static_cast<unsigned>(p.n_kv_heads), r.few ? 2 : 8);
-    if (r.few) hipLaunchKernelGGL((kv4_join_kernel<D, kRowsFew>), all, dim3(256), 0, st, p, PARTS == 1);
-    else hipLaunchKernelGGL((kv4_join_kernel<D, kRowsMany>), all, dim3(256), 0, st, p, PARTS == 1);
+    const unsigned tiles = static_cast<unsigned>(r.row_tiles), heads = static_cast<unsigned>(p.n_kv_heads);
+    constexpr int at_once = 256 / (D / 4);
+    const dim3 whole(tiles, heads, (r.rows + at_once - 1) / at_once), sliced(tiles, heads, r.rows);
+    if (r.few && r.pieces > kSliced) hipLaunchKernelGGL((kv4_join_kernel<D, kRowsFew, true>), sliced, dim3(256), 0, st, p, PARTS == 1);
+    else if (r.few) hipLaunchKernelGGL((kv4_join_kernel<D, kRowsFew, false>), whole, dim3(256), 0, st, p, PARTS == 1);
+    else if (r.pieces > kSliced) hipLaunchKernelGGL((kv4_join_kernel<D, kRowsMany, true>), sliced, dim3(256), 0, st, p, PARTS == 1);
+    else hipLaunchKernelGGL((kv4_join_kernel<D, kRowsMany, false>), whole, dim3(256), 0, st, p, PARTS == 1);
   }
   return cs::note_hip(hipGetLastError());
 }
