@@ -58,7 +58,6 @@ __global__ __launch_bounds__(kThreads) void plan_evict_kernel(Params p) {
   const int j0 = wave * rounds * 64 + lane;                // entry i of a thread: j0 + 64 i
   const int32_t* ids_old = p.bt_old + static_cast<int64_t>(stream) * p.max_blocks_old;
   const int32_t* ids_new = p.bt_new + static_cast<int64_t>(stream) * p.max_blocks_new;
-  auto rank_at = [&](int j) __attribute__((always_inline)) { return rank_of(weight[j], j < first || j >= last); };
   uint32_t held[HELD ? HELD : 1];
   if (HELD) {
     float w[HELD ? HELD : 1];
@@ -67,14 +66,23 @@ __global__ __launch_bounds__(kThreads) void plan_evict_kernel(Params p) {
 #pragma unroll
     for (int i = 0; i < HELD; ++i) held[i] = rank_of(w[i], j0 + 64 * i < first || j0 + 64 * i >= last);
   }
-  auto rank = [&](int i) __attribute__((always_inline)) { return HELD ? held[HELD ? i : 0] : rank_at(j0 + 64 * i); };
+  constexpr int kAtOnce = 8;             // entries that a thread asks for together where it holds none
   auto each = [&](auto f) __attribute__((always_inline)) {
     if (HELD) {
 #pragma unroll
       for (int i = 0; i < HELD; ++i)
-        if (i < rounds) f(i);
+        if (i < rounds) f(i, held[HELD ? i : 0]);
     } else {
-      for (int i = 0; i < rounds; ++i) f(i);
+      for (int i0 = 0; i0 < rounds; i0 += kAtOnce) {
+        float w[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) w[k] = weight[min(j0 + 64 * (i0 + k), n - 1)];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+          const int j = j0 + 64 * (i0 + k);
+          if (i0 + k < rounds) f(i0 + k, rank_of(w[k], j < first || j >= last));
+        }
+      }
     }
   };
 
@@ -88,9 +96,8 @@ __global__ __launch_bounds__(kThreads) void plan_evict_kernel(Params p) {
       s_bins[tid] = 0;
       s_bins[kThreads + tid] = 0;
       __syncthreads();
-      each([&](int i) __attribute__((always_inline)) {
+      each([&](int i, uint32_t r) __attribute__((always_inline)) {
         if (j0 + 64 * i >= n) return;
-        const uint32_t r = rank(i);
         if ((r & mask) == prefix) atomicAdd(&s_bins[(r >> shift) & ((1u << bits) - 1)], 1);
       });
       __syncthreads();
@@ -121,16 +128,15 @@ __global__ __launch_bounds__(kThreads) void plan_evict_kernel(Params p) {
 
   // ---- lists, in index order: before an entry stay the larger ones before it, and of its equals no more than `left`
   const bool all = keep == n;
-  auto marks = [&](int i, uint64_t* above, uint64_t* equal) __attribute__((always_inline)) {
+  auto marks = [&](int i, uint32_t r, uint64_t* above, uint64_t* equal) __attribute__((always_inline)) {
     const bool there = j0 + 64 * i < n;
-    const uint32_t r = there ? rank(i) : 0u;
     *above = __ballot(there && (all || r > prefix));
     *equal = __ballot(there && !all && r == prefix);
   };
   int above = 0, equal = 0;
-  each([&](int i) __attribute__((always_inline)) {
+  each([&](int i, uint32_t r) __attribute__((always_inline)) {
     uint64_t a, e;
-    marks(i, &a, &e);
+    marks(i, r, &a, &e);
     above += __popcll(a);
     equal += __popcll(e);
   });
@@ -156,9 +162,9 @@ __global__ __launch_bounds__(kThreads) void plan_evict_kernel(Params p) {
   };
   const uint64_t lower = (1ull << lane) - 1;
   if (keep > 0)
-    each([&](int i) __attribute__((always_inline)) {
+    each([&](int i, uint32_t r) __attribute__((always_inline)) {
       uint64_t a, e;
-      marks(i, &a, &e);
+      marks(i, r, &a, &e);
       const int before = equal + __popcll(e & lower), j = j0 + 64 * i;
       if ((a >> lane & 1) || ((e >> lane & 1) && before < left)) {
         const int at = above + __popcll(a & lower) + min(before, left);
