@@ -224,7 +224,7 @@ struct Kv4RerotateParams {
   const int32_t* __restrict__ src_slot;
   const int32_t* __restrict__ dst_slot;        // nullptr: in place, keys only
   int64_t n_rows, stride_layer, stride_slot, stride_head;
-  int32_t n_layers, n_kv_heads, head_dim, lanes_per_head, layers_per_block, rows_per_block;
+  int32_t n_layers, n_kv_heads, head_dim, lanes_per_head, layers_per_block, rows_per_block, scale_width;
 };
 
 // A workgroup evaluates the angles of its rows once, into LDS (all heads and layers of a row turn by them).  A lane owns 32 pairs of
@@ -268,20 +268,26 @@ __global__ __launch_bounds__(256) void kv4_rerotate_kernel(Kv4RerotateParams p) 
 
     const int off_a = kStyle == CS_ROPE_HALF_SPLIT ? j * N : 2 * j * N;
     const int off_b = kStyle == CS_ROPE_HALF_SPLIT ? p.head_dim / 2 + j * N : 2 * j * N + N;
+    const int at_a = p.scale_width == 1 ? 0 : 8 * (off_a / N), at_b = p.scale_width == 1 ? 8 : 8 * (off_b / N);
     const int64_t from = static_cast<int64_t>(src) * p.stride_slot + static_cast<int64_t>(head) * p.stride_head;
     const int64_t to = static_cast<int64_t>(dst) * p.stride_slot + static_cast<int64_t>(head) * p.stride_head;
     for (int l = l_begin; l < l_end; ++l) {
       const int64_t s = static_cast<int64_t>(l) * p.stride_layer + from, d = static_cast<int64_t>(l) * p.stride_layer + to;
       const cs::u32x4 wa = *reinterpret_cast<const cs::u32x4*>(p.k_codes + (s + off_a) / 2);
       const cs::u32x4 wb = *reinterpret_cast<const cs::u32x4*>(p.k_codes + (s + off_b) / 2);
-      const uint32_t ea = p.k_scales[(s + off_a) / N], eb = p.k_scales[(s + off_b) / N];
+      uint32_t ks = 0, vs = 0;           // scale bytes of the head where they are few, else the lane's two
+      auto scales = [&](const uint8_t* from_scales) __attribute__((always_inline)) {
+        if (p.scale_width == 4) return *reinterpret_cast<const uint32_t*>(from_scales + s / N);
+        if (p.scale_width == 2) return static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(from_scales + s / N));
+        return static_cast<uint32_t>(from_scales[(s + off_a) / N]) | static_cast<uint32_t>(from_scales[(s + off_b) / N]) << 8;
+      };
+      ks = scales(p.k_scales);
+      const uint32_t ea = ks >> at_a & 0xffu, eb = ks >> at_b & 0xffu;
       cs::u32x4 va, vb;
-      uint8_t fa = 0, fb = 0;
       if (p.dst_slot) {
         va = *reinterpret_cast<const cs::u32x4*>(p.v_codes + (s + off_a) / 2);
         vb = *reinterpret_cast<const cs::u32x4*>(p.v_codes + (s + off_b) / 2);
-        fa = p.v_scales[(s + off_a) / N];
-        fb = p.v_scales[(s + off_b) / N];
+        vs = scales(p.v_scales);
       }
       float a[N], b[N];
 #pragma unroll
@@ -321,13 +327,24 @@ __global__ __launch_bounds__(256) void kv4_rerotate_kernel(Kv4RerotateParams p) 
       }
       *reinterpret_cast<cs::u32x4*>(p.k_codes + (d + off_a) / 2) = oa;
       *reinterpret_cast<cs::u32x4*>(p.k_codes + (d + off_b) / 2) = ob;
-      p.k_scales[(d + off_a) / N] = static_cast<uint8_t>(na);
-      p.k_scales[(d + off_b) / N] = static_cast<uint8_t>(nb);
       if (p.dst_slot) {
         *reinterpret_cast<cs::u32x4*>(p.v_codes + (d + off_a) / 2) = va;
         *reinterpret_cast<cs::u32x4*>(p.v_codes + (d + off_b) / 2) = vb;
-        p.v_scales[(d + off_a) / N] = fa;
-        p.v_scales[(d + off_b) / N] = fb;
+      }
+      uint32_t kn = na << at_a | nb << at_b;
+      if (p.scale_width == 4) {          // two lanes a head: one writes the keys' scales, one the values'
+        kn |= static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(kn), 0xb1, 0xf, 0xf, true));       // lane ^ 1
+        if (j == 0 || p.dst_slot) *reinterpret_cast<uint32_t*>((j == 0 ? p.k_scales : p.v_scales) + d / N) = j == 0 ? kn : vs;
+      } else if (p.scale_width == 2) {
+        *reinterpret_cast<uint16_t*>(p.k_scales + d / N) = static_cast<uint16_t>(kn);
+        if (p.dst_slot) *reinterpret_cast<uint16_t*>(p.v_scales + d / N) = static_cast<uint16_t>(vs);
+      } else {
+        p.k_scales[(d + off_a) / N] = static_cast<uint8_t>(na);
+        p.k_scales[(d + off_b) / N] = static_cast<uint8_t>(nb);
+        if (p.dst_slot) {
+          p.v_scales[(d + off_a) / N] = static_cast<uint8_t>(vs);
+          p.v_scales[(d + off_b) / N] = static_cast<uint8_t>(vs >> 8);
+        }
       }
     }
   }
@@ -490,6 +507,12 @@ extern "C" int cs_kv4_rerotate(uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_c
   p.n_kv_heads = n_kv_heads;
   p.head_dim = head_dim;
   p.lanes_per_head = head_dim / 64;
+  // Scale bytes move as one word a row and head where they lie as one (head_dim 64 and 128): 15,023 rows of 28 layers,
+  // 4 heads of 128 each, take 265 us head-major and 120 us slot-major, with single bytes 297 and 125.
+  const int64_t strides = stride_layer | stride_slot | stride_head;
+  const uintptr_t scales = reinterpret_cast<uintptr_t>(k_scales) | (dst_slot ? reinterpret_cast<uintptr_t>(v_scales) : 0);
+  const int width = 2 * p.lanes_per_head;
+  p.scale_width = width <= 4 && strides / cs::kKv4Block % width == 0 && scales % width == 0 ? width : 1;
   const int units = n_kv_heads * p.lanes_per_head, places = kAngleRows / (head_dim / 2);
   p.rows_per_block = units >= 256 ? 1 : 256 / units < places ? 256 / units : places;
   const int64_t blocks_x = (n_rows + p.rows_per_block - 1) / p.rows_per_block;

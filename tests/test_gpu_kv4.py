@@ -248,6 +248,38 @@ def test_kv4_rerotate(cs, n, layers, hkv, d, axes, style, layout, in_place):
             assert np.array_equal(after[i][1][l], want)
 
 
+@pytest.mark.parametrize("d,pad,shift,in_place", [(64, 32, 0, False), (64, 0, 1, False), (64, 0, 1, True), (128, 64, 0, False), (128, 32, 0, True),
+                                                   (128, 0, 2, False), (128, 0, 1, True)])
+def test_kv4_rerotate_scales_at_any_byte(cs, d, pad, shift, in_place):
+    """Rows that lie `pad` elements apart and scales that start `shift` bytes into their memory: what dense, aligned pools give."""
+    say("kv4 rerotate, scales anywhere", d, pad, shift, in_place)
+    n, layers, hkv = 37, 2, 3
+    rng = np.random.default_rng(d + pad + shift)
+    n_slots, row = 2 * n, hkv * d + pad
+    perm = rng.permutation(n_slots).astype(np.int32)
+    src, dst, delta = dev(perm[:n].copy()), dev(perm[n:].copy()), dev(rng.integers(-400, 400, (n,)).astype(np.int32))
+    got = []
+    fill = [rng.integers(lo, hi, (layers, n_slots, hkv, d // per)).astype(np.uint8) for lo, hi, per in ((0, 256, 2), (0, 256, 2), (1, 255, 32), (1, 255, 32))]
+    for r, off in ((hkv * d, 0), (row, shift)):
+        ts, flats = [], []
+        for x, per in zip(fill, (2, 2, 32, 32)):
+            start = off if per == 32 else 0
+            flat = torch.full((start + layers * n_slots * r // per,), 7, dtype=torch.uint8, device=DEV)
+            t = torch.as_strided(flat, x.shape, (n_slots * r // per, r // per, d // per, 1), start)
+            t.copy_(dev(x))
+            ts.append(t)
+            flats.append(flat)
+        cs.cs_kv4_rerotate(ts[0], ts[2], None if in_place else ts[1], None if in_place else ts[3], src, None if in_place else dst, delta, None, n, layers,
+                           hkv, d, n_slots * r, r, d, 1e6, 0)
+        got.append([t.cpu().numpy() for t in ts])
+        for flat, t in zip(flats, ts):                     # nothing beside the rows is written
+            t.fill_(7)
+            assert bool((flat == 7).all())
+    assert not np.array_equal(got[0][0], fill[0])
+    for a, b in zip(*got):
+        assert np.array_equal(a, b)
+
+
 # ------------------------------------------------------------------------------------------ attention, attention weights
 
 class Batch:
