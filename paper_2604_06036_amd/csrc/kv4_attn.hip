@@ -822,9 +822,9 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Params p, int bf16) {
 // token over 919 entries takes 9.9 us uncut (8), 13.3 us in pieces (6), over 1,500 13.2 us at 8 and 11.8 at 16, over 17,630 15.1 and 17.1;
 // 424 tokens over 919 take 30.5 us at 6, 28.8 at 4, 31.4 at 3.
 constexpr int kLeastFew = 8, kLeastMany = 4;
-// Pieces above which a workgroup shares a row's.  64 tokens over 17,630 entries (51 pieces): 45.6 us, 61 us with one thread walking
-// all pieces of its columns; 16 tokens 25.7 and 45 us.
-constexpr int kSliced = 8;
+// Pieces above which a workgroup shares a row's: 64 tokens over 17,630 entries (48 pieces) take 45.6 us, 61 us with one thread walking
+// all pieces of its columns; 7 streams of 40 tokens over up to 5,000 (9 pieces) 57 us shared, 52 us walked.
+constexpr int kSliced = 16;
 struct Route {
   bool few;
   int rows, waves;
@@ -835,13 +835,20 @@ Route route(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_head
   Route r;
   const int group = n_q_heads / n_kv_heads;
   const int64_t busy = n_streams < n_q ? n_streams : n_q;
+  // The keys kernel up to four of its row tiles a stream: 8 tokens of 7 heads (56 rows) over 17,630 entries take 18.9 us in it, 22.1 us
+  // in the rows kernel; 16 tokens (112 rows) 26.7 and 24.0 us, 64 streams of those over 4,000 151 and 135.
   r.few = n_q * group <= 64 * busy;
   r.rows = r.few ? kRowsFew : kRowsMany;
   r.row_tiles = n_q * group / r.rows + busy;               // no less than the row tiles there are, whatever cu_q says
   const int64_t jobs = r.row_tiles * n_kv_heads, tiles = (static_cast<int64_t>(max_blocks) * CS_KV_BLOCK + kKeys - 1) / kKeys;
   r.waves = 4;
   const int64_t least = r.few ? kLeastFew : kLeastMany;
-  r.pieces = (r.few ? 1024 : 768) / jobs;
+  // Pieces for two rounds of what the card holds at once (keys: 4 waves each; half of it costs 14.2 -> 15.8 us for 16 tokens of 16
+  // streams, twice it changes nothing) and three workgroups a CU (rows: 64 tokens over 17,630 entries take 45 us, with half as
+  // many 47.8, with twice 51).  The rows kernel counts the row tiles that streams of one length would have (64 streams of 16 tokens over
+  // 4,000: 97 us, 135 by the bound on any lengths); the keys kernel the bound (64 streams of a token over 8,000: 103 us, 116 us).
+  const int64_t even = (n_q * group + busy * r.rows - 1) / (busy * r.rows) * busy * n_kv_heads;     // jobs of streams of one length
+  r.pieces = (r.few ? 1024 : 768) / (!r.few && even < jobs ? even : jobs);
   if (r.pieces > tiles / least) r.pieces = tiles / least;
   if (r.pieces > 64) r.pieces = 64;
   if (r.pieces < 1) r.pieces = 1;

@@ -453,6 +453,29 @@ def test_kv4_window_attn(cs, i, dtype):
     assert none is None and torch.equal(out, again)
 
 
+# sweeps cut into pieces, and their joins
+LONG = [
+    (7, 1, 64, [9000], [2], "any", "head"),                                 # few rows, many pieces
+    (16, 2, 128, [9300, 0, 5], [1, 1, 2], "any", "slot"),
+    (8, 2, 128, [4600, 30], [30, 17], "any", "head"),                       # many rows, many pieces
+    (16, 1, 64, [4700], [9], "any", "slot"),
+    (8, 1, 64, [3000, 1500, 20, 0], [150, 1, 1, 3], "any", "head"),         # streams of very different numbers of rows
+    (4, 4, 128, [1700, 900, 1800], [70, 200, 90], "sorted", "slot"),        # few pieces
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("i", range(len(LONG)))
+def test_kv4_window_attn_in_pieces(cs, i, dtype):
+    hq, hkv, d, kv, nq, where, layout = LONG[i]
+    say("kv4 attention in pieces", dtype, LONG[i])
+    b = Batch(cs, 50 + i, hq, hkv, d, kv, nq, dtype, layout=layout, where=where, extra=i % 3)
+    out, lse = b.attend()
+    b.check(out, lse)
+    again, stat = b.attend(ws_fill=0xFF)
+    assert torch.equal(out, again) and torch.equal(lse, stat)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("gain", [4.0, 30.0])
 def test_kv4_window_attn_peaked(cs, dtype, gain):
