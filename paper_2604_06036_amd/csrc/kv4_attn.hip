@@ -14,8 +14,13 @@
 //   O^T += V^T P^T   v_mfma_f32_32x32x16_bf16: P^T is in operand layout as it is, values are converted to bf16 on their way
 //                    into LDS and come back by its transposing read.
 // Many rows a stream (rows kernel): four waves of 32 rows share a tile in LDS.  Few rows (keys kernel): every wave holds the
-// same 32 rows and takes tiles of its own, with nothing but its own values in LDS; the waves join their results at the end.
-// Where there are few workgroups, the sweep of a row tile is cut into pieces of entries, whose results a second launch joins.
+// same 16 rows (16x16x32 instructions) and takes tiles of its own, with nothing but its own values in LDS; the waves join their
+// results at the end.  Where there are few workgroups, the sweep of a row tile is cut into pieces of entries, whose results a second
+// launch joins.
+// Bounds.  Rows kernel: the vector work of unpacking and softmax shares issue slots with the matrix products; 32 streams of up to 389
+// tokens of 28 heads over up to 1,100 entries take 120 us, 706 TFLOP/s (a large product of the library reaches 1,200).  Keys kernel: memory;
+// 64 streams of one token of 32 heads over up to 17,630 entries, 8 kv heads, take 197 us, 4.7 TB/s, as fast as a large copy.
+// One token over one window of 919 entries takes 8.9 us: a chain of one tile a wave, the join of eight waves and a launch.
 #include <math.h>
 
 #include <type_traits>
