@@ -517,12 +517,14 @@ int cs_refresh_prefill_attn(const void* k_new, const void* v_new, const int32_t*
  *     scale     one byte e: the element stands for its number times 2^(e - 127), e in 1..254 (0 is read as 1);
  *               255: the block held a NaN or an infinity, all of its elements are read as NaN
  * A block x of 32 numbers becomes: e the least in 1..254 with max |x| <= 7 * 2^(e - 127), elements the nearest numbers
- * to x / 2^(e - 127), ties to the even code, saturating at 6 (a number past 3.5 * 2^126 becomes 2^128, which reads as infinity).  (So the stored numbers of a row are bf16 numbers, and
- * a row that is written again unchanged keeps its numbers.)
+ * to x / 2^(e - 127), ties to the even code, saturating at 6 (a number past 3.5 * 2^126 becomes 2^128, which reads as
+ * infinity).  (So the stored numbers of a row are bf16 numbers, and a row that is written again unchanged keeps its numbers.)
  * A pool is a tensor of codes and one of scales for K and the same for V, addressed by ONE set of strides in elements,
  * multiples of 32: element (l, slot, h, c) is number i = l*stride_layer + slot*stride_slot + h*stride_head + c, its code
  * in byte i/2 of the codes, its scale in byte i/32 of the scales.  Codes are 16-byte aligned.  Head-major pools
  * (stride_slot = head_dim) are read in whole lines by attention, which takes one kv head at a time.
+ * CS_EUNSUPPORTED also answers calls past what a launch holds, 2^32 threads along an axis of its grid: (q1) a thread per 16
+ * elements of a head of all tokens, (q2) per 8 elements of an output, (w) 64 per token and query head where lse is NULL.
  * ------------------------------------------------------------------------------------------ */
 
 /* ------------------------------------------------------------------------------------------
@@ -664,11 +666,12 @@ int cs_attn_weights(const void* q, const float* lse, const void* k_cache_layer, 
  *  weight           in   float [n_streams][max_blocks_old * 16];   kv_len  in  int32 [n_streams] (clamped to the table's rows)
  *  block_table_old, block_table_new   in   int32 [n_streams][max_blocks_old / _new]
  *  kept, src_slot, dst_slot, delta    out  int32 [n_streams][budget]
- *  kv_len_new       out  int32 [n_streams]: m
- *  weight_new       out  float [n_streams][max_blocks_new * 16] or NULL: the kept entries' weights; places past m are left
+ *  kv_len_new       out  int32 [n_streams]: m; not kv_len
+ *  weight_new       out  float [n_streams][max_blocks_new * 16] or NULL: the kept entries' weights; places past m are left;
+ *                        not weight
  * Bit exact.
  * Errors: CS_EINVAL (null pointer, negative size, budget < 1, a block table without columns, a new table too narrow for what
- *         may stay), CS_EUNSUPPORTED (tables of 2^27 columns, budget > 2^30), CS_EHIP.  n_streams == 0 returns CS_OK.
+ *         may stay, kv_len_new == kv_len, weight_new == weight), CS_EUNSUPPORTED (tables of 2^27 columns, budget > 2^30, 2^22 streams), CS_EHIP.  n_streams == 0 returns CS_OK.
  * ------------------------------------------------------------------------------------------ */
 int cs_plan_evict(const float* weight, const int32_t* kv_len, const int32_t* block_table_old, int32_t max_blocks_old,
                   const int32_t* block_table_new, int32_t max_blocks_new, int32_t n_streams, int32_t budget,

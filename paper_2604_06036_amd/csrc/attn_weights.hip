@@ -457,7 +457,7 @@ Layout layout(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_he
   Layout w;
   const int64_t entries = static_cast<int64_t>(max_blocks) * CS_KV_BLOCK;
   w.key_tiles = static_cast<int>((entries + tile - 1) / tile);
-  // Shares of a stream's rows: until about four workgroups a CU are under way, but at least four steps of rows each.
+  // Shares of a stream's rows: until kGroups workgroups are under way, but at least kLeast steps of rows each.
   const int64_t jobs = static_cast<int64_t>(w.key_tiles) * n_streams * n_kv_heads;
   const int64_t steps = (n_q * (n_q_heads / n_kv_heads) / (n_streams > 0 ? n_streams : 1) + kStep - 1) / kStep;
   int64_t c = jobs > 0 ? kGroups / jobs : 1;
@@ -476,7 +476,7 @@ int launch(Params p, const Layout& w, bool have_lse, hipStream_t st) {
   const int64_t shares = static_cast<int64_t>(p.n_streams) * p.n_kv_heads * w.chunks;
   p.shares_per_xcd = shares >= 64;       // (few shares would load the XCDs unevenly)
   const int64_t jobs = (p.shares_per_xcd ? (shares + 7) / 8 * 8 : shares) * w.key_tiles;
-  if (jobs > 0x7fffffffll) return CS_EUNSUPPORTED;
+  if (jobs > cs::kMostThreads / 256) return CS_EUNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(jobs));
   const int64_t all = static_cast<int64_t>(p.max_blocks) * CS_KV_BLOCK * p.n_streams;
   if (!have_lse) {
@@ -514,8 +514,10 @@ extern "C" int cs_attn_weights(const void* q, const float* lse, const void* k_ca
   if ((head_dim != 64 && head_dim != 128) || block_size != CS_KV_BLOCK || n_q_heads / n_kv_heads > 16) return CS_EUNSUPPORTED;
   const int unit = cache_dtype == CS_KV4 ? cs::kKv4Block : cache_dtype == CS_BF16 ? 8 : 4;
   if (stride_slot % unit || stride_head % unit) return CS_EUNSUPPORTED;
-  if (n_q > 0x7fffffffll / n_q_heads || n_q * (n_q_heads / n_kv_heads) >= (1 << 28) || max_blocks > 0x7fffffff / CS_KV_BLOCK) return CS_EUNSUPPORTED;
-  if (static_cast<int64_t>(max_blocks) * CS_KV_BLOCK * n_streams > 0x7fffffffll * 255) return CS_EUNSUPPORTED;
+  if (n_q > 0x7fffffffll / n_q_heads || n_q * (n_q_heads / n_kv_heads) >= (1 << 28) || max_blocks > 0x7fffffff / CS_KV_BLOCK - 256)
+    return CS_EUNSUPPORTED;
+  if (static_cast<int64_t>(max_blocks) * CS_KV_BLOCK * n_streams > cs::kMostThreads - 255) return CS_EUNSUPPORTED;
+  if (!lse && n_q * n_q_heads > (cs::kMostThreads - 255) / 64) return CS_EUNSUPPORTED;     // (a wave a row joins the statistics)
   if (n_streams == 0) return CS_OK;
   if (!kv_len || !weight_out || max_blocks < 1) return CS_EINVAL;
   if (n_q == 0) {                        // earlier weights fade

@@ -11,6 +11,7 @@ typedef __attribute__((ext_vector_type(2))) float f32v2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16v2;
 
 constexpr int kKv4Block = 32;            // elements that share a scale
+constexpr int64_t kMostThreads = 0xffffffffll;   // of a launch, along one axis of its grid
 constexpr uint32_t kKv4NoNumber = 255;   // scale byte of a block that held a NaN or an infinity
 
 // Scale byte of a block whose largest magnitude has the given fp32 bits: the least power of two s with amax <= 7 s.

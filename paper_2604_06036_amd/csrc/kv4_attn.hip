@@ -909,7 +909,7 @@ extern "C" int cs_kv4_window_attn(const void* q, const uint8_t* k_codes_layer, c
     return CS_EINVAL;
   if (!cs::aligned16(q) || !cs::aligned16(out) || !cs::aligned16(k_codes_layer) || !cs::aligned16(v_codes_layer)) return CS_EUNSUPPORTED;
   const Route r = route(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, max_blocks);
-  if (r.jobs > 0x7fffffffll) return CS_EUNSUPPORTED;
+  if (r.jobs > cs::kMostThreads / 512) return CS_EUNSUPPORTED;
   if (r.total && (!workspace || workspace_bytes < r.total || !cs::aligned16(workspace))) return CS_EWORKSPACE;
 
   Params p;

@@ -419,8 +419,8 @@ extern "C" int cs_rope_refresh_scatter(const void* q, void* q_out, const void* k
   p.n_kv_heads = n_kv_heads;
   p.head_dim = head_dim;
   p.lanes_per_tok = head_dim / 2 / kPairs;
+  if (n_tok > (cs::kMostThreads - 255) / p.lanes_per_tok) return CS_EUNSUPPORTED;
   const int64_t blocks_x = (n_tok * p.lanes_per_tok + 255) / 256;
-  if (blocks_x > 0x7fffffffll) return CS_EUNSUPPORTED;
   // Heads a thread turns with one evaluation of its angles: all of them where the tokens alone fill the card, fewer below.
   const int heads = n_q_heads + 2 * n_kv_heads;
   const int64_t shares = blocks_x >= kRopeGroups ? 1 : (kRopeGroups + blocks_x - 1) / blocks_x;
@@ -475,9 +475,9 @@ extern "C" int cs_kv4_gather(const uint8_t* k_codes, const uint8_t* k_scales, co
   p.stride_head = stride_head;
   p.n_kv_heads = n_kv_heads;
   p.lanes_per_head = head_dim / 8;
+  if (n_rows > (cs::kMostThreads - 255) / n_layers / n_kv_heads / p.lanes_per_head) return CS_EUNSUPPORTED;
   p.n_units = n_rows * n_layers * n_kv_heads * p.lanes_per_head;
   const int64_t blocks = (p.n_units + 255) / 256;
-  if (blocks > 0x7fffffffll) return CS_EUNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(blocks), n);
   if (dtype == CS_BF16) hipLaunchKernelGGL(kv4_gather_kernel<true>, grid, dim3(256), 0, cs::as_stream(stream), p);
   else hipLaunchKernelGGL(kv4_gather_kernel<false>, grid, dim3(256), 0, cs::as_stream(stream), p);
@@ -521,8 +521,8 @@ extern "C" int cs_kv4_rerotate(uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_c
   p.scale_width = width <= 4 && strides / cs::kKv4Block % width == 0 && scales % width == 0 ? width : 1;
   const int units = n_kv_heads * p.lanes_per_head, places = kAngleRows / (head_dim / 2);
   p.rows_per_block = units >= 256 ? 1 : 256 / units < places ? 256 / units : places;
+  if (n_rows > cs::kMostThreads / 256 * p.rows_per_block) return CS_EUNSUPPORTED;
   const int64_t blocks_x = (n_rows + p.rows_per_block - 1) / p.rows_per_block;
-  if (blocks_x > 0x7fffffffll) return CS_EUNSUPPORTED;
   // Layers of a workgroup: all of them where the rows alone fill the card.
   const int64_t shares = blocks_x >= kRerotateGroups ? 1 : (kRerotateGroups + blocks_x - 1) / blocks_x;
   p.layers_per_block = static_cast<int32_t>(shares >= n_layers ? 1 : (n_layers + shares - 1) / shares);

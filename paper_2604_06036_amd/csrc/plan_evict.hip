@@ -209,12 +209,14 @@ extern "C" int cs_plan_evict(const float* weight, const int32_t* kv_len, const i
                              int32_t n_last, int32_t renumber, int32_t* kept, int32_t* src_slot, int32_t* dst_slot, int32_t* delta,
                              int32_t* kv_len_new, float* weight_new, void* stream) {
   if (n_streams < 0 || budget < 1 || n_first < 0 || n_last < 0 || max_blocks_old < 1 || max_blocks_new < 1) return CS_EINVAL;
-  if (max_blocks_old > 0x7fffffff / CS_KV_BLOCK - kThreads || max_blocks_new > 0x7fffffff / CS_KV_BLOCK - kThreads || budget > (1 << 30))
+  if (max_blocks_old > 0x7fffffff / CS_KV_BLOCK - kThreads || max_blocks_new > 0x7fffffff / CS_KV_BLOCK - kThreads || budget > (1 << 30) ||
+      n_streams >= (1 << 22))              // (2^32 threads)
     return CS_EUNSUPPORTED;
   // what may stay has to fit a row of the new table
   if ((budget < max_blocks_old * CS_KV_BLOCK ? budget : max_blocks_old * CS_KV_BLOCK) > max_blocks_new * CS_KV_BLOCK) return CS_EINVAL;
   if (n_streams == 0) return CS_OK;
   if (!weight || !kv_len || !block_table_old || !block_table_new || !kept || !src_slot || !dst_slot || !delta || !kv_len_new) return CS_EINVAL;
+  if (kv_len_new == kv_len || weight_new == weight) return CS_EINVAL;
   Params p;
   p.weight = weight;
   p.kv_len = kv_len;

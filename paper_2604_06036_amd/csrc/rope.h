@@ -16,17 +16,9 @@ struct RopeAngles {
   const uint8_t* __restrict__ axis_of_pair;    // [head_dim / 2] values 0..2
 };
 
-// (The frequencies of the last base and head_dim that a thread asked for are kept: 64 powers take longer than a small call.)
+// (64 powers: about 1 us of the host.)
 inline void rope_angles(RopeAngles* r, const int32_t* pos, const uint8_t* axis_of_pair, float base, int head_dim) {
-  static thread_local double theta[kRopeMaxPairs];
-  static thread_local float last_base = 0.0f;
-  static thread_local int last_dim = 0;
-  if (base != last_base || head_dim != last_dim) {
-    for (int i = 0; i < kRopeMaxPairs; ++i) theta[i] = i < head_dim / 2 ? pow(static_cast<double>(base), -2.0 * i / head_dim) : 0.0;
-    last_base = base;
-    last_dim = head_dim;
-  }
-  for (int i = 0; i < kRopeMaxPairs; ++i) r->theta[i] = theta[i];
+  for (int i = 0; i < kRopeMaxPairs; ++i) r->theta[i] = i < head_dim / 2 ? pow(static_cast<double>(base), -2.0 * i / head_dim) : 0.0;
   r->pos = pos;
   r->axis_of_pair = axis_of_pair;
 }

@@ -14,7 +14,7 @@ ATTN = dict(q=A, kc=A, ks=A, vc=A, vs=A, cu=A, pos=A, kv=A, bt=A, mb=4, bs=16, o
             dt=cs.CS_BF16, ws=A, wsb=1 << 40, stream=None)
 WEIGHTS = dict(q=A, lse=None, kc=A, ks=A, cu=A, pos=A, kv=A, bt=A, mb=4, bs=16, wi=A, wo=A, decay=1.0, n=3, s=1, hq=4, hkv=2, d=64, ss=128, sh=64, scale=0.1,
                dt=cs.CS_BF16, cdt=cs.CS_KV4, ws=A, wsb=1 << 40, stream=None)
-EVICT = dict(w=A, kv=A, bo=A, mbo=8, bn=A, mbn=4, s=2, budget=64, first=1, last=1, ren=1, kept=A, src=A, dst=A, delta=A, kvn=A, wn=None, stream=None)
+EVICT = dict(w=A, kv=A, bo=A, mbo=8, bn=A, mbn=4, s=2, budget=64, first=1, last=1, ren=1, kept=A, src=A, dst=A, delta=A, kvn=A + 4096, wn=None, stream=None)
 I, U, W = cs.CS_EINVAL, cs.CS_EUNSUPPORTED, cs.CS_EWORKSPACE
 NAN, INF = float("nan"), float("inf")
 
@@ -97,3 +97,13 @@ def test_binding_refuses_tensors_that_are_too_short():
         cs.cs_plan_evict(z(64), z(1), z(4), 4, z(4), 4, 1, 8, 0, 0, True, z(7), z(8), z(8), z(8), z(1), None)
     with pytest.raises(ValueError, match="device tensor"):
         cs.cs_plan_evict(z(64), z(1), z(4), 4, z(4), 4, 1, 8, 0, 0, True, z(8), z(8), z(8), z(8), z(1), None)
+
+
+@pytest.mark.parametrize("fn,good,code,change", [
+    ("cs_rope_refresh_scatter", ROPE, U, dict(n=1 << 30)), ("cs_rope_refresh_scatter", ROPE, U, dict(n=1 << 62)),
+    ("cs_kv4_gather", GATHER, U, dict(n=1 << 27)), ("cs_kv4_gather", GATHER, U, dict(n=1 << 62)), ("cs_kv4_gather", GATHER, U, dict(n=1 << 16, layers=1 << 16)),
+    ("cs_kv4_rerotate", MOVE, U, dict(n=1 << 31)), ("cs_kv4_rerotate", MOVE, U, dict(n=1 << 62)),
+    ("cs_attn_weights", WEIGHTS, U, dict(n=1 << 24)), ("cs_attn_weights", WEIGHTS, U, dict(mb=1 << 24, s=32)), ("cs_attn_weights", WEIGHTS, U, dict(mb=(1 << 27) - 1)),
+    ("cs_plan_evict", EVICT, U, dict(s=1 << 22)), ("cs_plan_evict", EVICT, I, dict(kvn=A, kv=A)), ("cs_plan_evict", EVICT, I, dict(w=A, wn=A))])
+def test_more_than_a_launch_holds_and_outputs_over_inputs(fn, good, code, change):
+    assert getattr(cs.lib(), fn)(*dict(good, **change).values()) == code
