@@ -13,8 +13,9 @@
 namespace {
 
 constexpr int kPairs = 8;                // pairs a lane owns
-// Workgroups wanted of the rotary write.  22,804 tokens of 32 + 2 x 8 heads of 128 take 141 us (4.1 TB/s; a large copy reaches 4.1 to 5.0)
-// at 4,096, 155 at 1,024 or 2,048, 153 at 16,384; 5,000 tokens of 28 + 2 x 4 heads 31, 27 and 43; a token alone 13 to 16 at any.
+// Workgroups wanted of the rotary write.  22,804 tokens of 32 + 2 x 8 heads of 128 take 112 us, 4.4 TB/s (a large copy reaches 4.1 to
+// 5.0).  With their rows read back as numbers: 141 us at 4,096, 155 at 1,024 or 2,048, 153 at 16,384; 5,000 tokens of 28 + 2 x 4 heads
+// 31, 27 and 43.  A token alone is 5 us, and 13 to 17 from the host with its row read back, at any.
 constexpr int kRopeGroups = 4096;
 
 template <bool kBf16>
