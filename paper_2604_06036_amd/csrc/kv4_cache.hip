@@ -14,9 +14,11 @@ namespace {
 
 constexpr int kPairs = 8;                // pairs a lane owns
 // Workgroups wanted of the rotary write.  22,804 tokens of 32 + 2 x 8 heads of 128 take 112 us, 4.4 TB/s (a large copy reaches 4.1 to
-// 5.0).  With their rows read back as numbers: 141 us at 4,096, 155 at 1,024 or 2,048, 153 at 16,384; 5,000 tokens of 28 + 2 x 4 heads
-// 31, 27 and 43.  A token alone is 5 us, and 13 to 17 from the host with its row read back, at any.
-constexpr int kRopeGroups = 4096;
+// 5.0).  With their rows read back as numbers: 141 us at 4,096, 155 at 1,024 or 2,048, 153 at 16,384.
+// A thread still takes up to four heads with one evaluation of its angles as long as two workgroups a CU are left: 3,000 tokens
+// of 28 + 2 x 4 heads 27.6 -> 19.2 us with the rows read back, 7,000 39.4 -> 35.8 (six heads: 20.4 and 37.0; four workgroups a CU: 20.9, 35.5).
+// A token alone is 5 us, and 13 to 18 from the host with its row read back.
+constexpr int kRopeGroups = 4096, kRopeHeads = 4, kRopeEnough = 512;
 
 template <bool kBf16>
 struct Eight;
@@ -426,6 +428,7 @@ extern "C" int cs_rope_refresh_scatter(const void* q, void* q_out, const void* k
   const int heads = n_q_heads + 2 * n_kv_heads;
   const int64_t shares = blocks_x >= kRopeGroups ? 1 : (kRopeGroups + blocks_x - 1) / blocks_x;
   p.heads_per_thread = static_cast<int32_t>(shares >= heads ? 1 : (heads + shares - 1) / shares);
+  while (p.heads_per_thread < kRopeHeads && blocks_x * ((heads + p.heads_per_thread) / (p.heads_per_thread + 1)) >= kRopeEnough) ++p.heads_per_thread;
   const dim3 grid(static_cast<unsigned>(blocks_x), static_cast<unsigned>((heads + p.heads_per_thread - 1) / p.heads_per_thread));
   if (grid.y > 65535u) return CS_EUNSUPPORTED;
   hipStream_t st = cs::as_stream(stream);
