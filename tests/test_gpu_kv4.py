@@ -136,6 +136,11 @@ def test_rope_refresh_scatter(cs, n, hq, hkv, d, dtype, cache, axes, style, layo
         assert bool((kc[0][other] == 7).all()) and bool((vc[0][other] == 7).all())
 
 
+@pytest.mark.parametrize("n,hq,hkv,d,cache", [(6000, 7, 2, 128, "kv4"), (9000, 5, 1, 64, "kv4"), (6000, 5, 3, 128, "same")])
+def test_rope_refresh_scatter_several_heads_a_thread(cs, n, hq, hkv, d, cache):
+    test_rope_refresh_scatter(cs, n, hq, hkv, d, "bf16", cache, "sections", 0, "head", True)
+
+
 def test_rope_in_place_and_its_transpose(cs):
     say("rope in place")
     rng = np.random.default_rng(1)
