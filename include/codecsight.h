@@ -627,6 +627,8 @@ int cs_kv4_window_attn(const void* q, const uint8_t* k_codes_layer, const uint8_
  *     weight_out[s][j] = decay * weight_in[s][j] + sum_{t, h} exp(softmax_scale * q[t][h] . K_j - lse[t][h])
  * over the queries t of stream s with j <= q_pos[t] and all query heads h, for the entries j < kv_len[s]; other places of
  * weight_out are left as they were.  Arguments as in the attention calls; any order of q_pos, negative ones see nothing.
+ * A query head whose statistics are no number (its query is none, or a key that it sees, or lse says so: NaN or -inf) makes the
+ * entries that it sees NaN, and no others; a key that is no number is NaN where a query sees it.
  * The sums' order is fixed: the same call gives the same bits.
  *
  *  lse           in   float [n_q][n_q_heads] as cs_kv4_window_attn leaves them, or NULL: computed here (keys are read twice)
