@@ -599,7 +599,8 @@ int cs_kv4_rerotate(uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_codes, uint8
  * As cs_window_prefill_attn, with the same meaning of cu_q, q_pos, kv_len, block_table and of n_q as an upper bound; besides,
  * q_pos needs no order inside a stream, and a negative q_pos is a query that sees nothing (out 0, lse -inf).
  * q and out are CS_BF16 (bf16 operands, fp32 scores, statistics and sums; weights are rounded to bf16) or CS_F32 (fp32
- * accuracy throughout).  Keys and values that are no numbers reach the queries that see them, and no others.
+ * accuracy throughout).  Keys and values that are no numbers, or infinite, reach the queries that see them, and no others; an infinite value only
+ * its own column.
  *
  *  lse          out  float [n_q][n_q_heads] or NULL: log sum_j exp(softmax_scale * q[t][h] . K_j), natural logarithm
  *  workspace         cs_kv4_window_attn_workspace() bytes, 16-byte aligned (may be 0, then NULL is accepted); contents need

@@ -13,6 +13,7 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16v2;
 constexpr int kKv4Block = 32;            // elements that share a scale
 constexpr int64_t kMostThreads = 0xffffffffll;   // of a launch, along one axis of its grid
 constexpr uint32_t kKv4NoNumber = 255;   // scale byte of a block that held a NaN or an infinity
+constexpr uint32_t kKv4Large = 253;      // least scale byte of a block with elements past the largest finite number
 
 // Scale byte of a block whose largest magnitude has the given fp32 bits: the least power of two s with amax <= 7 s.
 // (7 is as far above 6, the largest value, as 5 is above 4, so that saturating it costs no more than the rounding between

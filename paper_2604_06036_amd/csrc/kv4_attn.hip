@@ -319,13 +319,13 @@ struct Sums {
 };
 
 // A block of 32 elements -> bf16 in LDS.  A block without numbers becomes NaN (keys) or zeros (values, which must not meet a weight of
-// 0; it is reported).  KIND 0: keys, rows 16 bytes past a multiple of the banks' width.  Values: 1: rows 64 bytes past one, 2: 32
-// bytes; there blocks of neighbouring rows share banks, and lanes of different rows write a block's four pieces in
-// different orders (by two bits of `row`, or the second one).
+// 0; infinite elements of values become zeros as well, and such blocks are reported).  KIND 0: keys, rows 16 bytes past a multiple of the
+// banks' width.  Values: 1: rows 64 bytes past one, 2: 32 bytes; there blocks of neighbouring rows share banks, and lanes of different
+// rows write a block's four pieces in different orders (by two bits of `row`, or the second one).
 template <int KIND>
 __device__ __forceinline__ bool put_block(uint16_t* dst, const cs::u32x4& code, uint32_t scale, int row) {
-  const bool none = scale == cs::kKv4NoNumber;
-  const float sc = cs::kv4_scale(none ? 1u : scale);
+  const bool odd_one = scale >= (KIND == 0 ? cs::kKv4NoNumber : cs::kKv4Large);
+  const float sc = cs::kv4_scale(odd_one ? 1u : scale);
   cs::u32x4 c = code;
   const int turn = KIND == 1 ? row & 3 : KIND == 2 ? (row >> 1) & 1 : 0;       // c[w] = code[w ^ turn]
   if (KIND != 0) {
@@ -338,12 +338,50 @@ __device__ __forceinline__ bool put_block(uint16_t* dst, const cs::u32x4& code, 
   }
 #pragma unroll
   for (int w = 0; w < 4; ++w) *reinterpret_cast<cs::u32x4*>(dst + 8 * (w ^ turn)) = cs::kv4_unpack8_bf16(c[w], sc);
-  if (__builtin_expect(none, 0)) {
-    const uint32_t x = KIND != 0 ? 0u : 0x7fc07fc0u;
+  if (__builtin_expect(odd_one, 0)) {
 #pragma unroll
-    for (int w = 0; w < 4; ++w) *reinterpret_cast<cs::u32x4*>(dst + 8 * w) = cs::u32x4{x, x, x, x};
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t none = KIND != 0 ? 0u : 0x7fc07fc0u;
+      cs::u32x4 x = {none, none, none, none};
+      if (KIND != 0 && scale != cs::kKv4NoNumber) {
+        x = cs::kv4_unpack8_bf16(code[w], cs::kv4_scale(scale));
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          x[e] = ((x[e] & 0x7fffu) == 0x7f80u ? 0u : x[e] & 0xffffu) | ((x[e] & 0x7fff0000u) == 0x7f800000u ? 0u : x[e] & 0xffff0000u);
+      }
+      *reinterpret_cast<cs::u32x4*>(dst + 8 * w) = x;
+    }
   }
-  return none;
+  return odd_one;
+}
+
+// What element e of a block of values adds to a sum past the products: an infinity, or 0.  (Scale 253: 4 and 6 times 2^126 are past
+// the largest finite number, 254: 2 times 2^127 and more.)
+__device__ __forceinline__ float infinity_of(const cs::u32x4& code, uint32_t scale, int e) {
+  const uint32_t word = e < 16 ? (e < 8 ? code.x : code.y) : (e < 24 ? code.z : code.w), c = word >> (4 * (e & 7)) & 15u;
+  if ((c & 7u) < (scale == cs::kKv4Large ? 6u : 4u)) return 0.0f;
+  return c & 8u ? -INFINITY : INFINITY;
+}
+
+// Where a sweep has met infinite values (rare), it looks them up again: f(entry, block, codes, scale) for every block of the entries begin
+// .. end - 1 that may hold some, the whole wave at once.
+template <int DB, class F>
+__device__ __forceinline__ void each_large_block(const Params& p, const int32_t* ids, int kvh, int begin, int end, F f) {
+  const int mine = static_cast<int>(threadIdx.x & 63) / DB, block = static_cast<int>(threadIdx.x & 63) % DB;
+  for (int key0 = begin; key0 < end; key0 += 64 / DB) {
+    const int key = min(key0 + mine, end - 1);
+    const int64_t at = (static_cast<int64_t>(ids[key / CS_KV_BLOCK]) * CS_KV_BLOCK + key % CS_KV_BLOCK) * p.stride_slot +
+                       static_cast<int64_t>(kvh) * p.stride_head + block * cs::kKv4Block;
+    const uint32_t scale = p.v_scales[at / cs::kKv4Block];
+    const cs::u32x4 code = *reinterpret_cast<const cs::u32x4*>(p.v_codes + at / 2);
+    for (uint64_t left = __ballot(scale >= cs::kKv4Large && scale != cs::kKv4NoNumber && key == key0 + mine); left; left &= left - 1) {
+      const int l = __ffsll(static_cast<unsigned long long>(left)) - 1;
+      cs::u32x4 c;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) c[w] = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(code[w]), l));
+      f(key0 + l / DB, l % DB, c, static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(scale), l)));
+    }
+  }
 }
 
 __device__ __forceinline__ void store4(void* out, int64_t at, const float* x, bool bf16) {
@@ -369,7 +407,7 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 3 : D == 64 ? 2 : 1) void kv4_row
   __shared__ __attribute__((aligned(16))) uint16_t s_v[2][T * VROW];
   __shared__ uint8_t s_vs[2][128];
   __shared__ int s_last[4];
-  __shared__ int s_nan;
+  __shared__ uint32_t s_odd;                               // values met so far: 1: without numbers, 2: infinite
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
   const Job job = job_of(p);
@@ -378,7 +416,7 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 3 : D == 64 ? 2 : 1) void kv4_row
   const int kvh = job.kvh;
   const int entries = min(p.kv_len[t.stream], p.max_blocks * CS_KV_BLOCK);
   if (entries <= 0) return;
-  if (tid == 0) s_nan = 0;
+  if (tid == 0) s_odd = 0;
 
   // ---- this lane's query
   const int row0 = t.row0 + wave * 32;
@@ -443,7 +481,8 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 3 : D == 64 ? 2 : 1) void kv4_row
   };
   auto put = [&](int buf) __attribute__((always_inline)) {       // tile kt0 + k: stage k & 1 of the registers and of LDS
     if (of_v) {
-      if (put_block<1>(&s_v[buf][my_row * VROW + 32 * my_block], code[buf], scale[buf], my_row)) s_nan = 1;
+      if (put_block<1>(&s_v[buf][my_row * VROW + 32 * my_block], code[buf], scale[buf], my_row))
+        atomicOr(&s_odd, scale[buf] == cs::kKv4NoNumber ? 1u : 2u);
       s_vs[buf][tid & 127] = static_cast<uint8_t>(scale[buf]);
     } else {
       put_block<0>(&s_k[buf][my_row * KROW + 32 * my_block], code[buf], scale[buf], my_row);
@@ -454,7 +493,7 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 3 : D == 64 ? 2 : 1) void kv4_row
   sums.clear();
   auto tile = [&](int kt, auto stage) __attribute__((always_inline)) {
     constexpr int buf = decltype(stage)::value;
-    const int nan = s_nan;                                 // (read ahead of the products)
+    const uint32_t odd = s_odd;                            // (read ahead of the products)
 #pragma unroll
     for (int kb = 0; kb < T / 32; ++kb) {
       const int key0 = kt * T + 32 * kb;
@@ -465,7 +504,7 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 3 : D == 64 ? 2 : 1) void kv4_row
       sums.template add<VROW>(&s_v[buf][32 * kb * VROW], pf, lane);
       __builtin_amdgcn_s_setprio(0);
     }
-    if (__builtin_expect(__builtin_amdgcn_readfirstlane(nan), 0)) {      // (a tile so far held a value block without numbers)
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane(odd) & 1u, 0)) {      // (a tile so far held a value block without numbers)
       for (int c = 0; c < 128; ++c)
         if (s_vs[buf][c] == cs::kKv4NoNumber) sums.poison(c % DB, kt * T + c / DB <= pos);
     }
@@ -495,6 +534,16 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 3 : D == 64 ? 2 : 1) void kv4_row
 
   // ---- results
   sums.finish();
+  if (__builtin_expect(__builtin_amdgcn_readfirstlane(s_odd) & 2u, 0))
+    each_large_block<DB>(p, ids, kvh, kt0 * T, min(kt1 * T, last + 1), [&](int key, int block, const cs::u32x4& c, uint32_t sc) __attribute__((always_inline)) {
+      if (key > pos) return;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        if (db == block) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sums.o[db][r] += infinity_of(c, sc, 8 * (r / 4) + 4 * h + r % 4);
+        }
+    });
   if (p.pieces > 1) {                                      // the row tile's other pieces are joined to it by a launch of its own
     const int64_t r = static_cast<int64_t>(job.index) * kRowsMany + wave * 32 + n;
     if (h == 0) *reinterpret_cast<cs::f32v2*>(p.ws_ml + 2 * r) = cs::f32v2{sums.m, sums.l};
@@ -535,6 +584,7 @@ __global__ __launch_bounds__(64 * WAVES, PARTS == 1 ? 3 : 2) void kv4_keys_kerne
   constexpr int BYTES = 32 * VROW * 2 > 16 * OROW * 4 ? 32 * VROW * 2 : 16 * OROW * 4;
   __shared__ __attribute__((aligned(16))) uint8_t s_mem[WAVES][BYTES];
   __shared__ float s_m[WAVES][16], s_l[WAVES][16], s_sum[16];
+  __shared__ int s_pos[16], s_large[WAVES];                // positions of the rows; whether a wave met infinite values
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
   const Job job = job_of(p);
@@ -623,6 +673,7 @@ __global__ __launch_bounds__(64 * WAVES, PARTS == 1 ? 3 : 2) void kv4_keys_kerne
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) o[i] = f32x4{};
   float m = -INFINITY, l = 0.0f;                           // reference maximum (raw score), the lane's share of the sum
+  bool large = false;                                      // infinite values met
   uint32_t bad = 0;                                        // 32-column parts of the sums that a value without numbers has reached
   uint16_t* const v_mine = reinterpret_cast<uint16_t*>(s_mem[wave]);
   if (kt0 + wave < kt1) {
@@ -642,6 +693,11 @@ __global__ __launch_bounds__(64 * WAVES, PARTS == 1 ? 3 : 2) void kv4_keys_kerne
       for (int i = 0; i < VC; ++i) {
         const int r = DB == 4 ? v_row + CS_KV_BLOCK * i : v_row;
         none[i] = __ballot(put_block<2>(v_mine + r * VROW + 32 * v_block, vc[kb][i], vs[kb][i], v_row));
+        if (__builtin_expect(none[i] != 0, 0)) {
+          const uint64_t without = __ballot(vs[kb][i] == cs::kKv4NoNumber);
+          large |= none[i] != without;
+          none[i] = without;
+        }
       }
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       // ---- S^T
@@ -729,6 +785,8 @@ __global__ __launch_bounds__(64 * WAVES, PARTS == 1 ? 3 : 2) void kv4_keys_kerne
     s_m[wave][n] = m;
     s_l[wave][n] = l;
   }
+  if (lane == 0) s_large[wave] = large;
+  if (wave == 0 && g == 0) s_pos[n] = live ? pos : -1;
   __syncthreads();
   float top = s_m[0][n], sum = 0.0f;
 #pragma unroll
@@ -746,12 +804,23 @@ __global__ __launch_bounds__(64 * WAVES, PARTS == 1 ? 3 : 2) void kv4_keys_kerne
     else if (p.lse && live) p.lse[static_cast<int64_t>(tok) * p.n_q_heads + head] = log_sum(top, sum, p.scale_log2e);
   }
   __syncthreads();
+  int any_large = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) any_large |= s_large[w];
   for (int c = tid; c < 16 * D / 4; c += 64 * WAVES) {     // four columns of a row
     const int r = c / (D / 4), d = 4 * (c % (D / 4)), rr = t.row0 + r;
-    if (rr >= t.rows) continue;
     f32x4 y = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(s_mem[0]) + r * OROW + d);
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) y += *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(s_mem[w]) + r * OROW + d);
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane(any_large), 0)) {
+      const int sees = s_pos[r];
+      each_large_block<DB>(p, ids, kvh, kt0 * kKeys, min(kt1 * kKeys, last + 1), [&](int key, int block, const cs::u32x4& codes, uint32_t sc) __attribute__((always_inline)) {
+        if (key > sees || d / 32 != block) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] += infinity_of(codes, sc, d % 32 + i);
+      });
+    }
+    if (rr >= t.rows) continue;
     if (p.pieces > 1) {
       *reinterpret_cast<f32x4*>(p.ws_o + (job_row + r) * D + d) = y;
     } else {

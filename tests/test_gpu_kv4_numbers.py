@@ -6,7 +6,8 @@ import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_kv4 import CACHES, DEV, U, Batch, cs, dev, say  # noqa: F401 (cs: fixture)
+from oracle import kv4_oracle as ko
+from tests.test_gpu_kv4 import B, CACHES, DEV, U, Batch, cs, dev, say  # noqa: F401 (cs: fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +56,74 @@ def test_attn_weights_take_statistics_without_numbers_from_the_attention_call(cs
     assert np.argwhere(np.isnan(lse.cpu().numpy())).tolist() == [[20, 9]]
     got = b.weights(None, 1.0, lse=lse)[0].cpu().numpy()
     assert np.isnan(got[:121]).all() and np.isfinite(got[121:400]).all()
+
+# ------------------------------------------------------------------------------------------ attention over infinite values
+
+def put_value(b, s, j, x):
+    """Entry j of stream s gets the value row x [n_kv_heads][head_dim]."""
+    c, e = ko.quantise(x)
+    slot = int(b.table[s, j // 16]) * 16 + j % 16
+    b.pool[1][slot], b.scales[1][slot] = dev(c), dev(e)
+    with np.errstate(over="ignore"):
+        b.v[s][j] = ko.values(c, e).astype(np.float32)     # (2^128 reads as infinity)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,d,kv,nq", [
+    (8, 2, 128, [200, 40], [60, 20]), (8, 2, 64, [200, 40], [60, 20]),                  # many rows
+    (8, 2, 128, [200, 40], [3, 1]), (8, 2, 64, [200, 40], [3, 1]),                      # few rows
+    (16, 1, 64, [4700, 30], [30, 17]), (7, 1, 128, [9000, 30], [2, 1]),                 # sweeps in pieces
+])
+def test_kv4_attention_over_infinite_values(cs, hq, hkv, d, kv, nq, dtype):
+    """Values past the largest finite number, the last one that a query sees among them: infinite in the columns that hold them, for the queries
+    that see them, NaN where infinities of both signs meet, and nothing of it in other columns or queries."""
+    say("kv4 attention, infinite values", hq, hkv, d, kv, nq, dtype)
+    b = Batch(cs, 173, hq, hkv, d, kv, nq, dtype, where="sorted", layout="slot")
+    last = [n - 1 for n in kv]
+    b.pos[0][-1], b.pos[1][-1] = last
+    b.pos[0][0] = kv[0] // 4
+    b.q_pos = dev(np.concatenate(b.pos).astype(np.int32))
+    rng = np.random.default_rng(174)
+    for s, j, cols in ((0, kv[0] // 2, {3: 1, 40: -1}), (0, kv[0] // 2 + 5, {40: 1, d - 1: -1}), (0, last[0], {17: 1}), (1, last[1], {0: -1, 33: 1})):
+        x = rng.normal(size=(hkv, d))
+        for c, sign in cols.items():
+            x[-1, c] = sign * 3.2e38
+        put_value(b, s, j, x)
+    out, lse = b.attend()
+    seen = 0
+    for s in range(2):
+        rows, want, stat, p, e = b.oracle(s)
+        got = out[rows].double().cpu().numpy()
+        for kind in (np.isnan, np.isposinf, np.isneginf):
+            assert np.array_equal(kind(got), kind(want)), (s, kind)
+        seen += int(np.isinf(want).sum())
+        ok = np.isfinite(want)
+        v = np.abs(np.repeat(b.v[s], hq // hkv, 1))
+        mass = np.einsum("thj,jhc->thc", p, np.where(np.isfinite(v), v, 0.0))
+        rel = 2 * e + (8 + 2 * (kv[s] / 16 + 64)) * U + (2 * B if dtype == "bf16" else 0.0)
+        tol = rel[..., None] * mass + (B if dtype == "bf16" else 2 * U) * np.abs(np.where(ok, want, 0.0))
+        assert np.all(np.abs(np.where(ok, got, 0.0) - np.where(ok, want, 0.0)) <= tol + 1e-30)
+        assert np.all(np.isfinite(lse[rows].cpu().numpy()))
+    assert seen > 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq", [60, 3])
+def test_kv4_infinite_keys_reach_only_the_queries_that_see_them(cs, nq, dtype):
+    say("kv4 attention and weights, an infinite key", nq, dtype)
+    b = Batch(cs, 176, 4, 1, 128, [200], [nq], dtype, where="tail")
+    b.pos[0][:] = np.linspace(0, 199, nq).astype(int)
+    b.q_pos = dev(b.pos[0].astype(np.int32))
+    x = b.k[0][150].copy()
+    x[0, 7], x[0, 90] = 3.2e38, -3.2e38
+    c, e = ko.quantise(x)
+    slot = int(b.table[0, 150 // 16]) * 16 + 150 % 16
+    b.pool[0][slot], b.scales[0][slot] = dev(c), dev(e)
+    out, lse = b.attend()
+    n = int((b.pos[0] < 150).sum())                        # (in order: the queries that do not see the entry)
+    want, stat, p = ko.attention(b.q64[:n], b.k[0], b.v[0], b.pos[0][:n], b.scale)
+    mass = np.einsum("thj,jhc->thc", p, np.abs(np.repeat(b.v[0], 4, 1)))
+    size = b.scale * max(float((np.abs(b.q64[:n, h]) @ np.abs(b.k[0][:150, 0]).T).max()) for h in range(4))
+    err = 2 * ((128 / 8 + 8) * U * size + 8 * U * size) + (8 + 2 * (200 / 16 + 64)) * U
+    assert np.all(np.abs(out[:n].double().cpu().numpy() - want) <= (err + (2 * B if dtype == "bf16" else 0.0)) * mass + (B if dtype == "bf16" else 2 * U) * np.abs(want))
+    assert np.all(np.abs(lse[:n].double().cpu().numpy() - stat) <= err + 8 * U * np.abs(stat))
