@@ -583,7 +583,8 @@ int cs_kv4_gather(const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t
  *     int32 [n_rows]) and cs_kv_rerotate_axes (delta int32 [n_rows][3]) on a 4-bit cache of all layers.
  *
  * A key's numbers are turned in single precision and written as 4-bit rows again, so a key that stays in a window for
- * several slides is rounded once a slide (a shift of 0 keeps its numbers).  Values are copied code for code.
+ * several slides is rounded once a slide.  A shift of 0 keeps a key's codes and scales (of three shifts: 0 for all of 32 neighbouring pairs
+ * from a multiple of 32 on keeps their two blocks).  Values are copied code for code.
  * dst_slot == NULL: keys in place, the v pools are not touched (may be NULL).  Rows with a negative src_slot or dst_slot
  * are skipped; source and destination slot sets are disjoint, destination slots unique.
  * Errors: as cs_kv_rerotate; CS_EUNSUPPORTED also for head_dim not a multiple of 64, strides not multiples of 32.

@@ -274,6 +274,12 @@ __global__ __launch_bounds__(256) void kv4_rerotate_kernel(Kv4RerotateParams p) 
       cn[2 * i + 1] = __uint_as_float(v.z);
       sn[2 * i + 1] = __uint_as_float(v.w);
     }
+    // Blocks that nothing turns keep their codes: a sine of 0 would carry what is no number into the partner block.  (A sine of
+    // 0 means a cosine of 1: no multiple of pi but 0 is a number of 64 bits.)
+    uint32_t sines = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) sines |= cs::abs_bits(sn[i]);
+    const bool still = sines == 0;
 
     const int off_a = kStyle == CS_ROPE_HALF_SPLIT ? j * N : 2 * j * N;
     const int off_b = kStyle == CS_ROPE_HALF_SPLIT ? p.head_dim / 2 + j * N : 2 * j * N + N;
@@ -298,41 +304,45 @@ __global__ __launch_bounds__(256) void kv4_rerotate_kernel(Kv4RerotateParams p) 
         vb = *reinterpret_cast<const cs::u32x4*>(p.v_codes + (s + off_b) / 2);
         vs = scales(p.v_scales);
       }
-      float a[N], b[N];
+      uint32_t na = ea, nb = eb;
+      cs::u32x4 oa = wa, ob = wb;
+      if (!still) {
+        float a[N], b[N];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        cs::kv4_unpack8(wa[i], cs::kv4_scale(ea), a + 8 * i);
-        cs::kv4_unpack8(wb[i], cs::kv4_scale(eb), b + 8 * i);
-      }
-      if (ea == cs::kKv4NoNumber || eb == cs::kKv4NoNumber) {
+        for (int i = 0; i < 4; ++i) {
+          cs::kv4_unpack8(wa[i], cs::kv4_scale(ea), a + 8 * i);
+          cs::kv4_unpack8(wb[i], cs::kv4_scale(eb), b + 8 * i);
+        }
+        if (ea == cs::kKv4NoNumber || eb == cs::kKv4NoNumber) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            if (ea == cs::kKv4NoNumber) a[i] = NAN;
+            if (eb == cs::kKv4NoNumber) b[i] = NAN;
+          }
+        }
+        uint32_t ma = 0, mb = 0;
+        if (kStyle == CS_ROPE_HALF_SPLIT) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) cs::rope_turn(a[i], b[i], cn[i], sn[i], &a[i], &b[i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < N / 2; ++i) {
+            cs::rope_turn(a[2 * i], a[2 * i + 1], cn[i], sn[i], &a[2 * i], &a[2 * i + 1]);
+            cs::rope_turn(b[2 * i], b[2 * i + 1], cn[N / 2 + i], sn[N / 2 + i], &b[2 * i], &b[2 * i + 1]);
+          }
+        }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          if (ea == cs::kKv4NoNumber) a[i] = NAN;
-          if (eb == cs::kKv4NoNumber) b[i] = NAN;
+          ma = max(ma, cs::abs_bits(a[i]));
+          mb = max(mb, cs::abs_bits(b[i]));
         }
-      }
-      uint32_t ma = 0, mb = 0;
-      if (kStyle == CS_ROPE_HALF_SPLIT) {
+        na = cs::kv4_scale_byte(ma);
+        nb = cs::kv4_scale_byte(mb);
 #pragma unroll
-        for (int i = 0; i < N; ++i) cs::rope_turn(a[i], b[i], cn[i], sn[i], &a[i], &b[i]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-          cs::rope_turn(a[2 * i], a[2 * i + 1], cn[i], sn[i], &a[2 * i], &a[2 * i + 1]);
-          cs::rope_turn(b[2 * i], b[2 * i + 1], cn[N / 2 + i], sn[N / 2 + i], &b[2 * i], &b[2 * i + 1]);
+        for (int i = 0; i < 4; ++i) {
+          oa[i] = cs::kv4_pack8(a + 8 * i, cs::kv4_scale(na));
+          ob[i] = cs::kv4_pack8(b + 8 * i, cs::kv4_scale(nb));
         }
-      }
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        ma = max(ma, cs::abs_bits(a[i]));
-        mb = max(mb, cs::abs_bits(b[i]));
-      }
-      const uint32_t na = cs::kv4_scale_byte(ma), nb = cs::kv4_scale_byte(mb);
-      cs::u32x4 oa, ob;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        oa[i] = cs::kv4_pack8(a + 8 * i, cs::kv4_scale(na));
-        ob[i] = cs::kv4_pack8(b + 8 * i, cs::kv4_scale(nb));
       }
       *reinterpret_cast<cs::u32x4*>(p.k_codes + (d + off_a) / 2) = oa;
       *reinterpret_cast<cs::u32x4*>(p.k_codes + (d + off_b) / 2) = ob;

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from oracle import kv4_oracle as ko
-from tests.test_gpu_kv4 import B, CACHES, DEV, U, Batch, cs, dev, say  # noqa: F401 (cs: fixture)
+from tests.test_gpu_kv4 import AXES, B, CACHES, DEV, U, Batch, cs, dev, say  # noqa: F401 (cs: fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -110,7 +110,7 @@ def test_kv4_attention_over_infinite_values(cs, hq, hkv, d, kv, nq, dtype):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("nq", [60, 3])
 def test_kv4_infinite_keys_reach_only_the_queries_that_see_them(cs, nq, dtype):
-    say("kv4 attention and weights, an infinite key", nq, dtype)
+    say("kv4 attention, an infinite key", nq, dtype)
     b = Batch(cs, 176, 4, 1, 128, [200], [nq], dtype, where="tail")
     b.pos[0][:] = np.linspace(0, 199, nq).astype(int)
     b.q_pos = dev(b.pos[0].astype(np.int32))
@@ -127,3 +127,51 @@ def test_kv4_infinite_keys_reach_only_the_queries_that_see_them(cs, nq, dtype):
     err = 2 * ((128 / 8 + 8) * U * size + 8 * U * size) + (8 + 2 * (200 / 16 + 64)) * U
     assert np.all(np.abs(out[:n].double().cpu().numpy() - want) <= (err + (2 * B if dtype == "bf16" else 0.0)) * mass + (B if dtype == "bf16" else 2 * U) * np.abs(want))
     assert np.all(np.abs(lse[:n].double().cpu().numpy() - stat) <= err + 8 * U * np.abs(stat))
+
+# ------------------------------------------------------------------------------------------ a shift of 0
+
+@pytest.mark.parametrize("style", [0, 1])
+@pytest.mark.parametrize("d,axes,in_place", [(64, "one", False), (128, "one", True), (128, "sections", False), (192, "one", False), (256, "interleaved", True)])
+def test_kv4_rerotate_by_nothing_keeps_every_row(cs, d, axes, in_place, style):
+    """Codes and scales of any kind, blocks without numbers and infinite elements among them, behind a shift of 0."""
+    say("kv4 rerotate by 0", d, axes, in_place, style)
+    n, layers, hkv = 128, 2, 2
+    rng = np.random.default_rng(d)
+    axis = AXES[axes](d // 2)
+    codes = rng.integers(0, 256, (2, layers, 2 * n, hkv, d // 2)).astype(np.uint8)
+    scales = rng.integers(0, 256, (2, layers, 2 * n, hkv, d // 32)).astype(np.uint8)
+    scales[:, :, ::3] = rng.choice([0, 1, 252, 253, 254, 255], scales[:, :, ::3].shape)
+    kc, vc, ks, vs = (dev(t) for t in (*codes, *scales))
+    perm = rng.permutation(2 * n).astype(np.int32)
+    src, dst = perm[:n], perm[n:]
+    cs.cs_kv4_rerotate(kc, ks, None if in_place else vc, None if in_place else vs, dev(src), None if in_place else dev(dst),
+                       dev(np.zeros((n, 3) if axis is not None else (n,), np.int32)), None if axis is None else dev(axis), n, layers, hkv, d, 2 * n * hkv * d, hkv * d, d,
+                       1e6, style)
+    to = src if in_place else dst
+    with np.errstate(over="ignore"):
+        want = ko.values(codes[0], scales[0]).astype(np.float32)
+        got = ko.values(kc.cpu().numpy(), ks.cpu().numpy()).astype(np.float32)
+    want[:, to] = want[:, src]
+    assert np.isinf(want).any() and np.isnan(want).any()
+    assert np.array_equal(got, want, equal_nan=True)
+
+
+def test_kv4_rerotate_turns_only_the_pairs_of_an_axis_that_moved(cs):
+    say("kv4 rerotate, one axis of two moved")
+    d, n = 128, 40
+    rng = np.random.default_rng(175)
+    axis = np.repeat([0, 1], 32).astype(np.uint8)          # pairs 32..63: elements 32..63 and 96..127
+    codes = rng.integers(0, 256, (1, 2 * n, 1, d // 2)).astype(np.uint8)
+    scales = rng.integers(100, 140, (1, 2 * n, 1, d // 32)).astype(np.uint8)
+    scales[:, ::2, :, 1] = 255
+    delta = np.zeros((n, 3), np.int32)
+    delta[:, 0] = -5
+    kc, ks = dev(codes), dev(scales)
+    at = np.arange(n, dtype=np.int32)
+    cs.cs_kv4_rerotate(kc, ks, None, None, dev(at), None, dev(delta), dev(axis), n, 1, 1, d, 2 * n * d, d, d, 1e6, 0)
+    before, after = (ko.values(c, s)[0, :n, 0] for c, s in ((codes, scales), (kc.cpu().numpy(), ks.cpu().numpy())))
+    still = np.r_[32:64, 96:128]
+    assert np.array_equal(after[:, still], before[:, still], equal_nan=True) and np.isnan(before[0, 32:64]).all()
+    turned = ko.values(*ko.quantise(ko.rope_single(ko.values(codes, scales)[0, :n].astype(np.float32), delta, axis, 1e6, 0)))[:, 0]
+    moved = np.r_[0:32, 64:96]
+    assert np.array_equal(after[:, moved], turned[:, moved])
