@@ -366,6 +366,13 @@ def _here(fn: str, t: Optional[torch.Tensor]):
         raise ValueError(f"{fn}: tensors on device {t.get_device()}, the current device is {torch.cuda.current_device()}")
 
 
+def _axes(fn: str, t: Optional[torch.Tensor], head_dim: int):
+    """axis_of_pair holds a byte a pair: wider integers would be read as the axes of other pairs."""
+    _need(fn, t, head_dim // 2, "axis_of_pair")
+    if t is not None and (t.element_size() != 1 or not t.is_contiguous()):
+        raise ValueError(f"{fn}: axis_of_pair is not a contiguous tensor of bytes")
+
+
 def _span(t: Optional[torch.Tensor], rows: int, stride: int, row: int) -> bool:
     """Whether the memory from t's first element on holds `rows` rows of `row` elements, `stride` apart."""
     if t is None or rows < 1:
@@ -379,7 +386,7 @@ def cs_rope_refresh_scatter(q, q_out, k_new, v_new, slot, pos, axis_of_pair, k_c
     fn = "cs_rope_refresh_scatter"
     _here(fn, pos if k_cache_layer is None else k_cache_layer)
     _need(fn, slot, n_tok, "slot")
-    _need(fn, pos, n_tok if axis_of_pair is None else 3 * n_tok, "pos"); _need(fn, axis_of_pair, head_dim // 2, "axis_of_pair")
+    _need(fn, pos, n_tok if axis_of_pair is None else 3 * n_tok, "pos"); _axes(fn, axis_of_pair, head_dim)
     for t, stride, heads, what in ((q, stride_q, n_q_heads, "q"), (k_new, stride_k, n_kv_heads, "k_new"), (v_new, stride_v, n_kv_heads, "v_new")):
         if not _span(t, n_tok, stride, heads * head_dim):
             raise ValueError(f"{fn}: {what} holds fewer than {n_tok} tokens")
@@ -407,7 +414,7 @@ def cs_kv4_rerotate(k_codes, k_scales, v_codes, v_scales, src_slot, dst_slot, de
     fn = "cs_kv4_rerotate"
     _here(fn, k_codes)
     _need(fn, src_slot, n_rows, "src_slot"); _need(fn, dst_slot, n_rows, "dst_slot")
-    _need(fn, delta, n_rows if axis_of_pair is None else 3 * n_rows, "delta"); _need(fn, axis_of_pair, head_dim // 2, "axis_of_pair")
+    _need(fn, delta, n_rows if axis_of_pair is None else 3 * n_rows, "delta"); _axes(fn, axis_of_pair, head_dim)
     _check(fn, lib().cs_kv4_rerotate(_ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales), _ptr(src_slot), _ptr(dst_slot), _ptr(delta),
                                      _ptr(axis_of_pair), n_rows, n_layers, n_kv_heads, head_dim, stride_layer, stride_slot, stride_head,
                                      rope_base, rope_style, _stream()))

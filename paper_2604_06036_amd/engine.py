@@ -437,9 +437,14 @@ class Kv4Step(DeviceStep):
     def __init__(self, data: StepData, positions, axis_of_pair=None, reuse_cap: Optional[int] = None, q_cap: Optional[int] = None,
                  weigh: bool = False):
         import torch
+        as_tensor = lambda a: a if isinstance(a, torch.Tensor) else torch.from_numpy(np.ascontiguousarray(a))
+        if axis_of_pair is not None:
+            axis_of_pair, pairs = as_tensor(axis_of_pair), data.workload.head_dim // 2
+            if axis_of_pair.dtype != torch.uint8 or axis_of_pair.numel() != pairs or not axis_of_pair.is_contiguous():
+                raise ValueError(f"axis_of_pair: uint8 of {pairs} pairs expected")
         super().__init__(data, reuse_cap=reuse_cap, q_cap=q_cap, overlap=False, own_rows=False)
         cs, w, dev = self.cs, data.workload, self.dev
-        to = lambda a: (a if isinstance(a, torch.Tensor) else torch.from_numpy(np.ascontiguousarray(a))).to(dev)
+        to = lambda a: as_tensor(a).to(dev)
         self.positions = to(positions)
         self.axis_of_pair = None if axis_of_pair is None else to(axis_of_pair)
         width = 1 if axis_of_pair is None else 3

@@ -1,0 +1,32 @@
+"""Arguments that engine.Kv4Step and the 4-bit calls refuse before they touch a device."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_06036_amd import binding as cs
+from paper_2604_06036_amd import engine, synth
+from tests import helpers as hp
+
+
+@pytest.fixture(scope="module")
+def data():
+    return engine.assemble_step(synth.small_variant(synth.CFG1, n_layers=1), hp.oracle_scorer, device="cpu")
+
+
+@pytest.mark.parametrize("axis", [np.zeros(64, np.int64), [0] * 64, np.zeros(64, np.int32), torch.zeros((64,), dtype=torch.int64), torch.zeros((64,)), np.zeros(63, np.uint8),
+                                  np.zeros(128, np.uint8), torch.zeros((128,), dtype=torch.uint8)[::2]])
+def test_axes_of_another_type_or_number_are_refused(data, axis):
+    """(wider integers would be read byte by byte, and turn the wrong pairs)"""
+    with pytest.raises(ValueError, match="axis_of_pair"):
+        engine.Kv4Step(data, np.zeros((data.info["n_q"], 3), np.int32), axis)
+
+
+@pytest.mark.parametrize("axis", [torch.zeros((32,), dtype=torch.int64), torch.zeros((32,), dtype=torch.int32), torch.zeros((64,), dtype=torch.uint8)[::2],
+                                  torch.zeros((31,), dtype=torch.uint8)])
+def test_calls_refuse_axes_of_another_type(axis):
+    z = lambda n, dt=torch.int32: torch.zeros((n,), dtype=dt)
+    with pytest.raises(ValueError, match="axis_of_pair"):
+        cs.cs_kv4_rerotate(None, None, None, None, z(3), z(3), z(9), axis, 3, 1, 1, 64, 0, 64, 64, 1e6, 0)
+    with pytest.raises(ValueError, match="axis_of_pair"):
+        cs.cs_rope_refresh_scatter(z(192, torch.bfloat16), z(192, torch.bfloat16), None, None, None, z(9), axis, None, None, None, None, 3, 1, 0, 64, 64, 0, 0, 0, 0, 1e6, 0,
+                                   cs.CS_BF16, cs.CS_KV4)
