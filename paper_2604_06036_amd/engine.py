@@ -442,14 +442,16 @@ class Kv4Step(DeviceStep):
             axis_of_pair, pairs = as_tensor(axis_of_pair), data.workload.head_dim // 2
             if axis_of_pair.dtype != torch.uint8 or axis_of_pair.numel() != pairs or not axis_of_pair.is_contiguous():
                 raise ValueError(f"axis_of_pair: uint8 of {pairs} pairs expected")
+        # (rows behind one another: a [3][q_cap] tensor, or its transposed view, would be read as other rows' positions)
+        positions, rows, width = as_tensor(positions), int(data.info["n_q"]) if q_cap is None else int(q_cap), 1 if axis_of_pair is None else 3
+        if (positions.dtype != torch.int32 or positions.numel() < width * rows or not positions.is_contiguous()
+                or positions.dim() > 1 and int(positions.shape[-1]) != width):
+            raise ValueError(f"positions: contiguous int32 of {rows} executed rows of {width} expected")
         super().__init__(data, reuse_cap=reuse_cap, q_cap=q_cap, overlap=False, own_rows=False)
         cs, w, dev = self.cs, data.workload, self.dev
         to = lambda a: as_tensor(a).to(dev)
         self.positions = to(positions)
         self.axis_of_pair = None if axis_of_pair is None else to(axis_of_pair)
-        width = 1 if axis_of_pair is None else 3
-        if self.positions.dtype != torch.int32 or self.positions.numel() < width * self.q_cap:
-            raise ValueError(f"positions: int32 of {width} x {self.q_cap} executed rows expected")
         if self.axis_of_pair is not None:
             # one shift for all reused rows: whole frames along time
             self.delta3 = torch.zeros((max(1, self.reuse_cap), 3), dtype=torch.int32, device=dev)

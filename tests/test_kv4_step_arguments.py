@@ -30,3 +30,16 @@ def test_calls_refuse_axes_of_another_type(axis):
     with pytest.raises(ValueError, match="axis_of_pair"):
         cs.cs_rope_refresh_scatter(z(192, torch.bfloat16), z(192, torch.bfloat16), None, None, None, z(9), axis, None, None, None, None, 3, 1, 0, 64, 64, 0, 0, 0, 0, 1e6, 0,
                                    cs.CS_BF16, cs.CS_KV4)
+
+
+def test_positions_in_another_order_are_refused(data):
+    """(time, height, width) lie behind one another, a row at a time."""
+    n = data.info["n_q"]
+    axis = np.zeros(64, np.uint8)
+    for positions in (torch.zeros((3, n), dtype=torch.int32), torch.zeros((3, n), dtype=torch.int32).T, np.zeros((3, n), np.int32), torch.zeros((n, 4), dtype=torch.int32)[:, :3],
+                      torch.zeros((n, 3), dtype=torch.int64), np.zeros((n - 1, 3), np.int32)):
+        with pytest.raises(ValueError, match="positions"):
+            engine.Kv4Step(data, positions, axis)
+    for positions in (torch.zeros((2 * n,), dtype=torch.int32)[::2], np.zeros((n, 3), np.int32), np.zeros((n,), np.int64)):
+        with pytest.raises(ValueError, match="positions"):
+            engine.Kv4Step(data, positions)
