@@ -544,6 +544,9 @@ class Kv4Step(DeviceStep):
         if self.weight is None:
             raise ValueError("evict: the step was built without weigh=True")
         w, cs, dev = self.data.workload, self.cs, self.dev
+        # (read as rows of int32: wider ids, or a slice of a wider table, would name other blocks, of live windows among them)
+        if block_table.dtype != torch.int32 or block_table.dim() != 2 or int(block_table.shape[0]) != w.n_streams or not block_table.is_contiguous():
+            raise ValueError(f"evict: block_table: contiguous int32 [{w.n_streams}][..] expected")
         i32 = lambda *shape: torch.empty(shape, dtype=torch.int32, device=dev)
         n, columns = w.n_streams, int(block_table.shape[1])
         kept, src, dst, delta, kv_len = i32(n, budget), i32(n, budget), i32(n, budget), i32(n, budget), i32(n)

@@ -43,3 +43,15 @@ def test_positions_in_another_order_are_refused(data):
     for positions in (torch.zeros((2 * n,), dtype=torch.int32)[::2], np.zeros((n, 3), np.int32), np.zeros((n,), np.int64)):
         with pytest.raises(ValueError, match="positions"):
             engine.Kv4Step(data, positions)
+
+
+def test_eviction_refuses_tables_that_would_name_other_blocks(data):
+    step = engine.Kv4Step.__new__(engine.Kv4Step)          # (a step lives on a device; this check comes before that)
+    step.data, step.cs, step.dev, step.weight = data, cs, torch.device("cpu"), torch.zeros((1, 32))
+    good = torch.arange(40, dtype=torch.int32).view(1, 40)
+    for table in (good.long(), good[:, ::2], good.view(2, 20), good[0], torch.zeros((1, 40))):
+        with pytest.raises(ValueError, match="block_table"):
+            step.evict(100, table)
+    with pytest.raises(ValueError, match="device tensor"):
+        step.weight, step.kv_len, step.block_table, step.max_blocks = torch.zeros((1, 32)), torch.zeros((1,), dtype=torch.int32), torch.zeros((1, 2), dtype=torch.int32), 2
+        step.evict(100, good)
