@@ -524,7 +524,10 @@ int cs_refresh_prefill_attn(const void* k_new, const void* v_new, const int32_t*
  * in byte i/2 of the codes, its scale in byte i/32 of the scales.  Codes are 16-byte aligned.  Head-major pools
  * (stride_slot = head_dim) are read in whole lines by attention, which takes one kv head at a time.
  * CS_EUNSUPPORTED also answers calls past what a launch holds, 2^32 threads along an axis of its grid: (q1) a thread per 16
- * elements of a head of all tokens, (q2) per 8 elements of an output, (w) 64 per token and query head where lse is NULL.
+ * elements of a head of all tokens, (q2) per 8 elements of an output, (q3) up to 256 per row, (q4) 512 per
+ * kv head and row tile (128 rows, or 16 where a stream has at most 64 on average; a row is a token and a query head of the kv
+ * group, and every stream may leave one tile unfilled), (w) 256 per stream, kv head and tile of 256 entries (fp32 cache: 128) of
+ * max_blocks * 16, one per place of weight_out, and 64 per token and query head where lse is NULL.
  * ------------------------------------------------------------------------------------------ */
 
 /* ------------------------------------------------------------------------------------------
@@ -554,7 +557,7 @@ int cs_refresh_prefill_attn(const void* k_new, const void* v_new, const int32_t*
  * Errors: CS_EINVAL (null pointer, negative size, no heads at all, tokens that overlap, queries without positions, rope_base not
  *         a positive finite number), CS_EUNSUPPORTED (head_dim not a multiple of 16 (4-bit cache: 64) or > 256, unknown
  *         dtype / rope_style, a cache_dtype that is neither dtype nor CS_KV4, strides or pointers that are not aligned, more than
- *         65,535 heads), CS_EHIP.  n_tok == 0 returns CS_OK.
+ *         65,535 query heads or 32,767 key heads), CS_EHIP.  n_tok == 0 returns CS_OK.
  * ------------------------------------------------------------------------------------------ */
 int cs_rope_refresh_scatter(const void* q, void* q_out, const void* k_new, const void* v_new, const int32_t* slot,
                             const int32_t* pos, const uint8_t* axis_of_pair, void* k_cache_layer, void* v_cache_layer,
@@ -641,9 +644,11 @@ int cs_kv4_window_attn(const void* q, const uint8_t* k_codes_layer, const uint8_
  *  workspace          cs_attn_weights_workspace() bytes, 16-byte aligned, contents need not be initialised (8 bytes a query row
  *                     and 128 entries of max_blocks * 16 for calls without lse, and the partial sums).  Two calls that overlap in
  *                     time must not share a workspace.
- * Errors: as cs_kv4_window_attn (strides: multiples of 16 bytes, of 32 elements for a 4-bit cache); CS_EINVAL also for a decay
- *         outside 0 .. 1, CS_EUNSUPPORTED for a cache_dtype that is neither dtype nor CS_KV4, and for 2^28 rows of a kv head
- *         (n_q * n_q_heads / n_kv_heads).  n_streams == 0 returns CS_OK; n_q == 0 only lets weights fade.
+ * Errors: CS_EINVAL (null pointer, negative size, n_q_heads not a multiple of n_kv_heads, softmax_scale not a positive finite
+ *         number, decay outside 0 .. 1), CS_EUNSUPPORTED (head_dim not in {64,128}, block_size != 16, n_q_heads/n_kv_heads > 16,
+ *         unknown dtype, a cache_dtype that is neither dtype nor CS_KV4, strides not multiples of 16 bytes (4-bit cache: of 32
+ *         elements), alignment, n_q * n_q_heads >= 2^31, 2^28 rows of a kv head (n_q * n_q_heads / n_kv_heads), max_blocks >
+ *         2^27 - 257), CS_EWORKSPACE, CS_EHIP.  n_streams == 0 returns CS_OK; n_q == 0 only lets weights fade.
  * ------------------------------------------------------------------------------------------ */
 size_t cs_attn_weights_workspace(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                                  int32_t max_blocks);

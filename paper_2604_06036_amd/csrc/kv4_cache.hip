@@ -434,13 +434,13 @@ extern "C" int cs_rope_refresh_scatter(const void* q, void* q_out, const void* k
   p.lanes_per_tok = head_dim / 2 / kPairs;
   if (n_tok > (cs::kMostThreads - 255) / p.lanes_per_tok) return CS_EUNSUPPORTED;
   const int64_t blocks_x = (n_tok * p.lanes_per_tok + 255) / 256;
-  // Heads a thread turns with one evaluation of its angles: all of them where the tokens alone fill the card, fewer below.
+  // Heads a thread turns with one evaluation of its angles: all of them where the tokens alone fill the card, fewer below (shares: at
+  // most kRopeGroups, along the grid's second axis).
   const int heads = n_q_heads + 2 * n_kv_heads;
   const int64_t shares = blocks_x >= kRopeGroups ? 1 : (kRopeGroups + blocks_x - 1) / blocks_x;
   p.heads_per_thread = static_cast<int32_t>(shares >= heads ? 1 : (heads + shares - 1) / shares);
   while (p.heads_per_thread < kRopeHeads && blocks_x * ((heads + p.heads_per_thread) / (p.heads_per_thread + 1)) >= kRopeEnough) ++p.heads_per_thread;
   const dim3 grid(static_cast<unsigned>(blocks_x), static_cast<unsigned>((heads + p.heads_per_thread - 1) / p.heads_per_thread));
-  if (grid.y > 65535u) return CS_EUNSUPPORTED;
   hipStream_t st = cs::as_stream(stream);
   const bool half_split = rope_style == CS_ROPE_HALF_SPLIT, bf16 = dtype == CS_BF16;
 #define CS_LAUNCH_ROPE(BF16, STYLE)                                                                          \

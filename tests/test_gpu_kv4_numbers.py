@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from oracle import kv4_oracle as ko
-from tests.test_gpu_kv4 import AXES, B, CACHES, DEV, U, Batch, cs, dev, say  # noqa: F401 (cs: fixture)
+from tests.test_gpu_kv4 import AXES, B, CACHES, DEV, U, Batch, cs, dev, pool, say, single, strides  # noqa: F401 (cs: fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -175,3 +175,31 @@ def test_kv4_rerotate_turns_only_the_pairs_of_an_axis_that_moved(cs):
     turned = ko.values(*ko.quantise(ko.rope_single(ko.values(codes, scales)[0, :n].astype(np.float32), delta, axis, 1e6, 0)))[:, 0]
     moved = np.r_[0:32, 64:96]
     assert np.array_equal(after[:, moved], turned[:, moved])
+
+# ------------------------------------------------------------------------------------------ many heads
+
+@pytest.mark.parametrize("n", [1, 3])
+def test_rope_refresh_scatter_of_the_most_heads(cs, n):
+    """65,535 query heads beside key and value heads, the same for few and for many tokens."""
+    say("rope, 65,535 query heads, tokens:", n)
+    hq, hkv, d = 65535, 3, 64
+    rng = np.random.default_rng(n)
+    x64, x = single(rng.normal(size=(n, (hq + 2 * hkv) * d)), torch.bfloat16)
+    pos = rng.integers(0, 50000, n).astype(np.int32)
+    out = torch.full((n, hq, d), 5.0, dtype=torch.bfloat16, device=DEV)
+    kc, vc = (pool("slot", 1, n, hkv, d // 2) for _ in range(2))
+    ks, vs = (pool("slot", 1, n, hkv, d // 32) for _ in range(2))
+    _, sl, sh = strides(kc)
+    q, k, v = x[:, :hq * d], x[:, hq * d:(hq + hkv) * d], x[:, (hq + hkv) * d:]
+    row = (hq + 2 * hkv) * d
+    cs.cs_rope_refresh_scatter(q, out, k, v, dev(np.arange(n, dtype=np.int32)), dev(pos), None, kc, vc, ks, vs, n, hq, hkv, d, row, row, row, sl, sh, 1e6, 0, cs.CS_BF16,
+                               cs.CS_KV4)
+    q64 = x64[:, :hq * d].reshape(n, hq, d)
+    pair = np.abs(q64[..., :d // 2]) + np.abs(q64[..., d // 2:])
+    pair = np.concatenate([pair, pair], -1)
+    want = ko.rope(q64, pos, None, 1e6, 0)
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= 4 * U * pair + B * (np.abs(want) + 4 * U * pair))
+    k64, v64 = (x64[:, a * d:(a + hkv) * d].reshape(n, hkv, d) for a in (hq, hq + hkv))
+    for c, s, w in ((kc, ks, ko.rope_single(k64.astype(np.float32), pos, None, 1e6, 0)), (vc, vs, v64)):
+        wc, ws = ko.quantise(w)
+        assert np.array_equal(s[0].cpu().numpy(), ws) and np.array_equal(ko.values(c[0].cpu().numpy(), ws), ko.values(wc, ws))

@@ -107,3 +107,17 @@ def test_binding_refuses_tensors_that_are_too_short():
     ("cs_plan_evict", EVICT, U, dict(s=1 << 22)), ("cs_plan_evict", EVICT, I, dict(kvn=A, kv=A)), ("cs_plan_evict", EVICT, I, dict(w=A, wn=A))])
 def test_more_than_a_launch_holds_and_outputs_over_inputs(fn, good, code, change):
     assert getattr(cs.lib(), fn)(*dict(good, **change).values()) == code
+
+
+@pytest.mark.parametrize("fn,good,code,change", [
+    ("cs_rope_refresh_scatter", ROPE, U, dict(hq=65536, sq=65536 * 64)), ("cs_rope_refresh_scatter", ROPE, U, dict(n=100000, hq=65536, sq=65536 * 64)),
+    ("cs_rope_refresh_scatter", ROPE, U, dict(hkv=32768, sk=32768 * 64, sv=32768 * 64)),
+    ("cs_kv4_rerotate", MOVE, U, dict(n=(1 << 31) + 1, hkv=2)), ("cs_kv4_rerotate", MOVE, U, dict(n=1 << 24, hkv=256)),
+    ("cs_kv4_window_attn", ATTN, U, dict(n=(1 << 26) - 1, hq=64, hkv=64)),                 # 2^25 workgroups: row tiles of 128 rows
+    ("cs_kv4_window_attn", ATTN, U, dict(n=(1 << 26) - 1, s=1 << 26, hq=16, hkv=2)),       # row tiles of 16 rows
+    ("cs_attn_weights", WEIGHTS, U, dict(n=1, s=1 << 20, hq=32, hkv=32, mb=16)),           # 2^25 workgroups
+    ("cs_attn_weights", WEIGHTS, U, dict(n=1 << 26, hq=32, hkv=2, lse=A)), ("cs_attn_weights", WEIGHTS, U, dict(mb=(1 << 27) - 256, lse=A)),
+    ("cs_attn_weights", WEIGHTS, U, dict(d=96)), ("cs_attn_weights", WEIGHTS, U, dict(sh=40)), ("cs_attn_weights", WEIGHTS, U, dict(ss=66, sh=2, dt=cs.CS_F32, cdt=cs.CS_F32)),
+    ("cs_attn_weights", WEIGHTS, I, dict(hkv=0)), ("cs_attn_weights", WEIGHTS, I, dict(scale=INF)), ("cs_attn_weights", WEIGHTS, I, dict(ss=-32))])
+def test_limits_are_those_of_the_header(fn, good, code, change):
+    assert getattr(cs.lib(), fn)(*dict(good, **change).values()) == code
