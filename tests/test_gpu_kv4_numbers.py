@@ -1,6 +1,8 @@
 """Queries, keys and values that are no numbers, or infinite, and calls at the edges of what is accepted, over the 4-bit window cache,
 against oracle/kv4_oracle.py (needs an MI355X).  Tolerances as in tests/test_gpu_kv4.py."""
 import math
+import os
+import re
 
 import numpy as np
 import pytest
@@ -203,3 +205,69 @@ def test_rope_refresh_scatter_of_the_most_heads(cs, n):
     for c, s, w in ((kc, ks, ko.rope_single(k64.astype(np.float32), pos, None, 1e6, 0)), (vc, vs, v64)):
         wc, ws = ko.quantise(w)
         assert np.array_equal(s[0].cpu().numpy(), ws) and np.array_equal(ko.values(c[0].cpu().numpy(), ws), ko.values(wc, ws))
+
+# ------------------------------------------------------------------------------------------ attention weights: steps that are sorted out
+
+def weights_route(b):
+    """(steps of each stream, shares, whether each stream's steps are sorted out, most steps that can be), as attn_weights.hip has them."""
+    with open(os.path.join(os.path.dirname(b.cs.__file__), "csrc", "attn_weights.hip")) as f:
+        text = f.read()
+    k = {n: int(re.search(rf"\b{n} = (\d+)", text).group(1)) for n in ("kStep", "kListed", "kFewSteps", "kGroups", "kLeast")}
+    tile, group = 128 if b.cache == "f32" else 256, b.hq // b.hkv
+    jobs = -(-b.max_blocks * 16 // tile) * len(b.kv) * b.hkv
+    chunks = max(1, min(k["kGroups"] // jobs, -(-(b.n_q * group // len(b.kv)) // k["kStep"]) // k["kLeast"]))
+    steps = [-(-n * group // k["kStep"]) for n in b.nq]
+    return steps, chunks, [k["kFewSteps"] * chunks < s <= k["kListed"] for s in steps], k["kListed"]
+
+
+def weights_oracle(b, s):
+    """Weights, log-sum-exp and the slack of the weights of stream s, as Batch.oracle and check_weights have them, in whole matrices."""
+    at, group = sum(b.nq[:s]), b.hq // b.hkv
+    n, kv = b.nq[s], max(0, b.kv[s])
+    add, slack, lse = np.zeros(kv), np.zeros(kv), np.full((n, b.hq), -np.inf)
+    seen = np.arange(kv)[None] <= np.minimum(b.pos[s], kv - 1)[:, None]
+    for h in range(b.hq if n and kv else 0):
+        q, k = b.q64[at:at + n, h], b.k[s][:, h // group]
+        x = np.where(seen, b.scale * (q @ k.T), -np.inf)
+        some = seen.any(1)
+        top = np.where(some, x.max(1), 0.0)
+        w = np.exp(x - top[:, None])
+        lse[some, h] = (top + np.log(np.where(some, w.sum(1), 1.0)))[some]
+        p = w / np.where(some, w.sum(1), 1.0)[:, None]
+        size = b.scale * (np.abs(q) @ np.abs(k).T).max(1)
+        e = (b.d / 8 + 8) * U * size + 4 * U * (np.where(some, np.abs(lse[:, h]), 0.0) + size)
+        add += p.sum(0)
+        slack += (p * (2 * e + 16 * U)[:, None]).sum(0)
+    return add, lse, slack + (n * b.hq / 16 + 80) * U * add
+
+
+SORTED = [
+    # hq, hkv, d, kv, nq, which streams' steps are sorted out
+    (28, 4, 128, [300] + [20 + i for i in range(39)], [120] + [1] * 39, [True] + [False] * 39),            # a long stream beside many short ones
+    (24, 8, 64, [540 + 10 * i for i in range(24)], [200 + i for i in range(24)], [True] * 24),            # a token's three rows in two steps
+    (56, 8, 64, [4000], [450], [True]),                                                                    # ... its seven rows; many tiles
+    (16, 1, 64, [40] + [7] * 39, [4000] + [1] * 39, [True] + [False] * 39),                                # 2,000 steps
+    (16, 1, 64, [40] + [7] * 39, [4200] + [1] * 39, [False] * 40),                                         # 2,100: more than the list holds
+]
+
+
+@pytest.mark.parametrize("dtype,cache", CACHES)
+@pytest.mark.parametrize("i", range(len(SORTED)))
+def test_attn_weights_of_steps_that_are_sorted_out(cs, i, dtype, cache):
+    hq, hkv, d, kv, nq, which = SORTED[i]
+    b = Batch(cs, 180 + i, hq, hkv, d, kv, nq, dtype, cache=cache, layout=("head", "slot")[i % 2], where="any", extra=i % 3)
+    steps, chunks, is_sorted, most = weights_route(b)
+    say("attention weights, sorted steps", SORTED[i][:3], dtype, cache, "steps up to", max(steps), "shares", chunks)
+    assert is_sorted == which and (any(which) or max(steps) > most)
+    want = [weights_oracle(b, s) for s in range(len(kv))]
+    lse = dev(np.concatenate([w[1] for w in want] + [np.full((i % 3, hq), np.nan)]).astype(np.float32))
+    before = torch.rand((len(kv), 16 * b.max_blocks), device=DEV)
+    for stat in (None, lse):
+        got = b.weights(before, 0.75, lse=stat)
+        for s, n in enumerate(kv):
+            add, _, tol = want[s]
+            old = 0.75 * before[s, :n].double().cpu().numpy()
+            err = np.abs(got[s, :n].double().cpu().numpy() - old - add)
+            assert np.all(err <= tol + (len(b.pos[s]) * b.hq / 16 + 80) * U * old + 1e-30), (s, float(err.max()))
+            assert bool((got[s, n:] == 9.0).all())
+        assert torch.equal(got, b.weights(before, 0.75, lse=stat))
