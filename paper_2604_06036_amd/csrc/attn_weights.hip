@@ -88,7 +88,7 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
   uint16_t (*const s_q)[QP][kStep * QROW] = reinterpret_cast<uint16_t (*)[QP][kStep * QROW]>(s_mem);
   __shared__ __attribute__((aligned(16))) float s_lse[2][kStep];
   __shared__ __attribute__((aligned(16))) int s_pos[2][kStep];
-  __shared__ uint32_t s_none[2];                           // rows of the step whose statistics are no number
+  __shared__ int s_none;                                   // whether a row's statistics were no number
   __shared__ float s_m[2][4][kStep], s_l[2][4][kStep];
   __shared__ uint16_t s_list[kListed];
   __shared__ uint32_t s_bits[kListed / 32];
@@ -285,8 +285,7 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
       if (!STATS) {                                        // (+inf: such a row's weights are 0 here, those of keys past its position too)
         const bool none = pos >= 0 && !(next_lse[at_stage] > -INFINITY);
         s_lse[buf][tid] = none ? INFINITY : pos >= 0 ? next_lse[at_stage] * kLog2e : 0.0f;
-        const uint64_t rows_without = __ballot(none);
-        if (tid == 0) s_none[buf] = static_cast<uint32_t>(rows_without);
+        if (__builtin_expect(none, 0)) s_none = 1;
       }
     }
     if (step + AHEAD < step_end) request(step + AHEAD, at_stage);
@@ -294,7 +293,6 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
     if (STATS && step > step_begin) join(step - 1, buf ^ 1);
 
     const int my_pos = s_pos[buf][n];
-    const uint32_t none = STATS ? 0u : __builtin_amdgcn_readfirstlane(s_none[buf]);
     const bool sees = __any(my_pos >= key0);               // some row of the step sees a key of this wave
     const bool masked = __any(my_pos < key0 + 32 * KB - 1);
     if (sees) {
@@ -367,19 +365,13 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
         }
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) acc[kb] += sum[kb];
-        // (rows without statistics, rare: what they see, and nothing else, becomes NaN)
-        for (uint32_t left = none; __builtin_expect(left != 0, 0); left &= left - 1) {
-          const int pos = __builtin_amdgcn_readlane(my_pos, __ffs(left) - 1);
-#pragma unroll
-          for (int kb = 0; kb < KB; ++kb)
-            if (key0 + 32 * kb + n <= pos) acc[kb] = NAN;
-        }
       }
     } else if (STATS && h == 0) {
       s_m[buf][wave][n] = -INFINITY;
       s_l[buf][wave][n] = 0.0f;
     }
   };
+  if (tid == 0) s_none = 0;                                // (written by this wave alone)
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i)
     if (step_begin + i < step_end) request(step_begin + i, i);
@@ -400,6 +392,19 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(Params p) {
     }
     return;
   }
+  // Rows without statistics (rare) are looked up again: what they see, and nothing else, becomes NaN.
+  if (step_begin < step_end && __builtin_expect(__builtin_amdgcn_readfirstlane(s_none), 0))
+    for (int i = step_begin; i < step_end; ++i) {
+      const int r = min(step_at(i) * kStep + n, rows - 1), tok = token_of(p, r);
+      const int pos = min(p.q_pos[q0 + tok], entries - 1);
+      const bool none = pos >= 0 && !(lse_base[static_cast<int64_t>(tok) * p.n_q_heads + (r - tok * p.group)] > -INFINITY);
+      for (uint32_t left = static_cast<uint32_t>(__ballot(none)); left; left &= left - 1) {
+        const int last = __builtin_amdgcn_readlane(pos, __ffs(left) - 1);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+          if (key0 + 32 * kb + n <= last) acc[kb] = NAN;
+      }
+    }
   float* part = p.ws_part + ((static_cast<int64_t>(chunk) * p.n_kv_heads + kvh) * p.n_streams + stream) * (static_cast<int64_t>(p.max_blocks) * CS_KV_BLOCK);
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb) {
