@@ -8,9 +8,11 @@
 // Without statistics from the caller the same kernel computes S^T = K Q^T first (operands swapped: a lane owns one query and
 // 16 keys), which gives a row's maximum and sum over the workgroup's keys in registers; a second launch joins the key ranges.
 // fp32 operands are sums of three bf16 numbers: three products for 4-bit keys (exact in bf16), six for fp32 keys.
-// Bound by vector work between the matrix instructions (an exponential, a compare and an add per row and key, 64-wide): 16 streams of
-// up to 389 queries of 28 heads over up to 1,100 4-bit entries take 46 to 49 us, 466 TFLOP/s; 64 queries over 17,630 16-bit entries with
-// statistics to find first (two sweeps) 52 to 56 us.  For 2,082 queries over 17,630 entries with statistics at hand: 298 us.
+// 16 streams of up to 389 queries of 28 heads over up to 1,100 4-bit entries take 46 to 49 us, 437 to 466 TFLOP/s: while CUs are busy their
+// matrix units work 27 % and their vector units 50 % of the time (an exponential, a product and an add per row and key), a wave's one
+// after the other, and a wave waits half of its own time.  64 queries over 17,630 16-bit entries with statistics to find first (two sweeps)
+// take 52 to 55 us: matrix units 15 and 20 %, vector units 41 and 43 %, 828 workgroups on the 512 places that the statistics kernel's
+// registers leave, and on 768 for the weights.  2,082 queries over 17,630 entries with statistics at hand: 288 to 301 us.
 #include <math.h>
 
 #include <type_traits>

@@ -2,25 +2,28 @@
 //
 // out[t][h] = sum_j softmax_j(scale q[t][h] . K_j) V_j over the entries j <= q_pos[t] of the query's stream.
 // A "row" is one (query token, query head of a kv group) pair, so that a tile of keys serves all heads of the group.  Keys
-// pass in tiles of 64, 32 at a time:
+// pass in tiles of 64 (rows kernel at head_dim 128: of 32), 32 at a time:
 //   S^T = K Q^T      v_mfma_f32_32x32x16_bf16, a lane owns one query and 16 of 32 keys.  Keys are converted to bf16, which
 //                    is exact (a 4-bit value has one fraction bit).  fp32 queries are the sum of three bf16 numbers (8 + 8 + 8
 //                    bits).  (v_mfma_scale_f32_32x32x64 would take the codes as they lie in the cache, against queries in 8-bit
 //                    parts; but it drops what lies 2^14 below the largest product of an instruction, measured on integers:
 //                    one large channel would cost the scores their low bits, 4e-5 of a score of 1 for normal data.)
 //   softmax          one pass, running maximum and sum in fp32; the reference maximum is raised when a tile exceeds it by
-//                    more than 2^8, so that accumulators are rarely scaled.  Weights are rounded to bf16 (fp32 queries:
-//                    three bf16 parts); the sums of the statistics are over the unrounded ones.
+//                    more than 2^8, so that accumulators are rarely scaled.  Weights are rounded to bf16, which the products
+//                    take (half a step is 2^-8 of a weight; outputs are 0.0023 off in relative norm, 0.0017 if only they were
+//                    rounded; a second part would cost as many products again); fp32 queries: three bf16 parts.  The sums of
+//                    the statistics are over the unrounded ones.
 //   O^T += V^T P^T   v_mfma_f32_32x32x16_bf16: P^T is in operand layout as it is, values are converted to bf16 on their way
 //                    into LDS and come back by its transposing read.
 // Many rows a stream (rows kernel): four waves of 32 rows share a tile in LDS.  Few rows (keys kernel): every wave holds the
 // same 16 rows (16x16x32 instructions) and takes tiles of its own, with nothing but its own values in LDS; the waves join their
 // results at the end.  Where there are few workgroups, the sweep of a row tile is cut into pieces of entries, whose results a second
 // launch joins.
-// Bounds.  Rows kernel: the vector work of unpacking and softmax shares issue slots with the matrix products; 32 streams of up to 389
-// tokens of 28 heads over up to 1,100 entries take 120 us, 706 TFLOP/s (a large product of the library reaches 1,200).  Keys kernel: memory;
-// 64 streams of one token of 32 heads over up to 17,630 entries, 8 kv heads, take 197 us, 4.7 TB/s, as fast as a large copy.
-// One token over one window of 919 entries takes 8.9 us: a chain of one tile a wave, the join of eight waves and a launch.
+// Bounds.  Rows kernel: products and vector work (unpacking, softmax) of a wave follow each other; of the time that CUs are busy the matrix
+// units work 34 %, the vector units 49 %, LDS 36 % (a quarter of that is conflicts).  32 streams of up to 389 tokens of 28 heads over up to
+// 1,100 entries take 115 to 123 us, 690 to 737 TFLOP/s (a large product of the library reaches 1,200).  Keys kernel: memory; 64 streams of
+// one token of 32 heads over up to 17,630 entries, 8 kv heads, take 198 us and read 982 MB, 4.9 TB/s, as fast as a large copy.
+// One token over one window of 919 entries takes 9 us: a chain of one tile a wave, the join of eight waves and a launch.
 #include <math.h>
 
 #include <type_traits>
@@ -402,7 +405,7 @@ template <int D, int PARTS>
 __global__ __launch_bounds__(256, PARTS == 1 ? 3 : D == 64 ? 2 : 1) void kv4_rows_kernel(Params p) {
   constexpr int DB = D / 32;
   constexpr int T = 128 / DB;                              // keys of a tile
-  constexpr int KROW = D + 8, VROW = D + 32;               // padded: reads of eight rows, and the transposing ones, meet no bank twice
+  constexpr int KROW = D + 8, VROW = D + 32;               // padded: reads of eight rows, and the transposing ones, start in banks of their own
   __shared__ __attribute__((aligned(16))) uint16_t s_k[2][T * KROW];
   __shared__ __attribute__((aligned(16))) uint16_t s_v[2][T * VROW];
   __shared__ uint8_t s_vs[2][128];
@@ -578,7 +581,7 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 3 : D == 64 ? 2 : 1) void kv4_row
 template <int D, int PARTS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, PARTS == 1 ? 3 : 2) void kv4_keys_kernel(Params p) {
   constexpr int DB = D / 32, EL = D / 4, SW = EL / 8;      // blocks of a row; elements of a lane's key; steps of a key's sum
-  constexpr int VROW = D + 16;                             // padded: eight rows of 32 bytes meet no bank twice
+  constexpr int VROW = D + 16;                             // padded: eight rows of 32 bytes start in banks of their own (counted: two fifths of its LDS cycles are conflicts all the same)
   constexpr int VC = 32 * DB / 64;                         // value blocks of 32 keys that a lane moves
   constexpr int OROW = D + 4;
   constexpr int BYTES = 32 * VROW * 2 > 16 * OROW * 4 ? 32 * VROW * 2 : 16 * OROW * 4;
@@ -892,8 +895,9 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Params p, int bf16) {
 }
 
 // ---- which kernel, how many pieces
-// Tiles that make a piece worth its share of the join, of the keys and the rows kernel.  4 kv heads of 7 query heads, head_dim 128: one
-// token over 919 entries takes 9.9 us uncut (8), 13.3 us in pieces (6), over 1,500 13.2 us at 8 and 11.8 at 16, over 17,630 15.1 and 17.1;
+// Tiles that make a piece worth its share of the join, of the keys and the rows kernel.  4 kv heads of 7 query heads, head_dim 128, calls
+// back to back: one token over 919 entries takes 9.5 to 9.9 us uncut (8), 11.7 to 13.6 in pieces (6), over 1,500 12.1 to 12.6 at 8 and
+// 11.5 at 16, over 17,630 14.0 and 17.1;
 // 424 tokens over 919 take 30.5 us at 6, 28.8 at 4, 31.4 at 3.
 constexpr int kLeastFew = 8, kLeastMany = 4;
 // Pieces above which a workgroup shares a row's: 64 tokens over 17,630 entries (48 pieces) take 45.6 us, 61 us with one thread walking
@@ -918,7 +922,7 @@ Route route(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_head
   r.waves = 4;
   const int64_t least = r.few ? kLeastFew : kLeastMany;
   // Pieces for two rounds of what the card holds at once (keys: 4 waves each; half of it costs 14.2 -> 15.8 us for 16 tokens of 16
-  // streams, twice it changes nothing) and three workgroups a CU (rows: 64 tokens over 17,630 entries take 45 us, with half as
+  // streams, twice it changes nothing) and three workgroups a CU (rows; of fp32 queries two fit: 64 tokens over 17,630 entries take 45 us, with half as
   // many 47.8, with twice 51).  The rows kernel counts the row tiles that streams of one length would have (64 streams of 16 tokens over
   // 4,000: 97 us, 135 by the bound on any lengths); the keys kernel the bound (64 streams of a token over 8,000: 103 us, 116 us).
   const int64_t even = (n_q * group + busy * r.rows - 1) / (busy * r.rows) * busy * n_kv_heads;     // jobs of streams of one length

@@ -235,9 +235,10 @@ struct Kv4RerotateParams {
 
 // A workgroup evaluates the angles of its rows once, into LDS (all heads and layers of a row turn by them).  A lane owns 32 pairs of
 // a row and head, two blocks, in every layer of its share: 16-byte loads, and a block's largest magnitude is the lane's own.
-// Bound by memory, and by its requests where rows are not neighbours: 15,023 rows of 28 layers, 4 heads of 128, move at 3.8 TB/s
-// (120 us) in a slot-major cache, whose rows are 256 bytes of codes, and at 1.7 (265 us) head-major, 64 bytes.  2,051 rows take
-// 50 us with the gather behind them, 58 at 128 workgroups, 54 at 256 or 1,024, 62 at 2,048.
+// Bound by memory, and by its requests where rows are not neighbours: 15,023 rows of 28 layers, 4 heads of 128, move at 4.2 TB/s
+// (110 us) in a slot-major cache and 3.6 (127 us) head-major where slots run on within cache blocks, as a refresh plan's do.  Slots drawn
+// one by one, nearer to an eviction's: 116 to 126 us slot-major, whose rows are 256 bytes of codes, and 264 head-major, 64 bytes.
+// 2,051 rows take 48 us with the gather behind them; 58 at 128 workgroups, 54 at 256 or 1,024, 62 at 2,048, 50 then at 512.
 constexpr int kAngleRows = 4096;         // (row, pair) places in LDS
 constexpr int kRerotateGroups = 512;     // workgroups wanted
 
@@ -528,7 +529,7 @@ extern "C" int cs_kv4_rerotate(uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_c
   p.head_dim = head_dim;
   p.lanes_per_head = head_dim / 64;
   // Scale bytes move as one word a row and head where they lie as one (head_dim 64 and 128): 15,023 rows of 28 layers,
-  // 4 heads of 128 each, take 265 us head-major and 120 us slot-major, with single bytes 297 and 125.
+  // 4 heads of 128 each, in slots drawn one by one, take 265 us head-major and 120 us slot-major, with single bytes 297 and 125.
   const int64_t strides = stride_layer | stride_slot | stride_head;
   const uintptr_t scales = reinterpret_cast<uintptr_t>(k_scales) | (dst_slot ? reinterpret_cast<uintptr_t>(v_scales) : 0);
   const int width = 2 * p.lanes_per_head;
