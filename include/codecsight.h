@@ -603,16 +603,17 @@ int cs_kv4_rerotate(uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_codes, uint8
  * As cs_window_prefill_attn, with the same meaning of cu_q, q_pos, kv_len, block_table and of n_q as an upper bound; besides,
  * q_pos needs no order inside a stream, and a negative q_pos is a query that sees nothing (out 0, lse -inf).
  * q and out are CS_BF16 (bf16 operands, fp32 scores, statistics and sums; weights are rounded to bf16) or CS_F32 (fp32
- * accuracy throughout).  Keys and values that are no numbers, or infinite, reach the queries that see them, and no others; an infinite value only
- * its own column.
+ * accuracy throughout).  Keys and values that are no numbers, or infinite, reach the queries that see them, and no others; an
+ * infinite value only its own column.  Weighted values are summed before they are divided, weights up to 2^8: values past
+ * 2^120 / kv_len may overflow on the way.
  *
  *  lse          out  float [n_q][n_q_heads] or NULL: log sum_j exp(softmax_scale * q[t][h] . K_j), natural logarithm
  *  workspace         cs_kv4_window_attn_workspace() bytes, 16-byte aligned (may be 0, then NULL is accepted); contents need
  *                    not be initialised.  Two calls that overlap in time must not share a workspace.
  * Errors: CS_EINVAL (null pointer, negative size, n_q_heads not a multiple of n_kv_heads, softmax_scale not a positive
  *         finite number), CS_EUNSUPPORTED (head_dim not in {64,128}, block_size != 16, n_q_heads/n_kv_heads > 16, strides not
- *         multiples of 32, stride_slot >= 2^26, alignment, unknown dtype, n_q >= 2^26, n_kv_heads > 65,535), CS_EWORKSPACE,
- *         CS_EHIP.
+ *         multiples of 32, stride_slot >= 2^26, alignment, unknown dtype, n_q >= 2^26, n_kv_heads > 65,535, max_blocks >
+ *         2^27 - 65), CS_EWORKSPACE, CS_EHIP.
  *         n_q == 0 or n_streams == 0 returns CS_OK.
  * ------------------------------------------------------------------------------------------ */
 size_t cs_kv4_window_attn_workspace(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads,
@@ -680,7 +681,8 @@ int cs_attn_weights(const void* q, const float* lse, const void* k_cache_layer, 
  *                        not weight
  * Bit exact.
  * Errors: CS_EINVAL (null pointer, negative size, budget < 1, a block table without columns, a new table too narrow for what
- *         may stay, kv_len_new == kv_len, weight_new == weight), CS_EUNSUPPORTED (tables of 2^27 columns, budget > 2^30, 2^22 streams), CS_EHIP.  n_streams == 0 returns CS_OK.
+ *         may stay, kv_len_new == kv_len, weight_new == weight), CS_EUNSUPPORTED (a table of more than 2^27 - 1,025
+ *         columns, budget > 2^30, 2^22 streams), CS_EHIP.  n_streams == 0 returns CS_OK.
  * ------------------------------------------------------------------------------------------ */
 int cs_plan_evict(const float* weight, const int32_t* kv_len, const int32_t* block_table_old, int32_t max_blocks_old,
                   const int32_t* block_table_new, int32_t max_blocks_new, int32_t n_streams, int32_t budget,

@@ -118,6 +118,7 @@ def test_more_than_a_launch_holds_and_outputs_over_inputs(fn, good, code, change
     ("cs_attn_weights", WEIGHTS, U, dict(n=1, s=1 << 20, hq=32, hkv=32, mb=16)),           # 2^25 workgroups
     ("cs_attn_weights", WEIGHTS, U, dict(n=1 << 26, hq=32, hkv=2, lse=A)), ("cs_attn_weights", WEIGHTS, U, dict(mb=(1 << 27) - 256, lse=A)),
     ("cs_attn_weights", WEIGHTS, U, dict(d=96)), ("cs_attn_weights", WEIGHTS, U, dict(sh=40)), ("cs_attn_weights", WEIGHTS, U, dict(ss=66, sh=2, dt=cs.CS_F32, cdt=cs.CS_F32)),
+    ("cs_kv4_window_attn", ATTN, U, dict(mb=(1 << 27) - 64)), ("cs_plan_evict", EVICT, U, dict(mbo=(1 << 27) - 1024)), ("cs_plan_evict", EVICT, U, dict(mbn=(1 << 27) - 1024)),
     ("cs_attn_weights", WEIGHTS, I, dict(hkv=0)), ("cs_attn_weights", WEIGHTS, I, dict(scale=INF)), ("cs_attn_weights", WEIGHTS, I, dict(ss=-32))])
 def test_limits_are_those_of_the_header(fn, good, code, change):
     assert getattr(cs.lib(), fn)(*dict(good, **change).values()) == code
