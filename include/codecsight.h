@@ -689,6 +689,149 @@ int cs_plan_evict(const float* weight, const int32_t* kv_len, const int32_t* blo
                   int32_t n_first, int32_t n_last, int32_t renumber, int32_t* kept, int32_t* src_slot, int32_t* dst_slot,
                   int32_t* delta, int32_t* kv_len_new, float* weight_new, void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Long windows of models that norm their heads or rotate part of them.  (Paper Sec. 3.5 and Sec. 4 for the write, Sec. 3.4.2 for the
+ *     correction; the choice of blocks is not the paper's, whose queries read whole windows.)
+ *
+ * A layer is  (n1) norms, rotation and refresh write -> (s1) bounds of the new keys' blocks -> (s2) the blocks each query reads ->
+ * (s3) attention over them;  a slide begins with (n2).  16-bit and fp32 caches.
+ * Blocks of a selection hold sel_block entries, a multiple of CS_KV_BLOCK up to CS_SELECT_BLOCK_MOST: block b of a stream are its
+ * entries b*sel_block .. (b+1)*sel_block - 1, and n_sel = ceil(max_blocks * 16 / sel_block) blocks have places.
+ * CS_EUNSUPPORTED also answers calls past what a launch holds, 2^32 threads along an axis of its grid.
+ * ------------------------------------------------------------------------------------------ */
+#define CS_SELECT_BLOCK_MOST 128   /* entries of a block            */
+#define CS_SELECT_MOST 256         /* blocks that a query may list  */
+
+/* ------------------------------------------------------------------------------------------
+ * (n1) Norms of queries and keys for each head, rotary embedding, refresh write.     Paper Sec. 3.5 (write), Sec. 4.
+ *
+ * As cs_rope_refresh_scatter, into a cache of dtype, with y(x) in place of x for queries and keys:
+ *     y = weight * x / sqrt(mean(x^2) + norm_eps)      over the head_dim elements of a head;  weight == NULL: y = x
+ *     q_out[t][h] = R(pos[t]) y(q[t][h]),   K[slot[t]][h] = R(pos[t]) y(k_new[t][h]),   V[slot[t]][h] = v_new[t][h]   for slot[t] >= 0
+ * R turns the first rotary_dim elements of a head, pairs (i, i + rotary_dim/2) or (2i, 2i+1), pair i by pos[t] * inv_freq[i] or
+ * pos[t][axis_of_pair[i]] * inv_freq[i], and multiplies them by amplitude (1, or the factor that goes with scaled frequencies); elements
+ * from rotary_dim on are not turned and not multiplied.  Sums and products are single precision, angles double (products of the position
+ * and the table's number); results are rounded once.  Heads whose squares pass the largest single-precision number are normed as others.
+ * Values are copied bit for bit.
+ *
+ *  q_weight, k_weight  in  [head_dim] of dtype, 16-byte aligned, or NULL: that kind of head is not normed
+ *  pos           in   int32 [n_tok], or [n_tok][3] with axis_of_pair; NULL: nothing is turned or multiplied
+ *  axis_of_pair  in   uint8 [rotary_dim/2], values 0, 1, 2 (larger: read as 2), or NULL
+ *  inv_freq      in   float [rotary_dim/2] (may be NULL without pos)
+ *  other arguments as in cs_rope_refresh_scatter
+ * Errors: CS_EINVAL (null pointer, negative size, no heads at all, tokens that overlap, rotary_dim > head_dim, with weights a norm_eps
+ *         that is not a number from 1e-30 on, an amplitude that is no finite number), CS_EUNSUPPORTED (head_dim or rotary_dim not
+ *         multiples of 16, head_dim > 256, unknown dtype / rope_style, strides or pointers that are not aligned, more than 65,535 query
+ *         heads or 32,767 key heads), CS_EHIP.  n_tok == 0 returns CS_OK.
+ * ------------------------------------------------------------------------------------------ */
+int cs_norm_rope_refresh_scatter(const void* q, void* q_out, const void* k_new, const void* v_new, const void* q_weight,
+                                 const void* k_weight, const int32_t* slot, const int32_t* pos, const uint8_t* axis_of_pair,
+                                 const float* inv_freq, void* k_cache_layer, void* v_cache_layer, int64_t n_tok,
+                                 int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t rotary_dim,
+                                 int64_t stride_q, int64_t stride_k, int64_t stride_v, int64_t stride_slot,
+                                 int64_t stride_head, float norm_eps, float amplitude, int32_t rope_style, int32_t dtype,
+                                 void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * (n2) Position-corrected reuse of keys that (n1) wrote.       Paper Sec. 3.4.2, Eq. 6.
+ *
+ * As cs_kv_rerotate (axis_of_pair == NULL, delta int32 [n_rows]) and cs_kv_rerotate_axes (delta int32 [n_rows][3]), with the
+ * frequencies of a table: the first rotary_dim elements of a head are turned, pair i by delta * inv_freq[i]; those behind are copied
+ * when repacking and not touched in place.  (An amplitude is in the keys already.)
+ *
+ *  axis_of_pair  in   uint8 [rotary_dim/2] or NULL;   inv_freq  in  float [rotary_dim/2]
+ * Errors: as cs_kv_rerotate, without rope_base; CS_EINVAL also for rotary_dim < 16 or > head_dim, CS_EUNSUPPORTED for one that is not a
+ *         multiple of 16 and for more than 65,535 kv heads.
+ * ------------------------------------------------------------------------------------------ */
+int cs_kv_rerotate_freqs(void* k_cache, void* v_cache, const int32_t* src_slot, const int32_t* dst_slot,
+                         const int32_t* delta, const uint8_t* axis_of_pair, const float* inv_freq, int64_t n_rows,
+                         int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int32_t rotary_dim, int64_t stride_layer,
+                         int64_t stride_slot, int64_t stride_head, int32_t rope_style, int32_t dtype, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * (s1) Bounds of the keys of every block.
+ *
+ * For stream s, kv head h and block b, over its entries j < kv_len[s]:
+ *     hi_c = ceil(max_j K_j[h][c] / 2^k),  lo_c = floor(min_j K_j[h][c] / 2^k),  k >= -95 the least with |max|, |min| <= 127 * 2^k for all c
+ *     bounds[s][h][b][0][c] = hi_c,  bounds[s][h][b][1][c] = lo_c,  scales[s][h][b] = k + 127
+ * Scale 255, bounds 0: the block holds a NaN or an infinity.  Bit exact (no rounding but the ceil and the floor).
+ *
+ *  from         in   int32 [n_streams] or NULL: blocks that end at or before entry from[s] are left as they were (rows from from[s]
+ *                    on are new since the last call); NULL: all blocks are made.  Blocks from kv_len[s] on are left as they were
+ *  kv_len       in   int32 [n_streams] (clamped to the table's rows)
+ *  bounds       out  int8 [n_streams][n_kv_heads][n_sel][2][head_dim], 16-byte aligned
+ *  scales       out  uint8 [n_streams][n_kv_heads][n_sel]
+ * Errors: CS_EINVAL (null pointer, negative size), CS_EUNSUPPORTED (head_dim not in {64,128}, block_size != 16, sel_block as above, strides
+ *         not multiples of 16 bytes, alignment, unknown dtype, n_kv_heads > 65,535, max_blocks > 2^27 - 65), CS_EHIP.
+ *         n_streams == 0 returns CS_OK.
+ * ------------------------------------------------------------------------------------------ */
+int cs_key_bounds(const void* k_cache_layer, const int32_t* from, const int32_t* kv_len, const int32_t* block_table,
+                  int32_t max_blocks, int32_t block_size, int32_t sel_block, int8_t* bounds, uint8_t* scales,
+                  int32_t n_streams, int32_t n_kv_heads, int32_t head_dim, int64_t stride_slot, int64_t stride_head,
+                  int32_t dtype, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * (s2) The blocks that each query reads.
+ *
+ * For query token t of stream s and kv head g: the query heads h of the group become whole numbers,
+ *     qc_hc = q[t][h][c] / 2^f rounded to nearest, ties to even,   f >= -95 the least with |q| <= 127 * 2^f for all h, c
+ *     score(b) = 2^(scales[s][g][b] - 127) * max_h sum_c max(qc_hc hi_c, qc_hc lo_c)
+ * which bounds the products of the heads with the block's keys (up to the rounding of q).  Candidates are the blocks that begin at or before
+ * entry min(q_pos[t], kv_len[s] - 1).  selected[t][g] are the first n_first and the last n_last candidates and, of the others, those of the
+ * largest score, equal scores by the lowest index; n_select in all, or all candidates where there are no more; ascending, then -1.
+ * A block that holds what is no number goes before all others but the first and last ones; with a query that does, all scores are 0.
+ * A block's bounds take in its entries behind the query.  Whole numbers throughout: bit exact.
+ *
+ *  q            in   [n_q][n_q_heads][head_dim] of dtype, 16-byte aligned
+ *  cu_q, q_pos, kv_len  in  as in the attention calls (any order of q_pos; a negative one has no candidates); n_q is an upper bound, and
+ *                    rows from cu_q[n_streams] on are left as they were
+ *  bounds, scales  in  as (s1) leaves them, for every candidate
+ *  selected     out  int32 [n_q][n_kv_heads][n_select]
+ *  workspace         cs_select_blocks_workspace() bytes, 16-byte aligned (may be 0, then NULL is accepted); contents need not be
+ *                    initialised.  Two calls that overlap in time must not share a workspace.
+ * Errors: CS_EINVAL (null pointer, negative size, n_q_heads not a multiple of n_kv_heads, n_select < 1, n_first + n_last > n_select),
+ *         CS_EUNSUPPORTED (head_dim not in {64,128}, n_q_heads/n_kv_heads > 16, sel_block as above, n_select > CS_SELECT_MOST, n_sel >
+ *         32,768, n_q >= 2^26, alignment, unknown dtype, n_kv_heads > 65,535, max_blocks > 2^27 - 65), CS_EWORKSPACE, CS_EHIP.
+ *         n_q == 0 or n_streams == 0 returns CS_OK.
+ * ------------------------------------------------------------------------------------------ */
+size_t cs_select_blocks_workspace(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                  int32_t max_blocks, int32_t sel_block);
+
+int cs_select_blocks(const void* q, const int8_t* bounds, const uint8_t* scales, const int32_t* cu_q, const int32_t* q_pos,
+                     const int32_t* kv_len, int32_t max_blocks, int32_t sel_block, int32_t n_select, int32_t n_first,
+                     int32_t n_last, int32_t* selected, int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads,
+                     int32_t head_dim, int32_t dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * (s3) Attention over the blocks selected for each query: windows, questions, single tokens.
+ *
+ * As cs_kv4_window_attn on a cache of dtype (q_pos in any order, a negative one sees nothing: out 0, lse -inf), but a query token t and kv
+ * head g see, of the entries j <= q_pos[t], j < kv_len[s], only those of the blocks listed in selected[t][g].  Lists may be in any order;
+ * a block that stands twice counts once; indexes that are negative or lie behind the query are skipped; a query whose list leaves nothing
+ * gets out 0, lse -inf.  Rows of a stream with kv_len <= 0, and from cu_q[n_streams] on, are left as they were.
+ * CS_BF16: bf16 operands, fp32 scores, statistics and sums; weights are rounded to bf16.  CS_F32: fp32 throughout.  Keys and values that are
+ * no numbers, or infinite, reach the queries that see them, and no others.  Weighted values are summed before they are divided, weights
+ * up to 2^8: values past 2^120 / kv_len may overflow on the way.
+ *
+ *  selected     in   int32 [n_q][n_kv_heads][n_select]
+ *  lse          out  float [n_q][n_q_heads] or NULL: log sum_j exp(softmax_scale * q[t][h] . K_j) over the entries seen
+ *  workspace         cs_selected_attn_workspace() bytes, 16-byte aligned (may be 0, then NULL is accepted); contents need not be
+ *                    initialised.  Two calls that overlap in time must not share a workspace.
+ * Errors: CS_EINVAL (null pointer, negative size, n_q_heads not a multiple of n_kv_heads, n_select < 1, softmax_scale not a positive finite
+ *         number), CS_EUNSUPPORTED (head_dim not in {64,128}, block_size != 16, sel_block as above, n_select > CS_SELECT_MOST,
+ *         n_q_heads/n_kv_heads > 16, strides not multiples of 16 bytes, alignment, unknown dtype, n_q >= 2^26, n_kv_heads > 65,535,
+ *         max_blocks > 2^27 - 65), CS_EWORKSPACE, CS_EHIP.  n_q == 0 or n_streams == 0 returns CS_OK.
+ * ------------------------------------------------------------------------------------------ */
+size_t cs_selected_attn_workspace(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                  int32_t sel_block, int32_t n_select);
+
+int cs_selected_attn(const void* q, const void* k_cache_layer, const void* v_cache_layer, const int32_t* cu_q,
+                     const int32_t* q_pos, const int32_t* kv_len, const int32_t* block_table, int32_t max_blocks,
+                     int32_t block_size, const int32_t* selected, int32_t sel_block, int32_t n_select, void* out, float* lse,
+                     int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                     int64_t stride_slot, int64_t stride_head, float softmax_scale, int32_t dtype, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -23,6 +23,7 @@ CS_ATTN_OWN_ROWS = 1 << 16
 CS_FRAME_P, CS_FRAME_I = 0, 1
 CS_ROPE_HALF_SPLIT, CS_ROPE_INTERLEAVED = 0, 1
 CS_KV_BLOCK = 16
+CS_SELECT_BLOCK_MOST, CS_SELECT_MOST = 128, 256
 
 _ERR = {CS_EINVAL: "CS_EINVAL", CS_EUNSUPPORTED: "CS_EUNSUPPORTED", CS_EHIP: "CS_EHIP",
         CS_EWORKSPACE: "CS_EWORKSPACE"}
@@ -33,7 +34,9 @@ EXPORTS = ("cs_version", "cs_last_hip_error", "cs_mfma_rate_probe", "cs_project_
            "cs_window_prefill_attn_workspace",
            "cs_window_prefill_attn", "cs_refresh_prefill_attn_workspace", "cs_refresh_prefill_attn",
            "cs_rope_refresh_scatter", "cs_kv4_gather", "cs_kv4_rerotate", "cs_kv4_window_attn_workspace", "cs_kv4_window_attn",
-           "cs_attn_weights_workspace", "cs_attn_weights", "cs_plan_evict")
+           "cs_attn_weights_workspace", "cs_attn_weights", "cs_plan_evict",
+           "cs_norm_rope_refresh_scatter", "cs_kv_rerotate_freqs", "cs_key_bounds", "cs_select_blocks_workspace", "cs_select_blocks",
+           "cs_selected_attn_workspace", "cs_selected_attn")
 
 
 class CodecSightError(RuntimeError):
@@ -113,6 +116,20 @@ def lib() -> ctypes.CDLL:
     L.cs_attn_weights.argtypes = [vp] * 8 + [i32, i32, vp, vp, f32, i64, i32, i32, i32, i32, i64, i64, f32, i32, i32, vp, sz, vp]
     L.cs_plan_evict.restype = c.c_int
     L.cs_plan_evict.argtypes = [vp, vp, vp, i32, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp]
+    L.cs_norm_rope_refresh_scatter.restype = c.c_int
+    L.cs_norm_rope_refresh_scatter.argtypes = [vp] * 12 + [i64, i32, i32, i32, i32, i64, i64, i64, i64, i64, f32, f32, i32, i32, vp]
+    L.cs_kv_rerotate_freqs.restype = c.c_int
+    L.cs_kv_rerotate_freqs.argtypes = [vp] * 7 + [i64, i32, i32, i32, i32, i64, i64, i64, i32, i32, vp]
+    L.cs_key_bounds.restype = c.c_int
+    L.cs_key_bounds.argtypes = [vp] * 4 + [i32, i32, i32, vp, vp, i32, i32, i32, i64, i64, i32, vp]
+    L.cs_select_blocks_workspace.restype = sz
+    L.cs_select_blocks_workspace.argtypes = [i64, i32, i32, i32, i32, i32, i32]
+    L.cs_select_blocks.restype = c.c_int
+    L.cs_select_blocks.argtypes = [vp] * 6 + [i32, i32, i32, i32, i32, vp, i64, i32, i32, i32, i32, i32, vp, sz, vp]
+    L.cs_selected_attn_workspace.restype = sz
+    L.cs_selected_attn_workspace.argtypes = [i64, i32, i32, i32, i32, i32, i32]
+    L.cs_selected_attn.restype = c.c_int
+    L.cs_selected_attn.argtypes = [vp] * 7 + [i32, i32, vp, i32, i32, vp, vp, i64, i32, i32, i32, i32, i64, i64, f32, i32, vp, sz, vp]
     _lib = L
     return L
 
@@ -479,3 +496,139 @@ def cs_plan_evict(weight, kv_len, block_table_old, max_blocks_old, block_table_n
     _check(fn, lib().cs_plan_evict(
         _ptr(weight), _ptr(kv_len), _ptr(block_table_old), max_blocks_old, _ptr(block_table_new), max_blocks_new, n_streams, budget, n_first,
         n_last, int(bool(renumber)), _ptr(kept), _ptr(src_slot), _ptr(dst_slot), _ptr(delta), _ptr(kv_len_new), _ptr(weight_new), _stream()))
+
+
+def _kind(fn: str, t: Optional[torch.Tensor], dtype, what: str):
+    """Tensors that are read element by element, one behind another: of this type, contiguous."""
+    if t is not None and (t.dtype != dtype or not t.is_contiguous()):
+        raise ValueError(f"{fn}: {what} is not a contiguous tensor of {dtype}")
+
+
+def _element(dtype: int):
+    return {CS_F32: torch.float32, CS_BF16: torch.bfloat16}.get(dtype)
+
+
+def _bytes(workspace, workspace_bytes, fn: str) -> int:
+    held = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    if workspace_bytes is not None and held < workspace_bytes:
+        raise ValueError(f"{fn}: workspace tensor smaller than workspace_bytes")
+    return held if workspace_bytes is None else workspace_bytes
+
+
+def _blocks_of(max_blocks: int, sel_block: int) -> int:
+    per = max(1, sel_block // CS_KV_BLOCK)
+    return -(-max_blocks // per)
+
+
+def cs_norm_rope_refresh_scatter(q, q_out, k_new, v_new, q_weight, k_weight, slot, pos, axis_of_pair, inv_freq, k_cache_layer, v_cache_layer,
+                                 n_tok, n_q_heads, n_kv_heads, head_dim, rotary_dim, stride_q, stride_k, stride_v, stride_slot, stride_head,
+                                 norm_eps, amplitude, rope_style, dtype):
+    fn = "cs_norm_rope_refresh_scatter"
+    for t in (q, q_out, k_new, v_new, q_weight, k_weight, slot, pos, axis_of_pair, inv_freq, k_cache_layer, v_cache_layer):
+        _here(fn, t)
+    for t, what in ((slot, "slot"), (pos, "pos")):
+        _kind(fn, t, torch.int32, what)
+    _need(fn, slot, n_tok, "slot"); _need(fn, pos, n_tok if axis_of_pair is None else 3 * n_tok, "pos")
+    _axes(fn, axis_of_pair, rotary_dim); _kind(fn, inv_freq, torch.float32, "inv_freq"); _need(fn, inv_freq, rotary_dim // 2, "inv_freq")
+    for t, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        _need(fn, t, head_dim, what)
+        if t is not None:
+            _kind(fn, t, _element(dtype), what)
+    for t, what in ((q, "q"), (q_out, "q_out"), (k_new, "k_new"), (v_new, "v_new"), (k_cache_layer, "k_cache_layer"), (v_cache_layer, "v_cache_layer")):
+        if t is not None and _element(dtype) is not None and t.dtype != _element(dtype):
+            raise ValueError(f"{fn}: {what} is not of the call's dtype")
+    for t, stride, heads, what in ((q, stride_q, n_q_heads, "q"), (k_new, stride_k, n_kv_heads, "k_new"), (v_new, stride_v, n_kv_heads, "v_new")):
+        if not _span(t, n_tok, stride, heads * head_dim):
+            raise ValueError(f"{fn}: {what} holds fewer than {n_tok} tokens")
+    if q_out is not None and (q is None or q_out.data_ptr() != q.data_ptr()):
+        if not q_out.is_contiguous():
+            raise ValueError(f"{fn}: q_out is not contiguous")
+        _need(fn, q_out, n_tok * n_q_heads * head_dim, "q_out")
+    _check(fn, lib().cs_norm_rope_refresh_scatter(
+        _ptr(q), _ptr(q_out), _ptr(k_new), _ptr(v_new), _ptr(q_weight), _ptr(k_weight), _ptr(slot), _ptr(pos), _ptr(axis_of_pair), _ptr(inv_freq),
+        _ptr(k_cache_layer), _ptr(v_cache_layer), n_tok, n_q_heads, n_kv_heads, head_dim, rotary_dim, stride_q, stride_k, stride_v, stride_slot,
+        stride_head, norm_eps, amplitude, rope_style, dtype, _stream()))
+
+
+def cs_kv_rerotate_freqs(k_cache, v_cache, src_slot, dst_slot, delta, axis_of_pair, inv_freq, n_rows, n_layers, n_kv_heads, head_dim, rotary_dim,
+                         stride_layer, stride_slot, stride_head, rope_style, dtype):
+    fn = "cs_kv_rerotate_freqs"
+    for t in (k_cache, v_cache, src_slot, dst_slot, delta, axis_of_pair, inv_freq):
+        _here(fn, t)
+    for t, what in ((src_slot, "src_slot"), (dst_slot, "dst_slot"), (delta, "delta")):
+        _kind(fn, t, torch.int32, what)
+    _need(fn, src_slot, n_rows, "src_slot"); _need(fn, dst_slot, n_rows, "dst_slot")
+    _need(fn, delta, n_rows if axis_of_pair is None else 3 * n_rows, "delta")
+    _axes(fn, axis_of_pair, rotary_dim); _kind(fn, inv_freq, torch.float32, "inv_freq"); _need(fn, inv_freq, rotary_dim // 2, "inv_freq")
+    _check(fn, lib().cs_kv_rerotate_freqs(
+        _ptr(k_cache), _ptr(v_cache), _ptr(src_slot), _ptr(dst_slot), _ptr(delta), _ptr(axis_of_pair), _ptr(inv_freq), n_rows, n_layers, n_kv_heads,
+        head_dim, rotary_dim, stride_layer, stride_slot, stride_head, rope_style, dtype, _stream()))
+
+
+def cs_key_bounds(k_cache_layer, first_new, kv_len, block_table, max_blocks, block_size, sel_block, bounds, scales, n_streams, n_kv_heads,
+                  head_dim, stride_slot, stride_head, dtype):
+    """first_new: the C call's `from`."""
+    fn = "cs_key_bounds"
+    for t in (k_cache_layer, first_new, kv_len, block_table, bounds, scales):
+        _here(fn, t)
+    for t, what in ((first_new, "first_new"), (kv_len, "kv_len"), (block_table, "block_table")):
+        _kind(fn, t, torch.int32, what)
+    _need(fn, first_new, n_streams, "first_new"); _need(fn, kv_len, n_streams, "kv_len"); _need(fn, block_table, n_streams * max_blocks, "block_table")
+    places = n_streams * n_kv_heads * _blocks_of(max_blocks, sel_block)
+    _kind(fn, bounds, torch.int8, "bounds"); _need(fn, bounds, places * 2 * head_dim, "bounds")
+    _kind(fn, scales, torch.uint8, "scales"); _need(fn, scales, places, "scales")
+    _check(fn, lib().cs_key_bounds(
+        _ptr(k_cache_layer), _ptr(first_new), _ptr(kv_len), _ptr(block_table), max_blocks, block_size, sel_block, _ptr(bounds), _ptr(scales),
+        n_streams, n_kv_heads, head_dim, stride_slot, stride_head, dtype, _stream()))
+
+
+def cs_select_blocks_workspace(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, max_blocks, sel_block) -> int:
+    return int(lib().cs_select_blocks_workspace(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, max_blocks, sel_block))
+
+
+def cs_select_blocks(q, bounds, scales, cu_q, q_pos, kv_len, max_blocks, sel_block, n_select, n_first, n_last, selected, n_q, n_streams, n_q_heads,
+                     n_kv_heads, head_dim, dtype, workspace=None, workspace_bytes=None):
+    fn = "cs_select_blocks"
+    workspace_bytes = _bytes(workspace, workspace_bytes, fn)
+    for t in (q, bounds, scales, cu_q, q_pos, kv_len, selected, workspace):
+        _here(fn, t)
+    for t, what in ((cu_q, "cu_q"), (q_pos, "q_pos"), (kv_len, "kv_len"), (selected, "selected")):
+        _kind(fn, t, torch.int32, what)
+    if _element(dtype) is not None:
+        _kind(fn, q, _element(dtype), "q")
+    _need(fn, q, n_q * n_q_heads * head_dim, "q"); _need(fn, cu_q, n_streams + 1, "cu_q"); _need(fn, q_pos, n_q, "q_pos"); _need(fn, kv_len, n_streams, "kv_len")
+    places = n_streams * n_kv_heads * _blocks_of(max_blocks, sel_block)
+    _kind(fn, bounds, torch.int8, "bounds"); _need(fn, bounds, places * 2 * head_dim, "bounds")
+    _kind(fn, scales, torch.uint8, "scales"); _need(fn, scales, places, "scales")
+    _need(fn, selected, n_q * n_kv_heads * n_select, "selected")
+    _check(fn, lib().cs_select_blocks(
+        _ptr(q), _ptr(bounds), _ptr(scales), _ptr(cu_q), _ptr(q_pos), _ptr(kv_len), max_blocks, sel_block, n_select, n_first, n_last, _ptr(selected),
+        n_q, n_streams, n_q_heads, n_kv_heads, head_dim, dtype, _ptr(workspace), workspace_bytes, _stream()))
+
+
+def cs_selected_attn_workspace(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, sel_block, n_select) -> int:
+    return int(lib().cs_selected_attn_workspace(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, sel_block, n_select))
+
+
+def cs_selected_attn(q, k_cache_layer, v_cache_layer, cu_q, q_pos, kv_len, block_table, max_blocks, block_size, selected, sel_block, n_select, out,
+                     lse, n_q, n_streams, n_q_heads, n_kv_heads, head_dim, stride_slot, stride_head, softmax_scale, dtype, workspace=None,
+                     workspace_bytes=None):
+    fn = "cs_selected_attn"
+    workspace_bytes = _bytes(workspace, workspace_bytes, fn)
+    for t in (q, k_cache_layer, v_cache_layer, cu_q, q_pos, kv_len, block_table, selected, out, lse, workspace):
+        _here(fn, t)
+    for t, what in ((cu_q, "cu_q"), (q_pos, "q_pos"), (kv_len, "kv_len"), (block_table, "block_table"), (selected, "selected")):
+        _kind(fn, t, torch.int32, what)
+    if _element(dtype) is not None:
+        _kind(fn, q, _element(dtype), "q"); _kind(fn, out, _element(dtype), "out")
+        for t, what in ((k_cache_layer, "k_cache_layer"), (v_cache_layer, "v_cache_layer")):
+            if t is not None and t.dtype != _element(dtype):
+                raise ValueError(f"{fn}: {what} is not of the call's dtype")
+    _kind(fn, lse, torch.float32, "lse")
+    _need(fn, q, n_q * n_q_heads * head_dim, "q"); _need(fn, out, n_q * n_q_heads * head_dim, "out"); _need(fn, lse, n_q * n_q_heads, "lse")
+    _need(fn, cu_q, n_streams + 1, "cu_q"); _need(fn, q_pos, n_q, "q_pos"); _need(fn, kv_len, n_streams, "kv_len")
+    _need(fn, block_table, n_streams * max_blocks, "block_table"); _need(fn, selected, n_q * n_kv_heads * n_select, "selected")
+    _check(fn, lib().cs_selected_attn(
+        _ptr(q), _ptr(k_cache_layer), _ptr(v_cache_layer), _ptr(cu_q), _ptr(q_pos), _ptr(kv_len), _ptr(block_table), max_blocks, block_size,
+        _ptr(selected), sel_block, n_select, _ptr(out), _ptr(lse), n_q, n_streams, n_q_heads, n_kv_heads, head_dim, stride_slot, stride_head,
+        softmax_scale, dtype, _ptr(workspace), workspace_bytes, _stream()))

@@ -1,0 +1,457 @@
+// Which blocks of a long cache a query reads, gfx950: bounds of the keys of every block, and the choice by a bound on the products
+// with them.
+//
+// Bounds.  A block of `sel_block` entries of a stream and kv head is described by its channels' largest and smallest key as whole numbers
+// of a power of two:  hi_c = ceil(max_j K_jc / 2^k),  lo_c = floor(min_j K_jc / 2^k),  k the least with all |.| <= 127.  Largest and
+// smallest know no rounding and no order of sums, so the numbers are the same however they are found.
+//
+// Choice.  The heads of a query token and kv head become whole numbers too, qc = q / 2^f rounded to nearest (f the least with all |qc| <=
+// 127), and a block's score is
+//     2^k max_h sum_c max(qc_hc hi_c, qc_hc lo_c)      >= every q_h . K_j of the block, up to the rounding of q
+// The sum over c is  q+ . hi + q- . lo  with q+ = max(qc, 0), q- = min(qc, 0): a matrix product of bytes over 2 d, exact in 32 bits.  The
+// scores that are compared are one power of two times whole numbers below 2^21, exact in fp32: lists are the same on any machine, in any order.
+#include <math.h>
+
+#include <type_traits>
+
+#include "kv4.h"
+#include "token_tiles.h"
+
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef __attribute__((ext_vector_type(16))) int i32x16;
+
+constexpr uint32_t kNoNumber = 255;      // scale byte of a block that holds a NaN or an infinity
+constexpr int kLeast = 32;               // least scale byte: powers below 2^-95 are not needed, and scores stay normal numbers
+
+// Scale byte of numbers whose largest magnitude has the given fp32 bits: the least k >= kLeast - 127 with amax <= 127 * 2^k, biased by 127.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t amax_bits) {
+  if (amax_bits >= 0x7f800000u) return kNoNumber;
+  const int e = static_cast<int>((amax_bits + 0x1ffffu) >> 23) - 6;
+  return e < kLeast ? kLeast : static_cast<uint32_t>(e);
+}
+__device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }      // 2^-k
+
+// ------------------------------------------------------------------------------------------ bounds
+
+struct BoundsParams {
+  const void* __restrict__ k;
+  const int32_t* __restrict__ from;      // nullptr: all blocks
+  const int32_t* __restrict__ kv_len;
+  const int32_t* __restrict__ block_table;
+  int8_t* __restrict__ bounds;           // [n_streams][n_kv_heads][n_sel][2][head_dim]
+  uint8_t* __restrict__ scales;          // [n_streams][n_kv_heads][n_sel]
+  int64_t stride_slot, stride_head;
+  int32_t max_blocks, n_streams, n_kv_heads, n_sel, cache_blocks;      // cache_blocks: of a block
+  int32_t walkers;                       // waves that share the blocks of a stream and kv head
+};
+
+// A wave takes a block, lanes side by side on a row's channels; a wave goes on with the block `walkers` further.
+// UC cache blocks are asked for at once.
+template <bool kBf16, int D, int UC>
+__global__ __launch_bounds__(256) void key_bounds_kernel(BoundsParams p) {
+  using Elem = typename std::conditional<kBf16, uint16_t, float>::type;
+  constexpr int VE = kBf16 ? 8 : 4;      // elements a lane
+  constexpr int LR = D / VE;             // lanes a row
+  constexpr int RL = 64 / LR;            // rows a load
+  constexpr int NL = CS_KV_BLOCK / RL;   // loads a cache block
+  const int lane = threadIdx.x & 63;
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kvh = static_cast<int>(unit % p.n_kv_heads);
+  const int64_t rest = unit / p.n_kv_heads;
+  const int walker = static_cast<int>(rest % p.walkers);
+  const int64_t stream64 = rest / p.walkers;
+  if (stream64 >= p.n_streams) return;
+  const int stream = static_cast<int>(stream64);
+  const int entries = min(p.kv_len[stream], p.max_blocks * CS_KV_BLOCK);
+  const int size = p.cache_blocks * CS_KV_BLOCK;
+  const int first = p.from ? max(p.from[stream], 0) / size : 0;
+  const int32_t* ids = p.block_table + static_cast<int64_t>(stream) * p.max_blocks;
+  const int row = lane / LR, c = lane % LR;
+  const Elem* base = static_cast<const Elem*>(p.k) + static_cast<int64_t>(kvh) * p.stride_head + c * VE;
+  for (int64_t b = static_cast<int64_t>(first) + walker; b * size < entries; b += p.walkers) {
+    const int begin = static_cast<int>(b) * size, last = min(entries - begin, size) - 1;      // last: of the block's entries
+    float hi[VE], lo[VE];
+    uint32_t amax = 0;
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      hi[e] = -INFINITY;
+      lo[e] = INFINITY;
+    }
+    for (int cb0 = 0; cb0 * CS_KV_BLOCK <= last; cb0 += UC) {
+      cs::u32x4 v[UC][NL];
+#pragma unroll
+      for (int u = 0; u < UC; ++u) {
+        // (rows past the last one are that one again: it changes nothing)
+        const int cb = min((cb0 + u) * CS_KV_BLOCK, last) / CS_KV_BLOCK;
+        const int64_t at = static_cast<int64_t>(ids[begin / CS_KV_BLOCK + cb]) * CS_KV_BLOCK;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+          const int r = min((cb0 + u) * CS_KV_BLOCK + i * RL + row, last) - cb * CS_KV_BLOCK;
+          v[u][i] = *reinterpret_cast<const cs::u32x4*>(base + (at + r) * p.stride_slot);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < UC; ++u)
+#pragma unroll
+        for (int i = 0; i < NL; ++i)
+#pragma unroll
+          for (int e = 0; e < VE; ++e) {
+            const uint32_t w = v[u][i][kBf16 ? e / 2 : e];
+            const uint32_t bits = kBf16 ? (e & 1 ? w & 0xffff0000u : w << 16) : w;
+            amax = max(amax, bits & 0x7fffffffu);
+            hi[e] = fmaxf(hi[e], __uint_as_float(bits));
+            lo[e] = fminf(lo[e], __uint_as_float(bits));
+          }
+    }
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      if (LR <= 8) {
+        hi[e] = fmaxf(hi[e], __uint_as_float(cs::lane_dpp<0x128>(__float_as_uint(hi[e]))));      // lane ^ 8
+        lo[e] = fminf(lo[e], __uint_as_float(cs::lane_dpp<0x128>(__float_as_uint(lo[e]))));
+      }
+      if (LR <= 16) {
+        hi[e] = fmaxf(hi[e], cs::lane_xor16(hi[e]));
+        lo[e] = fminf(lo[e], cs::lane_xor16(lo[e]));
+      }
+      hi[e] = fmaxf(hi[e], cs::lane_xor32(hi[e]));
+      lo[e] = fminf(lo[e], cs::lane_xor32(lo[e]));
+    }
+    const uint32_t byte = scale_byte(cs::lanes_max<64>(amax));
+    const float inv = inverse_scale(byte == kNoNumber ? 127u : byte);
+    const int64_t at = (static_cast<int64_t>(stream) * p.n_kv_heads + kvh) * p.n_sel + b;
+    if (lane == 0) p.scales[at] = static_cast<uint8_t>(byte);
+    if (row > 1) continue;               // the first row of lanes writes the upper bounds, the second the lower ones
+    uint32_t word[VE / 4] = {};
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      // (a number that 2^-k takes below the smallest one still lies past 0)
+      const float x = row == 0 ? hi[e] : -lo[e];
+      int code = static_cast<int>(ceilf(x * inv));
+      if (x > 0.0f) code = max(code, 1);
+      if (row != 0) code = -code;
+      if (byte == kNoNumber) code = 0;
+      word[e / 4] |= (static_cast<uint32_t>(code) & 0xffu) << (8 * (e % 4));
+    }
+    int8_t* dst = p.bounds + at * 2 * D + row * D + c * VE;
+    if constexpr (VE == 8) *reinterpret_cast<cs::u32x2*>(dst) = cs::u32x2{word[0], word[1]};
+    else *reinterpret_cast<uint32_t*>(dst) = word[0];
+  }
+}
+
+// ------------------------------------------------------------------------------------------ choice
+
+struct SelectParams {
+  const void* __restrict__ q;
+  const int8_t* __restrict__ bounds;
+  const uint8_t* __restrict__ scales;
+  const int32_t* __restrict__ cu_q;
+  const int32_t* __restrict__ q_pos;
+  const int32_t* __restrict__ kv_len;
+  int32_t* __restrict__ selected;        // [n_q][n_kv_heads][n_select]
+  int64_t n_q;
+  int32_t max_blocks, n_streams, n_q_heads, n_kv_heads, group, n_sel, size, n_select, n_first, n_last, tile, pitch;
+};
+
+constexpr int kWaves = 4;
+constexpr int kMostBlocks = 32768;       // whose scores a workgroup holds in LDS for one token
+constexpr int kTileScores = 8192;        // ... for a tile of tokens
+
+// Scores in the order of unsigned numbers; every one is past 0.
+__device__ __forceinline__ uint32_t ordered(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+constexpr uint32_t kFixed = 0xffffffffu, kOdd = 0xfffffffeu;     // always kept, a block that holds what is no number
+
+// The query's list from the scores of its n blocks: `at(c)` is the lane's of chunk c, of 64 blocks.  C: chunks (at least n / 64), or 0: counted
+// when the kernel runs.  The threshold is found bit by bit, counting by ballots: the largest T with at least n_select scores >= T.
+template <int C, class F>
+__device__ __forceinline__ void write_list(const F& at, int n, int n_select, int32_t* out, int lane) {
+  const int chunks = C ? C : (n + 63) / 64;
+  uint32_t t = 0;
+  for (int bit = 31; bit >= 0; --bit) {
+    const uint32_t cand = t | 1u << bit;
+    int count = 0;
+#pragma unroll
+    for (int c = 0; c < chunks; ++c) count += __popcll(__ballot(at(c) >= cand));
+    if (count >= n_select) {
+      t = cand;
+      if (count == n_select) break;
+    }
+  }
+  int above = 0;
+#pragma unroll
+  for (int c = 0; c < chunks; ++c) above += __popcll(__ballot(at(c) > t));
+  int ties = n_select - above, place = 0;              // (more than n_select scores: the threshold is one of them)
+  const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+  for (int c = 0; c < chunks; ++c) {
+    const uint32_t x = at(c);
+    const uint64_t equal = __ballot(x == t);
+    const bool taken = x > t || (x == t && __popcll(equal & below) < ties);
+    const uint64_t all = __ballot(taken);
+    if (taken) out[place + __popcll(all & below)] = c * 64 + lane;
+    place += __popcll(all);
+    ties -= min(ties, __popcll(equal));
+  }
+}
+
+template <int C, class F>
+__device__ __forceinline__ void write_list_held(const F& key, int n, int n_select, int32_t* out, int lane) {
+  uint32_t held[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) held[c] = key(c * 64 + lane);
+  write_list<C>([&](int c) __attribute__((always_inline)) { return held[c]; }, n, n_select, out, lane);
+}
+
+// A workgroup takes a tile of a stream's tokens and a kv head.  Rows of the product are (token, head), the heads of a token padded to GP
+// by the last of them and spread so that they are neighbouring registers of a lane; columns are blocks, 32 at a time, the waves in turn.
+template <bool kBf16, int D, int GP>
+__global__ __launch_bounds__(64 * kWaves) void select_blocks_kernel(SelectParams p) {
+  constexpr int STEPS = 2 * D / 32;
+  constexpr int QROW = 2 * D + 16;
+  constexpr int TOK = 32 / GP;           // tokens that 32 rows hold
+  __shared__ __attribute__((aligned(16))) uint8_t s_q[32 * QROW];
+  extern __shared__ __attribute__((aligned(16))) uint32_t s_score[];      // [tile][pitch]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kvh = static_cast<int>(blockIdx.x % p.n_kv_heads);
+  cs::TokenTile t;
+  if (!cs::find_token_tile(p.cu_q, p.n_streams, p.n_q, p.tile, static_cast<int>(blockIdx.x / p.n_kv_heads), &t)) return;
+  const int entries = min(p.kv_len[t.stream], p.max_blocks * CS_KV_BLOCK);
+  const auto candidates = [&](int i) __attribute__((always_inline)) {
+    const int last = min(p.q_pos[t.first + i], entries - 1);
+    return last < 0 ? 0 : last / p.size + 1;
+  };
+
+  // ---- whole numbers of the tile's queries: a wave takes a token, 16 bytes a lane
+  for (int i = tid; i < 32 * QROW / 16; i += 64 * kWaves) reinterpret_cast<cs::u32x4*>(s_q)[i] = cs::u32x4{0, 0, 0, 0};
+  __syncthreads();
+  int most = 0;                          // candidates of any of the tokens
+  for (int i = 0; i < t.count; ++i) most = max(most, candidates(i));
+  for (int i = wave; i < t.count; i += kWaves) {
+    constexpr int VE = kBf16 ? 8 : 4;
+    const int chunks = p.group * (D / VE);
+    const int64_t from = (static_cast<int64_t>(t.first + i) * p.n_q_heads + static_cast<int64_t>(kvh) * p.group) * D;
+    uint32_t amax = 0;
+    for (int c = lane; c < chunks; c += 64) {
+      cs::u32x4 v;
+      if constexpr (kBf16) v = *reinterpret_cast<const cs::u32x4*>(static_cast<const uint16_t*>(p.q) + from + c * VE);
+      else v = *reinterpret_cast<const cs::u32x4*>(static_cast<const float*>(p.q) + from + c * VE);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        const uint32_t w = v[kBf16 ? e / 2 : e];
+        amax = max(amax, (kBf16 ? (e & 1 ? w & 0xffff0000u : w << 16) : w) & 0x7fffffffu);
+      }
+    }
+    const uint32_t byte = scale_byte(cs::lanes_max<64>(amax));
+    if (byte == kNoNumber) continue;     // (its rows stay 0)
+    const float inv = inverse_scale(byte);
+    for (int c = lane; c < GP * (D / VE); c += 64) {
+      const int slot = c / (D / VE), head = min(slot, p.group - 1), col = c % (D / VE) * VE;
+      cs::u32x4 v;
+      if constexpr (kBf16) v = *reinterpret_cast<const cs::u32x4*>(static_cast<const uint16_t*>(p.q) + from + head * D + col);
+      else v = *reinterpret_cast<const cs::u32x4*>(static_cast<const float*>(p.q) + from + head * D + col);
+      uint32_t up[VE / 4] = {}, down[VE / 4] = {};
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        const uint32_t w = v[kBf16 ? e / 2 : e];
+        const int code = static_cast<int>(rintf(__uint_as_float(kBf16 ? (e & 1 ? w & 0xffff0000u : w << 16) : w) * inv));
+        up[e / 4] |= static_cast<uint32_t>(max(code, 0)) << (8 * (e % 4));
+        down[e / 4] |= (static_cast<uint32_t>(min(code, 0)) & 0xffu) << (8 * (e % 4));
+      }
+      // token i is pair i / 2 of half i % 2: registers GP (i / 2) + slot of the lanes of that half, rows 8 (r / 4) + 4 half + r % 4
+      const int r = GP * (i / 2) + slot, row = 8 * (r / 4) + 4 * (i % 2) + r % 4;
+      uint8_t* dst = s_q + row * QROW + col;
+      if constexpr (VE == 8) {
+        *reinterpret_cast<cs::u32x2*>(dst) = cs::u32x2{up[0], up[1]};
+        *reinterpret_cast<cs::u32x2*>(dst + D) = cs::u32x2{down[0], down[1]};
+      } else {
+        *reinterpret_cast<uint32_t*>(dst) = up[0];
+        *reinterpret_cast<uint32_t*>(dst + D) = down[0];
+      }
+    }
+  }
+  __syncthreads();
+
+  // ---- scores
+  if (most > p.n_select) {
+    const int n = lane & 31, h = lane >> 5;
+    i32x4 a[STEPS];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) a[s] = *reinterpret_cast<const i32x4*>(s_q + n * QROW + 32 * s + 16 * h);
+    const int64_t head_at = (static_cast<int64_t>(t.stream) * p.n_kv_heads + kvh) * p.n_sel;
+    for (int b0 = wave * 32; b0 < most; b0 += 32 * kWaves) {
+      const int block = min(b0 + n, most - 1);
+      const int8_t* from = p.bounds + (head_at + block) * 2 * D + 16 * h;
+      const uint32_t byte = p.scales[head_at + block];
+      i32x4 b[STEPS];
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) b[s] = *reinterpret_cast<const i32x4*>(from + 32 * s);
+      i32x16 acc = {};
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[s], b[s], acc, 0, 0, 0);
+      const float scale = __uint_as_float((byte - 21u) << 23);           // 2^(k - 21)
+      if (b0 + n < most) {
+#pragma unroll
+        for (int g = 0; g < 16 / GP; ++g) {
+          int top = acc[g * GP];
+#pragma unroll
+          for (int i = 1; i < GP; ++i) top = max(top, acc[g * GP + i]);
+          const int tok = 2 * g + h;
+          if (tok < t.count) s_score[tok * p.pitch + block] = byte == kNoNumber ? kOdd : ordered(static_cast<float>(top) * scale);
+        }
+      }
+    }
+  }
+  __syncthreads();
+
+  // ---- lists: a wave takes a token
+  for (int i = wave; i < t.count; i += kWaves) {
+    const int n = candidates(i);
+    int32_t* out = p.selected + (static_cast<int64_t>(t.first + i) * p.n_kv_heads + kvh) * p.n_select;
+    if (n <= p.n_select) {
+      for (int c = lane; c < p.n_select; c += 64) out[c] = c < n ? c : -1;
+      continue;
+    }
+    const uint32_t* score = s_score + i * p.pitch;
+    const auto key = [&](int b) __attribute__((always_inline)) -> uint32_t {
+      if (b >= n) return 0u;
+      return b < p.n_first || b >= n - p.n_last ? kFixed : score[b];
+    };
+    if (n <= 256) write_list_held<4>(key, n, p.n_select, out, lane);
+    else if (n <= 512) write_list_held<8>(key, n, p.n_select, out, lane);
+    else write_list<0>([&](int c) __attribute__((always_inline)) { return key(c * 64 + lane); }, n, p.n_select, out, lane);
+  }
+}
+
+}  // namespace
+
+extern "C" int cs_key_bounds(const void* k_cache_layer, const int32_t* from, const int32_t* kv_len, const int32_t* block_table,
+                             int32_t max_blocks, int32_t block_size, int32_t sel_block, int8_t* bounds, uint8_t* scales,
+                             int32_t n_streams, int32_t n_kv_heads, int32_t head_dim, int64_t stride_slot, int64_t stride_head,
+                             int32_t dtype, void* stream) {
+  if (n_streams < 0 || n_kv_heads < 1 || max_blocks < 1 || sel_block < 1 || stride_slot < 0 || stride_head < 0) return CS_EINVAL;
+  if (dtype != CS_F32 && dtype != CS_BF16) return CS_EUNSUPPORTED;
+  if ((head_dim != 64 && head_dim != 128) || block_size != CS_KV_BLOCK) return CS_EUNSUPPORTED;
+  if (sel_block % CS_KV_BLOCK || sel_block > CS_SELECT_BLOCK_MOST || n_kv_heads > 65535 || max_blocks > (1 << 27) - 65) return CS_EUNSUPPORTED;
+  const int elems = dtype == CS_BF16 ? 8 : 4;
+  if (stride_slot % elems || stride_head % elems) return CS_EUNSUPPORTED;
+  if (n_streams == 0) return CS_OK;
+  if (!k_cache_layer || !kv_len || !block_table || !bounds || !scales) return CS_EINVAL;
+  if (!cs::aligned16(k_cache_layer) || !cs::aligned16(bounds)) return CS_EUNSUPPORTED;
+  BoundsParams p;
+  p.k = k_cache_layer;
+  p.from = from;
+  p.kv_len = kv_len;
+  p.block_table = block_table;
+  p.bounds = bounds;
+  p.scales = scales;
+  p.stride_slot = stride_slot;
+  p.stride_head = stride_head;
+  p.max_blocks = max_blocks;
+  p.n_streams = n_streams;
+  p.n_kv_heads = n_kv_heads;
+  p.cache_blocks = sel_block / CS_KV_BLOCK;
+  p.n_sel = (max_blocks + p.cache_blocks - 1) / p.cache_blocks;
+  const int64_t pairs = static_cast<int64_t>(n_streams) * n_kv_heads;
+  const int64_t wanted = (16384 + pairs - 1) / pairs;
+  p.walkers = static_cast<int32_t>(wanted < p.n_sel ? wanted : p.n_sel);
+  const int64_t groups = (pairs * p.walkers + 3) / 4;
+  if (groups > cs::kMostThreads / 256) return CS_EUNSUPPORTED;
+  const dim3 grid(static_cast<unsigned>(groups));
+  hipStream_t st = cs::as_stream(stream);
+#define CS_LAUNCH_BOUNDS(BF16, D)                                                                                           \
+  do {                                                                                                                      \
+    if (p.cache_blocks == 1) hipLaunchKernelGGL((key_bounds_kernel<BF16, D, 1>), grid, dim3(256), 0, st, p);                \
+    else if (p.cache_blocks == 2) hipLaunchKernelGGL((key_bounds_kernel<BF16, D, 2>), grid, dim3(256), 0, st, p);           \
+    else hipLaunchKernelGGL((key_bounds_kernel<BF16, D, 4>), grid, dim3(256), 0, st, p);                                    \
+  } while (0)
+  if (dtype == CS_BF16) {
+    if (head_dim == 128) CS_LAUNCH_BOUNDS(true, 128);
+    else CS_LAUNCH_BOUNDS(true, 64);
+  } else {
+    if (head_dim == 128) CS_LAUNCH_BOUNDS(false, 128);
+    else CS_LAUNCH_BOUNDS(false, 64);
+  }
+#undef CS_LAUNCH_BOUNDS
+  return cs::note_hip(hipGetLastError());
+}
+
+extern "C" size_t cs_select_blocks_workspace(int64_t, int32_t, int32_t, int32_t, int32_t, int32_t, int32_t) { return 0; }
+
+extern "C" int cs_select_blocks(const void* q, const int8_t* bounds, const uint8_t* scales, const int32_t* cu_q, const int32_t* q_pos,
+                                const int32_t* kv_len, int32_t max_blocks, int32_t sel_block, int32_t n_select, int32_t n_first,
+                                int32_t n_last, int32_t* selected, int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads,
+                                int32_t head_dim, int32_t dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  (void)workspace;
+  (void)workspace_bytes;
+  if (n_q < 0 || n_streams < 0 || n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % n_kv_heads || max_blocks < 1 || sel_block < 1) return CS_EINVAL;
+  if (n_select < 1 || n_first < 0 || n_last < 0 || static_cast<int64_t>(n_first) + n_last > n_select) return CS_EINVAL;
+  if (dtype != CS_F32 && dtype != CS_BF16) return CS_EUNSUPPORTED;
+  if ((head_dim != 64 && head_dim != 128) || n_q_heads / n_kv_heads > 16) return CS_EUNSUPPORTED;
+  if (sel_block % CS_KV_BLOCK || sel_block > CS_SELECT_BLOCK_MOST || n_kv_heads > 65535 || max_blocks > (1 << 27) - 65) return CS_EUNSUPPORTED;
+  if (n_select > CS_SELECT_MOST || n_q >= 1ll << 26) return CS_EUNSUPPORTED;
+  const int32_t per = sel_block / CS_KV_BLOCK, n_sel = (max_blocks + per - 1) / per;
+  if (n_sel > kMostBlocks) return CS_EUNSUPPORTED;
+  if (n_q == 0 || n_streams == 0) return CS_OK;
+  if (!q || !bounds || !scales || !cu_q || !q_pos || !kv_len || !selected) return CS_EINVAL;
+  if (!cs::aligned16(q) || !cs::aligned16(bounds)) return CS_EUNSUPPORTED;
+  SelectParams p;
+  p.q = q;
+  p.bounds = bounds;
+  p.scales = scales;
+  p.cu_q = cu_q;
+  p.q_pos = q_pos;
+  p.kv_len = kv_len;
+  p.selected = selected;
+  p.n_q = n_q;
+  p.max_blocks = max_blocks;
+  p.n_streams = n_streams;
+  p.n_q_heads = n_q_heads;
+  p.n_kv_heads = n_kv_heads;
+  p.group = n_q_heads / n_kv_heads;
+  p.n_sel = n_sel;
+  p.size = sel_block;
+  p.n_select = n_select;
+  p.n_first = n_first;
+  p.n_last = n_last;
+  int gp = 1;
+  while (gp < p.group) gp *= 2;
+  p.pitch = n_sel;
+  p.tile = 32 / gp < 8 ? 32 / gp : 8;
+  while (p.tile > 1 && static_cast<int64_t>(p.tile) * p.pitch > kTileScores) p.tile /= 2;
+  const int64_t tiles = cs::most_token_tiles(n_q, n_streams, p.tile), groups = tiles * n_kv_heads;
+  if (groups > cs::kMostThreads / (64 * kWaves)) return CS_EUNSUPPORTED;
+  const dim3 grid(static_cast<unsigned>(groups));
+  const size_t lds = static_cast<size_t>(p.tile) * p.pitch * sizeof(uint32_t);
+  hipStream_t st = cs::as_stream(stream);
+#define CS_LAUNCH_SELECT(BF16, D, GP)                                                                                                       \
+  do {                                                                                                                                     \
+    if (lds > 48 * 1024) {                                                                                                                 \
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(select_blocks_kernel<BF16, D, GP>),                           \
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));                         \
+      if (e != hipSuccess) return cs::note_hip(e);                                                                                         \
+    }                                                                                                                                      \
+    hipLaunchKernelGGL((select_blocks_kernel<BF16, D, GP>), grid, dim3(64 * kWaves), lds, st, p);                                          \
+  } while (0)
+#define CS_LAUNCH_SELECT_GROUP(BF16, D)              \
+  do {                                               \
+    if (gp == 1) CS_LAUNCH_SELECT(BF16, D, 1);       \
+    else if (gp == 2) CS_LAUNCH_SELECT(BF16, D, 2);  \
+    else if (gp == 4) CS_LAUNCH_SELECT(BF16, D, 4);  \
+    else if (gp == 8) CS_LAUNCH_SELECT(BF16, D, 8);  \
+    else CS_LAUNCH_SELECT(BF16, D, 16);              \
+  } while (0)
+  if (dtype == CS_BF16) {
+    if (head_dim == 128) CS_LAUNCH_SELECT_GROUP(true, 128);
+    else CS_LAUNCH_SELECT_GROUP(true, 64);
+  } else {
+    if (head_dim == 128) CS_LAUNCH_SELECT_GROUP(false, 128);
+    else CS_LAUNCH_SELECT_GROUP(false, 64);
+  }
+#undef CS_LAUNCH_SELECT_GROUP
+#undef CS_LAUNCH_SELECT
+  return cs::note_hip(hipGetLastError());
+}

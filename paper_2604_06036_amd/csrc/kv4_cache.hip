@@ -9,8 +9,11 @@
 
 #include "kv4.h"
 #include "rope.h"
+#include "vec8.h"
 
 namespace {
+
+using cs::Eight;
 
 constexpr int kPairs = 8;                // pairs a lane owns
 // Workgroups wanted of the rotary write.  22,804 tokens of 32 + 2 x 8 heads of 128 take 112 us, 4.4 TB/s (a large copy reaches 4.1 to
@@ -19,49 +22,6 @@ constexpr int kPairs = 8;                // pairs a lane owns
 // of 28 + 2 x 4 heads 27.6 -> 19.2 us with the rows read back, 7,000 39.4 -> 35.8 (six heads: 20.4 and 37.0; four workgroups a CU: 20.9, 35.5).
 // A token alone is 5 us, and 13 to 18 from the host with its row read back.
 constexpr int kRopeGroups = 4096, kRopeHeads = 4, kRopeEnough = 512;
-
-template <bool kBf16>
-struct Eight;
-template <>
-struct Eight<true> {                     // eight bf16: one 16-byte vector
-  cs::u32x4 v;
-  __device__ __forceinline__ void load(const uint16_t* p) { v = __builtin_nontemporal_load(reinterpret_cast<const cs::u32x4*>(p)); }
-  __device__ __forceinline__ void get(float* f) const {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[2 * i] = __uint_as_float(w[i] << 16);
-      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  }
-  static __device__ __forceinline__ void store(uint16_t* p, const float* f) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const cs::f32v2 x = {f[2 * i], f[2 * i + 1]};
-      w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, cs::bf16v2));
-    }
-    __builtin_nontemporal_store(cs::u32x4{w[0], w[1], w[2], w[3]}, reinterpret_cast<cs::u32x4*>(p));
-  }
-};
-template <>
-struct Eight<false> {
-  cs::u32x4 v, w;
-  __device__ __forceinline__ void load(const float* p) {
-    v = __builtin_nontemporal_load(reinterpret_cast<const cs::u32x4*>(p));
-    w = __builtin_nontemporal_load(reinterpret_cast<const cs::u32x4*>(p + 4));
-  }
-  __device__ __forceinline__ void get(float* f) const {
-    f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
-    f[4] = __uint_as_float(w.x); f[5] = __uint_as_float(w.y); f[6] = __uint_as_float(w.z); f[7] = __uint_as_float(w.w);
-  }
-  static __device__ __forceinline__ void store(float* p, const float* f) {
-    __builtin_nontemporal_store(cs::u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])},
-                                reinterpret_cast<cs::u32x4*>(p));
-    __builtin_nontemporal_store(cs::u32x4{__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])},
-                                reinterpret_cast<cs::u32x4*>(p + 4));
-  }
-};
 
 // Largest of the lanes of a quad (kLanes 4) or of a pair (2).
 template <int kLanes>

@@ -19,6 +19,9 @@
 // Multidimensional RoPE (Sec. 3.4.2: each rotary dimension is corrected by the positional
 // component the model maps to it): a row's shift is a triple (d_t, d_h, d_w) and frequency pair i
 // is driven by component axis_of_pair[i]; everything else is the same kernel (template flag).
+//
+// Frequencies from a table (template flag): pair i of the first rotary_dim elements of a head turns by the caller's inv_freq[i]; the
+// elements behind them carry no position, and are copied when repacking.
 #include <math.h>
 
 #include "common.h"
@@ -42,6 +45,8 @@ struct RerotateParams {
   int32_t units_per_head;
   int32_t layers_per_block;
   double neg_log2_base_2_over_d;         // -2 log2(base) / head_dim:  theta_i = 2^(i * this)
+  const float* __restrict__ inv_freq;    // [rotary_dim / 2], table kernels only
+  int32_t rotary_dim;                    // ... head_dim without a table
 };
 
 template <bool kBf16>
@@ -97,7 +102,7 @@ __device__ __forceinline__ void sincos_reduced(double ang, float* sn, float* cs_
   *cs_out = ((quad + 1) & 2) ? -c_q : c_q;
 }
 
-template <bool kBf16, int kStyle, bool kAxes>
+template <bool kBf16, int kStyle, bool kAxes, bool kTable>
 __global__ __launch_bounds__(256) void rerotate_kernel(RerotateParams p) {
   using V = Vec<kBf16>;
   constexpr int E = V::kElems;           // pairs per thread = elements per vector
@@ -109,11 +114,13 @@ __global__ __launch_bounds__(256) void rerotate_kernel(RerotateParams p) {
   const int rem = static_cast<int>(unit - row * p.units_per_row);
   const int head = rem / p.units_per_head;
   const int j = rem - head * p.units_per_head;          // which group of E pairs inside the head
-  const int half = p.head_dim / 2;
+  const int half = (kTable ? p.rotary_dim : p.head_dim) / 2;
+  const bool still = kTable && j * E >= half;           // elements behind the rotated ones
 
   const int src = p.src_slot[row];
   const int dst = p.dst_slot ? p.dst_slot[row] : src;
   if (src < 0 || dst < 0) return;        // padding rows of a list sized to its capacity
+  if (still && !p.dst_slot) return;
   double dlt[3];
   if (kAxes) {
     dlt[0] = static_cast<double>(p.delta[row * 3]);
@@ -126,9 +133,10 @@ __global__ __launch_bounds__(256) void rerotate_kernel(RerotateParams p) {
   float cs_[E], sn_[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    const double theta = exp2(static_cast<double>(j * E + e) * p.neg_log2_base_2_over_d);
+    const double theta = kTable ? (still ? 0.0 : static_cast<double>(p.inv_freq[j * E + e]))
+                                : exp2(static_cast<double>(j * E + e) * p.neg_log2_base_2_over_d);
     double shift = dlt[0];
-    if (kAxes) {
+    if (kAxes && !still) {
       const int axis = p.axis_of_pair[j * E + e];
       shift = axis == 0 ? dlt[0] : axis == 1 ? dlt[1] : dlt[2];
     }
@@ -136,8 +144,9 @@ __global__ __launch_bounds__(256) void rerotate_kernel(RerotateParams p) {
   }
 
   // element offsets of the thread's two vectors inside a head
-  const int off_a = kStyle == CS_ROPE_HALF_SPLIT ? j * E : 2 * j * E;
-  const int off_b = kStyle == CS_ROPE_HALF_SPLIT ? half + j * E : 2 * j * E + E;
+  const bool apart = kStyle == CS_ROPE_HALF_SPLIT && !still;
+  const int off_a = apart ? j * E : 2 * j * E;
+  const int off_b = apart ? half + j * E : 2 * j * E + E;
   const int64_t src_off = static_cast<int64_t>(src) * p.stride_slot + head * p.stride_head;
   const int64_t dst_off = static_cast<int64_t>(dst) * p.stride_slot + head * p.stride_head;
   const bool repack = p.dst_slot != nullptr;
@@ -189,6 +198,10 @@ __global__ __launch_bounds__(256) void rerotate_kernel(RerotateParams p) {
         V oa, ob;
         oa.pack(ya);
         ob.pack(yb);
+        if (still) {                     // (bit for bit; a sine of 0 would carry what is no number into the partner)
+          oa.raw = ka[i];
+          ob.raw = kb[i];
+        }
         const int64_t lo = static_cast<int64_t>(l0 + i) * p.stride_layer + dst_off;
         __builtin_nontemporal_store(oa.raw, reinterpret_cast<cs::u32x4*>(kbase + lo + off_a));
         __builtin_nontemporal_store(ob.raw, reinterpret_cast<cs::u32x4*>(kbase + lo + off_b));
@@ -251,10 +264,11 @@ __global__ __launch_bounds__(256) void scatter_kernel(ScatterParams p) {
 
 namespace {
 
-// delta: [n_rows] shifts, or with axis_of_pair [n_rows][3] shifts per positional component.
+// delta: [n_rows] shifts, or with axis_of_pair [n_rows][3] shifts per positional component.  inv_freq: frequencies of the first
+// rotary_dim elements' pairs, or nullptr: powers of rope_base, rotary_dim == head_dim.
 int rerotate_launch(void* k_cache, void* v_cache, const int32_t* src_slot, const int32_t* dst_slot,
-                    const int32_t* delta, const uint8_t* axis_of_pair, int64_t n_rows, int32_t n_layers,
-                    int32_t n_kv_heads, int32_t head_dim, int64_t stride_layer, int64_t stride_slot,
+                    const int32_t* delta, const uint8_t* axis_of_pair, const float* inv_freq, int64_t n_rows, int32_t n_layers,
+                    int32_t n_kv_heads, int32_t head_dim, int32_t rotary_dim, int64_t stride_layer, int64_t stride_slot,
                     int64_t stride_head, float rope_base, int32_t rope_style, int32_t dtype, void* stream) {
   if (n_rows < 0 || n_layers < 0 || n_kv_heads < 1 || head_dim < 1) return CS_EINVAL;
   if (stride_layer < 0 || stride_slot < 0 || stride_head < 0) return CS_EINVAL;
@@ -286,9 +300,12 @@ int rerotate_launch(void* k_cache, void* v_cache, const int32_t* src_slot, const
   p.head_dim = head_dim;
   p.style = rope_style;
   p.neg_log2_base_2_over_d = -2.0 * log2(static_cast<double>(rope_base)) / head_dim;
+  p.inv_freq = inv_freq;
+  p.rotary_dim = rotary_dim;
   p.units_per_head = half / elems;
   p.units_per_row = n_kv_heads * p.units_per_head;
 
+  if (inv_freq && n_rows > 0xffffff00ll / p.units_per_row) return CS_EUNSUPPORTED;       // (threads along an axis of a grid)
   const int64_t n_units = n_rows * p.units_per_row;
   const int64_t blocks_x = (n_units + 255) / 256;
   if (blocks_x > 0x7fffffffll) return CS_EUNSUPPORTED;
@@ -302,19 +319,25 @@ int rerotate_launch(void* k_cache, void* v_cache, const int32_t* src_slot, const
   hipStream_t st = cs::as_stream(stream);
   const bool half_split = rope_style == CS_ROPE_HALF_SPLIT;
   const bool bf16 = dtype == CS_BF16;
-#define CS_LAUNCH_REROTATE(AXES)                                                                             \
+#define CS_LAUNCH_REROTATE(AXES, TABLE)                                                                      \
   do {                                                                                                       \
     if (bf16 && half_split)                                                                                  \
-      hipLaunchKernelGGL((rerotate_kernel<true, CS_ROPE_HALF_SPLIT, AXES>), grid, dim3(256), 0, st, p);      \
+      hipLaunchKernelGGL((rerotate_kernel<true, CS_ROPE_HALF_SPLIT, AXES, TABLE>), grid, dim3(256), 0, st, p);   \
     else if (bf16)                                                                                           \
-      hipLaunchKernelGGL((rerotate_kernel<true, CS_ROPE_INTERLEAVED, AXES>), grid, dim3(256), 0, st, p);     \
+      hipLaunchKernelGGL((rerotate_kernel<true, CS_ROPE_INTERLEAVED, AXES, TABLE>), grid, dim3(256), 0, st, p);  \
     else if (half_split)                                                                                     \
-      hipLaunchKernelGGL((rerotate_kernel<false, CS_ROPE_HALF_SPLIT, AXES>), grid, dim3(256), 0, st, p);     \
+      hipLaunchKernelGGL((rerotate_kernel<false, CS_ROPE_HALF_SPLIT, AXES, TABLE>), grid, dim3(256), 0, st, p);  \
     else                                                                                                     \
-      hipLaunchKernelGGL((rerotate_kernel<false, CS_ROPE_INTERLEAVED, AXES>), grid, dim3(256), 0, st, p);    \
+      hipLaunchKernelGGL((rerotate_kernel<false, CS_ROPE_INTERLEAVED, AXES, TABLE>), grid, dim3(256), 0, st, p); \
   } while (0)
-  if (axis_of_pair) CS_LAUNCH_REROTATE(true);
-  else CS_LAUNCH_REROTATE(false);
+  if (inv_freq) {
+    if (axis_of_pair) CS_LAUNCH_REROTATE(true, true);
+    else CS_LAUNCH_REROTATE(false, true);
+  } else if (axis_of_pair) {
+    CS_LAUNCH_REROTATE(true, false);
+  } else {
+    CS_LAUNCH_REROTATE(false, false);
+  }
 #undef CS_LAUNCH_REROTATE
   return cs::note_hip(hipGetLastError());
 }
@@ -326,8 +349,8 @@ extern "C" int cs_kv_rerotate(void* k_cache, void* v_cache, const int32_t* src_s
                               int32_t n_layers, int32_t n_kv_heads, int32_t head_dim,
                               int64_t stride_layer, int64_t stride_slot, int64_t stride_head,
                               float rope_base, int32_t rope_style, int32_t dtype, void* stream) {
-  return rerotate_launch(k_cache, v_cache, src_slot, dst_slot, delta, nullptr, n_rows, n_layers, n_kv_heads,
-                         head_dim, stride_layer, stride_slot, stride_head, rope_base, rope_style, dtype, stream);
+  return rerotate_launch(k_cache, v_cache, src_slot, dst_slot, delta, nullptr, nullptr, n_rows, n_layers, n_kv_heads,
+                         head_dim, head_dim, stride_layer, stride_slot, stride_head, rope_base, rope_style, dtype, stream);
 }
 
 extern "C" int cs_kv_rerotate_axes(void* k_cache, void* v_cache, const int32_t* src_slot,
@@ -337,8 +360,21 @@ extern "C" int cs_kv_rerotate_axes(void* k_cache, void* v_cache, const int32_t* 
                                    int64_t stride_slot, int64_t stride_head, float rope_base,
                                    int32_t rope_style, int32_t dtype, void* stream) {
   if (n_rows > 0 && n_layers > 0 && !axis_of_pair) return CS_EINVAL;
-  return rerotate_launch(k_cache, v_cache, src_slot, dst_slot, delta3, axis_of_pair, n_rows, n_layers,
-                         n_kv_heads, head_dim, stride_layer, stride_slot, stride_head, rope_base, rope_style,
+  return rerotate_launch(k_cache, v_cache, src_slot, dst_slot, delta3, axis_of_pair, nullptr, n_rows, n_layers,
+                         n_kv_heads, head_dim, head_dim, stride_layer, stride_slot, stride_head, rope_base, rope_style,
+                         dtype, stream);
+}
+
+extern "C" int cs_kv_rerotate_freqs(void* k_cache, void* v_cache, const int32_t* src_slot,
+                                    const int32_t* dst_slot, const int32_t* delta, const uint8_t* axis_of_pair,
+                                    const float* inv_freq, int64_t n_rows, int32_t n_layers, int32_t n_kv_heads,
+                                    int32_t head_dim, int32_t rotary_dim, int64_t stride_layer, int64_t stride_slot,
+                                    int64_t stride_head, int32_t rope_style, int32_t dtype, void* stream) {
+  if (rotary_dim < 16 || rotary_dim > head_dim) return CS_EINVAL;
+  if (rotary_dim % 16 != 0 || n_kv_heads > 65535) return CS_EUNSUPPORTED;
+  if (n_rows > 0 && n_layers > 0 && !inv_freq) return CS_EINVAL;
+  return rerotate_launch(k_cache, v_cache, src_slot, dst_slot, delta, axis_of_pair, inv_freq, n_rows, n_layers,
+                         n_kv_heads, head_dim, rotary_dim, stride_layer, stride_slot, stride_head, 1.0f, rope_style,
                          dtype, stream);
 }
 

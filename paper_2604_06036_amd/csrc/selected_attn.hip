@@ -1,0 +1,609 @@
+// Attention over the blocks that were selected for each query, paged 16-bit or fp32 cache, gfx950: single tokens, questions, windows.
+//
+//     out[t][h] = sum_j softmax_j(scale q[t][h] . K_j) V_j    over the entries j <= q_pos[t] of the blocks listed for (t, kv head of h)
+//
+// A row is one (query token, query head of the kv group) pair; 16 rows are a tile: as many tokens of a stream as fit, T = 16 / group (one
+// token where its heads fill the tile).  A workgroup takes a tile and a kv head, or a piece of its sweep:
+//   lists      the tokens' lists become one ascending list of different blocks, each with a mask of the tokens that read it: every
+//              element counts the ones before it (at most 256 of them, in LDS), so the caller's order does not matter and an
+//              index that stands twice counts once
+//   S^T        = K Q^T over 16 keys (bf16: v_mfma_f32_16x16x32_bf16, fp32: v_mfma_f32_16x16x4_f32), keys straight from memory in operand
+//              layout; a lane owns one row and 4 keys
+//   softmax    one pass, running maximum and sum in fp32; the reference maximum is raised when a tile exceeds it by more than 2^8.
+//              bf16: weights are rounded to bf16, which the products take (half a step is 2^-8 of a weight); their sum is not
+//   O^T       += V^T P^T; P^T is in operand layout as it is.  bf16 values pass through a wave's own part of LDS, whose transposing read
+//              gives the operand; fp32 values come from memory in operand layout
+// The waves of a workgroup take key tiles in turn and join their results at the end; pieces are joined by a second launch.
+//
+// Entries that a query does not see have weight 0, and values there may be anything: addresses stop at the last entry that a token of the
+// tile sees, and where a sum comes out as no number or infinite, the sweep is done again token by token with the values that the token
+// does not see as 0.
+#include <math.h>
+
+#include <type_traits>
+
+#include "kv4.h"
+#include "token_tiles.h"
+
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+struct Params {
+  const void* __restrict__ q;
+  const void* __restrict__ k;
+  const void* __restrict__ v;
+  const int32_t* __restrict__ cu_q;
+  const int32_t* __restrict__ q_pos;
+  const int32_t* __restrict__ kv_len;
+  const int32_t* __restrict__ block_table;
+  const int32_t* __restrict__ selected;  // [n_q][n_kv_heads][n_select]
+  void* __restrict__ out;
+  float* __restrict__ lse;
+  float* __restrict__ ws_ml;             // [tile][kv head][piece][16][2]: reference maximum (raw score), sum
+  float* __restrict__ ws_o;              // [tile][kv head][piece][16][D]: sums, not divided
+  int64_t n_q, stride_slot, stride_head;
+  int32_t max_blocks, n_streams, n_q_heads, n_kv_heads, group, tile, n_select, cache_blocks, pieces;
+  float scale_log2e;
+};
+
+constexpr int kRows = 16;
+constexpr int kMostListed = 256;         // list elements of a tile
+constexpr float kSlack = 8.0f;           // log2 of how far weights may exceed the reference maximum's
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  const cs::f32v2 v = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, cs::bf16v2));
+}
+
+__device__ __forceinline__ void store4(void* out, int64_t at, const float* x, bool bf16) {
+  if (bf16)
+    *reinterpret_cast<cs::u32x2*>(static_cast<uint16_t*>(out) + at) = cs::u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])};
+  else
+    *reinterpret_cast<cs::u32x4*>(static_cast<float*>(out) + at) =
+        cs::u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+}
+
+__device__ __forceinline__ float log_sum(float m, float l, float c) { return l == 0.0f ? -INFINITY : (m * c + __builtin_amdgcn_logf(l)) * kLn2; }
+
+// ---- where the 16 keys of a group lie
+struct Group {
+  int first;                             // first entry
+  int mask;                              // tokens that read it (0: past the list)
+  int64_t at;                            // element offset of row 0 of its cache block, kv head included
+  int top;                               // rows from here on are row `top`: past the last entry that is seen
+};
+
+// Sixteen rows' sums, and what a lane's row has seen: o holds channels as the kind of cache has them.
+template <int D>
+struct Sums {
+  f32x4 o[D / 16];
+  float m, l;
+};
+
+// ---- bf16: 64 keys a step
+template <int D>
+struct Bf16 {
+  static constexpr bool kBf16 = true;
+  static constexpr int KB = 4;           // groups a step
+  static constexpr int VROW = D + 16;    // of LDS: the transposing reads of 16 rows spread over the banks
+  static constexpr int kLds = KB * 16 * VROW * 2;      // bytes a wave
+  bf16x8 query[D / 32];
+
+  __device__ __forceinline__ void load_query(const void* q, int64_t row, int g) {
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) query[s] = *reinterpret_cast<const bf16x8*>(static_cast<const uint16_t*>(q) + row + 32 * s + 8 * g);
+  }
+
+  struct Tile {
+    bf16x8 k[KB][D / 32];
+    cs::u32x4 v[KB][D / 32];
+  };
+
+  __device__ __forceinline__ void load(const Params& p, const Group (&gr)[KB], Tile& t, int lane) const {
+    const int r16 = lane & 15, g = lane >> 4;
+    constexpr int LR = D / 8;            // lanes of a row of values
+    constexpr int RL = 64 / LR;
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+      const uint16_t* k = static_cast<const uint16_t*>(p.k) + gr[b].at + static_cast<int64_t>(min(r16, gr[b].top)) * p.stride_slot + 8 * g;
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) t.k[b][s] = *reinterpret_cast<const bf16x8*>(k + 32 * s);
+    }
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        const int r = i * RL + lane / LR;
+        t.v[b][i] = *reinterpret_cast<const cs::u32x4*>(static_cast<const uint16_t*>(p.v) + gr[b].at +
+                                                        static_cast<int64_t>(min(r, gr[b].top)) * p.stride_slot + lane % LR * 8);
+      }
+    }
+  }
+
+  __device__ __forceinline__ void scores(const Tile& t, f32x4 (&s)[KB]) const {
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+      s[b] = f32x4{};
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(t.k[b][i], query[i], s[b], 0, 0, 0);
+    }
+  }
+
+  // only: the token whose unseen values are taken as 0 (limit[b]: its last entry in group b), or nobody's
+  __device__ __forceinline__ void add(const Tile& t, const Group (&gr)[KB], const f32x4 (&w)[KB], Sums<D>& sums, uint8_t* lds, int lane, bool careful,
+                                      const int (&limit)[KB]) const {
+    constexpr int LR = D / 8, RL = 64 / LR;
+    const int r16 = lane & 15, g = lane >> 4;
+    uint16_t* v = reinterpret_cast<uint16_t*>(lds);
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        const int r = i * RL + lane / LR;
+        cs::u32x4 x = t.v[b][i];
+        if (careful && gr[b].first + r > limit[b]) x = cs::u32x4{0, 0, 0, 0};
+        *reinterpret_cast<cs::u32x4*>(v + (16 * b + r) * VROW + lane % LR * 8) = x;
+      }
+    // Of the 32 keys of a product a lane's weights are of 4 g + 0..3 of two groups; the transposing read gives 16 lanes four rows of
+    // 16 elements.
+    const uint16_t* at = v + (4 * g + (r16 >> 2)) * VROW + 4 * (r16 & 3);
+#pragma unroll
+    for (int st = 0; st < KB / 2; ++st) {
+      const cs::u32x4 pw = {pack2(w[2 * st][0], w[2 * st][1]), pack2(w[2 * st][2], w[2 * st][3]), pack2(w[2 * st + 1][0], w[2 * st + 1][1]),
+                            pack2(w[2 * st + 1][2], w[2 * st + 1][3])};
+      const bf16x8 pf = __builtin_bit_cast(bf16x8, pw);
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) {
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 32 * st * VROW + 16 * db));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + (32 * st + 16) * VROW + 16 * db));
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        sums.o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, sums.o[db], 0, 0, 0);
+      }
+    }
+  }
+
+  // Channels of o[i][0..3]: 16 i + 4 g + 0..3.
+  template <class F>
+  static __device__ __forceinline__ void each4(const Sums<D>& s, int g, const F& f) {
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      const float x[4] = {s.o[i][0], s.o[i][1], s.o[i][2], s.o[i][3]};
+      f(16 * i + 4 * g, x);
+    }
+  }
+};
+
+// ---- fp32: 32 keys a step
+template <int D>
+struct F32 {
+  static constexpr bool kBf16 = false;
+  static constexpr int KB = 2;
+  static constexpr int kLds = 0;
+  f32x4 query[D / 16];
+
+  __device__ __forceinline__ void load_query(const void* q, int64_t row, int g) {
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) query[s] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(q) + row + 16 * s + 4 * g);
+  }
+
+  struct Tile {
+    f32x4 k[KB][D / 16];
+    f32x4 v[KB][4][D / 64];
+  };
+
+  __device__ __forceinline__ void load(const Params& p, const Group (&gr)[KB], Tile& t, int lane) const {
+    const int r16 = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+      const float* k = static_cast<const float*>(p.k) + gr[b].at + static_cast<int64_t>(min(r16, gr[b].top)) * p.stride_slot + 4 * g;
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s) t.k[b][s] = *reinterpret_cast<const f32x4*>(k + 16 * s);
+    }
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float* v = static_cast<const float*>(p.v) + gr[b].at + static_cast<int64_t>(min(4 * g + r, gr[b].top)) * p.stride_slot + 4 * r16;
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) t.v[b][r][j] = *reinterpret_cast<const f32x4*>(v + 64 * j);
+      }
+  }
+
+  // (the sum over channels may run in any order: element e of the lanes' vectors is one step of it)
+  __device__ __forceinline__ void scores(const Tile& t, f32x4 (&s)[KB]) const {
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+      s[b] = f32x4{};
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.k[b][i][e], query[i][e], s[b], 0, 0, 0);
+    }
+  }
+
+  __device__ __forceinline__ void add(const Tile& t, const Group (&gr)[KB], const f32x4 (&w)[KB], Sums<D>& sums, uint8_t*, int lane, bool careful,
+                                      const int (&limit)[KB]) const {
+    const int g = lane >> 4;
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const bool none = careful && gr[b].first + 4 * g + r > limit[b];
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            sums.o[4 * j + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(none ? 0.0f : t.v[b][r][j][e], w[b][r], sums.o[4 * j + e], 0, 0, 0);
+      }
+  }
+
+  // Channels of o[4 j + 0..3][r]: 64 j + 16 g + 4 r + 0..3.
+  template <class F>
+  static __device__ __forceinline__ void each4(const Sums<D>& s, int g, const F& f) {
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float x[4] = {s.o[4 * j][r], s.o[4 * j + 1][r], s.o[4 * j + 2][r], s.o[4 * j + 3][r]};
+        f(64 * j + 16 * g + 4 * r, x);
+      }
+  }
+};
+
+// What is joined: WAYS results of 16 rows, `ml` [way][16][2] and `o` [way][16][D].  A thread takes four channels of a row.
+template <int D>
+__device__ __forceinline__ void join_rows(const float* ml, const float* o, int ways, int row, int ch, float c, float* m_out, float* l_out, float (&x)[4]) {
+  float m = -INFINITY;
+  for (int w = 0; w < ways; ++w) m = fmaxf(m, ml[(w * kRows + row) * 2]);
+  float l = 0.0f;
+  x[0] = x[1] = x[2] = x[3] = 0.0f;
+  for (int w = 0; w < ways; ++w) {
+    const float mw = ml[(w * kRows + row) * 2], lw = ml[(w * kRows + row) * 2 + 1];
+    if (mw == -INFINITY && lw == 0.0f) continue;         // (saw nothing)
+    const float f = mw == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((mw - m) * c);
+    const f32x4 v = *reinterpret_cast<const f32x4*>(o + (w * kRows + row) * D + ch);
+    l = fmaf(lw, f, l);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = fmaf(v[e], f, x[e]);
+  }
+  *m_out = m;
+  *l_out = l;
+}
+
+template <int D>
+__device__ __forceinline__ void write_row(const Params& p, int tok, int head, int ch, float m, float l, float (&x)[4], bool bf16) {
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] *= inv;
+  store4(p.out, (static_cast<int64_t>(tok) * p.n_q_heads + head) * D + ch, x, bf16);
+  if (ch == 0 && p.lse) p.lse[static_cast<int64_t>(tok) * p.n_q_heads + head] = log_sum(m, l, p.scale_log2e);
+}
+
+template <class Kind, int D, int NW>
+__global__ __launch_bounds__(64 * NW) void selected_attn_kernel(Params p) {
+  constexpr int KB = Kind::KB;
+  constexpr int kJoin = NW > 1 ? NW * kRows * (D + 2) * 4 : 16;          // results of the waves, where values were
+  constexpr int kBytes = NW * Kind::kLds > kJoin ? NW * Kind::kLds : kJoin;
+  __shared__ __attribute__((aligned(16))) uint8_t s_mem[kBytes];
+  __shared__ __attribute__((aligned(16))) int s_key[kMostListed], s_sorted[kMostListed], s_tok[kMostListed], s_list[kMostListed], s_mask[kMostListed];
+  __shared__ int s_count;
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, g = lane >> 4;
+  const int kvh = static_cast<int>(blockIdx.x % p.n_kv_heads);
+  const int job = static_cast<int>(blockIdx.x / p.n_kv_heads), piece = job % p.pieces, tile = job / p.pieces;
+  cs::TokenTile t;
+  if (!cs::find_token_tile(p.cu_q, p.n_streams, p.n_q, p.tile, tile, &t)) return;
+  const int entries = min(p.kv_len[t.stream], p.max_blocks * CS_KV_BLOCK);
+  if (entries <= 0) return;              // (such a stream's rows are left as they were)
+  const int size = p.cache_blocks * CS_KV_BLOCK;
+
+  // ---- the tile's lists as one
+  const int n_keys = t.count * p.n_select;
+  for (int i = tid; i < kMostListed; i += 64 * NW) {
+    int key = 0x7fffffff;
+    if (i < n_keys) {
+      const int tok = t.first + i / p.n_select;
+      const int last = min(p.q_pos[tok], entries - 1);
+      const int block = p.selected[(static_cast<int64_t>(tok) * p.n_kv_heads + kvh) * p.n_select + i % p.n_select];
+      if (block >= 0 && last >= 0 && block <= last / size) key = block;
+    }
+    s_key[i] = key;
+  }
+  __syncthreads();
+  const int padded = (n_keys + 3) & ~3;
+  for (int i = tid; i < padded; i += 64 * NW) {
+    const int key = s_key[i];
+    int rank = 0;
+    for (int j = 0; j < padded; j += 4) {
+      const cs::u32x4 other = *reinterpret_cast<const cs::u32x4*>(s_key + j);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int o = static_cast<int>(other[e]);
+        rank += o < key || (o == key && j + e < i) ? 1 : 0;
+      }
+    }
+    s_sorted[rank] = key;
+    s_tok[rank] = i / p.n_select;
+  }
+  __syncthreads();
+  if (wave == 0) {
+    int base = 0;
+    for (int i0 = 0; i0 < padded; i0 += 64) {
+      const int i = i0 + lane;
+      const int key = i < padded ? s_sorted[i] : 0x7fffffff;
+      const bool first = key != 0x7fffffff && (i == 0 || s_sorted[i - 1] != key);
+      const uint64_t all = __ballot(first);
+      if (first) {
+        int mask = 0;
+        for (int j = i; j < padded && s_sorted[j] == key; ++j) mask |= 1 << s_tok[j];
+        const int at = base + __popcll(all & ((1ull << lane) - 1));
+        s_list[at] = key;
+        s_mask[at] = mask;
+      }
+      base += __popcll(all);
+    }
+    if (lane == 0) s_count = base;
+  }
+  __syncthreads();
+  const int n_groups = __builtin_amdgcn_readfirstlane(s_count) * p.cache_blocks;
+
+  // ---- the lane's row
+  const int tau = r16 / p.group;
+  const bool live = tau < t.count && r16 < p.tile * p.group;
+  const int tok = t.first + (live ? tau : 0), head = kvh * p.group + (live ? r16 % p.group : 0);
+  const int pos = live ? min(p.q_pos[tok], entries - 1) : -1;
+  const int top = __builtin_amdgcn_readfirstlane(static_cast<int>(cs::lanes_max<64>(static_cast<uint32_t>(max(pos, 0)))));      // last entry that anyone sees
+  Kind kind;
+  kind.load_query(p.q, (static_cast<int64_t>(tok) * p.n_q_heads + head) * D, g);
+  const int32_t* ids = p.block_table + static_cast<int64_t>(t.stream) * p.max_blocks;
+  const int64_t head_at = static_cast<int64_t>(kvh) * p.stride_head;
+  uint8_t* lds = s_mem + wave * Kind::kLds;
+  const float c = p.scale_log2e;
+
+  const auto locate = [&](int first_group, Group (&gr)[KB]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+      const bool there = first_group + b < n_groups;
+      const int gi = there ? first_group + b : first_group;
+      const int u = gi / p.cache_blocks;
+      gr[b].first = (__builtin_amdgcn_readfirstlane(s_list[u]) * p.cache_blocks + (gi - u * p.cache_blocks)) * CS_KV_BLOCK;
+      gr[b].mask = there ? __builtin_amdgcn_readfirstlane(s_mask[u]) : 0;
+      const int cb = min(gr[b].first, top) / CS_KV_BLOCK;
+      gr[b].at = static_cast<int64_t>(ids[cb]) * CS_KV_BLOCK * p.stride_slot + head_at;
+      gr[b].top = min(CS_KV_BLOCK - 1, top - cb * CS_KV_BLOCK);
+    }
+  };
+
+  // One pass over the wave's share.  only >= 0: for the rows of that token alone, values that it does not see taken as 0.
+  Sums<D> sums;
+  const auto sweep = [&](int only) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) sums.o[i] = f32x4{};
+    sums.m = -INFINITY;
+    sums.l = 0.0f;
+    const int only_pos = only < 0 ? 0 : min(p.q_pos[t.first + only], entries - 1);
+    for (int g0 = (piece * NW + wave) * KB; g0 < n_groups; g0 += p.pieces * NW * KB) {
+      Group gr[KB];
+      locate(g0, gr);
+      typename Kind::Tile tl;
+      kind.load(p, gr, tl, lane);
+      f32x4 s[KB];
+      kind.scores(tl, s);
+      float high = -INFINITY;
+      int limit[KB];
+#pragma unroll
+      for (int b = 0; b < KB; ++b) {
+        limit[b] = gr[b].mask >> (only < 0 ? 0 : only) & 1 ? only_pos : -1;
+        const int lim = (gr[b].mask >> tau & 1) && (only < 0 || tau == only) ? pos : -1;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          if (gr[b].first + 4 * g + r > lim) s[b][r] = -INFINITY;
+          high = fmaxf(high, s[b][r]);
+        }
+      }
+      high = fmaxf(high, cs::lane_xor16(high));
+      high = fmaxf(high, cs::lane_xor32(high));
+      if (__any((high - sums.m) * c > kSlack || sums.m == -INFINITY)) {
+        const float raised = fmaxf(sums.m, high);
+        const float f = sums.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((sums.m - raised) * c);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sums.o[i][r] *= f;
+        sums.l *= f;
+        sums.m = raised;
+      }
+      const float base = sums.m == -INFINITY ? 0.0f : -sums.m * c;
+#pragma unroll
+      for (int b = 0; b < KB; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, base));
+          sums.l += s[b][r];
+        }
+      kind.add(tl, gr, s, sums, lds, lane, only >= 0, limit);
+    }
+  };
+  sweep(-1);
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) odd |= (__float_as_uint(sums.o[i][r]) & 0x7f800000u) == 0x7f800000u;
+  if (__builtin_expect(__any(odd), 0)) {
+    Sums<D> kept = sums;
+    for (int only = 0; only < t.count; ++only) {
+      sweep(only);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) kept.o[i][r] = tau == only ? sums.o[i][r] : kept.o[i][r];
+      kept.m = tau == only ? sums.m : kept.m;
+      kept.l = tau == only ? sums.l : kept.l;
+    }
+    sums = kept;
+  }
+  sums.l += cs::lane_xor16(sums.l);
+  sums.l += cs::lane_xor32(sums.l);
+
+  // ---- results
+  const int64_t at_job = (static_cast<int64_t>(tile) * p.n_kv_heads + kvh) * p.pieces + piece;
+  if constexpr (NW == 1) {
+    if (p.pieces == 1) {
+      if (live) {
+        Kind::each4(sums, g, [&](int ch, const float (&x)[4]) __attribute__((always_inline)) {
+          float y[4] = {x[0], x[1], x[2], x[3]};
+          write_row<D>(p, tok, head, ch, sums.m, sums.l, y, Kind::kBf16);
+        });
+      }
+    } else {
+      if (g == 0) *reinterpret_cast<cs::f32v2*>(p.ws_ml + (at_job * kRows + r16) * 2) = cs::f32v2{sums.m, sums.l};
+      Kind::each4(sums, g, [&](int ch, const float (&x)[4]) __attribute__((always_inline)) {
+        *reinterpret_cast<f32x4*>(p.ws_o + (at_job * kRows + r16) * D + ch) = f32x4{x[0], x[1], x[2], x[3]};
+      });
+    }
+  } else {
+    __syncthreads();                     // (values of other waves are no longer read)
+    float* s_o = reinterpret_cast<float*>(s_mem);
+    float* s_ml = s_o + NW * kRows * D;
+    if (g == 0) *reinterpret_cast<cs::f32v2*>(s_ml + (wave * kRows + r16) * 2) = cs::f32v2{sums.m, sums.l};
+    Kind::each4(sums, g, [&](int ch, const float (&x)[4]) __attribute__((always_inline)) {
+      *reinterpret_cast<f32x4*>(s_o + (wave * kRows + r16) * D + ch) = f32x4{x[0], x[1], x[2], x[3]};
+    });
+    __syncthreads();
+    for (int i = tid; i < kRows * (D / 4); i += 64 * NW) {
+      const int row = i / (D / 4), ch = i % (D / 4) * 4;
+      if (row >= t.count * p.group) continue;
+      float m, l, x[4];
+      join_rows<D>(s_ml, s_o, NW, row, ch, c, &m, &l, x);
+      if (p.pieces == 1) {
+        write_row<D>(p, t.first + row / p.group, kvh * p.group + row % p.group, ch, m, l, x, Kind::kBf16);
+      } else {
+        if (ch == 0) *reinterpret_cast<cs::f32v2*>(p.ws_ml + (at_job * kRows + row) * 2) = cs::f32v2{m, l};
+        *reinterpret_cast<f32x4*>(p.ws_o + (at_job * kRows + row) * D + ch) = f32x4{x[0], x[1], x[2], x[3]};
+      }
+    }
+  }
+}
+
+// The pieces of a tile and kv head, joined.
+template <int D>
+__global__ __launch_bounds__(256) void selected_join_kernel(Params p, int bf16) {
+  const int kvh = static_cast<int>(blockIdx.x % p.n_kv_heads), tile = static_cast<int>(blockIdx.x / p.n_kv_heads);
+  cs::TokenTile t;
+  if (!cs::find_token_tile(p.cu_q, p.n_streams, p.n_q, p.tile, tile, &t)) return;
+  if (min(p.kv_len[t.stream], p.max_blocks * CS_KV_BLOCK) <= 0) return;
+  const int64_t at_job = (static_cast<int64_t>(tile) * p.n_kv_heads + kvh) * p.pieces;
+  for (int i = threadIdx.x; i < t.count * p.group * (D / 4); i += 256) {
+    const int row = i / (D / 4), ch = i % (D / 4) * 4;
+    float m, l, x[4];
+    join_rows<D>(p.ws_ml + at_job * kRows * 2, p.ws_o + at_job * kRows * D, p.pieces, row, ch, p.scale_log2e, &m, &l, x);
+    write_row<D>(p, t.first + row / p.group, kvh * p.group + row % p.group, ch, m, l, x, bf16 != 0);
+  }
+}
+
+// ---- shapes: tokens of a tile, and pieces of a sweep
+int tile_of(int32_t group, int32_t n_select) {
+  const int by_rows = kRows / group, by_lists = kMostListed / n_select;
+  return by_rows < by_lists ? by_rows : by_lists;
+}
+
+struct Shape {
+  int tile, pieces, waves;
+  int64_t tiles;
+};
+Shape shape_of(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads, int32_t sel_block, int32_t n_select) {
+  Shape s;
+  s.tile = tile_of(n_q_heads / n_kv_heads, n_select);
+  s.tiles = cs::most_token_tiles(n_q, n_streams, s.tile);
+  s.waves = 4;
+  s.pieces = 1;
+  return s;
+}
+
+}  // namespace
+
+extern "C" size_t cs_selected_attn_workspace(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                             int32_t sel_block, int32_t n_select) {
+  if (n_q < 1 || n_streams < 1 || n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % n_kv_heads || n_q_heads / n_kv_heads > kRows) return 0;
+  if (sel_block < 1 || n_select < 1 || n_select > CS_SELECT_MOST || head_dim < 1 || n_q >= 1ll << 26) return 0;
+  const Shape s = shape_of(n_q, n_streams, n_q_heads, n_kv_heads, sel_block, n_select);
+  if (s.pieces == 1) return 0;
+  return static_cast<size_t>(s.tiles) * n_kv_heads * s.pieces * kRows * (head_dim + 2) * sizeof(float);
+}
+
+extern "C" int cs_selected_attn(const void* q, const void* k_cache_layer, const void* v_cache_layer, const int32_t* cu_q, const int32_t* q_pos,
+                                const int32_t* kv_len, const int32_t* block_table, int32_t max_blocks, int32_t block_size,
+                                const int32_t* selected, int32_t sel_block, int32_t n_select, void* out, float* lse, int64_t n_q,
+                                int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t stride_slot,
+                                int64_t stride_head, float softmax_scale, int32_t dtype, void* workspace, size_t workspace_bytes,
+                                void* stream) {
+  if (n_q < 0 || n_streams < 0 || n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % n_kv_heads || max_blocks < 1 || sel_block < 1 || n_select < 1)
+    return CS_EINVAL;
+  if (stride_slot < 0 || stride_head < 0 || !(softmax_scale > 0.0f && softmax_scale <= 3.0e38f)) return CS_EINVAL;
+  if (dtype != CS_F32 && dtype != CS_BF16) return CS_EUNSUPPORTED;
+  if ((head_dim != 64 && head_dim != 128) || block_size != CS_KV_BLOCK || n_q_heads / n_kv_heads > kRows) return CS_EUNSUPPORTED;
+  if (sel_block % CS_KV_BLOCK || sel_block > CS_SELECT_BLOCK_MOST || n_select > CS_SELECT_MOST || n_kv_heads > 65535 || max_blocks > (1 << 27) - 65)
+    return CS_EUNSUPPORTED;
+  if (n_q >= 1ll << 26) return CS_EUNSUPPORTED;
+  const int elems = dtype == CS_BF16 ? 8 : 4;
+  if (stride_slot % elems || stride_head % elems) return CS_EUNSUPPORTED;
+  if (n_q == 0 || n_streams == 0) return CS_OK;
+  if (!q || !k_cache_layer || !v_cache_layer || !cu_q || !q_pos || !kv_len || !block_table || !selected || !out) return CS_EINVAL;
+  if (!cs::aligned16(q) || !cs::aligned16(k_cache_layer) || !cs::aligned16(v_cache_layer) || !cs::aligned16(out)) return CS_EUNSUPPORTED;
+  const Shape s = shape_of(n_q, n_streams, n_q_heads, n_kv_heads, sel_block, n_select);
+  const size_t need = cs_selected_attn_workspace(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, sel_block, n_select);
+  if (need && (!workspace || !cs::aligned16(workspace) || workspace_bytes < need)) return CS_EWORKSPACE;
+  const int64_t groups = s.tiles * n_kv_heads * s.pieces;
+  if (groups > cs::kMostThreads / 512) return CS_EUNSUPPORTED;
+  Params p;
+  p.q = q;
+  p.k = k_cache_layer;
+  p.v = v_cache_layer;
+  p.cu_q = cu_q;
+  p.q_pos = q_pos;
+  p.kv_len = kv_len;
+  p.block_table = block_table;
+  p.selected = selected;
+  p.out = out;
+  p.lse = lse;
+  p.ws_o = static_cast<float*>(workspace);
+  p.ws_ml = need ? p.ws_o + groups * kRows * head_dim : nullptr;
+  p.n_q = n_q;
+  p.stride_slot = stride_slot;
+  p.stride_head = stride_head;
+  p.max_blocks = max_blocks;
+  p.n_streams = n_streams;
+  p.n_q_heads = n_q_heads;
+  p.n_kv_heads = n_kv_heads;
+  p.group = n_q_heads / n_kv_heads;
+  p.tile = s.tile;
+  p.n_select = n_select;
+  p.cache_blocks = sel_block / CS_KV_BLOCK;
+  p.pieces = s.pieces;
+  p.scale_log2e = softmax_scale * 1.4426950408889634f;
+  hipStream_t st = cs::as_stream(stream);
+  const dim3 grid(static_cast<unsigned>(groups));
+#define CS_LAUNCH_SELECTED(KIND, D) hipLaunchKernelGGL((selected_attn_kernel<KIND<D>, D, 4>), grid, dim3(256), 0, st, p)
+  if (dtype == CS_BF16) {
+    if (head_dim == 128) CS_LAUNCH_SELECTED(Bf16, 128);
+    else CS_LAUNCH_SELECTED(Bf16, 64);
+  } else {
+    if (head_dim == 128) CS_LAUNCH_SELECTED(F32, 128);
+    else CS_LAUNCH_SELECTED(F32, 64);
+  }
+#undef CS_LAUNCH_SELECTED
+  if (s.pieces > 1) {
+    const int status = cs::note_hip(hipGetLastError());
+    if (status != CS_OK) return status;
+    const dim3 joins(static_cast<unsigned>(s.tiles * n_kv_heads));
+    if (head_dim == 128) hipLaunchKernelGGL(selected_join_kernel<128>, joins, dim3(256), 0, st, p, dtype == CS_BF16);
+    else hipLaunchKernelGGL(selected_join_kernel<64>, joins, dim3(256), 0, st, p, dtype == CS_BF16);
+  }
+  return cs::note_hip(hipGetLastError());
+}

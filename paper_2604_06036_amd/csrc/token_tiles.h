@@ -1,0 +1,76 @@
+// Tiles of consecutive query tokens of one stream, and lane exchanges of the kernels that take them.  Internal to the library.
+#pragma once
+
+#include "common.h"
+
+namespace cs {
+
+struct TokenTile {
+  int stream, first, count;              // its stream, its first token, how many (1 .. tile)
+};
+
+// Tile `target` of the launch's order: stream by stream, `tile` tokens each, a stream's last tile holding what is left.  cu_q's
+// tokens from n_q on do not exist.  Every wave scans the streams for itself, 64 at a time; false: there are fewer tiles.
+__device__ __forceinline__ bool find_token_tile(const int32_t* __restrict__ cu_q, int n_streams, int64_t n_q, int tile, int target, TokenTile* t) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int s0 = 0; s0 < n_streams; s0 += 64) {
+    const int s = s0 + lane;
+    int a = 0, n = 0;
+    if (s < n_streams) {
+      a = cu_q[s];
+      n = max(0, min(cu_q[s + 1], static_cast<int>(n_q)) - a);
+    }
+    const int tiles = (n + tile - 1) / tile;
+    int incl = tiles;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int up = __shfl_up(incl, d);
+      if (lane >= d) incl += up;
+    }
+    const int total = __builtin_amdgcn_readlane(incl, 63);
+    if (target >= before + total) {
+      before += total;
+      continue;
+    }
+    const int l = __builtin_amdgcn_readfirstlane(__ffsll(static_cast<unsigned long long>(__ballot(before + incl > target))) - 1);
+    const int skip = (target - before - __builtin_amdgcn_readlane(incl - tiles, l)) * tile;
+    t->stream = s0 + l;
+    t->first = __builtin_amdgcn_readlane(a, l) + skip;
+    t->count = min(tile, __builtin_amdgcn_readlane(n, l) - skip);
+    return true;
+  }
+  return false;
+}
+
+// Tiles that n_q tokens of n_streams streams make at most.
+inline int64_t most_token_tiles(int64_t n_q, int32_t n_streams, int tile) { return n_q / tile + (n_q < n_streams ? n_q : n_streams); }
+
+__device__ __forceinline__ float lane_xor32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+__device__ __forceinline__ float lane_xor16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 16) ? r[0] : r[1]);
+}
+
+template <int kCtrl>
+__device__ __forceinline__ uint32_t lane_dpp(uint32_t x) {
+  return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), kCtrl, 0xf, 0xf, true));
+}
+
+// Largest of the wave, or of its aligned groups of `kLanes` lanes.
+template <int kLanes>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t x) {
+  if (kLanes > 1) x = max(x, lane_dpp<0xb1>(x));
+  if (kLanes > 2) x = max(x, lane_dpp<0x4e>(x));
+  if (kLanes > 4) x = max(x, lane_dpp<0x141>(x));
+  if (kLanes > 8) x = max(x, lane_dpp<0x140>(x));
+  if (kLanes > 16) x = max(x, __float_as_uint(lane_xor16(__uint_as_float(x))));
+  if (kLanes > 32) x = max(x, __float_as_uint(lane_xor32(__uint_as_float(x))));
+  return x;
+}
+
+}  // namespace cs
