@@ -29,6 +29,7 @@ namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
@@ -85,11 +86,11 @@ struct Sums {
   float m, l;
 };
 
-// ---- bf16: 64 keys a step
-template <int D>
+// ---- bf16: 16 * GROUPS keys a step
+template <int D, int GROUPS = 4>
 struct Bf16 {
   static constexpr bool kBf16 = true;
-  static constexpr int KB = 4;           // groups a step
+  static constexpr int KB = GROUPS;      // groups a step
   static constexpr int VROW = D + 16;    // of LDS: the transposing reads of 16 rows spread over the banks
   static constexpr int kLds = KB * 16 * VROW * 2;      // bytes a wave
   bf16x8 query[D / 32];
@@ -255,6 +256,63 @@ struct F32 {
   }
 };
 
+// ---- one pass of a wave over groups of keys
+// 16 rows' sums over groups g0, g0 + KB .. of every `stride` from `begin` on; locate(g0, gr) says where they lie.  A lane's row belongs to the token of
+// mask bit `bit` and sees up to entry `pos`.  careful: values past only_pos, or in blocks that the token of mask bit `only` does not read, are
+// taken as 0 (the sums of other tokens' rows are then worth nothing).
+template <class Kind, int D, class Locate>
+__device__ __forceinline__ void sweep(const Params& p, const Kind& kind, const Locate& locate, int begin, int stride, int n_groups, int bit, int pos, bool careful,
+                                      int only, int only_pos, uint8_t* lds, int lane, Sums<D>& sums) {
+  constexpr int KB = Kind::KB;
+  const int g = lane >> 4;
+  const float c = p.scale_log2e;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) sums.o[i] = f32x4{};
+  sums.m = -INFINITY;
+  sums.l = 0.0f;
+  for (int g0 = begin; g0 < n_groups; g0 += stride) {
+    Group gr[KB];
+    locate(g0, gr);
+    typename Kind::Tile tl;
+    kind.load(p, gr, tl, lane);
+    f32x4 s[KB];
+    kind.scores(tl, s);
+    float high = -INFINITY;
+    int limit[KB];
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+      limit[b] = gr[b].mask >> only & 1 ? only_pos : -1;
+      const int lim = (gr[b].mask >> bit & 1) && (!careful || bit == only) ? pos : -1;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (gr[b].first + 4 * g + r > lim) s[b][r] = -INFINITY;
+        high = fmaxf(high, s[b][r]);
+      }
+    }
+    high = fmaxf(high, cs::lane_xor16(high));
+    high = fmaxf(high, cs::lane_xor32(high));
+    if (__any((high - sums.m) * c > kSlack || sums.m == -INFINITY)) {
+      const float raised = fmaxf(sums.m, high);
+      const float f = sums.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((sums.m - raised) * c);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sums.o[i][r] *= f;
+      sums.l *= f;
+      sums.m = raised;
+    }
+    const float base = sums.m == -INFINITY ? 0.0f : -sums.m * c;
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, base));
+        sums.l += s[b][r];
+      }
+    kind.add(tl, gr, s, sums, lds, lane, careful, limit);
+  }
+}
+
 // What is joined: WAYS results of 16 rows, `ml` [way][16][2] and `o` [way][16][D].  A thread takes four channels of a row.
 template <int D>
 __device__ __forceinline__ void join_rows(const float* ml, const float* o, int ways, int row, int ch, float c, float* m_out, float* l_out, float (&x)[4]) {
@@ -379,57 +437,9 @@ __global__ __launch_bounds__(64 * NW) void selected_attn_kernel(Params p) {
     }
   };
 
-  // One pass over the wave's share.  only >= 0: for the rows of that token alone, values that it does not see taken as 0.
   Sums<D> sums;
-  const auto sweep = [&](int only) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) sums.o[i] = f32x4{};
-    sums.m = -INFINITY;
-    sums.l = 0.0f;
-    const int only_pos = only < 0 ? 0 : min(p.q_pos[t.first + only], entries - 1);
-    for (int g0 = (piece * NW + wave) * KB; g0 < n_groups; g0 += p.pieces * NW * KB) {
-      Group gr[KB];
-      locate(g0, gr);
-      typename Kind::Tile tl;
-      kind.load(p, gr, tl, lane);
-      f32x4 s[KB];
-      kind.scores(tl, s);
-      float high = -INFINITY;
-      int limit[KB];
-#pragma unroll
-      for (int b = 0; b < KB; ++b) {
-        limit[b] = gr[b].mask >> (only < 0 ? 0 : only) & 1 ? only_pos : -1;
-        const int lim = (gr[b].mask >> tau & 1) && (only < 0 || tau == only) ? pos : -1;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          if (gr[b].first + 4 * g + r > lim) s[b][r] = -INFINITY;
-          high = fmaxf(high, s[b][r]);
-        }
-      }
-      high = fmaxf(high, cs::lane_xor16(high));
-      high = fmaxf(high, cs::lane_xor32(high));
-      if (__any((high - sums.m) * c > kSlack || sums.m == -INFINITY)) {
-        const float raised = fmaxf(sums.m, high);
-        const float f = sums.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((sums.m - raised) * c);
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) sums.o[i][r] *= f;
-        sums.l *= f;
-        sums.m = raised;
-      }
-      const float base = sums.m == -INFINITY ? 0.0f : -sums.m * c;
-#pragma unroll
-      for (int b = 0; b < KB; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, base));
-          sums.l += s[b][r];
-        }
-      kind.add(tl, gr, s, sums, lds, lane, only >= 0, limit);
-    }
-  };
-  sweep(-1);
+  const int begin = (piece * NW + wave) * KB, stride = p.pieces * NW * KB;
+  sweep<Kind, D>(p, kind, locate, begin, stride, n_groups, tau, pos, false, 0, 0, lds, lane, sums);
   bool odd = false;
 #pragma unroll
   for (int i = 0; i < D / 16; ++i)
@@ -438,7 +448,7 @@ __global__ __launch_bounds__(64 * NW) void selected_attn_kernel(Params p) {
   if (__builtin_expect(__any(odd), 0)) {
     Sums<D> kept = sums;
     for (int only = 0; only < t.count; ++only) {
-      sweep(only);
+      sweep<Kind, D>(p, kind, locate, begin, stride, n_groups, tau, pos, true, only, min(p.q_pos[t.first + only], entries - 1), lds, lane, sums);
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -507,6 +517,319 @@ __global__ __launch_bounds__(256) void selected_join_kernel(Params p, int bf16) 
   }
 }
 
+// ------------------------------------------------------------------------------------------
+// Many tokens a stream, bf16.  Neighbouring tokens read much the same blocks, so a workgroup takes as many as its four waves hold, 32
+// rows each (a token's heads may lie in two waves), and moves every block that any of them reads through LDS once, 64 keys a step.  A wave
+// skips the steps that none of its tokens reads.
+//   S^T = K Q^T, O^T += V^T P^T      v_mfma_f32_32x32x16_bf16; a lane owns one row and 16 of the 32 keys
+// Rows go from memory to LDS directly (global_load_lds_dwordx4: lane l lands at base + 16 l), a step ahead, in two stages, one barrier a step.  Lanes choose which 16-byte chunk of a row they fetch, so that reads spread over the banks: row r of keys holds chunk c at
+// place c ^ k_place(r), of values at c ^ v_place(r).
+constexpr int kStepKeys = 64, kStepGroups = kStepKeys / CS_KV_BLOCK;
+constexpr int kRowsWave = 32, kRowsWaves = 4;
+constexpr int kRowsListed = 1024;        // list elements of a workgroup's tokens
+constexpr int kChunk = 1024;             // blocks whose readers are collected at once
+constexpr int kStages = 2;
+constexpr int kPlaces = 256;             // groups whose places are looked up at once
+
+// Tokens of a workgroup: as many as fit, and as masks of 32 bits hold.
+inline int rows_tokens(int group) { return kRowsWaves * kRowsWave / group < 32 ? kRowsWaves * kRowsWave / group : 32; }
+
+template <int D>
+__device__ __forceinline__ int k_place(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
+template <int D>
+__device__ __forceinline__ int v_place(int r) { return D == 128 ? 4 * (r & 3) + 2 * ((r >> 2) & 1) : 4 * ((r >> 1) & 1) + 2 * ((r >> 2) & 1); }
+
+// 16 bytes a lane from sbase + off to LDS.  Inline assembly, so that the compiler does not wait for all of them at the next read of LDS:
+// the pipeline's own waits do.
+__device__ __forceinline__ void to_lds(uint32_t off, const void* sbase, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(sbase), "s"(lds_addr) : "memory", "m0");
+}
+typedef __attribute__((address_space(3))) void lds_void;
+__device__ __forceinline__ uint32_t lds_address(const void* at) { return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)at)); }
+
+template <typename T>
+__device__ __forceinline__ T* uniform(T* at) {
+  const uint64_t x = reinterpret_cast<uintptr_t>(at);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x >> 32));
+  return reinterpret_cast<T*>(static_cast<uintptr_t>(static_cast<uint64_t>(hi) << 32 | lo));
+}
+
+// This wave's requests are in LDS, and its reads of LDS are done; then the others' too.
+__device__ __forceinline__ void gate() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
+
+template <int D>
+__global__ __launch_bounds__(64 * kRowsWaves, 2) void selected_rows_kernel(Params p) {
+  constexpr int DB = D / 32, STEPS = D / 16;
+  constexpr int kTensor = kStepKeys * D * 2;               // bytes of a step's keys, or values
+  static_assert(kRowsWaves == kStepGroups, "a wave asks for a group");
+  constexpr int kStage = 2 * kTensor;
+  constexpr int kAsks = kTensor / 1024 / kRowsWaves;       // requests of a wave for a step's keys (and as many for its values)
+  typedef Bf16<D, 2> Again;
+  constexpr int kBytes = kStages * kStage > kRowsWaves * Again::kLds ? kStages * kStage : kRowsWaves * Again::kLds;
+  static_assert(kBytes >= kChunk * 4, "readers are collected where tiles are later");
+  __shared__ __attribute__((aligned(16))) uint8_t s_mem[kBytes];
+  __shared__ int s_list[kRowsListed];
+  __shared__ uint32_t s_mask[kRowsListed];
+  __shared__ int s_odd;
+  __shared__ __attribute__((aligned(16))) cs::u32x4 s_place[kPlaces];      // of a group: first entry, readers, cache block, last row
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
+  const int kvh = static_cast<int>(blockIdx.x % p.n_kv_heads);
+  cs::TokenTile t;
+  if (!cs::find_token_tile(p.cu_q, p.n_streams, p.n_q, p.tile, static_cast<int>(blockIdx.x / p.n_kv_heads), &t)) return;
+  const int entries = min(p.kv_len[t.stream], p.max_blocks * CS_KV_BLOCK);
+  if (entries <= 0) return;
+  const int size = p.cache_blocks * CS_KV_BLOCK;
+
+  // ---- the blocks that the tokens read, ascending, each with the mask of its readers
+  constexpr int kHeld = kRowsListed / (64 * kRowsWaves);
+  const int n_keys = t.count * p.n_select;
+  int held[kHeld];
+  int top = 0;                           // last entry that anyone sees
+  for (int i = lane; i < t.count; i += 64) top = max(top, min(p.q_pos[t.first + i], entries - 1));
+  top = __builtin_amdgcn_readfirstlane(static_cast<int>(cs::lanes_max<64>(static_cast<uint32_t>(top))));
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int at = i * 64 * kRowsWaves + tid;
+    held[i] = -1;
+    if (at < n_keys) {
+      const int tok = t.first + at / p.n_select;
+      const int last = min(p.q_pos[tok], entries - 1);
+      const int block = p.selected[(static_cast<int64_t>(tok) * p.n_kv_heads + kvh) * p.n_select + at % p.n_select];
+      if (block >= 0 && last >= 0 && block <= last / size) held[i] = block;
+    }
+  }
+  uint32_t* readers = reinterpret_cast<uint32_t*>(s_mem);
+  const int candidates = top / size + 1;
+  int count = 0;
+  for (int c0 = 0; c0 < candidates; c0 += kChunk) {
+    for (int i = tid; i < kChunk; i += 64 * kRowsWaves) readers[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (held[i] >= c0 && held[i] < c0 + kChunk) atomicOr(&readers[held[i] - c0], 1u << ((i * 64 * kRowsWaves + tid) / p.n_select));
+    __syncthreads();
+    const int here = min(kChunk, candidates - c0);
+    for (int i0 = 0; i0 < here; i0 += 64) {                // (every wave counts, the first one writes)
+      const uint32_t mask = i0 + lane < here ? readers[i0 + lane] : 0;
+      const uint64_t all = __ballot(mask != 0);
+      if (wave == 0 && mask) {
+        const int at = count + __popcll(all & ((1ull << lane) - 1));
+        s_list[at] = c0 + i0 + lane;
+        s_mask[at] = mask;
+      }
+      count += __popcll(all);
+    }
+    __syncthreads();
+  }
+  const int n_groups = __builtin_amdgcn_readfirstlane(count) * p.cache_blocks;
+
+  // ---- the lane's row
+  const int in_group = wave * kRowsWave + n, bit = in_group / p.group;      // bit: the token, of the workgroup's
+  const bool live = bit < t.count;
+  const int tok = t.first + (live ? bit : 0), head = kvh * p.group + (live ? in_group % p.group : 0);
+  const int pos = live ? min(p.q_pos[tok], entries - 1) : -1;
+  const int bits0 = wave * kRowsWave / p.group, bits1 = min((wave * kRowsWave + kRowsWave - 1) / p.group, t.count - 1);       // the wave's tokens
+  const uint32_t wave_mask = bits1 < bits0 ? 0u : (~0u >> (31 - (bits1 - bits0))) << bits0;
+  int least = live ? pos : 0x7fffffff;                     // how far all of them see
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) least = min(least, __shfl_xor(least, d));
+  least = __builtin_amdgcn_readfirstlane(least);
+  const int64_t at_q = (static_cast<int64_t>(tok) * p.n_q_heads + head) * D;
+  bf16x8 query[STEPS];
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) query[s] = *reinterpret_cast<const bf16x8*>(static_cast<const uint16_t*>(p.q) + at_q + 16 * s + 8 * h);
+
+  const int32_t* ids = p.block_table + static_cast<int64_t>(t.stream) * p.max_blocks;
+  const int64_t head_at = static_cast<int64_t>(kvh) * p.stride_head;
+  const float c = p.scale_log2e;
+
+  // ---- this wave's part of a step's requests: the rows of one group
+  constexpr int LR = D / 8, RL = 64 / LR;                  // lanes of a row, rows of a request
+  const uint32_t mem = __builtin_amdgcn_readfirstlane(lds_address(s_mem));
+  const uint32_t row_bytes = static_cast<uint32_t>(p.stride_slot * 2);
+  // (i: the step, of those whose places are at hand; at: its cache block and last row)
+  const auto place_of = [&](int i) __attribute__((always_inline)) {
+    return *reinterpret_cast<const cs::u32x2*>(reinterpret_cast<const uint32_t*>(&s_place[kStepGroups * i + wave]) + 2);
+  };
+  const auto request = [&](int i, cs::u32x2 at) __attribute__((always_inline)) {
+    const int id = __builtin_amdgcn_readfirstlane(static_cast<int>(at.x)), last = __builtin_amdgcn_readfirstlane(static_cast<int>(at.y));
+    const int64_t from = (static_cast<int64_t>(id) * CS_KV_BLOCK * p.stride_slot + head_at) * 2;
+    const char* k = uniform(static_cast<const char*>(p.k) + from);
+    const char* v = uniform(static_cast<const char*>(p.v) + from);
+    const uint32_t to = mem + (i % kStages) * kStage + wave * (kTensor / kRowsWaves);
+#pragma unroll
+    for (int j = 0; j < kAsks; ++j) {
+      const int row = j * RL + lane / LR;
+      const uint32_t off = static_cast<uint32_t>(min(row, last)) * row_bytes;
+      to_lds(off + 16 * (lane % LR ^ k_place<D>(row)), k, to + 1024 * j);
+      to_lds(off + 16 * (lane % LR ^ v_place<D>(row)), v, to + kTensor + 1024 * j);
+    }
+  };
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) o[db] = f32x16{};
+  float m = -INFINITY, l = 0.0f;
+  // the lane's places in a stage
+  const int i16 = lane & 15, gid = (lane >> 4) & 1, v_row = 4 * h + (i16 >> 2);
+  const int k_at = n * D * 2, k_turn = k_place<D>(n), v_at = v_row * D * 2 + 8 * (i16 & 1), v_turn = v_place<D>(v_row);
+  struct Seen {
+    int first[kStepGroups];
+    uint32_t mask[kStepGroups];
+  };
+  const auto seen_of = [&](int i, Seen& w) __attribute__((always_inline)) {
+#pragma unroll
+    for (int b = 0; b < kStepGroups; ++b) {
+      const cs::u32x2 at = *reinterpret_cast<const cs::u32x2*>(&s_place[kStepGroups * i + b]);
+      w.first[b] = __builtin_amdgcn_readfirstlane(static_cast<int>(at.x));
+      w.mask[b] = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(at.y)));
+    }
+  };
+  const auto compute = [&](int i, const Seen& w) __attribute__((always_inline)) {
+    if (((w.mask[0] | w.mask[1] | w.mask[2] | w.mask[3]) & wave_mask) == 0) return;
+    const uint8_t* k = s_mem + (i % kStages) * kStage;
+    const uint8_t* v = k + kTensor;
+    f32x16 s[2] = {};
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j)
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(k + k_at + b * 32 * D * 2 + 16 * ((2 * j + h) ^ k_turn)), query[j], s[b], 0, 0, 0);
+    // Keys of register r of 32: 8 (r / 4) + 4 h + r % 4, so registers 0..7 are the first group's.  A group that the lane's token does not read
+    // has the exponent -inf; only a group that ends behind one of the tokens is masked key by key.
+    if (max(max(w.first[0], w.first[1]), max(w.first[2], w.first[3])) + CS_KV_BLOCK - 1 > least) {
+#pragma unroll
+      for (int b = 0; b < kStepGroups; ++b) {
+        const int lim = pos - w.first[b] - 4 * h;
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+          if (8 * (r / 4) + r % 4 > lim) s[b / 2][8 * (b % 2) + r] = -INFINITY;
+      }
+    }
+    float high = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < kStepGroups; ++b) {
+      const f32x16& x = s[b / 2];
+      const int r = 8 * (b % 2);
+      const float a0 = fmaxf(fmaxf(x[r], x[r + 1]), x[r + 2]), a1 = fmaxf(fmaxf(x[r + 3], x[r + 4]), x[r + 5]), a2 = fmaxf(x[r + 6], x[r + 7]);
+      const float a = fmaxf(fmaxf(a0, a1), a2);
+      high = fmaxf(high, w.mask[b] >> bit & 1 ? a : -INFINITY);
+    }
+    high = fmaxf(high, cs::lane_xor32(high));
+    if (__any((high - m) * c > kSlack || m == -INFINITY)) {
+      const float raised = fmaxf(m, high);
+      const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - raised) * c);
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[db][r] *= f;
+      l *= f;
+      m = raised;
+    }
+    const float base = m == -INFINITY ? 0.0f : -m * c;
+    float total[4] = {};
+    // of the 16 keys of a product a lane's weights are of 4 h + 0..3 and 8 + 4 h + 0..3; a row's place does not change 8 rows further
+#pragma unroll
+    for (int st = 0; st < kStepGroups; ++st) {
+      const float from = w.mask[st] >> bit & 1 ? base : -INFINITY;
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] = __builtin_amdgcn_exp2f(fmaf(s[st / 2][8 * (st % 2) + e], c, from));
+        total[e % 4] += x[e];
+      }
+      const bf16x8 pf = __builtin_bit_cast(bf16x8, cs::u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])});
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const uint8_t* at = v + v_at + 16 * ((4 * db + 2 * gid + ((i16 >> 1) & 1)) ^ v_turn) + 16 * st * D * 2;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * D * 2));
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[db], 0, 0, 0);
+      }
+    }
+    l += (total[0] + total[1]) + (total[2] + total[3]);
+  };
+
+  // ---- the steps, kPlaces groups at a time
+  for (int g0 = 0; g0 < n_groups; g0 += kPlaces) {
+    const int here = min(kPlaces, n_groups - g0), steps = (here + kStepGroups - 1) / kStepGroups;
+    __syncthreads();                     // (places and stages are free)
+    for (int i = tid; i < kStepGroups * steps; i += 64 * kRowsWaves) {
+      const int gi = g0 + min(i, here - 1), u = gi / p.cache_blocks;
+      const int first = (s_list[u] * p.cache_blocks + (gi - u * p.cache_blocks)) * CS_KV_BLOCK;
+      const int cb = min(first, top) / CS_KV_BLOCK;
+      s_place[i] = cs::u32x4{static_cast<uint32_t>(first), i < here ? s_mask[u] : 0u, static_cast<uint32_t>(ids[cb]),
+                             static_cast<uint32_t>(min(CS_KV_BLOCK - 1, top - cb * CS_KV_BLOCK))};
+    }
+    __syncthreads();
+    request(0, place_of(0));
+    for (int i = 0; i < steps; ++i) {
+      const cs::u32x2 next = place_of(min(i + 1, steps - 1));
+      Seen w;
+      seen_of(i, w);
+      gate();
+      if (i + 1 < steps) request(i + 1, next);             // (into the stage that everyone has read a step ago)
+      compute(i, w);
+    }
+  }
+  l += cs::lane_xor32(l);
+
+  // ---- results; where something is no number or infinite, again token by token, the waves in turn
+  if (tid == 0) s_odd = 0;
+  bool odd = false;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) odd |= (__float_as_uint(o[db][r]) & 0x7f800000u) == 0x7f800000u;
+  __syncthreads();
+  if (__builtin_expect(__any(odd), 0)) s_odd = 1;
+  __syncthreads();
+  if (__builtin_expect(s_odd, 0)) {
+    const int r16 = lane & 15, g = lane >> 4;
+    uint8_t* lds = s_mem + wave * Again::kLds;
+    const auto locate = [&](int first_group, Group (&gr)[2]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const bool there = first_group + b < n_groups;
+        const int gi = there ? first_group + b : first_group, u = gi / p.cache_blocks;
+        gr[b].first = (__builtin_amdgcn_readfirstlane(s_list[u]) * p.cache_blocks + (gi - u * p.cache_blocks)) * CS_KV_BLOCK;
+        gr[b].mask = there ? __builtin_amdgcn_readfirstlane(static_cast<int>(s_mask[u])) : 0;
+        const int cb = min(gr[b].first, top) / CS_KV_BLOCK;
+        gr[b].at = static_cast<int64_t>(ids[cb]) * CS_KV_BLOCK * p.stride_slot + head_at;
+        gr[b].top = min(CS_KV_BLOCK - 1, top - cb * CS_KV_BLOCK);
+      }
+    };
+    for (int i = wave; i < t.count; i += kRowsWaves) {
+      const int tok1 = t.first + i, pos1 = min(p.q_pos[tok1], entries - 1);
+      const bool live1 = r16 < p.group;
+      const int head1 = kvh * p.group + (live1 ? r16 : 0);
+      Again kind;
+      kind.load_query(p.q, (static_cast<int64_t>(tok1) * p.n_q_heads + head1) * D, g);
+      Sums<D> one;
+      sweep<Again, D>(p, kind, locate, 0, 2, n_groups, i, live1 ? pos1 : -1, true, i, pos1, lds, lane, one);
+      one.l += cs::lane_xor16(one.l);
+      one.l += cs::lane_xor32(one.l);
+      if (live1) {
+        Again::each4(one, g, [&](int ch, const float (&x)[4]) __attribute__((always_inline)) {
+          float y[4] = {x[0], x[1], x[2], x[3]};
+          write_row<D>(p, tok1, head1, ch, one.m, one.l, y, true);
+        });
+      }
+    }
+    return;
+  }
+  if (!live) return;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float x[4] = {o[db][4 * r], o[db][4 * r + 1], o[db][4 * r + 2], o[db][4 * r + 3]};
+      write_row<D>(p, tok, head, 32 * db + 8 * r + 4 * h, m, l, x, true);
+    }
+}
+
 // ---- shapes: tokens of a tile, and pieces of a sweep
 int tile_of(int32_t group, int32_t n_select) {
   const int by_rows = kRows / group, by_lists = kMostListed / n_select;
@@ -514,12 +837,23 @@ int tile_of(int32_t group, int32_t n_select) {
 }
 
 struct Shape {
+  bool rows;                             // the kernel for many tokens a stream
   int tile, pieces, waves;
   int64_t tiles;
 };
-Shape shape_of(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads, int32_t sel_block, int32_t n_select) {
+constexpr int kManyTokens = 8;           // a stream, on average, from which the rows kernel is taken
+Shape shape_of(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_select, bool bf16, int64_t stride_slot) {
   Shape s;
-  s.tile = tile_of(n_q_heads / n_kv_heads, n_select);
+  const int group = n_q_heads / n_kv_heads;
+  s.rows = bf16 && n_q >= static_cast<int64_t>(kManyTokens) * n_streams && stride_slot < 1ll << 26;      // (offsets of a cache block in 32 bits)
+  if (s.rows) {
+    const int all = rows_tokens(group), by_lists = kRowsListed / n_select;
+    s.tile = all < by_lists ? all : by_lists;
+    s.tiles = cs::most_token_tiles(n_q, n_streams, s.tile);
+    s.pieces = 1;
+    return s;
+  }
+  s.tile = tile_of(group, n_select);
   s.tiles = cs::most_token_tiles(n_q, n_streams, s.tile);
   s.waves = 4;
   s.pieces = 1;
@@ -532,7 +866,7 @@ extern "C" size_t cs_selected_attn_workspace(int64_t n_q, int32_t n_streams, int
                                              int32_t sel_block, int32_t n_select) {
   if (n_q < 1 || n_streams < 1 || n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % n_kv_heads || n_q_heads / n_kv_heads > kRows) return 0;
   if (sel_block < 1 || n_select < 1 || n_select > CS_SELECT_MOST || head_dim < 1 || n_q >= 1ll << 26) return 0;
-  const Shape s = shape_of(n_q, n_streams, n_q_heads, n_kv_heads, sel_block, n_select);
+  const Shape s = shape_of(n_q, n_streams, n_q_heads, n_kv_heads, n_select, false, 0);
   if (s.pieces == 1) return 0;
   return static_cast<size_t>(s.tiles) * n_kv_heads * s.pieces * kRows * (head_dim + 2) * sizeof(float);
 }
@@ -556,7 +890,7 @@ extern "C" int cs_selected_attn(const void* q, const void* k_cache_layer, const 
   if (n_q == 0 || n_streams == 0) return CS_OK;
   if (!q || !k_cache_layer || !v_cache_layer || !cu_q || !q_pos || !kv_len || !block_table || !selected || !out) return CS_EINVAL;
   if (!cs::aligned16(q) || !cs::aligned16(k_cache_layer) || !cs::aligned16(v_cache_layer) || !cs::aligned16(out)) return CS_EUNSUPPORTED;
-  const Shape s = shape_of(n_q, n_streams, n_q_heads, n_kv_heads, sel_block, n_select);
+  const Shape s = shape_of(n_q, n_streams, n_q_heads, n_kv_heads, n_select, dtype == CS_BF16, stride_slot);
   const size_t need = cs_selected_attn_workspace(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, sel_block, n_select);
   if (need && (!workspace || !cs::aligned16(workspace) || workspace_bytes < need)) return CS_EWORKSPACE;
   const int64_t groups = s.tiles * n_kv_heads * s.pieces;
@@ -590,7 +924,10 @@ extern "C" int cs_selected_attn(const void* q, const void* k_cache_layer, const 
   hipStream_t st = cs::as_stream(stream);
   const dim3 grid(static_cast<unsigned>(groups));
 #define CS_LAUNCH_SELECTED(KIND, D) hipLaunchKernelGGL((selected_attn_kernel<KIND<D>, D, 4>), grid, dim3(256), 0, st, p)
-  if (dtype == CS_BF16) {
+  if (s.rows) {
+    if (head_dim == 128) hipLaunchKernelGGL(selected_rows_kernel<128>, grid, dim3(64 * kRowsWaves), 0, st, p);
+    else hipLaunchKernelGGL(selected_rows_kernel<64>, grid, dim3(64 * kRowsWaves), 0, st, p);
+  } else if (dtype == CS_BF16) {
     if (head_dim == 128) CS_LAUNCH_SELECTED(Bf16, 128);
     else CS_LAUNCH_SELECTED(Bf16, 64);
   } else {
