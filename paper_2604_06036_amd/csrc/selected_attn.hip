@@ -29,7 +29,6 @@ namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
@@ -291,7 +290,7 @@ __device__ __forceinline__ void sweep(const Params& p, const Kind& kind, const L
     }
     high = fmaxf(high, cs::lane_xor16(high));
     high = fmaxf(high, cs::lane_xor32(high));
-    if (__any((high - sums.m) * c > kSlack || sums.m == -INFINITY)) {
+    if (__any((high - sums.m) * c > kSlack)) {            // (-inf - -inf: no)
       const float raised = fmaxf(sums.m, high);
       const float f = sums.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((sums.m - raised) * c);
 #pragma unroll
@@ -518,18 +517,18 @@ __global__ __launch_bounds__(256) void selected_join_kernel(Params p, int bf16) 
 }
 
 // ------------------------------------------------------------------------------------------
-// Many tokens a stream, bf16.  Neighbouring tokens read much the same blocks, so a workgroup takes as many as its four waves hold, 32
-// rows each (a token's heads may lie in two waves), and moves every block that any of them reads through LDS once, 64 keys a step.  A wave
+// Many tokens a stream, bf16.  Neighbouring tokens read much the same blocks, so a workgroup takes as many as its four waves hold, 16
+// rows each (a token's heads may lie in two waves), and moves every block that any of them reads through LDS once, 32 keys a step.  A wave
 // skips the steps that none of its tokens reads.
-//   S^T = K Q^T, O^T += V^T P^T      v_mfma_f32_32x32x16_bf16; a lane owns one row and 16 of the 32 keys
+//   S^T = K Q^T, O^T += V^T P^T      v_mfma_f32_16x16x32_bf16; a lane owns one row and 4 of 16 keys
 // Rows go from memory to LDS directly (global_load_lds_dwordx4: lane l lands at base + 16 l), a step ahead, in two stages, one barrier a step.  Lanes choose which 16-byte chunk of a row they fetch, so that reads spread over the banks: row r of keys holds chunk c at
 // place c ^ k_place(r), of values at c ^ v_place(r).
-constexpr int kStepKeys = 64, kStepGroups = kStepKeys / CS_KV_BLOCK;
-constexpr int kRowsWave = 32, kRowsWaves = 4;
-constexpr int kRowsListed = 1024;        // list elements of a workgroup's tokens
+constexpr int kStepKeys = 32, kStepGroups = kStepKeys / CS_KV_BLOCK;
+constexpr int kRowsWave = kRows, kRowsWaves = 4;
+constexpr int kRowsListed = 512;         // list elements of a workgroup's tokens
 constexpr int kChunk = 1024;             // blocks whose readers are collected at once
 constexpr int kStages = 2;
-constexpr int kPlaces = 256;             // groups whose places are looked up at once
+constexpr int kPlaces = 64;              // groups whose places are looked up at once, a lane each
 
 // Tokens of a workgroup: as many as fit, and as masks of 32 bits hold.
 inline int rows_tokens(int group) { return kRowsWaves * kRowsWave / group < 32 ? kRowsWaves * kRowsWave / group : 32; }
@@ -537,7 +536,7 @@ inline int rows_tokens(int group) { return kRowsWaves * kRowsWave / group < 32 ?
 template <int D>
 __device__ __forceinline__ int k_place(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
 template <int D>
-__device__ __forceinline__ int v_place(int r) { return D == 128 ? 4 * (r & 3) + 2 * ((r >> 2) & 1) : 4 * ((r >> 1) & 1) + 2 * ((r >> 2) & 1); }
+__device__ __forceinline__ int v_place(int r) { return D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); }
 
 // 16 bytes a lane from sbase + off to LDS.  Inline assembly, so that the compiler does not wait for all of them at the next read of LDS:
 // the pipeline's own waits do.
@@ -558,22 +557,23 @@ __device__ __forceinline__ T* uniform(T* at) {
 __device__ __forceinline__ void gate() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
 
 template <int D>
-__global__ __launch_bounds__(64 * kRowsWaves, 2) void selected_rows_kernel(Params p) {
-  constexpr int DB = D / 32, STEPS = D / 16;
+__global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Params p) {
+  constexpr int DB = D / 16, STEPS = D / 32;
   constexpr int kTensor = kStepKeys * D * 2;               // bytes of a step's keys, or values
-  static_assert(kRowsWaves == kStepGroups, "a wave asks for a group");
   constexpr int kStage = 2 * kTensor;
-  constexpr int kAsks = kTensor / 1024 / kRowsWaves;       // requests of a wave for a step's keys (and as many for its values)
+  constexpr int kParts = kTensor / 1024;                   // requests for a step's keys, and as many for its values
+  constexpr int kAsks = kParts / kRowsWaves;               // ... of a wave
+  static_assert(kRowsWaves == 2 * kStepGroups && kAsks >= 1, "a wave asks for half a group");
   typedef Bf16<D, 2> Again;
-  constexpr int kBytes = kStages * kStage > kRowsWaves * Again::kLds ? kStages * kStage : kRowsWaves * Again::kLds;
+  constexpr int kBytes = kStages * kStage;
+  constexpr int kAgainWaves = kBytes / Again::kLds < kRowsWaves ? kBytes / Again::kLds : kRowsWaves;
   static_assert(kBytes >= kChunk * 4, "readers are collected where tiles are later");
   __shared__ __attribute__((aligned(16))) uint8_t s_mem[kBytes];
   __shared__ int s_list[kRowsListed];
   __shared__ uint32_t s_mask[kRowsListed];
   __shared__ int s_odd;
-  __shared__ __attribute__((aligned(16))) cs::u32x4 s_place[kPlaces];      // of a group: first entry, readers, cache block, last row
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, g = lane >> 4;
   const int kvh = static_cast<int>(blockIdx.x % p.n_kv_heads);
   cs::TokenTile t;
   if (!cs::find_token_tile(p.cu_q, p.n_streams, p.n_q, p.tile, static_cast<int>(blockIdx.x / p.n_kv_heads), &t)) return;
@@ -582,7 +582,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void selected_rows_kernel(Param
   const int size = p.cache_blocks * CS_KV_BLOCK;
 
   // ---- the blocks that the tokens read, ascending, each with the mask of its readers
-  constexpr int kHeld = kRowsListed / (64 * kRowsWaves);
+  constexpr int kHeld = (kRowsListed + 64 * kRowsWaves - 1) / (64 * kRowsWaves);
   const int n_keys = t.count * p.n_select;
   int held[kHeld];
   int top = 0;                           // last entry that anyone sees
@@ -625,7 +625,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void selected_rows_kernel(Param
   const int n_groups = __builtin_amdgcn_readfirstlane(count) * p.cache_blocks;
 
   // ---- the lane's row
-  const int in_group = wave * kRowsWave + n, bit = in_group / p.group;      // bit: the token, of the workgroup's
+  const int in_group = wave * kRowsWave + r16, bit = in_group / p.group;      // bit: the token, of the workgroup's
   const bool live = bit < t.count;
   const int tok = t.first + (live ? bit : 0), head = kvh * p.group + (live ? in_group % p.group : 0);
   const int pos = live ? min(p.q_pos[tok], entries - 1) : -1;
@@ -633,148 +633,148 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void selected_rows_kernel(Param
   const uint32_t wave_mask = bits1 < bits0 ? 0u : (~0u >> (31 - (bits1 - bits0))) << bits0;
   int least = live ? pos : 0x7fffffff;                     // how far all of them see
 #pragma unroll
-  for (int d = 1; d < 32; d <<= 1) least = min(least, __shfl_xor(least, d));
+  for (int d = 1; d < 16; d <<= 1) least = min(least, __shfl_xor(least, d));
   least = __builtin_amdgcn_readfirstlane(least);
   const int64_t at_q = (static_cast<int64_t>(tok) * p.n_q_heads + head) * D;
   bf16x8 query[STEPS];
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) query[s] = *reinterpret_cast<const bf16x8*>(static_cast<const uint16_t*>(p.q) + at_q + 16 * s + 8 * h);
+  for (int s = 0; s < STEPS; ++s) query[s] = *reinterpret_cast<const bf16x8*>(static_cast<const uint16_t*>(p.q) + at_q + 32 * s + 8 * g);
 
   const int32_t* ids = p.block_table + static_cast<int64_t>(t.stream) * p.max_blocks;
   const int64_t head_at = static_cast<int64_t>(kvh) * p.stride_head;
   const float c = p.scale_log2e;
 
-  // ---- this wave's part of a step's requests: the rows of one group
+  // ---- this wave's part of a step's requests: half the rows of a group
   constexpr int LR = D / 8, RL = 64 / LR;                  // lanes of a row, rows of a request
   const uint32_t mem = __builtin_amdgcn_readfirstlane(lds_address(s_mem));
   const uint32_t row_bytes = static_cast<uint32_t>(p.stride_slot * 2);
-  // (i: the step, of those whose places are at hand; at: its cache block and last row)
-  const auto place_of = [&](int i) __attribute__((always_inline)) {
-    return *reinterpret_cast<const cs::u32x2*>(reinterpret_cast<const uint32_t*>(&s_place[kStepGroups * i + wave]) + 2);
-  };
-  const auto request = [&](int i, cs::u32x2 at) __attribute__((always_inline)) {
-    const int id = __builtin_amdgcn_readfirstlane(static_cast<int>(at.x)), last = __builtin_amdgcn_readfirstlane(static_cast<int>(at.y));
-    const int64_t from = (static_cast<int64_t>(id) * CS_KV_BLOCK * p.stride_slot + head_at) * 2;
-    const char* k = uniform(static_cast<const char*>(p.k) + from);
-    const char* v = uniform(static_cast<const char*>(p.v) + from);
-    const uint32_t to = mem + (i % kStages) * kStage + wave * (kTensor / kRowsWaves);
+  uint32_t row_off[kAsks], k_off[kAsks], v_off[kAsks];
+#pragma unroll
+  for (int j = 0; j < kAsks; ++j) {
+    const int row = 8 * (wave & 1) + j * RL + lane / LR;
+    row_off[j] = static_cast<uint32_t>(row) * row_bytes;
+    k_off[j] = 16 * (lane % LR ^ k_place<D>(row));
+    v_off[j] = 16 * (lane % LR ^ v_place<D>(row));
+  }
+  // A lane's group, of those whose places are at hand: first entry, readers, offsets in bytes of its last row and of its cache block.
+  int at_first = 0, at_last = 0;
+  uint32_t at_mask = 0, at_low = 0, at_high = 0;
+  const auto request = [&](int i) __attribute__((always_inline)) {
+    const int from = kStepGroups * i + (wave >> 1);
+    const uint64_t off64 = static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at_high), from))) << 32 |
+                           static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at_low), from));
+    const uint32_t last_off = static_cast<uint32_t>(__builtin_amdgcn_readlane(at_last, from));
+    const char* k = static_cast<const char*>(p.k) + off64;
+    const char* v = static_cast<const char*>(p.v) + off64;
+    const uint32_t to = mem + (i % kStages) * kStage + wave * (1024 * kAsks);
 #pragma unroll
     for (int j = 0; j < kAsks; ++j) {
-      const int row = j * RL + lane / LR;
-      const uint32_t off = static_cast<uint32_t>(min(row, last)) * row_bytes;
-      to_lds(off + 16 * (lane % LR ^ k_place<D>(row)), k, to + 1024 * j);
-      to_lds(off + 16 * (lane % LR ^ v_place<D>(row)), v, to + kTensor + 1024 * j);
+      const uint32_t off = min(row_off[j], last_off);
+      to_lds(off + k_off[j], k, to + 1024 * j);
+      to_lds(off + v_off[j], v, to + kTensor + 1024 * j);
     }
   };
 
-  f32x16 o[DB];
+  Sums<D> sums;
 #pragma unroll
-  for (int db = 0; db < DB; ++db) o[db] = f32x16{};
-  float m = -INFINITY, l = 0.0f;
+  for (int db = 0; db < DB; ++db) sums.o[db] = f32x4{};
+  sums.m = -INFINITY;
+  sums.l = 0.0f;
   // the lane's places in a stage
-  const int i16 = lane & 15, gid = (lane >> 4) & 1, v_row = 4 * h + (i16 >> 2);
-  const int k_at = n * D * 2, k_turn = k_place<D>(n), v_at = v_row * D * 2 + 8 * (i16 & 1), v_turn = v_place<D>(v_row);
-  struct Seen {
+  const int v_row = 4 * g + (r16 >> 2), k_at = r16 * D * 2, k_turn = k_place<D>(r16), v_at = v_row * D * 2 + 16 * ((r16 >> 1) & 1) + 8 * (r16 & 1), v_turn = v_place<D>(v_row);
+  const auto compute = [&](int i) __attribute__((always_inline)) {
     int first[kStepGroups];
     uint32_t mask[kStepGroups];
-  };
-  const auto seen_of = [&](int i, Seen& w) __attribute__((always_inline)) {
 #pragma unroll
     for (int b = 0; b < kStepGroups; ++b) {
-      const cs::u32x2 at = *reinterpret_cast<const cs::u32x2*>(&s_place[kStepGroups * i + b]);
-      w.first[b] = __builtin_amdgcn_readfirstlane(static_cast<int>(at.x));
-      w.mask[b] = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(at.y)));
+      first[b] = __builtin_amdgcn_readlane(at_first, kStepGroups * i + b);
+      mask[b] = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at_mask), kStepGroups * i + b));
     }
-  };
-  const auto compute = [&](int i, const Seen& w) __attribute__((always_inline)) {
-    if (((w.mask[0] | w.mask[1] | w.mask[2] | w.mask[3]) & wave_mask) == 0) return;
     const uint8_t* k = s_mem + (i % kStages) * kStage;
     const uint8_t* v = k + kTensor;
-    f32x16 s[2] = {};
+    f32x4 s[kStepGroups] = {};
 #pragma unroll
     for (int j = 0; j < STEPS; ++j)
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
-        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(k + k_at + b * 32 * D * 2 + 16 * ((2 * j + h) ^ k_turn)), query[j], s[b], 0, 0, 0);
-    // Keys of register r of 32: 8 (r / 4) + 4 h + r % 4, so registers 0..7 are the first group's.  A group that the lane's token does not read
-    // has the exponent -inf; only a group that ends behind one of the tokens is masked key by key.
-    if (max(max(w.first[0], w.first[1]), max(w.first[2], w.first[3])) + CS_KV_BLOCK - 1 > least) {
+      for (int b = 0; b < kStepGroups; ++b)
+        s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8*>(k + k_at + b * 16 * D * 2 + 16 * ((4 * j + g) ^ k_turn)), query[j], s[b], 0, 0, 0);
+    // A group that the lane's token does not read has the exponent -inf; only a group that ends behind one of the tokens is masked key
+    // by key.
+    if (max(first[0], first[1]) + CS_KV_BLOCK - 1 > least) {
 #pragma unroll
       for (int b = 0; b < kStepGroups; ++b) {
-        const int lim = pos - w.first[b] - 4 * h;
+        const int lim = pos - first[b] - 4 * g;
 #pragma unroll
-        for (int r = 0; r < 8; ++r)
-          if (8 * (r / 4) + r % 4 > lim) s[b / 2][8 * (b % 2) + r] = -INFINITY;
+        for (int r = 0; r < 4; ++r)
+          if (r > lim) s[b][r] = -INFINITY;
       }
     }
     float high = -INFINITY;
 #pragma unroll
     for (int b = 0; b < kStepGroups; ++b) {
-      const f32x16& x = s[b / 2];
-      const int r = 8 * (b % 2);
-      const float a0 = fmaxf(fmaxf(x[r], x[r + 1]), x[r + 2]), a1 = fmaxf(fmaxf(x[r + 3], x[r + 4]), x[r + 5]), a2 = fmaxf(x[r + 6], x[r + 7]);
-      const float a = fmaxf(fmaxf(a0, a1), a2);
-      high = fmaxf(high, w.mask[b] >> bit & 1 ? a : -INFINITY);
+      const float a = fmaxf(fmaxf(s[b][0], s[b][1]), fmaxf(s[b][2], s[b][3]));
+      high = fmaxf(high, mask[b] >> bit & 1 ? a : -INFINITY);
     }
+    high = fmaxf(high, cs::lane_xor16(high));
     high = fmaxf(high, cs::lane_xor32(high));
-    if (__any((high - m) * c > kSlack || m == -INFINITY)) {
-      const float raised = fmaxf(m, high);
-      const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - raised) * c);
+    if (__any((high - sums.m) * c > kSlack)) {             // (-inf - -inf: no)
+      const float raised = fmaxf(sums.m, high);
+      const float f = sums.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((sums.m - raised) * c);
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[db][r] *= f;
-      l *= f;
-      m = raised;
+        for (int r = 0; r < 4; ++r) sums.o[db][r] *= f;
+      sums.l *= f;
+      sums.m = raised;
     }
-    const float base = m == -INFINITY ? 0.0f : -m * c;
+    const float base = sums.m == -INFINITY ? 0.0f : -sums.m * c;
     float total[4] = {};
-    // of the 16 keys of a product a lane's weights are of 4 h + 0..3 and 8 + 4 h + 0..3; a row's place does not change 8 rows further
+    // of the 32 keys of a product a lane's weights are of 4 g + 0..3 of two groups; a row's place does not change 16 rows further
 #pragma unroll
-    for (int st = 0; st < kStepGroups; ++st) {
-      const float from = w.mask[st] >> bit & 1 ? base : -INFINITY;
+    for (int st = 0; st < kStepGroups / 2; ++st) {
       float x[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        x[e] = __builtin_amdgcn_exp2f(fmaf(s[st / 2][8 * (st % 2) + e], c, from));
+        const int b = 2 * st + e / 4;
+        x[e] = __builtin_amdgcn_exp2f(fmaf(s[b][e % 4], c, mask[b] >> bit & 1 ? base : -INFINITY));
         total[e % 4] += x[e];
       }
       const bf16x8 pf = __builtin_bit_cast(bf16x8, cs::u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])});
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        const uint8_t* at = v + v_at + 16 * ((4 * db + 2 * gid + ((i16 >> 1) & 1)) ^ v_turn) + 16 * st * D * 2;
+        const uint8_t* at = v + v_at + 16 * ((2 * db) ^ v_turn) + 32 * st * D * 2;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * D * 2));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * D * 2));
         const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[db], 0, 0, 0);
+        sums.o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, sums.o[db], 0, 0, 0);
       }
     }
-    l += (total[0] + total[1]) + (total[2] + total[3]);
+    sums.l += (total[0] + total[1]) + (total[2] + total[3]);
   };
 
   // ---- the steps, kPlaces groups at a time
   for (int g0 = 0; g0 < n_groups; g0 += kPlaces) {
     const int here = min(kPlaces, n_groups - g0), steps = (here + kStepGroups - 1) / kStepGroups;
-    __syncthreads();                     // (places and stages are free)
-    for (int i = tid; i < kStepGroups * steps; i += 64 * kRowsWaves) {
-      const int gi = g0 + min(i, here - 1), u = gi / p.cache_blocks;
-      const int first = (s_list[u] * p.cache_blocks + (gi - u * p.cache_blocks)) * CS_KV_BLOCK;
-      const int cb = min(first, top) / CS_KV_BLOCK;
-      s_place[i] = cs::u32x4{static_cast<uint32_t>(first), i < here ? s_mask[u] : 0u, static_cast<uint32_t>(ids[cb]),
-                             static_cast<uint32_t>(min(CS_KV_BLOCK - 1, top - cb * CS_KV_BLOCK))};
-    }
-    __syncthreads();
-    request(0, place_of(0));
+    const int gi = g0 + min(lane, here - 1), u = gi / p.cache_blocks;
+    at_first = (s_list[u] * p.cache_blocks + (gi - u * p.cache_blocks)) * CS_KV_BLOCK;
+    at_mask = lane < here ? s_mask[u] : 0;
+    const int cb = min(at_first, top) / CS_KV_BLOCK;
+    const uint64_t off64 = static_cast<uint64_t>((static_cast<int64_t>(ids[cb]) * CS_KV_BLOCK * p.stride_slot + head_at) * 2);
+    at_low = static_cast<uint32_t>(off64);
+    at_high = static_cast<uint32_t>(off64 >> 32);
+    at_last = static_cast<int>(min(CS_KV_BLOCK - 1, top - cb * CS_KV_BLOCK) * row_bytes);
+    // (bit i: whether a token of this wave reads something of step i)
+    const uint64_t groups = __ballot((at_mask & wave_mask) != 0), active = groups | groups >> 1;
+    __syncthreads();                     // (the stages are free)
+    request(0);
     for (int i = 0; i < steps; ++i) {
-      const cs::u32x2 next = place_of(min(i + 1, steps - 1));
-      Seen w;
-      seen_of(i, w);
       gate();
-      if (i + 1 < steps) request(i + 1, next);             // (into the stage that everyone has read a step ago)
-      compute(i, w);
+      if (i + 1 < steps) request(i + 1);                   // (into the stage that everyone has read a step ago)
+      if (active >> (kStepGroups * i) & 1) compute(i);
     }
   }
-  l += cs::lane_xor32(l);
+  sums.l += cs::lane_xor16(sums.l);
+  sums.l += cs::lane_xor32(sums.l);
 
   // ---- results; where something is no number or infinite, again token by token, the waves in turn
   if (tid == 0) s_odd = 0;
@@ -782,12 +782,12 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void selected_rows_kernel(Param
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) odd |= (__float_as_uint(o[db][r]) & 0x7f800000u) == 0x7f800000u;
+    for (int r = 0; r < 4; ++r) odd |= (__float_as_uint(sums.o[db][r]) & 0x7f800000u) == 0x7f800000u;
   __syncthreads();
   if (__builtin_expect(__any(odd), 0)) s_odd = 1;
   __syncthreads();
   if (__builtin_expect(s_odd, 0)) {
-    const int r16 = lane & 15, g = lane >> 4;
+    if (wave >= kAgainWaves) return;
     uint8_t* lds = s_mem + wave * Again::kLds;
     const auto locate = [&](int first_group, Group (&gr)[2]) __attribute__((always_inline)) {
 #pragma unroll
@@ -801,7 +801,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void selected_rows_kernel(Param
         gr[b].top = min(CS_KV_BLOCK - 1, top - cb * CS_KV_BLOCK);
       }
     };
-    for (int i = wave; i < t.count; i += kRowsWaves) {
+    for (int i = wave; i < t.count; i += kAgainWaves) {
       const int tok1 = t.first + i, pos1 = min(p.q_pos[tok1], entries - 1);
       const bool live1 = r16 < p.group;
       const int head1 = kvh * p.group + (live1 ? r16 : 0);
@@ -821,13 +821,10 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void selected_rows_kernel(Param
     return;
   }
   if (!live) return;
-#pragma unroll
-  for (int db = 0; db < DB; ++db)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float x[4] = {o[db][4 * r], o[db][4 * r + 1], o[db][4 * r + 2], o[db][4 * r + 3]};
-      write_row<D>(p, tok, head, 32 * db + 8 * r + 4 * h, m, l, x, true);
-    }
+  Again::each4(sums, g, [&](int ch, const float (&x)[4]) __attribute__((always_inline)) {
+    float y[4] = {x[0], x[1], x[2], x[3]};
+    write_row<D>(p, tok, head, ch, sums.m, sums.l, y, true);
+  });
 }
 
 // ---- shapes: tokens of a tile, and pieces of a sweep
