@@ -498,88 +498,87 @@ def cs_plan_evict(weight, kv_len, block_table_old, max_blocks_old, block_table_n
         n_last, int(bool(renumber)), _ptr(kept), _ptr(src_slot), _ptr(dst_slot), _ptr(delta), _ptr(kv_len_new), _ptr(weight_new), _stream()))
 
 
-def _kind(fn: str, t: Optional[torch.Tensor], dtype, what: str):
-    """Tensors that are read element by element, one behind another: of this type, contiguous."""
-    if t is not None and (t.dtype != dtype or not t.is_contiguous()):
-        raise ValueError(f"{fn}: {what} is not a contiguous tensor of {dtype}")
+_ELEMENT = {CS_F32: torch.float32, CS_BF16: torch.bfloat16}
 
 
-def _element(dtype: int):
-    return {CS_F32: torch.float32, CS_BF16: torch.bfloat16}.get(dtype)
-
-
-def _bytes(workspace, workspace_bytes, fn: str) -> int:
-    held = 0 if workspace is None else workspace.numel() * workspace.element_size()
+def _held(fn: str, specs, workspace=None, workspace_bytes=None):
+    """Addresses of a call's tensors, the bytes of its workspace, and the stream.  specs: (tensor or None, name, least number of elements
+    or None, type or None, whether its elements have to lie behind one another).  One pass: this is most of what a small call costs."""
+    ptrs, devices = [], set()
+    for t, what, n, dtype, dense in specs:
+        if t is None:
+            ptrs.append(None)
+            continue
+        if dtype is not None and t.dtype is not dtype:
+            raise ValueError(f"{fn}: {what} is not of {dtype}")
+        if dense and not t.is_contiguous():
+            raise ValueError(f"{fn}: {what} is not contiguous")
+        if n is not None and t.numel() < n:
+            raise ValueError(f"{fn}: {what} holds {t.numel()} elements, {n} needed")
+        devices.add(t.get_device())
+        ptrs.append(t.data_ptr())
+    held = 0
+    if workspace is not None:
+        held = workspace.numel() * workspace.element_size()
+        devices.add(workspace.get_device())
     if workspace_bytes is not None and held < workspace_bytes:
         raise ValueError(f"{fn}: workspace tensor smaller than workspace_bytes")
-    return held if workspace_bytes is None else workspace_bytes
+    if -1 in devices:
+        raise ValueError(f"{fn}: device tensor expected")
+    device = torch.cuda.current_device()
+    if devices and devices != {device}:      # the work goes to the current device's stream
+        raise ValueError(f"{fn}: tensors on device {sorted(devices)}, the current device is {device}")
+    return (ptrs, None if workspace is None else workspace.data_ptr(), held if workspace_bytes is None else workspace_bytes,
+            torch._C._cuda_getCurrentRawStream(device))
 
 
 def _blocks_of(max_blocks: int, sel_block: int) -> int:
-    per = max(1, sel_block // CS_KV_BLOCK)
-    return -(-max_blocks // per)
+    return -(-max_blocks // max(1, sel_block // CS_KV_BLOCK))
 
 
 def cs_norm_rope_refresh_scatter(q, q_out, k_new, v_new, q_weight, k_weight, slot, pos, axis_of_pair, inv_freq, k_cache_layer, v_cache_layer,
                                  n_tok, n_q_heads, n_kv_heads, head_dim, rotary_dim, stride_q, stride_k, stride_v, stride_slot, stride_head,
                                  norm_eps, amplitude, rope_style, dtype):
     fn = "cs_norm_rope_refresh_scatter"
-    for t in (q, q_out, k_new, v_new, q_weight, k_weight, slot, pos, axis_of_pair, inv_freq, k_cache_layer, v_cache_layer):
-        _here(fn, t)
-    for t, what in ((slot, "slot"), (pos, "pos")):
-        _kind(fn, t, torch.int32, what)
-    _need(fn, slot, n_tok, "slot"); _need(fn, pos, n_tok if axis_of_pair is None else 3 * n_tok, "pos")
-    _axes(fn, axis_of_pair, rotary_dim); _kind(fn, inv_freq, torch.float32, "inv_freq"); _need(fn, inv_freq, rotary_dim // 2, "inv_freq")
-    for t, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        _need(fn, t, head_dim, what)
-        if t is not None:
-            _kind(fn, t, _element(dtype), what)
-    for t, what in ((q, "q"), (q_out, "q_out"), (k_new, "k_new"), (v_new, "v_new"), (k_cache_layer, "k_cache_layer"), (v_cache_layer, "v_cache_layer")):
-        if t is not None and _element(dtype) is not None and t.dtype != _element(dtype):
-            raise ValueError(f"{fn}: {what} is not of the call's dtype")
+    el, i32 = _ELEMENT.get(dtype), torch.int32
     for t, stride, heads, what in ((q, stride_q, n_q_heads, "q"), (k_new, stride_k, n_kv_heads, "k_new"), (v_new, stride_v, n_kv_heads, "v_new")):
-        if not _span(t, n_tok, stride, heads * head_dim):
+        if t is not None and t.numel() < (n_tok - 1) * stride + heads * head_dim and not _span(t, n_tok, stride, heads * head_dim):
             raise ValueError(f"{fn}: {what} holds fewer than {n_tok} tokens")
-    if q_out is not None and (q is None or q_out.data_ptr() != q.data_ptr()):
-        if not q_out.is_contiguous():
-            raise ValueError(f"{fn}: q_out is not contiguous")
-        _need(fn, q_out, n_tok * n_q_heads * head_dim, "q_out")
+    apart = q_out is not None and (q is None or q_out.data_ptr() != q.data_ptr())      # (else q_out is q, with its stride)
+    p, _, _, stream = _held(fn, (
+        (q, "q", None, el, False), (q_out, "q_out", n_tok * n_q_heads * head_dim if apart else None, el, apart), (k_new, "k_new", None, el, False),
+        (v_new, "v_new", None, el, False), (q_weight, "q_weight", head_dim, el, True), (k_weight, "k_weight", head_dim, el, True),
+        (slot, "slot", n_tok, i32, True), (pos, "pos", n_tok if axis_of_pair is None else 3 * n_tok, i32, True), (axis_of_pair, "axis_of_pair", rotary_dim // 2, torch.uint8, True),
+        (inv_freq, "inv_freq", rotary_dim // 2, torch.float32, True), (k_cache_layer, "k_cache_layer", None, el, False),
+        (v_cache_layer, "v_cache_layer", None, el, False)))
     _check(fn, lib().cs_norm_rope_refresh_scatter(
-        _ptr(q), _ptr(q_out), _ptr(k_new), _ptr(v_new), _ptr(q_weight), _ptr(k_weight), _ptr(slot), _ptr(pos), _ptr(axis_of_pair), _ptr(inv_freq),
-        _ptr(k_cache_layer), _ptr(v_cache_layer), n_tok, n_q_heads, n_kv_heads, head_dim, rotary_dim, stride_q, stride_k, stride_v, stride_slot,
-        stride_head, norm_eps, amplitude, rope_style, dtype, _stream()))
+        *p, n_tok, n_q_heads, n_kv_heads, head_dim, rotary_dim, stride_q, stride_k, stride_v, stride_slot, stride_head, norm_eps, amplitude, rope_style,
+        dtype, stream))
 
 
 def cs_kv_rerotate_freqs(k_cache, v_cache, src_slot, dst_slot, delta, axis_of_pair, inv_freq, n_rows, n_layers, n_kv_heads, head_dim, rotary_dim,
                          stride_layer, stride_slot, stride_head, rope_style, dtype):
     fn = "cs_kv_rerotate_freqs"
-    for t in (k_cache, v_cache, src_slot, dst_slot, delta, axis_of_pair, inv_freq):
-        _here(fn, t)
-    for t, what in ((src_slot, "src_slot"), (dst_slot, "dst_slot"), (delta, "delta")):
-        _kind(fn, t, torch.int32, what)
-    _need(fn, src_slot, n_rows, "src_slot"); _need(fn, dst_slot, n_rows, "dst_slot")
-    _need(fn, delta, n_rows if axis_of_pair is None else 3 * n_rows, "delta")
-    _axes(fn, axis_of_pair, rotary_dim); _kind(fn, inv_freq, torch.float32, "inv_freq"); _need(fn, inv_freq, rotary_dim // 2, "inv_freq")
-    _check(fn, lib().cs_kv_rerotate_freqs(
-        _ptr(k_cache), _ptr(v_cache), _ptr(src_slot), _ptr(dst_slot), _ptr(delta), _ptr(axis_of_pair), _ptr(inv_freq), n_rows, n_layers, n_kv_heads,
-        head_dim, rotary_dim, stride_layer, stride_slot, stride_head, rope_style, dtype, _stream()))
+    el, i32 = _ELEMENT.get(dtype), torch.int32
+    p, _, _, stream = _held(fn, (
+        (k_cache, "k_cache", None, el, False), (v_cache, "v_cache", None, el, False), (src_slot, "src_slot", n_rows, i32, True),
+        (dst_slot, "dst_slot", n_rows, i32, True), (delta, "delta", n_rows if axis_of_pair is None else 3 * n_rows, i32, True),
+        (axis_of_pair, "axis_of_pair", rotary_dim // 2, torch.uint8, True), (inv_freq, "inv_freq", rotary_dim // 2, torch.float32, True)))
+    _check(fn, lib().cs_kv_rerotate_freqs(*p, n_rows, n_layers, n_kv_heads, head_dim, rotary_dim, stride_layer, stride_slot, stride_head, rope_style,
+                                          dtype, stream))
 
 
 def cs_key_bounds(k_cache_layer, first_new, kv_len, block_table, max_blocks, block_size, sel_block, bounds, scales, n_streams, n_kv_heads,
                   head_dim, stride_slot, stride_head, dtype):
     """first_new: the C call's `from`."""
     fn = "cs_key_bounds"
-    for t in (k_cache_layer, first_new, kv_len, block_table, bounds, scales):
-        _here(fn, t)
-    for t, what in ((first_new, "first_new"), (kv_len, "kv_len"), (block_table, "block_table")):
-        _kind(fn, t, torch.int32, what)
-    _need(fn, first_new, n_streams, "first_new"); _need(fn, kv_len, n_streams, "kv_len"); _need(fn, block_table, n_streams * max_blocks, "block_table")
-    places = n_streams * n_kv_heads * _blocks_of(max_blocks, sel_block)
-    _kind(fn, bounds, torch.int8, "bounds"); _need(fn, bounds, places * 2 * head_dim, "bounds")
-    _kind(fn, scales, torch.uint8, "scales"); _need(fn, scales, places, "scales")
-    _check(fn, lib().cs_key_bounds(
-        _ptr(k_cache_layer), _ptr(first_new), _ptr(kv_len), _ptr(block_table), max_blocks, block_size, sel_block, _ptr(bounds), _ptr(scales),
-        n_streams, n_kv_heads, head_dim, stride_slot, stride_head, dtype, _stream()))
+    i32, places = torch.int32, n_streams * n_kv_heads * _blocks_of(max_blocks, sel_block)
+    p, _, _, stream = _held(fn, (
+        (k_cache_layer, "k_cache_layer", None, _ELEMENT.get(dtype), False), (first_new, "first_new", n_streams, i32, True), (kv_len, "kv_len", n_streams, i32, True),
+        (block_table, "block_table", n_streams * max_blocks, i32, True), (bounds, "bounds", places * 2 * head_dim, torch.int8, True),
+        (scales, "scales", places, torch.uint8, True)))
+    _check(fn, lib().cs_key_bounds(*p[:4], max_blocks, block_size, sel_block, p[4], p[5], n_streams, n_kv_heads, head_dim, stride_slot, stride_head, dtype,
+                                   stream))
 
 
 def cs_select_blocks_workspace(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, max_blocks, sel_block) -> int:
@@ -589,21 +588,13 @@ def cs_select_blocks_workspace(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, 
 def cs_select_blocks(q, bounds, scales, cu_q, q_pos, kv_len, max_blocks, sel_block, n_select, n_first, n_last, selected, n_q, n_streams, n_q_heads,
                      n_kv_heads, head_dim, dtype, workspace=None, workspace_bytes=None):
     fn = "cs_select_blocks"
-    workspace_bytes = _bytes(workspace, workspace_bytes, fn)
-    for t in (q, bounds, scales, cu_q, q_pos, kv_len, selected, workspace):
-        _here(fn, t)
-    for t, what in ((cu_q, "cu_q"), (q_pos, "q_pos"), (kv_len, "kv_len"), (selected, "selected")):
-        _kind(fn, t, torch.int32, what)
-    if _element(dtype) is not None:
-        _kind(fn, q, _element(dtype), "q")
-    _need(fn, q, n_q * n_q_heads * head_dim, "q"); _need(fn, cu_q, n_streams + 1, "cu_q"); _need(fn, q_pos, n_q, "q_pos"); _need(fn, kv_len, n_streams, "kv_len")
-    places = n_streams * n_kv_heads * _blocks_of(max_blocks, sel_block)
-    _kind(fn, bounds, torch.int8, "bounds"); _need(fn, bounds, places * 2 * head_dim, "bounds")
-    _kind(fn, scales, torch.uint8, "scales"); _need(fn, scales, places, "scales")
-    _need(fn, selected, n_q * n_kv_heads * n_select, "selected")
-    _check(fn, lib().cs_select_blocks(
-        _ptr(q), _ptr(bounds), _ptr(scales), _ptr(cu_q), _ptr(q_pos), _ptr(kv_len), max_blocks, sel_block, n_select, n_first, n_last, _ptr(selected),
-        n_q, n_streams, n_q_heads, n_kv_heads, head_dim, dtype, _ptr(workspace), workspace_bytes, _stream()))
+    i32, places = torch.int32, n_streams * n_kv_heads * _blocks_of(max_blocks, sel_block)
+    p, ws, ws_bytes, stream = _held(fn, (
+        (q, "q", n_q * n_q_heads * head_dim, _ELEMENT.get(dtype), True), (bounds, "bounds", places * 2 * head_dim, torch.int8, True),
+        (scales, "scales", places, torch.uint8, True), (cu_q, "cu_q", n_streams + 1, i32, True), (q_pos, "q_pos", n_q, i32, True),
+        (kv_len, "kv_len", n_streams, i32, True), (selected, "selected", n_q * n_kv_heads * n_select, i32, True)), workspace, workspace_bytes)
+    _check(fn, lib().cs_select_blocks(*p[:6], max_blocks, sel_block, n_select, n_first, n_last, p[6], n_q, n_streams, n_q_heads, n_kv_heads, head_dim, dtype,
+                                      ws, ws_bytes, stream))
 
 
 def cs_selected_attn_workspace(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, sel_block, n_select) -> int:
@@ -614,21 +605,11 @@ def cs_selected_attn(q, k_cache_layer, v_cache_layer, cu_q, q_pos, kv_len, block
                      lse, n_q, n_streams, n_q_heads, n_kv_heads, head_dim, stride_slot, stride_head, softmax_scale, dtype, workspace=None,
                      workspace_bytes=None):
     fn = "cs_selected_attn"
-    workspace_bytes = _bytes(workspace, workspace_bytes, fn)
-    for t in (q, k_cache_layer, v_cache_layer, cu_q, q_pos, kv_len, block_table, selected, out, lse, workspace):
-        _here(fn, t)
-    for t, what in ((cu_q, "cu_q"), (q_pos, "q_pos"), (kv_len, "kv_len"), (block_table, "block_table"), (selected, "selected")):
-        _kind(fn, t, torch.int32, what)
-    if _element(dtype) is not None:
-        _kind(fn, q, _element(dtype), "q"); _kind(fn, out, _element(dtype), "out")
-        for t, what in ((k_cache_layer, "k_cache_layer"), (v_cache_layer, "v_cache_layer")):
-            if t is not None and t.dtype != _element(dtype):
-                raise ValueError(f"{fn}: {what} is not of the call's dtype")
-    _kind(fn, lse, torch.float32, "lse")
-    _need(fn, q, n_q * n_q_heads * head_dim, "q"); _need(fn, out, n_q * n_q_heads * head_dim, "out"); _need(fn, lse, n_q * n_q_heads, "lse")
-    _need(fn, cu_q, n_streams + 1, "cu_q"); _need(fn, q_pos, n_q, "q_pos"); _need(fn, kv_len, n_streams, "kv_len")
-    _need(fn, block_table, n_streams * max_blocks, "block_table"); _need(fn, selected, n_q * n_kv_heads * n_select, "selected")
-    _check(fn, lib().cs_selected_attn(
-        _ptr(q), _ptr(k_cache_layer), _ptr(v_cache_layer), _ptr(cu_q), _ptr(q_pos), _ptr(kv_len), _ptr(block_table), max_blocks, block_size,
-        _ptr(selected), sel_block, n_select, _ptr(out), _ptr(lse), n_q, n_streams, n_q_heads, n_kv_heads, head_dim, stride_slot, stride_head,
-        softmax_scale, dtype, _ptr(workspace), workspace_bytes, _stream()))
+    el, i32 = _ELEMENT.get(dtype), torch.int32
+    p, ws, ws_bytes, stream = _held(fn, (
+        (q, "q", n_q * n_q_heads * head_dim, el, True), (k_cache_layer, "k_cache_layer", None, el, False), (v_cache_layer, "v_cache_layer", None, el, False),
+        (cu_q, "cu_q", n_streams + 1, i32, True), (q_pos, "q_pos", n_q, i32, True), (kv_len, "kv_len", n_streams, i32, True),
+        (block_table, "block_table", n_streams * max_blocks, i32, True), (selected, "selected", n_q * n_kv_heads * n_select, i32, True),
+        (out, "out", n_q * n_q_heads * head_dim, el, True), (lse, "lse", n_q * n_q_heads, torch.float32, True)), workspace, workspace_bytes)
+    _check(fn, lib().cs_selected_attn(*p[:7], max_blocks, block_size, p[7], sel_block, n_select, p[8], p[9], n_q, n_streams, n_q_heads, n_kv_heads, head_dim,
+                                      stride_slot, stride_head, softmax_scale, dtype, ws, ws_bytes, stream))

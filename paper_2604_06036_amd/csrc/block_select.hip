@@ -47,6 +47,7 @@ struct BoundsParams {
   int32_t walkers;                       // waves that share the blocks of a stream and kv head
 };
 
+constexpr int kManyWaves = 1 << 20, kFewWaves = 1024;      // waves at most, and where only the blocks from `from` on are made
 // A wave takes a block, lanes side by side on a row's channels; a wave goes on with the block `walkers` further.
 // UC cache blocks are asked for at once.
 template <bool kBf16, int D, int UC>
@@ -57,13 +58,11 @@ __global__ __launch_bounds__(256) void key_bounds_kernel(BoundsParams p) {
   constexpr int RL = 64 / LR;            // rows a load
   constexpr int NL = CS_KV_BLOCK / RL;   // loads a cache block
   const int lane = threadIdx.x & 63;
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kvh = static_cast<int>(unit % p.n_kv_heads);
-  const int64_t rest = unit / p.n_kv_heads;
-  const int walker = static_cast<int>(rest % p.walkers);
-  const int64_t stream64 = rest / p.walkers;
-  if (stream64 >= p.n_streams) return;
-  const int stream = static_cast<int>(stream64);
+  const uint32_t unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // (below 2^26 * 4)
+  const uint32_t rest = unit / static_cast<uint32_t>(p.n_kv_heads);
+  const int kvh = static_cast<int>(unit - rest * p.n_kv_heads), stream = static_cast<int>(rest / static_cast<uint32_t>(p.walkers));
+  const int walker = static_cast<int>(rest - static_cast<uint32_t>(stream) * p.walkers);
+  if (stream >= p.n_streams) return;
   const int entries = min(p.kv_len[stream], p.max_blocks * CS_KV_BLOCK);
   const int size = p.cache_blocks * CS_KV_BLOCK;
   const int first = p.from ? max(p.from[stream], 0) / size : 0;
@@ -154,7 +153,7 @@ struct SelectParams {
   int32_t max_blocks, n_streams, n_q_heads, n_kv_heads, group, n_sel, size, n_select, n_first, n_last, tile, pitch;
 };
 
-constexpr int kWaves = 4;
+constexpr int kManyTokens = 8;           // a stream, on average, from which workgroups take two tiles of rows
 constexpr int kMostBlocks = 32768;       // whose scores a workgroup holds in LDS for one token
 constexpr int kTileScores = 8192;        // ... for a tile of tokens
 
@@ -163,107 +162,120 @@ __device__ __forceinline__ uint32_t ordered(float x) {
   const uint32_t u = __float_as_uint(x);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-constexpr uint32_t kFixed = 0xffffffffu, kOdd = 0xfffffffeu;     // always kept, a block that holds what is no number
+constexpr uint32_t kOdd = 0xfffffffeu;    // ... of a block that holds what is no number
 
-// The query's list from the scores of its n blocks: `at(c)` is the lane's of chunk c, of 64 blocks.  C: chunks (at least n / 64), or 0: counted
-// when the kernel runs.  The threshold is found bit by bit, counting by ballots: the largest T with at least n_select scores >= T.
+// The query's list from the scores of its n blocks, more than n_select: those of the first n_first, the last n_last, and the n_select -
+// n_first - n_last largest of the others.  `at(c)` is the lane's score of chunk c, of 64 blocks; fixed blocks and places past n have 0.
+// C: chunks (at least n / 64), or 0: counted when the kernel runs.  The threshold is found bit by bit from the first one in which the
+// scores differ, counting by ballots: the largest T with at least as many scores >= T as are wanted.
 template <int C, class F>
-__device__ __forceinline__ void write_list(const F& at, int n, int n_select, int32_t* out, int lane) {
-  const int chunks = C ? C : (n + 63) / 64;
-  uint32_t t = 0;
-  for (int bit = 31; bit >= 0; --bit) {
-    const uint32_t cand = t | 1u << bit;
-    int count = 0;
+__device__ __forceinline__ void write_list(const F& at, int n, int n_first, int n_last, int n_select, int32_t* out, int lane) {
+  const int chunks = C ? C : (n + 63) / 64, wanted = n_select - n_first - n_last;
+  uint32_t t = 0xffffffffu;                            // (nothing is wanted)
+  int above = 0;                                       // scores > T
+  if (wanted > 0) {
+    uint32_t high = 0, low = 0xffffffffu;
 #pragma unroll
-    for (int c = 0; c < chunks; ++c) count += __popcll(__ballot(at(c) >= cand));
-    if (count >= n_select) {
-      t = cand;
-      if (count == n_select) break;
+    for (int c = 0; c < chunks; ++c) {
+      const uint32_t x = at(c);
+      high = max(high, x);
+      low = min(low, x ? x : 0xffffffffu);
     }
-  }
-  int above = 0;
+    high = __builtin_amdgcn_readfirstlane(cs::lanes_max<64>(high));
+    low = ~__builtin_amdgcn_readfirstlane(cs::lanes_max<64>(~low));
+    const int first_bit = 31 - __clz(high ^ low);      // (-1: all are equal)
+    t = first_bit < 0 ? high : high & ~(0xffffffffu >> (31 - first_bit));
+    for (int bit = first_bit; bit >= 0; --bit) {
+      const uint32_t cand = t | 1u << bit;
+      int count = 0;
 #pragma unroll
-  for (int c = 0; c < chunks; ++c) above += __popcll(__ballot(at(c) > t));
-  int ties = n_select - above, place = 0;              // (more than n_select scores: the threshold is one of them)
+      for (int c = 0; c < chunks; ++c) count += __popcll(__ballot(at(c) >= cand));
+      if (count >= wanted) {
+        t = cand;
+        if (count == wanted) break;
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < chunks; ++c) above += __popcll(__ballot(at(c) > t));
+  }
+  int ties = wanted - above, place = 0;
   const uint64_t below = (1ull << lane) - 1;
 #pragma unroll
   for (int c = 0; c < chunks; ++c) {
     const uint32_t x = at(c);
+    const int block = c * 64 + lane;
+    const bool fixed = block < n && (block < n_first || block >= n - n_last);
     const uint64_t equal = __ballot(x == t);
-    const bool taken = x > t || (x == t && __popcll(equal & below) < ties);
+    const bool taken = fixed || x > t || (x == t && __popcll(equal & below) < ties);
     const uint64_t all = __ballot(taken);
-    if (taken) out[place + __popcll(all & below)] = c * 64 + lane;
+    if (taken) out[place + __popcll(all & below)] = block;
     place += __popcll(all);
     ties -= min(ties, __popcll(equal));
   }
 }
 
 template <int C, class F>
-__device__ __forceinline__ void write_list_held(const F& key, int n, int n_select, int32_t* out, int lane) {
+__device__ __forceinline__ void write_list_held(const F& key, int n, int n_first, int n_last, int n_select, int32_t* out, int lane) {
   uint32_t held[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) held[c] = key(c * 64 + lane);
-  write_list<C>([&](int c) __attribute__((always_inline)) { return held[c]; }, n, n_select, out, lane);
+  write_list<C>([&](int c) __attribute__((always_inline)) { return held[c]; }, n, n_first, n_last, n_select, out, lane);
 }
 
-// A workgroup takes a tile of a stream's tokens and a kv head.  Rows of the product are (token, head), the heads of a token padded to GP
-// by the last of them and spread so that they are neighbouring registers of a lane; columns are blocks, 32 at a time, the waves in turn.
-template <bool kBf16, int D, int GP>
-__global__ __launch_bounds__(64 * kWaves) void select_blocks_kernel(SelectParams p) {
+// A workgroup of W waves takes a tile of a stream's tokens and a kv head.  Rows of the product are (token, head), MT times 32, the heads of a
+// token padded to GP by the last of them and spread so that they are neighbouring registers of a lane; columns are blocks, 32 at a time, the
+// waves in turn.
+template <bool kBf16, int D, int GP, int W, int MT>
+__global__ __launch_bounds__(64 * W) void select_blocks_kernel(SelectParams p) {
   constexpr int STEPS = 2 * D / 32;
   constexpr int QROW = 2 * D + 16;
-  constexpr int TOK = 32 / GP;           // tokens that 32 rows hold
-  __shared__ __attribute__((aligned(16))) uint8_t s_q[32 * QROW];
+  constexpr int TOK = 32 / GP < 8 ? 32 / GP : 8;         // tokens of 32 rows
+  constexpr int VE = kBf16 ? 8 : 4;
+  constexpr int CHUNKS = D / VE, HELD = (GP * CHUNKS + 63) / 64;       // 16-byte pieces of a head, and of a token a lane holds
+  __shared__ __attribute__((aligned(16))) uint8_t s_q[MT * 32 * QROW];
   extern __shared__ __attribute__((aligned(16))) uint32_t s_score[];      // [tile][pitch]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = static_cast<int>(blockIdx.x % p.n_kv_heads);
   cs::TokenTile t;
   if (!cs::find_token_tile(p.cu_q, p.n_streams, p.n_q, p.tile, static_cast<int>(blockIdx.x / p.n_kv_heads), &t)) return;
-  const int entries = min(p.kv_len[t.stream], p.max_blocks * CS_KV_BLOCK);
-  const auto candidates = [&](int i) __attribute__((always_inline)) {
-    const int last = min(p.q_pos[t.first + i], entries - 1);
-    return last < 0 ? 0 : last / p.size + 1;
-  };
 
   // ---- whole numbers of the tile's queries: a wave takes a token, 16 bytes a lane
-  for (int i = tid; i < 32 * QROW / 16; i += 64 * kWaves) reinterpret_cast<cs::u32x4*>(s_q)[i] = cs::u32x4{0, 0, 0, 0};
-  __syncthreads();
-  int most = 0;                          // candidates of any of the tokens
-  for (int i = 0; i < t.count; ++i) most = max(most, candidates(i));
-  for (int i = wave; i < t.count; i += kWaves) {
-    constexpr int VE = kBf16 ? 8 : 4;
-    const int chunks = p.group * (D / VE);
+  const auto number = [&](const cs::u32x4& v, int e) __attribute__((always_inline)) {
+    const uint32_t w = v[kBf16 ? e / 2 : e];
+    return kBf16 ? (e & 1 ? w & 0xffff0000u : w << 16) : w;
+  };
+  for (int i = wave; i < t.count; i += W) {
     const int64_t from = (static_cast<int64_t>(t.first + i) * p.n_q_heads + static_cast<int64_t>(kvh) * p.group) * D;
+    cs::u32x4 v[HELD];
     uint32_t amax = 0;
-    for (int c = lane; c < chunks; c += 64) {
-      cs::u32x4 v;
-      if constexpr (kBf16) v = *reinterpret_cast<const cs::u32x4*>(static_cast<const uint16_t*>(p.q) + from + c * VE);
-      else v = *reinterpret_cast<const cs::u32x4*>(static_cast<const float*>(p.q) + from + c * VE);
 #pragma unroll
-      for (int e = 0; e < VE; ++e) {
-        const uint32_t w = v[kBf16 ? e / 2 : e];
-        amax = max(amax, (kBf16 ? (e & 1 ? w & 0xffff0000u : w << 16) : w) & 0x7fffffffu);
-      }
+    for (int j = 0; j < HELD; ++j) {
+      const int c = j * 64 + lane, head = min(c / CHUNKS, p.group - 1);      // (past the group: its last head again)
+      const int64_t at = from + head * D + c % CHUNKS * VE;
+      if constexpr (kBf16) v[j] = *reinterpret_cast<const cs::u32x4*>(static_cast<const uint16_t*>(p.q) + at);
+      else v[j] = *reinterpret_cast<const cs::u32x4*>(static_cast<const float*>(p.q) + at);
     }
+#pragma unroll
+    for (int j = 0; j < HELD; ++j)
+#pragma unroll
+      for (int e = 0; e < VE; ++e) amax = max(amax, number(v[j], e) & 0x7fffffffu);
     const uint32_t byte = scale_byte(cs::lanes_max<64>(amax));
-    if (byte == kNoNumber) continue;     // (its rows stay 0)
-    const float inv = inverse_scale(byte);
-    for (int c = lane; c < GP * (D / VE); c += 64) {
-      const int slot = c / (D / VE), head = min(slot, p.group - 1), col = c % (D / VE) * VE;
-      cs::u32x4 v;
-      if constexpr (kBf16) v = *reinterpret_cast<const cs::u32x4*>(static_cast<const uint16_t*>(p.q) + from + head * D + col);
-      else v = *reinterpret_cast<const cs::u32x4*>(static_cast<const float*>(p.q) + from + head * D + col);
+    const float inv = byte == kNoNumber ? 0.0f : inverse_scale(byte);
+#pragma unroll
+    for (int j = 0; j < HELD; ++j) {
+      const int c = j * 64 + lane, slot = c / CHUNKS;
+      if (slot >= GP) continue;
       uint32_t up[VE / 4] = {}, down[VE / 4] = {};
 #pragma unroll
       for (int e = 0; e < VE; ++e) {
-        const uint32_t w = v[kBf16 ? e / 2 : e];
-        const int code = static_cast<int>(rintf(__uint_as_float(kBf16 ? (e & 1 ? w & 0xffff0000u : w << 16) : w) * inv));
+        // (a query that holds what is no number: 0 throughout)
+        const int code = byte == kNoNumber ? 0 : static_cast<int>(rintf(__uint_as_float(number(v[j], e)) * inv));
         up[e / 4] |= static_cast<uint32_t>(max(code, 0)) << (8 * (e % 4));
         down[e / 4] |= (static_cast<uint32_t>(min(code, 0)) & 0xffu) << (8 * (e % 4));
       }
-      // token i is pair i / 2 of half i % 2: registers GP (i / 2) + slot of the lanes of that half, rows 8 (r / 4) + 4 half + r % 4
-      const int r = GP * (i / 2) + slot, row = 8 * (r / 4) + 4 * (i % 2) + r % 4;
-      uint8_t* dst = s_q + row * QROW + col;
+      // of 32 rows, token k is pair k / 2 of half k % 2: registers GP (k / 2) + slot of the lanes of that half, rows 8 (r / 4) + 4 half + r % 4
+      const int k = i % TOK, r = GP * (k / 2) + slot, row = i / TOK * 32 + 8 * (r / 4) + 4 * (k % 2) + r % 4;
+      uint8_t* dst = s_q + row * QROW + c % CHUNKS * VE;
       if constexpr (VE == 8) {
         *reinterpret_cast<cs::u32x2*>(dst) = cs::u32x2{up[0], up[1]};
         *reinterpret_cast<cs::u32x2*>(dst + D) = cs::u32x2{down[0], down[1]};
@@ -273,34 +285,42 @@ __global__ __launch_bounds__(64 * kWaves) void select_blocks_kernel(SelectParams
       }
     }
   }
+  // candidates of the token of a lane, and of any
+  const int entries = min(p.kv_len[t.stream], p.max_blocks * CS_KV_BLOCK);
+  const int last = lane < t.count ? min(p.q_pos[t.first + lane], entries - 1) : -1;
+  const int candidates = last < 0 ? 0 : last / p.size + 1;
+  const int most = __builtin_amdgcn_readfirstlane(static_cast<int>(cs::lanes_max<64>(static_cast<uint32_t>(candidates))));
   __syncthreads();
 
-  // ---- scores
+  // ---- scores (rows without a token hold anything: nobody reads theirs)
   if (most > p.n_select) {
     const int n = lane & 31, h = lane >> 5;
-    i32x4 a[STEPS];
-#pragma unroll
-    for (int s = 0; s < STEPS; ++s) a[s] = *reinterpret_cast<const i32x4*>(s_q + n * QROW + 32 * s + 16 * h);
     const int64_t head_at = (static_cast<int64_t>(t.stream) * p.n_kv_heads + kvh) * p.n_sel;
-    for (int b0 = wave * 32; b0 < most; b0 += 32 * kWaves) {
+    i32x4 a[MT][STEPS];
+#pragma unroll
+    for (int k = 0; k < MT; ++k)
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) a[k][s] = *reinterpret_cast<const i32x4*>(s_q + (32 * k + n) * QROW + 32 * s + 16 * h);
+    for (int b0 = wave * 32; b0 < most; b0 += 32 * W) {
       const int block = min(b0 + n, most - 1);
       const int8_t* from = p.bounds + (head_at + block) * 2 * D + 16 * h;
       const uint32_t byte = p.scales[head_at + block];
       i32x4 b[STEPS];
 #pragma unroll
       for (int s = 0; s < STEPS; ++s) b[s] = *reinterpret_cast<const i32x4*>(from + 32 * s);
-      i32x16 acc = {};
-#pragma unroll
-      for (int s = 0; s < STEPS; ++s) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[s], b[s], acc, 0, 0, 0);
       const float scale = __uint_as_float((byte - 21u) << 23);           // 2^(k - 21)
-      if (b0 + n < most) {
 #pragma unroll
-        for (int g = 0; g < 16 / GP; ++g) {
+      for (int k = 0; k < MT; ++k) {
+        i32x16 acc = {};
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[k][s], b[s], acc, 0, 0, 0);
+#pragma unroll
+        for (int g = 0; g < (TOK + 1) / 2; ++g) {
           int top = acc[g * GP];
 #pragma unroll
           for (int i = 1; i < GP; ++i) top = max(top, acc[g * GP + i]);
-          const int tok = 2 * g + h;
-          if (tok < t.count) s_score[tok * p.pitch + block] = byte == kNoNumber ? kOdd : ordered(static_cast<float>(top) * scale);
+          const int tok = k * TOK + 2 * g + h;
+          if (b0 + n < most && tok < t.count) s_score[tok * p.pitch + block] = byte == kNoNumber ? kOdd : ordered(static_cast<float>(top) * scale);
         }
       }
     }
@@ -308,21 +328,22 @@ __global__ __launch_bounds__(64 * kWaves) void select_blocks_kernel(SelectParams
   __syncthreads();
 
   // ---- lists: a wave takes a token
-  for (int i = wave; i < t.count; i += kWaves) {
-    const int n = candidates(i);
+  for (int i = wave; i < t.count; i += W) {
+    const int n = __builtin_amdgcn_readlane(candidates, i);
     int32_t* out = p.selected + (static_cast<int64_t>(t.first + i) * p.n_kv_heads + kvh) * p.n_select;
     if (n <= p.n_select) {
       for (int c = lane; c < p.n_select; c += 64) out[c] = c < n ? c : -1;
       continue;
     }
     const uint32_t* score = s_score + i * p.pitch;
-    const auto key = [&](int b) __attribute__((always_inline)) -> uint32_t {
-      if (b >= n) return 0u;
-      return b < p.n_first || b >= n - p.n_last ? kFixed : score[b];
-    };
-    if (n <= 256) write_list_held<4>(key, n, p.n_select, out, lane);
-    else if (n <= 512) write_list_held<8>(key, n, p.n_select, out, lane);
-    else write_list<0>([&](int c) __attribute__((always_inline)) { return key(c * 64 + lane); }, n, p.n_select, out, lane);
+    const auto key = [&](int b) __attribute__((always_inline)) -> uint32_t { return b < p.n_first || b >= n - p.n_last ? 0u : score[b]; };
+#define CS_LIST(C) write_list_held<C>(key, n, p.n_first, p.n_last, p.n_select, out, lane)
+    if (n <= 128) CS_LIST(2);
+    else if (n <= 256) CS_LIST(4);
+    else if (n <= 320) CS_LIST(5);
+    else if (n <= 512) CS_LIST(8);
+    else write_list<0>([&](int c) __attribute__((always_inline)) { return key(c * 64 + lane); }, n, p.n_first, p.n_last, p.n_select, out, lane);
+#undef CS_LIST
   }
 }
 
@@ -356,7 +377,7 @@ extern "C" int cs_key_bounds(const void* k_cache_layer, const int32_t* from, con
   p.cache_blocks = sel_block / CS_KV_BLOCK;
   p.n_sel = (max_blocks + p.cache_blocks - 1) / p.cache_blocks;
   const int64_t pairs = static_cast<int64_t>(n_streams) * n_kv_heads;
-  const int64_t wanted = (16384 + pairs - 1) / pairs;
+  const int64_t wanted = ((from ? kFewWaves : kManyWaves) + pairs - 1) / pairs;
   p.walkers = static_cast<int32_t>(wanted < p.n_sel ? wanted : p.n_sel);
   const int64_t groups = (pairs * p.walkers + 3) / 4;
   if (groups > cs::kMostThreads / 256) return CS_EUNSUPPORTED;
@@ -420,21 +441,30 @@ extern "C" int cs_select_blocks(const void* q, const int8_t* bounds, const uint8
   int gp = 1;
   while (gp < p.group) gp *= 2;
   p.pitch = n_sel;
-  p.tile = 32 / gp < 8 ? 32 / gp : 8;
+  // Few tokens: a workgroup's 16 waves share the blocks of one 32-row tile; many: four waves take two tiles, so that bounds are read half
+  // as often.
+  const int tok = 32 / gp < 8 ? 32 / gp : 8;
+  const bool many = n_q >= static_cast<int64_t>(kManyTokens) * n_streams;
+  p.tile = many ? 2 * tok : tok;
   while (p.tile > 1 && static_cast<int64_t>(p.tile) * p.pitch > kTileScores) p.tile /= 2;
   const int64_t tiles = cs::most_token_tiles(n_q, n_streams, p.tile), groups = tiles * n_kv_heads;
-  if (groups > cs::kMostThreads / (64 * kWaves)) return CS_EUNSUPPORTED;
+  if (groups > cs::kMostThreads / 1024) return CS_EUNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(groups));
   const size_t lds = static_cast<size_t>(p.tile) * p.pitch * sizeof(uint32_t);
   hipStream_t st = cs::as_stream(stream);
-#define CS_LAUNCH_SELECT(BF16, D, GP)                                                                                                       \
+#define CS_LAUNCH_SELECT_SHAPE(BF16, D, GP, W, MT)                                                                                         \
   do {                                                                                                                                     \
     if (lds > 48 * 1024) {                                                                                                                 \
-      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(select_blocks_kernel<BF16, D, GP>),                           \
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(select_blocks_kernel<BF16, D, GP, W, MT>),                    \
                                                hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));                         \
       if (e != hipSuccess) return cs::note_hip(e);                                                                                         \
     }                                                                                                                                      \
-    hipLaunchKernelGGL((select_blocks_kernel<BF16, D, GP>), grid, dim3(64 * kWaves), lds, st, p);                                          \
+    hipLaunchKernelGGL((select_blocks_kernel<BF16, D, GP, W, MT>), grid, dim3(64 * W), lds, st, p);                                        \
+  } while (0)
+#define CS_LAUNCH_SELECT(BF16, D, GP)                        \
+  do {                                                       \
+    if (many) CS_LAUNCH_SELECT_SHAPE(BF16, D, GP, 4, 2);     \
+    else CS_LAUNCH_SELECT_SHAPE(BF16, D, GP, 16, 1);         \
   } while (0)
 #define CS_LAUNCH_SELECT_GROUP(BF16, D)              \
   do {                                               \
@@ -452,6 +482,7 @@ extern "C" int cs_select_blocks(const void* q, const int8_t* bounds, const uint8
     else CS_LAUNCH_SELECT_GROUP(false, 64);
   }
 #undef CS_LAUNCH_SELECT_GROUP
+#undef CS_LAUNCH_SELECT_SHAPE
 #undef CS_LAUNCH_SELECT
   return cs::note_hip(hipGetLastError());
 }

@@ -312,21 +312,37 @@ __device__ __forceinline__ void sweep(const Params& p, const Kind& kind, const L
   }
 }
 
-// What is joined: WAYS results of 16 rows, `ml` [way][16][2] and `o` [way][16][D].  A thread takes four channels of a row.
+constexpr int kJoinBatch = 8;
+// What is joined: results of 16 rows, `ml` [way][16][2] and `o` [way][16][D].  A thread takes four channels of a row, kJoinBatch ways at a time.
 template <int D>
 __device__ __forceinline__ void join_rows(const float* ml, const float* o, int ways, int row, int ch, float c, float* m_out, float* l_out, float (&x)[4]) {
-  float m = -INFINITY;
-  for (int w = 0; w < ways; ++w) m = fmaxf(m, ml[(w * kRows + row) * 2]);
-  float l = 0.0f;
+  float m = -INFINITY, l = 0.0f;
   x[0] = x[1] = x[2] = x[3] = 0.0f;
-  for (int w = 0; w < ways; ++w) {
-    const float mw = ml[(w * kRows + row) * 2], lw = ml[(w * kRows + row) * 2 + 1];
-    if (mw == -INFINITY && lw == 0.0f) continue;         // (saw nothing)
-    const float f = mw == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((mw - m) * c);
-    const f32x4 v = *reinterpret_cast<const f32x4*>(o + (w * kRows + row) * D + ch);
-    l = fmaf(lw, f, l);
+  for (int w0 = 0; w0 < ways; w0 += kJoinBatch) {
+    cs::f32v2 stat[kJoinBatch];
+    f32x4 v[kJoinBatch];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = fmaf(v[e], f, x[e]);
+    for (int i = 0; i < kJoinBatch; ++i) {
+      const int w = min(w0 + i, ways - 1);
+      stat[i] = *reinterpret_cast<const cs::f32v2*>(ml + (w * kRows + row) * 2);
+      v[i] = *reinterpret_cast<const f32x4*>(o + (w * kRows + row) * D + ch);
+    }
+    float high = m;
+#pragma unroll
+    for (int i = 0; i < kJoinBatch; ++i) high = fmaxf(high, stat[i].x);
+    const float back = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - high) * c);      // (without a maximum there are only zeros, or what is no number)
+    l *= back;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] *= back;
+    m = high;
+#pragma unroll
+    for (int i = 0; i < kJoinBatch; ++i) {
+      if (w0 + i >= ways) break;
+      const float f = stat[i].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((stat[i].x - m) * c);
+      l = fmaf(stat[i].y, f, l);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = fmaf(v[i][e], f, x[e]);
+    }
   }
   *m_out = m;
   *l_out = l;
@@ -355,59 +371,70 @@ __global__ __launch_bounds__(64 * NW) void selected_attn_kernel(Params p) {
   const int job = static_cast<int>(blockIdx.x / p.n_kv_heads), piece = job % p.pieces, tile = job / p.pieces;
   cs::TokenTile t;
   if (!cs::find_token_tile(p.cu_q, p.n_streams, p.n_q, p.tile, tile, &t)) return;
-  const int entries = min(p.kv_len[t.stream], p.max_blocks * CS_KV_BLOCK);
-  if (entries <= 0) return;              // (such a stream's rows are left as they were)
   const int size = p.cache_blocks * CS_KV_BLOCK;
+  const int n_keys = t.count * p.n_select;
+  const auto listed = [&](int i) __attribute__((always_inline)) {
+    return i < n_keys ? p.selected[(static_cast<int64_t>(t.first + i / p.n_select) * p.n_kv_heads + kvh) * p.n_select + i % p.n_select] : -1;
+  };
+  const int mine = listed(lane);         // (asked for with the length and the position)
+  const int entries = min(p.kv_len[t.stream], p.max_blocks * CS_KV_BLOCK);
+  const int first_pos = p.q_pos[t.first];
+  if (entries <= 0) return;              // (such a stream's rows are left as they were)
 
   // ---- the tile's lists as one
-  const int n_keys = t.count * p.n_select;
-  for (int i = tid; i < kMostListed; i += 64 * NW) {
-    int key = 0x7fffffff;
-    if (i < n_keys) {
-      const int tok = t.first + i / p.n_select;
-      const int last = min(p.q_pos[tok], entries - 1);
-      const int block = p.selected[(static_cast<int64_t>(tok) * p.n_kv_heads + kvh) * p.n_select + i % p.n_select];
-      if (block >= 0 && last >= 0 && block <= last / size) key = block;
-    }
-    s_key[i] = key;
-  }
-  __syncthreads();
-  const int padded = (n_keys + 3) & ~3;
-  for (int i = tid; i < padded; i += 64 * NW) {
-    const int key = s_key[i];
-    int rank = 0;
-    for (int j = 0; j < padded; j += 4) {
-      const cs::u32x4 other = *reinterpret_cast<const cs::u32x4*>(s_key + j);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int o = static_cast<int>(other[e]);
-        rank += o < key || (o == key && j + e < i) ? 1 : 0;
+  int n_blocks;
+  const auto usable = [&](int block, int pos) __attribute__((always_inline)) {
+    const int last = min(pos, entries - 1);
+    return block >= 0 && last >= 0 && block <= last / size ? block : 0x7fffffff;
+  };
+  const int key0 = usable(mine, first_pos);
+  const int before0 = __builtin_amdgcn_update_dpp(-1, key0, 0x138, 0xf, 0xf, false);      // of the lane before (wave_shr:1)
+  if (t.count == 1 && n_keys <= 64 && __all(key0 > before0 || key0 == 0x7fffffff)) {
+    // One token whose list ascends, as a selection leaves it: every wave writes it for itself (what the others write is the same).
+    s_list[lane] = key0;
+    s_mask[lane] = 1;
+    n_blocks = __popcll(__ballot(key0 != 0x7fffffff));
+  } else {
+    for (int i = tid; i < kMostListed; i += 64 * NW) s_key[i] = i < n_keys ? usable(listed(i), p.q_pos[t.first + i / p.n_select]) : 0x7fffffff;
+    __syncthreads();
+    const int padded = (n_keys + 3) & ~3;
+    for (int i = tid; i < padded; i += 64 * NW) {
+      const int key = s_key[i];
+      int rank = 0;
+      for (int j = 0; j < padded; j += 4) {
+        const cs::u32x4 other = *reinterpret_cast<const cs::u32x4*>(s_key + j);
+  #pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int o = static_cast<int>(other[e]);
+          rank += o < key || (o == key && j + e < i) ? 1 : 0;
+        }
       }
+      s_sorted[rank] = key;
+      s_tok[rank] = i / p.n_select;
     }
-    s_sorted[rank] = key;
-    s_tok[rank] = i / p.n_select;
-  }
-  __syncthreads();
-  if (wave == 0) {
-    int base = 0;
-    for (int i0 = 0; i0 < padded; i0 += 64) {
-      const int i = i0 + lane;
-      const int key = i < padded ? s_sorted[i] : 0x7fffffff;
-      const bool first = key != 0x7fffffff && (i == 0 || s_sorted[i - 1] != key);
-      const uint64_t all = __ballot(first);
-      if (first) {
-        int mask = 0;
-        for (int j = i; j < padded && s_sorted[j] == key; ++j) mask |= 1 << s_tok[j];
-        const int at = base + __popcll(all & ((1ull << lane) - 1));
-        s_list[at] = key;
-        s_mask[at] = mask;
+    __syncthreads();
+    if (wave == 0) {
+      int base = 0;
+      for (int i0 = 0; i0 < padded; i0 += 64) {
+        const int i = i0 + lane;
+        const int key = i < padded ? s_sorted[i] : 0x7fffffff;
+        const bool first = key != 0x7fffffff && (i == 0 || s_sorted[i - 1] != key);
+        const uint64_t all = __ballot(first);
+        if (first) {
+          int mask = 0;
+          for (int j = i; j < padded && s_sorted[j] == key; ++j) mask |= 1 << s_tok[j];
+          const int at = base + __popcll(all & ((1ull << lane) - 1));
+          s_list[at] = key;
+          s_mask[at] = mask;
+        }
+        base += __popcll(all);
       }
-      base += __popcll(all);
+      if (lane == 0) s_count = base;
     }
-    if (lane == 0) s_count = base;
+    __syncthreads();
+    n_blocks = __builtin_amdgcn_readfirstlane(s_count);
   }
-  __syncthreads();
-  const int n_groups = __builtin_amdgcn_readfirstlane(s_count) * p.cache_blocks;
+  const int n_groups = n_blocks * p.cache_blocks;
 
   // ---- the lane's row
   const int tau = r16 / p.group;
@@ -838,8 +865,10 @@ struct Shape {
   int tile, pieces, waves;
   int64_t tiles;
 };
+constexpr int kGroupsWanted = 512;       // workgroups wanted of the few-rows kernel
+constexpr int kMostPieces = 8;
 constexpr int kManyTokens = 8;           // a stream, on average, from which the rows kernel is taken
-Shape shape_of(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_select, bool bf16, int64_t stride_slot) {
+Shape shape_of(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads, int32_t sel_block, int32_t n_select, bool bf16, int64_t stride_slot) {
   Shape s;
   const int group = n_q_heads / n_kv_heads;
   s.rows = bf16 && n_q >= static_cast<int64_t>(kManyTokens) * n_streams && stride_slot < 1ll << 26;      // (offsets of a cache block in 32 bits)
@@ -852,8 +881,11 @@ Shape shape_of(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_h
   }
   s.tile = tile_of(group, n_select);
   s.tiles = cs::most_token_tiles(n_q, n_streams, s.tile);
-  s.waves = 4;
-  s.pieces = 1;
+  const int64_t jobs = s.tiles * n_kv_heads, steps = (static_cast<int64_t>(n_select) * sel_block + 63) / 64;
+  const int64_t spare = kGroupsWanted / jobs, most = spare < kMostPieces ? spare : kMostPieces;
+  s.pieces = static_cast<int>(most < 1 ? 1 : most < steps ? most : steps);
+  const int64_t each = (steps + s.pieces - 1) / s.pieces;
+  s.waves = each >= 4 ? 4 : each >= 2 ? 2 : 1;
   return s;
 }
 
@@ -863,7 +895,7 @@ extern "C" size_t cs_selected_attn_workspace(int64_t n_q, int32_t n_streams, int
                                              int32_t sel_block, int32_t n_select) {
   if (n_q < 1 || n_streams < 1 || n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % n_kv_heads || n_q_heads / n_kv_heads > kRows) return 0;
   if (sel_block < 1 || n_select < 1 || n_select > CS_SELECT_MOST || head_dim < 1 || n_q >= 1ll << 26) return 0;
-  const Shape s = shape_of(n_q, n_streams, n_q_heads, n_kv_heads, n_select, false, 0);
+  const Shape s = shape_of(n_q, n_streams, n_q_heads, n_kv_heads, sel_block, n_select, false, 0);
   if (s.pieces == 1) return 0;
   return static_cast<size_t>(s.tiles) * n_kv_heads * s.pieces * kRows * (head_dim + 2) * sizeof(float);
 }
@@ -887,7 +919,7 @@ extern "C" int cs_selected_attn(const void* q, const void* k_cache_layer, const 
   if (n_q == 0 || n_streams == 0) return CS_OK;
   if (!q || !k_cache_layer || !v_cache_layer || !cu_q || !q_pos || !kv_len || !block_table || !selected || !out) return CS_EINVAL;
   if (!cs::aligned16(q) || !cs::aligned16(k_cache_layer) || !cs::aligned16(v_cache_layer) || !cs::aligned16(out)) return CS_EUNSUPPORTED;
-  const Shape s = shape_of(n_q, n_streams, n_q_heads, n_kv_heads, n_select, dtype == CS_BF16, stride_slot);
+  const Shape s = shape_of(n_q, n_streams, n_q_heads, n_kv_heads, sel_block, n_select, dtype == CS_BF16, stride_slot);
   const size_t need = cs_selected_attn_workspace(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, sel_block, n_select);
   if (need && (!workspace || !cs::aligned16(workspace) || workspace_bytes < need)) return CS_EWORKSPACE;
   const int64_t groups = s.tiles * n_kv_heads * s.pieces;
@@ -920,7 +952,12 @@ extern "C" int cs_selected_attn(const void* q, const void* k_cache_layer, const 
   p.scale_log2e = softmax_scale * 1.4426950408889634f;
   hipStream_t st = cs::as_stream(stream);
   const dim3 grid(static_cast<unsigned>(groups));
-#define CS_LAUNCH_SELECTED(KIND, D) hipLaunchKernelGGL((selected_attn_kernel<KIND<D>, D, 4>), grid, dim3(256), 0, st, p)
+#define CS_LAUNCH_SELECTED(KIND, D)                                                                                        \
+  do {                                                                                                                     \
+    if (s.waves == 4) hipLaunchKernelGGL((selected_attn_kernel<KIND<D>, D, 4>), grid, dim3(256), 0, st, p);                \
+    else if (s.waves == 2) hipLaunchKernelGGL((selected_attn_kernel<KIND<D>, D, 2>), grid, dim3(128), 0, st, p);           \
+    else hipLaunchKernelGGL((selected_attn_kernel<KIND<D>, D, 1>), grid, dim3(64), 0, st, p);                              \
+  } while (0)
   if (s.rows) {
     if (head_dim == 128) hipLaunchKernelGGL(selected_rows_kernel<128>, grid, dim3(64 * kRowsWaves), 0, st, p);
     else hipLaunchKernelGGL(selected_rows_kernel<64>, grid, dim3(64 * kRowsWaves), 0, st, p);

@@ -9,6 +9,16 @@ struct TokenTile {
   int stream, first, count;              // its stream, its first token, how many (1 .. tile)
 };
 
+// Sum over the lanes up to and with this one.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);      // row_shr:1, 2, 4, 8: inside each 16 lanes
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // row_bcast:15: lane 15 to the second 16, 47 to the fourth
+  return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);      // row_bcast:31: lane 31 to the upper half
+}
+
 // Tile `target` of the launch's order: stream by stream, `tile` tokens each, a stream's last tile holding what is left.  cu_q's
 // tokens from n_q on do not exist.  Every wave scans the streams for itself, 64 at a time; false: there are fewer tiles.
 __device__ __forceinline__ bool find_token_tile(const int32_t* __restrict__ cu_q, int n_streams, int64_t n_q, int tile, int target, TokenTile* t) {
@@ -22,12 +32,7 @@ __device__ __forceinline__ bool find_token_tile(const int32_t* __restrict__ cu_q
       n = max(0, min(cu_q[s + 1], static_cast<int>(n_q)) - a);
     }
     const int tiles = (n + tile - 1) / tile;
-    int incl = tiles;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int up = __shfl_up(incl, d);
-      if (lane >= d) incl += up;
-    }
+    const int incl = wave_scan(tiles);
     const int total = __builtin_amdgcn_readlane(incl, 63);
     if (target >= before + total) {
       before += total;
@@ -43,8 +48,11 @@ __device__ __forceinline__ bool find_token_tile(const int32_t* __restrict__ cu_q
   return false;
 }
 
-// Tiles that n_q tokens of n_streams streams make at most.
-inline int64_t most_token_tiles(int64_t n_q, int32_t n_streams, int tile) { return n_q / tile + (n_q < n_streams ? n_q : n_streams); }
+// Tiles that n_q tokens of n_streams streams make at most: every stream one of a single token, the other tokens in whole ones.
+inline int64_t most_token_tiles(int64_t n_q, int32_t n_streams, int tile) {
+  const int64_t one = n_q < n_streams ? n_q : n_streams;
+  return one + (n_q - one) / tile;
+}
 
 __device__ __forceinline__ float lane_xor32(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);

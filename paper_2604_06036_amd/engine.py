@@ -557,6 +557,173 @@ class Kv4Step(DeviceStep):
         return kept, kv_len, weight
 
 
+class SelectStep(DeviceStep):
+    """A step over long windows, for models that norm queries and keys head by head (`q_weight`, `k_weight`: [n_layers][head_dim], or None),
+    rotate the first `rotary_dim` elements of a head by the frequencies `inv_freq` (float32 [rotary_dim/2], scaled ones with their
+    `amplitude`), and whose queries read `n_select` blocks of `sel_block` entries of their window: the first `n_first`, the last `n_last`, and those
+    whose keys may give the largest products.  Fresh queries and keys arrive as the projections leave them.
+
+    Scoring and planning are DeviceStep's, the cache is of the workload's dtype.  The reused keys' position correction is
+    cs_kv_rerotate_freqs; a layer is cs_norm_rope_refresh_scatter, cs_key_bounds, cs_select_blocks and cs_selected_attn.  `positions`,
+    `axis_of_pair` (uint8 [rotary_dim/2]) as in Kv4Step.
+
+    `token` answers: a token a stream behind the window, in every layer.  Its rows go to `answer_blocks` cache blocks a stream that the step
+    keeps behind the window's own."""
+
+    def __init__(self, data: StepData, positions, inv_freq, axis_of_pair=None, rotary_dim: Optional[int] = None, q_weight=None, k_weight=None,
+                 norm_eps: float = 1e-6, amplitude: float = 1.0, sel_block: int = 64, n_select: int = 16, n_first: int = 1, n_last: int = 2,
+                 answer_blocks: int = 0, reuse_cap: Optional[int] = None, q_cap: Optional[int] = None):
+        import torch
+        from dataclasses import replace
+        as_tensor = lambda a: a if isinstance(a, torch.Tensor) else torch.from_numpy(np.ascontiguousarray(a))
+        w = data.workload
+        rotary_dim = w.head_dim if rotary_dim is None else int(rotary_dim)
+        if rotary_dim < 16 or rotary_dim > w.head_dim or rotary_dim % 16:
+            raise ValueError(f"rotary_dim: a multiple of 16 up to {w.head_dim} expected")
+        inv_freq = as_tensor(inv_freq)
+        if inv_freq.dtype != torch.float32 or inv_freq.numel() != rotary_dim // 2 or not inv_freq.is_contiguous():
+            raise ValueError(f"inv_freq: float32 of {rotary_dim // 2} pairs expected")
+        if axis_of_pair is not None:
+            axis_of_pair = as_tensor(axis_of_pair)
+            if axis_of_pair.dtype != torch.uint8 or axis_of_pair.numel() != rotary_dim // 2 or not axis_of_pair.is_contiguous():
+                raise ValueError(f"axis_of_pair: uint8 of {rotary_dim // 2} pairs expected")
+        width = 1 if axis_of_pair is None else 3
+        positions, rows = as_tensor(positions), int(data.info["n_q"]) if q_cap is None else int(q_cap)
+        if (positions.dtype != torch.int32 or positions.numel() < width * rows or not positions.is_contiguous()
+                or positions.dim() > 1 and int(positions.shape[-1]) != width):
+            raise ValueError(f"positions: contiguous int32 of {rows} executed rows of {width} expected")
+        dtype = torch.bfloat16 if w.dtype == "bf16" else torch.float32
+        weights = []
+        for what, t in (("q_weight", q_weight), ("k_weight", k_weight)):
+            t = None if t is None else as_tensor(t)
+            if t is not None and (t.dtype != dtype or tuple(t.shape) != (w.n_layers, w.head_dim)):
+                raise ValueError(f"{what}: {dtype} [{w.n_layers}][{w.head_dim}] expected")
+            weights.append(t)
+        if sel_block < 16 or sel_block % 16 or sel_block > 128 or not 1 <= n_select <= 256 or min(n_first, n_last) < 0 or n_first + n_last > n_select:
+            raise ValueError("selection: blocks of a multiple of 16 entries up to 128, 1 to 256 of them, the first and last among them, expected")
+        if answer_blocks:
+            data = replace(data, **_with_answer_blocks(data, int(answer_blocks)))
+        super().__init__(data, reuse_cap=reuse_cap, q_cap=q_cap, overlap=False, own_rows=False)
+        cs, dev = self.cs, self.dev
+        to = lambda t: None if t is None else t.to(dev).contiguous()
+        self.positions, self.inv_freq, self.axis_of_pair = to(positions), to(inv_freq), to(axis_of_pair)
+        self.q_weight, self.k_weight = (to(t) for t in weights)
+        self.rotary_dim, self.norm_eps, self.amplitude = rotary_dim, float(norm_eps), float(amplitude)
+        self.sel_block, self.n_select, self.n_first, self.n_last = int(sel_block), int(n_select), int(n_first), int(n_last)
+        if self.axis_of_pair is not None:      # one shift for all reused rows: whole frames along time
+            self.delta3 = torch.zeros((max(1, self.reuse_cap), 3), dtype=torch.int32, device=dev)
+            self.delta3[:, 0] = -w.stride
+        n_sel = -(-self.max_blocks * cs.CS_KV_BLOCK // self.sel_block)
+        self.bounds = torch.zeros((w.n_layers, w.n_streams, w.n_kv_heads, n_sel, 2, w.head_dim), dtype=torch.int8, device=dev)
+        self.scales = torch.zeros((w.n_layers, w.n_streams, w.n_kv_heads, n_sel), dtype=torch.uint8, device=dev)
+        self.q_turned = torch.empty_like(self.q[0])
+        self.selected = torch.empty((self.n_q, w.n_kv_heads, self.n_select), dtype=torch.int32, device=dev)
+        self.lse = torch.empty((self.n_q, w.n_q_heads), dtype=torch.float32, device=dev)
+        self.ws_d = self._workspaces(self.n_q)
+        # single tokens: a query a stream; entries that each stream's own blocks hold
+        n = w.n_streams
+        blocks = planner.blocks_needed(data.new_layout.seq_len) + data.info.get("answer_blocks", 0)
+        self.room = torch.from_numpy((blocks * cs.CS_KV_BLOCK).astype(np.int32)).to(dev)
+        self.one_cu = torch.arange(n + 1, dtype=torch.int32, device=dev)
+        self.one_q = torch.empty((n, w.n_q_heads, w.head_dim), dtype=dtype, device=dev)
+        self.one_selected = torch.empty((n, w.n_kv_heads, self.n_select), dtype=torch.int32, device=dev)
+        self.ws_one = self._workspaces(n)
+
+    def _workspaces(self, n_q):
+        """Workspaces of selection and attention for n_q queries."""
+        import torch
+        w, cs = self.data.workload, self.cs
+        heads = (w.n_q_heads, w.n_kv_heads, w.head_dim)
+        sizes = (cs.cs_select_blocks_workspace(n_q, w.n_streams, *heads, self.max_blocks, self.sel_block),
+                 cs.cs_selected_attn_workspace(n_q, w.n_streams, *heads, self.sel_block, self.n_select))
+        return tuple(torch.empty((max(16, size),), dtype=torch.uint8, device=self.dev) for size in sizes)
+
+    def rerotate(self, in_place: bool = False, layers=None):
+        w, cs = self.data.workload, self.cs
+        if self.reuse_cap == 0:
+            return
+        l0, l1 = layers if layers is not None else (0, w.n_layers)
+        cs.cs_kv_rerotate_freqs(self.k_pool[l0:l1], None if in_place else self.v_pool[l0:l1], self.src_slot, None if in_place else self.dst_slot,
+                                self.delta if self.axis_of_pair is None else self.delta3, self.axis_of_pair, self.inv_freq,
+                                int(self.src_slot.shape[0]), l1 - l0, w.n_kv_heads, w.head_dim, self.rotary_dim, self.stride_layer, self.stride_slot,
+                                self.stride_head, cs.CS_ROPE_HALF_SPLIT, self.dtype)
+
+    def _write(self, layer, q, q_out, k, v, slot, positions, n):
+        w, cs = self.data.workload, self.cs
+        cs.cs_norm_rope_refresh_scatter(q, q_out, k, v, None if self.q_weight is None else self.q_weight[layer],
+                                        None if self.k_weight is None else self.k_weight[layer], slot, positions, self.axis_of_pair, self.inv_freq,
+                                        self.k_pool[layer], self.v_pool[layer], n, w.n_q_heads, w.n_kv_heads, w.head_dim, self.rotary_dim, q.stride(0),
+                                        k.stride(0), v.stride(0), self.stride_slot, self.stride_head, self.norm_eps, self.amplitude,
+                                        cs.CS_ROPE_HALF_SPLIT, self.dtype)
+
+    def _read(self, layer, q, cu_q, q_pos, since, selected, out, lse, n, ws):
+        """Bounds of the blocks with entries from `since` on (None: of all), the queries' choice, attention."""
+        w, cs = self.data.workload, self.cs
+        heads = (w.n_q_heads, w.n_kv_heads, w.head_dim)
+        k, v, bounds, scales = self.k_pool[layer], self.v_pool[layer], self.bounds[layer], self.scales[layer]
+        cs.cs_key_bounds(k, since, self.kv_len, self.block_table, self.max_blocks, cs.CS_KV_BLOCK, self.sel_block, bounds, scales, w.n_streams,
+                         w.n_kv_heads, w.head_dim, self.stride_slot, self.stride_head, self.dtype)
+        cs.cs_select_blocks(q, bounds, scales, cu_q, q_pos, self.kv_len, self.max_blocks, self.sel_block, self.n_select, self.n_first, self.n_last,
+                            selected, n, w.n_streams, *heads, self.dtype, ws[0])
+        cs.cs_selected_attn(q, k, v, cu_q, q_pos, self.kv_len, self.block_table, self.max_blocks, cs.CS_KV_BLOCK, selected, self.sel_block,
+                            self.n_select, out, lse, n, w.n_streams, *heads, self.stride_slot, self.stride_head, self.data.softmax_scale, self.dtype,
+                            ws[1])
+
+    def refresh_scatter(self, layer: int):
+        """Queries of the layer normed and rotated (into q_turned), keys normed, rotated and written, values written."""
+        self._write(layer, self.q[layer], self.q_turned, self.k_new[layer], self.v_new[layer], self.q_slot, self.positions, self.n_q)
+
+    def attention(self, layer: int, reuse_plan: bool = False):
+        """Bounds of the layer's windows, the blocks of every query of q_turned (into `selected`), attention over them."""
+        self._read(layer, self.q_turned, self.cu_q, self.q_pos, None, self.selected, self.out[layer], self.lse, self.n_q, self.ws_d)
+
+    def refresh_and_attention(self, layer: int, reuse_plan: bool = False, own_rows: bool = False):
+        self.refresh_scatter(layer)
+        self.attention(layer)
+
+    def attention_status(self) -> int:
+        return 0                        # (no launch-wide barrier)
+
+    def run(self):
+        self.prepare()
+        self.rerotate()
+        for layer in range(self.data.workload.n_layers):
+            self.refresh_and_attention(layer)
+
+    def token(self, q, k_new, v_new, positions, out):
+        """One token a stream behind its window, in every layer: q [n_layers][n_streams][n_q_heads][head_dim] as the projections leave it,
+        k_new and v_new alike, positions int32 [n_streams] or [n_streams][3]; out like q.  Windows grow by the token (`kv_len`), which is read by
+        itself too; where a stream's blocks are full its rows are not written, and the window stays as it is.
+        (Layers at once, as the inputs of a step are: a model calls `_write` and `_read` layer by layer.)"""
+        import torch
+        w, cs = self.data.workload, self.cs
+        n, entry = w.n_streams, self.kv_len.clone()
+        place = entry.clamp(max=self.max_blocks * cs.CS_KV_BLOCK - 1).long()
+        slot = self.block_table.gather(1, (place // cs.CS_KV_BLOCK)[:, None])[:, 0] * cs.CS_KV_BLOCK + (place % cs.CS_KV_BLOCK).int()
+        slot = torch.where(entry < self.room, slot, -1)
+        self.kv_len.copy_(torch.where(slot >= 0, entry + 1, entry))
+        last = self.kv_len - 1
+        for layer in range(w.n_layers):
+            self._write(layer, q[layer], self.one_q, k_new[layer], v_new[layer], slot, positions, n)
+            self._read(layer, self.one_q, self.one_cu, last, entry, self.one_selected, out[layer], None, n, self.ws_one)
+
+
+def _with_answer_blocks(data: StepData, extra: int) -> dict:
+    """Fields of a step whose new windows have `extra` cache blocks a stream behind their own, at the end of the pool."""
+    import torch
+    from dataclasses import replace
+    new = data.new_layout
+    need = planner.blocks_needed(new.seq_len)
+    n_streams, first = len(need), data.n_slots // synth.KV_BLOCK
+    table = np.zeros((n_streams, max(int(new.block_table.shape[1]), int(need.max()) + extra)), np.int32)
+    for s in range(n_streams):
+        table[s, : need[s]] = new.block_table[s, : need[s]]
+        table[s, need[s]: need[s] + extra] = first + s * extra + np.arange(extra)
+    grow = lambda t: torch.cat([t, torch.zeros((t.shape[0], n_streams * extra * synth.KV_BLOCK) + tuple(t.shape[2:]), dtype=t.dtype, device=t.device)], dim=1)
+    return dict(new_layout=replace(new, block_table=table), n_slots=data.n_slots + n_streams * extra * synth.KV_BLOCK,
+                k_pool=grow(data.k_pool), v_pool=grow(data.v_pool), info=dict(data.info, answer_blocks=extra), _plan=None)
+
+
 @dataclass
 class FrontEndData:
     """Inputs of a slide step that starts from decoder output: coding blocks, a motion field and

@@ -604,3 +604,213 @@ def test_a_query_without_numbers_keeps_to_its_heads(cs):
         out, stat = c.attend(qs, dev(listed), 16)
         assert bool(torch.isnan(out[1, 2]).all()) and bool(torch.isnan(stat[1, 2])) and bool(torch.isnan(out[3, 0]).all())
         c.check_attention(qs, listed, 16, out, stat)
+
+
+# ------------------------------------------------------------------------------------------ how calls are made
+
+def test_rows_past_32_bits(cs):
+    """Cache blocks whose offsets pass 2^32 elements: a pool of more than 2^32 elements in bf16, of which few rows are touched."""
+    say("offsets past 32 bits")
+    hkv, d, kv = 4, 128, [200, 90]
+    n_slots = 16 * (-(-(1 << 32) // (16 * hkv * d)) + 40)
+    k, v = (torch.empty((n_slots, hkv, d), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    small = Cache(cs, 12, hkv, d, kv, "bf16")
+    ids = small.table.cpu().numpy()
+    top = n_slots // 16
+    far = np.where(ids % 2 == 0, ids, top - 1 - ids).astype(np.int32)          # half of the blocks at the pool's end
+    for old, new in {int(a): int(b) for a, b in zip(ids.ravel(), far.ravel())}.items():
+        for src, dst in ((small.pool[0], k), (small.pool[1], v)):
+            dst[16 * new:16 * new + 16] = src[16 * old:16 * old + 16]
+    want = {}
+    for pools, table in ((small.pool, small.table), ([k, v], dev(far))):
+        small.pool, small.table = pools, table
+        for nq, where in (([1, 1], "tail"), ([40, 20], "any")):
+            small.rng = np.random.default_rng(3)
+            qs = small.queries(nq, 28, where=where)
+            listed = small.select(qs, 16, 5, 1, 1)
+            got = [small.bounds(16), listed, small.attend(qs, listed, 16)]
+            if nq[0] in want:
+                b0, l0, a0 = want[nq[0]]
+                assert torch.equal(got[0][0], b0[0]) and torch.equal(got[0][1], b0[1]) and torch.equal(listed, l0)
+                assert torch.equal(got[2][0], a0[0]) and torch.equal(got[2][1], a0[1])
+            want[nq[0]] = got
+    # writes and corrections there
+    n = 7
+    slot = dev(np.array([0, 16 * top - 1, 5, 16 * top - 17, -1, 33, 16 * top - 40], np.int32))
+    x = torch.randn((n, hkv, d), device=DEV).to(torch.bfloat16)
+    w = torch.ones((d,), dtype=torch.bfloat16, device=DEV)
+    f = torch.full((d // 2,), 0.01, device=DEV)
+    pos = torch.arange(n, dtype=torch.int32, device=DEV)
+    cs.cs_norm_rope_refresh_scatter(None, None, x, x, None, w, slot, pos, None, f, k, v, n, 0, hkv, d, d, 0, hkv * d, hkv * d, hkv * d, d, 1e-6, 1.0, 0, cs.CS_BF16)
+    near = torch.zeros((40, hkv, d), dtype=torch.bfloat16, device=DEV), torch.zeros((40, hkv, d), dtype=torch.bfloat16, device=DEV)
+    cs.cs_norm_rope_refresh_scatter(None, None, x, x, None, w, pos, pos, None, f, near[0], near[1], n, 0, hkv, d, d, 0, hkv * d, hkv * d, hkv * d, d, 1e-6, 1.0, 0, cs.CS_BF16)
+    live = [0, 1, 2, 3, 5, 6]
+    assert torch.equal(k[slot[live].long()], near[0][live]) and torch.equal(v[slot[live].long()], x[live])
+    src, dst, delta = dev(np.array([16 * top - 1, 0], np.int32)), dev(np.array([7, 16 * top - 3], np.int32)), dev(np.array([5, -9], np.int32))
+    cs.cs_kv_rerotate_freqs(k, v, src, dst, delta, None, f, 2, 1, hkv, d, d, 0, hkv * d, d, 0, cs.CS_BF16)
+    cs.cs_kv_rerotate_freqs(near[0], near[1], dev(np.array([1, 0], np.int32)), dev(np.array([20, 21], np.int32)), delta, None, f, 2, 1, hkv, d, d, 0, hkv * d, d, 0, cs.CS_BF16)
+    assert torch.equal(k[dst.long()], near[0][20:22]) and torch.equal(v[dst.long()], x[[1, 0]])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_graphs_replayed_beside_eager_calls(cs, dtype):
+    """Two captured chains of different shapes that share a workspace, replayed in turn with eager calls and changed inputs between: each gives
+    what eager calls give, bit for bit."""
+    say("graphs", dtype)
+    c = Cache(cs, 21, 4, 128, [700, 333, 90], dtype)
+    shapes = []
+    for nq, size, n_select in (([1, 1, 1], 64, 6), ([30, 11, 20], 16, 9)):
+        qs = c.queries(nq, 28, where="tail")
+        n_sel = c.n_sel(size)
+        b, sc = torch.zeros((3, 4, n_sel, 2, 128), dtype=torch.int8, device=DEV), torch.zeros((3, 4, n_sel), dtype=torch.uint8, device=DEV)
+        listed = torch.zeros((qs["n_q"], 4, n_select), dtype=torch.int32, device=DEV)
+        out, stat = torch.zeros_like(qs["q"]), torch.zeros((qs["n_q"], 28), device=DEV)
+        shapes.append((qs, size, n_select, b, sc, listed, out, stat))
+    nbytes = max(max(cs.cs_selected_attn_workspace(s[0]["n_q"], 3, 28, 4, 128, s[1], s[2]), cs.cs_select_blocks_workspace(s[0]["n_q"], 3, 28, 4, 128, c.max_blocks, s[1])) for s in shapes)
+    ws = torch.full((max(16, nbytes),), 255, dtype=torch.uint8, device=DEV)
+
+    def chain(s):
+        qs, size, n_select, b, sc, listed, out, stat = s
+        cs.cs_key_bounds(c.pool[0], None, c.kv_len, c.table, c.max_blocks, 16, size, b, sc, 3, 4, 128, *c.stride, c.code)
+        cs.cs_select_blocks(qs["q"], b, sc, qs["cu_q"], qs["q_pos"], c.kv_len, c.max_blocks, size, n_select, 1, 1, listed, qs["n_q"], 3, 28, 4, 128, c.code, ws)
+        cs.cs_selected_attn(qs["q"], c.pool[0], c.pool[1], qs["cu_q"], qs["q_pos"], c.kv_len, c.table, c.max_blocks, 16, listed, size, n_select, out, stat, qs["n_q"], 3, 28, 4, 128,
+                            *c.stride, 0.09, c.code, ws)
+
+    side = torch.cuda.Stream()
+    graphs = []
+    with torch.cuda.stream(side):
+        for s in shapes:
+            chain(s)
+            torch.cuda.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                chain(s)
+            graphs.append(g)
+    torch.cuda.synchronize()
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    for i in range(5):
+        for s in shapes:
+            s[0]["q"].copy_(torch.randn(s[0]["q"].shape, generator=gen, device=DEV))
+        want = []
+        for s in shapes:
+            chain(s)
+            torch.cuda.synchronize()
+            want.append([x.clone() for x in s[3:]])
+        for s in shapes:
+            for x in s[5:]:
+                x.zero_()
+        for g in (graphs if i % 2 else graphs[::-1]):
+            g.replay()
+        torch.cuda.synchronize()
+        for s, w in zip(shapes, want):
+            for x, y in zip(s[3:], w):
+                assert bool((x.view(torch.uint8) == y.view(torch.uint8)).all())
+
+
+def test_work_goes_to_the_current_stream(cs):
+    """Calls on a side stream whose inputs a long kernel there is still making."""
+    say("side stream")
+    c = Cache(cs, 22, 4, 128, [600, 50], "bf16")
+    qs = c.queries([40, 9], 28, where="tail")
+    listed = c.select(qs, 32, 5, 1, 1)
+    want, _ = c.attend(qs, listed, 32)
+    side = torch.cuda.Stream()
+    keep = c.pool[1].clone()
+    c.pool[1].zero_()
+    torch.cuda.synchronize()
+    big = torch.randn((4096, 4096), device=DEV)
+    with torch.cuda.stream(side):
+        for _ in range(10):
+            big = big @ big * 1e-2
+        c.pool[1].copy_(keep)
+        out = torch.zeros_like(want)
+        nbytes = cs.cs_selected_attn_workspace(qs["n_q"], 2, 28, 4, 128, 32, 5)
+        ws = torch.empty((max(16, nbytes),), dtype=torch.uint8, device=DEV)
+        cs.cs_selected_attn(qs["q"], c.pool[0], c.pool[1], qs["cu_q"], qs["q_pos"], c.kv_len, c.table, c.max_blocks, 16, listed, 32, 5, out, None, qs["n_q"], 2, 28, 4, 128, *c.stride,
+                            1 / math.sqrt(128), cs.CS_BF16, ws)
+    side.synchronize()
+    assert torch.equal(out, want)
+
+
+def test_two_calls_at_once_with_workspaces_of_their_own(cs):
+    say("two streams at once")
+    c = Cache(cs, 23, 4, 128, [900] * 3, "bf16")
+    work = []
+    for seed, nq in ((1, [1, 1, 1]), (2, [50, 60, 70]), (3, [1, 0, 1])):
+        c.rng = np.random.default_rng(seed)
+        qs = c.queries(nq, 28, where="tail")
+        listed = c.select(qs, 64, 6, 1, 1)
+        work.append((qs, listed, c.attend(qs, listed, 64)))
+    streams = [torch.cuda.Stream() for _ in work]
+    outs = [[torch.zeros_like(w[2][0]), torch.zeros_like(w[2][1])] for w in work]
+    ws = [torch.full((max(16, cs.cs_selected_attn_workspace(w[0]["n_q"], 3, 28, 4, 128, 64, 6)),), 255, dtype=torch.uint8, device=DEV) for w in work]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for (qs, listed, _), (out, stat), st, one in zip(work, outs, streams, ws):
+            with torch.cuda.stream(st):
+                cs.cs_selected_attn(qs["q"], c.pool[0], c.pool[1], qs["cu_q"], qs["q_pos"], c.kv_len, c.table, c.max_blocks, 16, listed, 64, 6, out, stat, qs["n_q"], 3, 28, 4, 128,
+                                    *c.stride, 1 / math.sqrt(128), cs.CS_BF16, one)
+    torch.cuda.synchronize()
+    for (_, _, (want, lse)), (out, stat) in zip(work, outs):
+        assert torch.equal(out, want) and torch.equal(stat, lse)
+
+
+def test_strides_wider_than_the_rows(cs):
+    """Pools whose slots and heads lie further apart than they have to: the same bits."""
+    say("wide strides")
+    for dtype in ("bf16", "f32"):
+        c = Cache(cs, 24, 3, 64, [300, 77], dtype)
+        for nq in ([1, 1], [40, 12]):
+            qs = c.queries(nq, 12, where="tail")
+            b, sc = c.bounds(48)
+            listed = c.select(qs, 48, 4, 1, 1, (b, sc))
+            want = c.attend(qs, listed, 48)
+            pools, stride = c.pool, c.stride
+            wide = []
+            for x in pools:
+                y = torch.full((x.shape[0], 5, 96), float("nan"), dtype=x.dtype, device=DEV)
+                y[:, :3, :64] = x
+                wide.append(y[:, :3, :64])
+            c.pool, c.stride = wide, (480, 96)
+            b2, sc2 = c.bounds(48)
+            got = c.attend(qs, listed, 48)
+            c.pool, c.stride = pools, stride
+            assert torch.equal(b, b2) and torch.equal(sc, sc2) and torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+def test_lengths_that_the_table_does_not_hold(cs):
+    """kv_len past the table's rows is clamped to them, for selection and attention alike; positions past it see all of it."""
+    say("clamped lengths")
+    for dtype in ("bf16", "f32"):
+        c = Cache(cs, 25, 2, 64, [64, 64], dtype)
+        c.max_blocks, c.table = 4, c.table[:, :4].contiguous()
+        for nq in ([1, 1], [20, 30]):
+            qs = c.queries(nq, 4, where="tail")
+            qs["pos"][:] = 1 << 30
+            qs["q_pos"].copy_(dev(qs["pos"]))
+            listed = c.select(qs, 16, 3, 1, 1)
+            want = c.attend(qs, listed, 16)
+            c.kv_len.fill_(0x7fffffff)
+            assert torch.equal(c.select(qs, 16, 3, 1, 1), listed)
+            got = c.attend(qs, listed, 16)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+            c.kv_len.fill_(64)
+            c.check_attention(qs, listed, 16, *got)
+
+
+def test_more_tokens_than_said(cs):
+    """cu_q past n_q: tokens from n_q on do not exist."""
+    say("n_q below cu_q")
+    c = Cache(cs, 26, 2, 64, [300, 200], "bf16")
+    qs = c.queries([9, 14], 6, where="tail")
+    listed = c.select(qs, 16, 4, 1, 1)
+    want = c.attend(qs, listed, 16)
+    for n in (3, 9, 17):
+        out, sel = torch.full_like(want[0], 9.0), torch.full_like(listed, -7)
+        cs.cs_selected_attn(qs["q"], c.pool[0], c.pool[1], qs["cu_q"], qs["q_pos"], c.kv_len, c.table, c.max_blocks, 16, listed, 16, 4, out, None, n, 2, 6, 2, 64, *c.stride, 0.125,
+                            cs.CS_BF16, torch.empty((max(16, cs.cs_selected_attn_workspace(n, 2, 6, 2, 64, 16, 4)),), dtype=torch.uint8, device=DEV))
+        b, sc = c.bounds(16)
+        cs.cs_select_blocks(qs["q"], b, sc, qs["cu_q"], qs["q_pos"], c.kv_len, c.max_blocks, 16, 4, 1, 1, sel, n, 2, 6, 2, 64, cs.CS_BF16)
+        assert torch.equal(sel[:n], listed[:n]) and bool((sel[n:] == -7).all()) and bool((out[n:] == 9).all())
+        # (fewer tokens may take the other kernel: the same precision)
+        assert float((out[:n].float() - want[0][:n].float()).abs().max()) <= 4 * B * float(c.pool[1][c.slots[0]].float().abs().max())
