@@ -15,6 +15,7 @@
 #include <type_traits>
 
 #include "kv4.h"
+#include "lds_rows.h"
 #include "token_tiles.h"
 
 namespace {
@@ -153,7 +154,7 @@ struct SelectParams {
   int32_t max_blocks, n_streams, n_q_heads, n_kv_heads, group, n_sel, size, n_select, n_first, n_last, tile, pitch;
 };
 
-constexpr int kManyTokens = 8;           // a stream, on average, from which workgroups take two tiles of rows
+constexpr int kManyTokens = 8;           // a stream, on average, from which every wave has rows of its own
 constexpr int kMostBlocks = 32768;       // whose scores a workgroup holds in LDS for one token
 constexpr int kTileScores = 8192;        // ... for a tile of tokens
 
@@ -175,7 +176,7 @@ __device__ __forceinline__ void write_list(const F& at, int n, int n_first, int 
   int above = 0;                                       // scores > T
   if (wanted > 0) {
     uint32_t high = 0, low = 0xffffffffu;
-#pragma unroll
+#pragma unroll(C ? C : 8)
     for (int c = 0; c < chunks; ++c) {
       const uint32_t x = at(c);
       high = max(high, x);
@@ -188,19 +189,19 @@ __device__ __forceinline__ void write_list(const F& at, int n, int n_first, int 
     for (int bit = first_bit; bit >= 0; --bit) {
       const uint32_t cand = t | 1u << bit;
       int count = 0;
-#pragma unroll
+#pragma unroll(C ? C : 8)
       for (int c = 0; c < chunks; ++c) count += __popcll(__ballot(at(c) >= cand));
       if (count >= wanted) {
         t = cand;
         if (count == wanted) break;
       }
     }
-#pragma unroll
+#pragma unroll(C ? C : 8)
     for (int c = 0; c < chunks; ++c) above += __popcll(__ballot(at(c) > t));
   }
   int ties = wanted - above, place = 0;
   const uint64_t below = (1ull << lane) - 1;
-#pragma unroll
+#pragma unroll(C ? C : 8)
   for (int c = 0; c < chunks; ++c) {
     const uint32_t x = at(c);
     const int block = c * 64 + lane;
@@ -222,32 +223,26 @@ __device__ __forceinline__ void write_list_held(const F& key, int n, int n_first
   write_list<C>([&](int c) __attribute__((always_inline)) { return held[c]; }, n, n_first, n_last, n_select, out, lane);
 }
 
-// A workgroup of W waves takes a tile of a stream's tokens and a kv head.  Rows of the product are (token, head), MT times 32, the heads of a
-// token padded to GP by the last of them and spread so that they are neighbouring registers of a lane; columns are blocks, 32 at a time, the
-// waves in turn.
-template <bool kBf16, int D, int GP, int W, int MT>
-__global__ __launch_bounds__(64 * W) void select_blocks_kernel(SelectParams p) {
-  constexpr int STEPS = 2 * D / 32;
-  constexpr int QROW = 2 * D + 16;
-  constexpr int TOK = 32 / GP < 8 ? 32 / GP : 8;         // tokens of 32 rows
-  constexpr int VE = kBf16 ? 8 : 4;
-  constexpr int CHUNKS = D / VE, HELD = (GP * CHUNKS + 63) / 64;       // 16-byte pieces of a head, and of a token a lane holds
-  __shared__ __attribute__((aligned(16))) uint8_t s_q[MT * 32 * QROW];
-  extern __shared__ __attribute__((aligned(16))) uint32_t s_score[];      // [tile][pitch]
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int kvh = static_cast<int>(blockIdx.x % p.n_kv_heads);
-  cs::TokenTile t;
-  if (!cs::find_token_tile(p.cu_q, p.n_streams, p.n_q, p.tile, static_cast<int>(blockIdx.x / p.n_kv_heads), &t)) return;
+constexpr int kWide = 16;                // waves of a workgroup that takes few tokens
+constexpr int kRowsWaves = 8, kPairs = kRowsWaves / 2;     // ... many
 
-  // ---- whole numbers of the tile's queries: a wave takes a token, 16 bytes a lane
-  const auto number = [&](const cs::u32x4& v, int e) __attribute__((always_inline)) {
-    const uint32_t w = v[kBf16 ? e / 2 : e];
+// Tokens whose heads, padded to GP, are 32 rows (8 at most).
+template <int GP>
+constexpr int kTokens = 32 / GP < 8 ? 32 / GP : 8;
+
+// Whole numbers of a token's heads: 16 bytes a lane are asked for, then written to the token's rows of 32 in LDS, q+ and q- behind one another.
+// Token k of the 32 rows is pair k / 2 of half k % 2: registers GP (k / 2) + slot of the lanes of that half, rows 8 (r / 4) + 4 half + r % 4.
+template <bool kBf16, int D, int GP>
+struct Query {
+  static constexpr int VE = kBf16 ? 8 : 4, CHUNKS = D / VE, HELD = (GP * CHUNKS + 63) / 64, QROW = 2 * D + 16;
+  cs::u32x4 v[HELD];
+
+  static __device__ __forceinline__ uint32_t number(const cs::u32x4& x, int e) {
+    const uint32_t w = x[kBf16 ? e / 2 : e];
     return kBf16 ? (e & 1 ? w & 0xffff0000u : w << 16) : w;
-  };
-  for (int i = wave; i < t.count; i += W) {
-    const int64_t from = (static_cast<int64_t>(t.first + i) * p.n_q_heads + static_cast<int64_t>(kvh) * p.group) * D;
-    cs::u32x4 v[HELD];
-    uint32_t amax = 0;
+  }
+  __device__ __forceinline__ void ask(const SelectParams& p, int tok, int kvh, int lane) {
+    const int64_t from = (static_cast<int64_t>(tok) * p.n_q_heads + static_cast<int64_t>(kvh) * p.group) * D;
 #pragma unroll
     for (int j = 0; j < HELD; ++j) {
       const int c = j * 64 + lane, head = min(c / CHUNKS, p.group - 1);      // (past the group: its last head again)
@@ -255,6 +250,9 @@ __global__ __launch_bounds__(64 * W) void select_blocks_kernel(SelectParams p) {
       if constexpr (kBf16) v[j] = *reinterpret_cast<const cs::u32x4*>(static_cast<const uint16_t*>(p.q) + at);
       else v[j] = *reinterpret_cast<const cs::u32x4*>(static_cast<const float*>(p.q) + at);
     }
+  }
+  __device__ __forceinline__ void put(uint8_t* rows, int k, int lane) const {
+    uint32_t amax = 0;
 #pragma unroll
     for (int j = 0; j < HELD; ++j)
 #pragma unroll
@@ -273,9 +271,8 @@ __global__ __launch_bounds__(64 * W) void select_blocks_kernel(SelectParams p) {
         up[e / 4] |= static_cast<uint32_t>(max(code, 0)) << (8 * (e % 4));
         down[e / 4] |= (static_cast<uint32_t>(min(code, 0)) & 0xffu) << (8 * (e % 4));
       }
-      // of 32 rows, token k is pair k / 2 of half k % 2: registers GP (k / 2) + slot of the lanes of that half, rows 8 (r / 4) + 4 half + r % 4
-      const int k = i % TOK, r = GP * (k / 2) + slot, row = i / TOK * 32 + 8 * (r / 4) + 4 * (k % 2) + r % 4;
-      uint8_t* dst = s_q + row * QROW + c % CHUNKS * VE;
+      const int r = GP * (k / 2) + slot, row = 8 * (r / 4) + 4 * (k % 2) + r % 4;
+      uint8_t* dst = rows + row * QROW + c % CHUNKS * VE;
       if constexpr (VE == 8) {
         *reinterpret_cast<cs::u32x2*>(dst) = cs::u32x2{up[0], up[1]};
         *reinterpret_cast<cs::u32x2*>(dst + D) = cs::u32x2{down[0], down[1]};
@@ -285,66 +282,155 @@ __global__ __launch_bounds__(64 * W) void select_blocks_kernel(SelectParams p) {
       }
     }
   }
-  // candidates of the token of a lane, and of any
+};
+
+// Scores of a lane's block for the tokens of 32 rows, from the products with all of their heads: f(token, score).
+template <int GP, class F>
+__device__ __forceinline__ void each_score(const i32x16& acc, uint32_t byte, int h, const F& f) {
+  const float scale = __uint_as_float((byte - 21u) << 23);               // 2^(k - 21)
+#pragma unroll
+  for (int g = 0; g < (kTokens<GP> + 1) / 2; ++g) {
+    int top = acc[g * GP];
+#pragma unroll
+    for (int i = 1; i < GP; ++i) top = max(top, acc[g * GP + i]);
+    f(2 * g + h, byte == kNoNumber ? kOdd : ordered(static_cast<float>(top) * scale));
+  }
+}
+
+// Candidates of the tile's token `lane` (0: none, or no such token).
+__device__ __forceinline__ int candidates_of(const SelectParams& p, const cs::TokenTile& t, int lane) {
   const int entries = min(p.kv_len[t.stream], p.max_blocks * CS_KV_BLOCK);
   const int last = lane < t.count ? min(p.q_pos[t.first + lane], entries - 1) : -1;
-  const int candidates = last < 0 ? 0 : last / p.size + 1;
+  return last < 0 ? 0 : last / p.size + 1;
+}
+
+// The list of token `tok` from its scores, by a wave.
+__device__ __forceinline__ void select_token(const SelectParams& p, const uint32_t* score, int tok, int kvh, int n, int lane) {
+  int32_t* out = p.selected + (static_cast<int64_t>(tok) * p.n_kv_heads + kvh) * p.n_select;
+  if (n <= p.n_select) {
+    for (int c = lane; c < p.n_select; c += 64) out[c] = c < n ? c : -1;
+    return;
+  }
+  const auto key = [&](int b) __attribute__((always_inline)) -> uint32_t { return b < p.n_first || b >= n - p.n_last ? 0u : score[b]; };
+#define CS_LIST(C) write_list_held<C>(key, n, p.n_first, p.n_last, p.n_select, out, lane)
+  if (n <= 128) CS_LIST(2);
+  else if (n <= 256) CS_LIST(4);
+  else if (n <= 320) CS_LIST(5);
+  else if (n <= 512) CS_LIST(8);
+  else if (n <= 1024) CS_LIST(16);
+  else if (n <= 2048) CS_LIST(32);
+  else write_list<0>([&](int c) __attribute__((always_inline)) { return key(c * 64 + lane); }, n, p.n_first, p.n_last, p.n_select, out, lane);
+#undef CS_LIST
+}
+
+// Few tokens a stream: a workgroup takes those of 32 rows and a kv head, its waves the blocks in turn, 32 columns at a time; then each wave the
+// list of a token.  Rows are (token, head), the heads of a token padded to GP by the last of them and spread so that they are
+// neighbouring registers of a lane.
+template <bool kBf16, int D, int GP>
+__global__ __launch_bounds__(64 * kWide) void select_blocks_kernel(SelectParams p) {
+  typedef Query<kBf16, D, GP> Q;
+  constexpr int STEPS = 2 * D / 32;
+  __shared__ __attribute__((aligned(16))) uint8_t s_q[32 * Q::QROW];
+  extern __shared__ __attribute__((aligned(16))) uint32_t s_score[];      // [tile][pitch]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
+  const int kvh = static_cast<int>(blockIdx.x % p.n_kv_heads);
+  cs::TokenTile t;
+  if (!cs::find_token_tile(p.cu_q, p.n_streams, p.n_q, p.tile, static_cast<int>(blockIdx.x / p.n_kv_heads), &t)) return;
+  if (wave < t.count) {
+    Q q;
+    q.ask(p, t.first + wave, kvh, lane);
+    q.put(s_q, wave, lane);
+  }
+  const int candidates = candidates_of(p, t, lane);
   const int most = __builtin_amdgcn_readfirstlane(static_cast<int>(cs::lanes_max<64>(static_cast<uint32_t>(candidates))));
   __syncthreads();
 
-  // ---- scores (rows without a token hold anything: nobody reads theirs)
-  if (most > p.n_select) {
-    const int n = lane & 31, h = lane >> 5;
+  if (most > p.n_select) {               // (rows without a token hold anything: nobody reads their scores)
+    i32x4 a[STEPS];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) a[s] = *reinterpret_cast<const i32x4*>(s_q + n * Q::QROW + 32 * s + 16 * h);
     const int64_t head_at = (static_cast<int64_t>(t.stream) * p.n_kv_heads + kvh) * p.n_sel;
-    i32x4 a[MT][STEPS];
-#pragma unroll
-    for (int k = 0; k < MT; ++k)
-#pragma unroll
-      for (int s = 0; s < STEPS; ++s) a[k][s] = *reinterpret_cast<const i32x4*>(s_q + (32 * k + n) * QROW + 32 * s + 16 * h);
-    for (int b0 = wave * 32; b0 < most; b0 += 32 * W) {
+    for (int b0 = wave * 32; b0 < most; b0 += 32 * kWide) {
       const int block = min(b0 + n, most - 1);
       const int8_t* from = p.bounds + (head_at + block) * 2 * D + 16 * h;
       const uint32_t byte = p.scales[head_at + block];
       i32x4 b[STEPS];
 #pragma unroll
       for (int s = 0; s < STEPS; ++s) b[s] = *reinterpret_cast<const i32x4*>(from + 32 * s);
-      const float scale = __uint_as_float((byte - 21u) << 23);           // 2^(k - 21)
+      i32x16 acc = {};
 #pragma unroll
-      for (int k = 0; k < MT; ++k) {
-        i32x16 acc = {};
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[k][s], b[s], acc, 0, 0, 0);
-#pragma unroll
-        for (int g = 0; g < (TOK + 1) / 2; ++g) {
-          int top = acc[g * GP];
-#pragma unroll
-          for (int i = 1; i < GP; ++i) top = max(top, acc[g * GP + i]);
-          const int tok = k * TOK + 2 * g + h;
-          if (b0 + n < most && tok < t.count) s_score[tok * p.pitch + block] = byte == kNoNumber ? kOdd : ordered(static_cast<float>(top) * scale);
-        }
-      }
+      for (int s = 0; s < STEPS; ++s) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[s], b[s], acc, 0, 0, 0);
+      each_score<GP>(acc, byte, h, [&](int tok, uint32_t x) __attribute__((always_inline)) {
+        if (b0 + n < most && tok < t.count) s_score[tok * p.pitch + block] = x;
+      });
     }
   }
   __syncthreads();
+  if (wave < t.count) select_token(p, s_score + wave * p.pitch, t.first + wave, kvh, __builtin_amdgcn_readlane(candidates, wave), lane);
+}
 
-  // ---- lists: a wave takes a token
-  for (int i = wave; i < t.count; i += W) {
-    const int n = __builtin_amdgcn_readlane(candidates, i);
-    int32_t* out = p.selected + (static_cast<int64_t>(t.first + i) * p.n_kv_heads + kvh) * p.n_select;
-    if (n <= p.n_select) {
-      for (int c = lane; c < p.n_select; c += 64) out[c] = c < n ? c : -1;
-      continue;
+// Many tokens a stream: two waves of a workgroup share 32 rows, four pairs take 64 columns a step, one wave of a pair the first 32 of them, the
+// other the others.  Columns pass through LDS once, a step ahead; the second stage and the scores take the queries' place.  Then each wave
+// makes the lists of every second token of its pair.
+template <bool kBf16, int D, int GP>
+__global__ __launch_bounds__(64 * kRowsWaves) void select_rows_kernel(SelectParams p) {
+  typedef Query<kBf16, D, GP> Q;
+  constexpr int STEPS = 2 * D / 32;
+  constexpr int kStage = 64 * 2 * D, kParts = kStage / 1024 / kRowsWaves;    // bytes of 64 blocks, requests of a wave for them
+  constexpr int LR = 2 * D / 16, RL = 64 / LR;             // lanes of a block, blocks of a request
+  // a stage, then the queries [pairs][32 rows], or the other stage and the scores [tile][pitch]
+  extern __shared__ __attribute__((aligned(16))) uint8_t s_mem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
+  const int kvh = static_cast<int>(blockIdx.x % p.n_kv_heads);
+  cs::TokenTile t;
+  if (!cs::find_token_tile(p.cu_q, p.n_streams, p.n_q, p.tile, static_cast<int>(blockIdx.x / p.n_kv_heads), &t)) return;
+  const int pair = wave >> 1, half = wave & 1;
+  const int first = pair * (p.tile / kPairs), mine = min(p.tile / kPairs, t.count - first);      // the pair's tokens (fewer than one: none)
+  const int64_t head_at = (static_cast<int64_t>(t.stream) * p.n_kv_heads + kvh) * p.n_sel;
+  const char* bounds = reinterpret_cast<const char*>(p.bounds + head_at * 2 * D);
+  const uint32_t to = __builtin_amdgcn_readfirstlane(cs::lds_address(s_mem)) + wave * kParts * 1024;
+  const auto request = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < kParts; ++j) {
+      const int row = (wave * kParts + j) * RL + lane / LR;
+      cs::to_lds(static_cast<uint32_t>(min(64 * i + row, p.n_sel - 1)) * (2 * D) + 16 * (lane % LR ^ cs::row_place<D>(row)), bounds, to + (i & 1) * kStage + 1024 * j);
     }
-    const uint32_t* score = s_score + i * p.pitch;
-    const auto key = [&](int b) __attribute__((always_inline)) -> uint32_t { return b < p.n_first || b >= n - p.n_last ? 0u : score[b]; };
-#define CS_LIST(C) write_list_held<C>(key, n, p.n_first, p.n_last, p.n_select, out, lane)
-    if (n <= 128) CS_LIST(2);
-    else if (n <= 256) CS_LIST(4);
-    else if (n <= 320) CS_LIST(5);
-    else if (n <= 512) CS_LIST(8);
-    else write_list<0>([&](int c) __attribute__((always_inline)) { return key(c * 64 + lane); }, n, p.n_first, p.n_last, p.n_select, out, lane);
-#undef CS_LIST
+  };
+  request(0);                            // (before anything else: it lands while the queries are looked at)
+  const int candidates = candidates_of(p, t, lane);
+  uint8_t* rows = s_mem + kStage + pair * 32 * Q::QROW;
+  for (int i0 = half; i0 < mine; i0 += 4) {
+    Q q[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) q[i].ask(p, t.first + first + min(i0 + 2 * i, mine - 1), kvh, lane);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (i0 + 2 * i < mine) q[i].put(rows, i0 + 2 * i, lane);
   }
+  const int most = __builtin_amdgcn_readfirstlane(static_cast<int>(cs::lanes_max<64>(static_cast<uint32_t>(candidates))));
+  __syncthreads();
+  i32x4 a[STEPS];
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) a[s] = *reinterpret_cast<const i32x4*>(rows + n * Q::QROW + 32 * s + 16 * h);
+  uint32_t* score = reinterpret_cast<uint32_t*>(s_mem + 2 * kStage) + first * p.pitch;
+
+  const int steps = most > p.n_select ? (most + 63) / 64 : 0;
+  for (int i = 0; i < steps; ++i) {
+    const int block = 64 * i + 32 * half + n;
+    const uint32_t byte = p.scales[head_at + min(block, most - 1)];
+    cs::rows_gate();                     // (the first one: everyone holds its queries)
+    if (i + 1 < steps) request(i + 1);
+    const uint8_t* b = s_mem + (i & 1) * kStage + (32 * half + n) * 2 * D;
+    i32x16 acc = {};
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s)
+      acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[s], *reinterpret_cast<const i32x4*>(b + 16 * ((2 * s + h) ^ cs::row_place<D>(n))), acc, 0, 0, 0);
+    each_score<GP>(acc, byte, h, [&](int tok, uint32_t x) __attribute__((always_inline)) {
+      if (block < most && tok < mine) score[tok * p.pitch + block] = x;
+    });
+  }
+  cs::rows_gate();                       // (also where no step has waited for the first request)
+  for (int i = half; i < mine; i += 2) select_token(p, score + i * p.pitch, t.first + first + i, kvh, __builtin_amdgcn_readlane(candidates, first + i), lane);
 }
 
 }  // namespace
@@ -441,30 +527,31 @@ extern "C" int cs_select_blocks(const void* q, const int8_t* bounds, const uint8
   int gp = 1;
   while (gp < p.group) gp *= 2;
   p.pitch = n_sel;
-  // Few tokens: a workgroup's 16 waves share the blocks of one 32-row tile; many: four waves take two tiles, so that bounds are read half
-  // as often.
   const int tok = 32 / gp < 8 ? 32 / gp : 8;
-  const bool many = n_q >= static_cast<int64_t>(kManyTokens) * n_streams;
-  p.tile = many ? 2 * tok : tok;
-  while (p.tile > 1 && static_cast<int64_t>(p.tile) * p.pitch > kTileScores) p.tile /= 2;
+  // Many tokens: as long as a wave's scores of one token fit beside those of the others.
+  const bool many = n_q >= static_cast<int64_t>(kManyTokens) * n_streams && static_cast<int64_t>(kPairs) * n_sel <= kTileScores;
+  p.tile = many ? kPairs * tok : tok;
+  while (p.tile > (many ? kPairs : 1) && static_cast<int64_t>(p.tile) * p.pitch > kTileScores) p.tile /= 2;
   const int64_t tiles = cs::most_token_tiles(n_q, n_streams, p.tile), groups = tiles * n_kv_heads;
   if (groups > cs::kMostThreads / 1024) return CS_EUNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(groups));
-  const size_t lds = static_cast<size_t>(p.tile) * p.pitch * sizeof(uint32_t);
+  const size_t scores = static_cast<size_t>(p.tile) * p.pitch * sizeof(uint32_t), stage = 64 * 2 * static_cast<size_t>(head_dim);
+  const size_t queries = static_cast<size_t>(kPairs) * 32 * (2 * head_dim + 16);
+  const size_t lds = many ? stage + (queries > stage + scores ? queries : stage + scores) : scores;
   hipStream_t st = cs::as_stream(stream);
-#define CS_LAUNCH_SELECT_SHAPE(BF16, D, GP, W, MT)                                                                                         \
+#define CS_LAUNCH_SELECT_KERNEL(KERNEL, THREADS)                                                                                           \
   do {                                                                                                                                     \
-    if (lds > 48 * 1024) {                                                                                                                 \
-      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(select_blocks_kernel<BF16, D, GP, W, MT>),                    \
-                                               hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));                         \
+    if (lds > 32 * 1024) {                                                                                                                 \
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize,          \
+                                               static_cast<int>(lds));                                                                     \
       if (e != hipSuccess) return cs::note_hip(e);                                                                                         \
     }                                                                                                                                      \
-    hipLaunchKernelGGL((select_blocks_kernel<BF16, D, GP, W, MT>), grid, dim3(64 * W), lds, st, p);                                        \
+    hipLaunchKernelGGL(KERNEL, grid, dim3(THREADS), lds, st, p);                                                                           \
   } while (0)
-#define CS_LAUNCH_SELECT(BF16, D, GP)                        \
-  do {                                                       \
-    if (many) CS_LAUNCH_SELECT_SHAPE(BF16, D, GP, 4, 2);     \
-    else CS_LAUNCH_SELECT_SHAPE(BF16, D, GP, 16, 1);         \
+#define CS_LAUNCH_SELECT(BF16, D, GP)                                                                    \
+  do {                                                                                                   \
+    if (many) CS_LAUNCH_SELECT_KERNEL((select_rows_kernel<BF16, D, GP>), 64 * kRowsWaves);               \
+    else CS_LAUNCH_SELECT_KERNEL((select_blocks_kernel<BF16, D, GP>), 64 * kWide);                       \
   } while (0)
 #define CS_LAUNCH_SELECT_GROUP(BF16, D)              \
   do {                                               \
@@ -482,7 +569,7 @@ extern "C" int cs_select_blocks(const void* q, const int8_t* bounds, const uint8
     else CS_LAUNCH_SELECT_GROUP(false, 64);
   }
 #undef CS_LAUNCH_SELECT_GROUP
-#undef CS_LAUNCH_SELECT_SHAPE
+#undef CS_LAUNCH_SELECT_KERNEL
 #undef CS_LAUNCH_SELECT
   return cs::note_hip(hipGetLastError());
 }

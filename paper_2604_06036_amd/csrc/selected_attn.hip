@@ -23,6 +23,7 @@
 #include <type_traits>
 
 #include "kv4.h"
+#include "lds_rows.h"
 #include "token_tiles.h"
 
 namespace {
@@ -549,7 +550,7 @@ __global__ __launch_bounds__(256) void selected_join_kernel(Params p, int bf16) 
 // skips the steps that none of its tokens reads.
 //   S^T = K Q^T, O^T += V^T P^T      v_mfma_f32_16x16x32_bf16; a lane owns one row and 4 of 16 keys
 // Rows go from memory to LDS directly (global_load_lds_dwordx4: lane l lands at base + 16 l), a step ahead, in two stages, one barrier a step.  Lanes choose which 16-byte chunk of a row they fetch, so that reads spread over the banks: row r of keys holds chunk c at
-// place c ^ k_place(r), of values at c ^ v_place(r).
+// place c ^ row_place(r), of values at c ^ v_place(r).
 constexpr int kStepKeys = 32, kStepGroups = kStepKeys / CS_KV_BLOCK;
 constexpr int kRowsWave = kRows, kRowsWaves = 4;
 constexpr int kRowsListed = 512;         // list elements of a workgroup's tokens
@@ -561,27 +562,7 @@ constexpr int kPlaces = 64;              // groups whose places are looked up at
 inline int rows_tokens(int group) { return kRowsWaves * kRowsWave / group < 32 ? kRowsWaves * kRowsWave / group : 32; }
 
 template <int D>
-__device__ __forceinline__ int k_place(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
-template <int D>
 __device__ __forceinline__ int v_place(int r) { return D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); }
-
-// 16 bytes a lane from sbase + off to LDS.  Inline assembly, so that the compiler does not wait for all of them at the next read of LDS:
-// the pipeline's own waits do.
-__device__ __forceinline__ void to_lds(uint32_t off, const void* sbase, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(sbase), "s"(lds_addr) : "memory", "m0");
-}
-typedef __attribute__((address_space(3))) void lds_void;
-__device__ __forceinline__ uint32_t lds_address(const void* at) { return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)at)); }
-
-template <typename T>
-__device__ __forceinline__ T* uniform(T* at) {
-  const uint64_t x = reinterpret_cast<uintptr_t>(at);
-  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x >> 32));
-  return reinterpret_cast<T*>(static_cast<uintptr_t>(static_cast<uint64_t>(hi) << 32 | lo));
-}
-
-// This wave's requests are in LDS, and its reads of LDS are done; then the others' too.
-__device__ __forceinline__ void gate() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
 
 template <int D>
 __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Params p) {
@@ -673,14 +654,14 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
 
   // ---- this wave's part of a step's requests: half the rows of a group
   constexpr int LR = D / 8, RL = 64 / LR;                  // lanes of a row, rows of a request
-  const uint32_t mem = __builtin_amdgcn_readfirstlane(lds_address(s_mem));
+  const uint32_t mem = __builtin_amdgcn_readfirstlane(cs::lds_address(s_mem));
   const uint32_t row_bytes = static_cast<uint32_t>(p.stride_slot * 2);
   uint32_t row_off[kAsks], k_off[kAsks], v_off[kAsks];
 #pragma unroll
   for (int j = 0; j < kAsks; ++j) {
     const int row = 8 * (wave & 1) + j * RL + lane / LR;
     row_off[j] = static_cast<uint32_t>(row) * row_bytes;
-    k_off[j] = 16 * (lane % LR ^ k_place<D>(row));
+    k_off[j] = 16 * (lane % LR ^ cs::row_place<D>(row));
     v_off[j] = 16 * (lane % LR ^ v_place<D>(row));
   }
   // A lane's group, of those whose places are at hand: first entry, readers, offsets in bytes of its last row and of its cache block.
@@ -697,8 +678,8 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
 #pragma unroll
     for (int j = 0; j < kAsks; ++j) {
       const uint32_t off = min(row_off[j], last_off);
-      to_lds(off + k_off[j], k, to + 1024 * j);
-      to_lds(off + v_off[j], v, to + kTensor + 1024 * j);
+      cs::to_lds(off + k_off[j], k, to + 1024 * j);
+      cs::to_lds(off + v_off[j], v, to + kTensor + 1024 * j);
     }
   };
 
@@ -708,7 +689,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
   sums.m = -INFINITY;
   sums.l = 0.0f;
   // the lane's places in a stage
-  const int v_row = 4 * g + (r16 >> 2), k_at = r16 * D * 2, k_turn = k_place<D>(r16), v_at = v_row * D * 2 + 16 * ((r16 >> 1) & 1) + 8 * (r16 & 1), v_turn = v_place<D>(v_row);
+  const int v_row = 4 * g + (r16 >> 2), k_at = r16 * D * 2, k_turn = cs::row_place<D>(r16), v_at = v_row * D * 2 + 16 * ((r16 >> 1) & 1) + 8 * (r16 & 1), v_turn = v_place<D>(v_row);
   const auto compute = [&](int i) __attribute__((always_inline)) {
     int first[kStepGroups];
     uint32_t mask[kStepGroups];
@@ -795,7 +776,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
     __syncthreads();                     // (the stages are free)
     request(0);
     for (int i = 0; i < steps; ++i) {
-      gate();
+      cs::rows_gate();
       if (i + 1 < steps) request(i + 1);                   // (into the stage that everyone has read a step ago)
       if (active >> (kStepGroups * i) & 1) compute(i);
     }

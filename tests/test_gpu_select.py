@@ -458,6 +458,8 @@ def test_bounds_table_shorter_than_said(cs):
     ([5000], [3], 6, 2, 64, "bf16", 16, 256, 0, 7, "tail"),                      # past 256 blocks
     ([12000], [2], 4, 1, 64, "bf16", 16, 20, 1, 2, "tail"),                      # past 512 blocks
     ([100] * 70, [1] * 70, 7, 1, 64, "bf16", 16, 4, 1, 1, "any"),                # more streams than lanes
+    ([15000], [9], 2, 1, 64, "bf16", 16, 30, 1, 2, "tail"),                      # past 512 blocks, many tokens
+    ([20000], [1], 2, 1, 64, "bf16", 16, 12, 1, 2, "tail"),                      # past 1,024
 ])
 def test_selection(cs, kv, nq, hq, hkv, d, dtype, size, n_select, n_first, n_last, where):
     say("select", len(kv), sum(nq), hq, hkv, d, dtype, size, n_select, n_first, n_last, where)
@@ -465,6 +467,30 @@ def test_selection(cs, kv, nq, hq, hkv, d, dtype, size, n_select, n_first, n_las
     qs = c.queries(nq, hq, where=where, extra=3)
     got = c.select(qs, size, n_select, n_first, n_last).cpu().numpy()
     assert np.array_equal(got, c.want_selected(qs, size, n_select, n_first, n_last))
+
+
+@pytest.mark.parametrize("n_blocks,nq", [(2500, 1), (2500, 11), (32768, 2)])
+def test_selection_among_thousands_of_blocks(cs, n_blocks, nq):
+    """The longest tables: scores by whole numbers in float64 (all below 2^24), sorted."""
+    say("select, thousands of blocks", n_blocks, nq)
+    d, hq, want = 64, 4, 20
+    gen = torch.Generator(device="cuda").manual_seed(n_blocks)
+    hi = torch.randint(-100, 128, (n_blocks, d), generator=gen, device=DEV)
+    lo = hi - torch.randint(0, 28, hi.shape, generator=gen, device=DEV)
+    bounds = torch.stack([hi, lo], 1).to(torch.int8).contiguous()
+    scales = torch.randint(118, 123, (n_blocks,), generator=gen, device=DEV).to(torch.uint8)
+    q = torch.randn((nq, hq, d), generator=gen, device=DEV).to(torch.bfloat16)
+    last = 16 * n_blocks - 1
+    pos = torch.tensor([last - 700 * i for i in range(nq)], dtype=torch.int32, device=DEV)
+    out = torch.full((nq, 1, want), -7, dtype=torch.int32, device=DEV)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    cs.cs_select_blocks(q, bounds, scales, i32(0, nq), pos, i32(16 * n_blocks), n_blocks, 16, want, 2, 3, out, nq, 1, hq, 1, d, cs.CS_BF16)
+    for t in range(nq):
+        codes = so.query_codes(f64(q[t]))
+        c = torch.from_numpy(codes).double().to(DEV)
+        score = (torch.maximum(c[:, None] * hi.double(), c[:, None] * lo.double()).sum(-1).amax(0) * torch.exp2(scales.double() - 127)).cpu().numpy()
+        n = int(pos[t]) // 16 + 1
+        assert out[t, 0].tolist() == so.select(score.tolist(), n, want, 2, 3)
 
 
 def test_selection_of_equal_scores_and_odd_numbers(cs):
