@@ -504,7 +504,7 @@ _ELEMENT = {CS_F32: torch.float32, CS_BF16: torch.bfloat16}
 def _held(fn: str, specs, workspace=None, workspace_bytes=None):
     """Addresses of a call's tensors, the bytes of its workspace, and the stream.  specs: (tensor or None, name, least number of elements
     or None, type or None, whether its elements have to lie behind one another).  One pass: this is most of what a small call costs."""
-    ptrs, devices = [], set()
+    ptrs, devices = [], []
     for t, what, n, dtype, dense in specs:
         if t is None:
             ptrs.append(None)
@@ -515,19 +515,19 @@ def _held(fn: str, specs, workspace=None, workspace_bytes=None):
             raise ValueError(f"{fn}: {what} is not contiguous")
         if n is not None and t.numel() < n:
             raise ValueError(f"{fn}: {what} holds {t.numel()} elements, {n} needed")
-        devices.add(t.get_device())
+        devices.append(t.get_device())
         ptrs.append(t.data_ptr())
     held = 0
     if workspace is not None:
         held = workspace.numel() * workspace.element_size()
-        devices.add(workspace.get_device())
+        devices.append(workspace.get_device())
     if workspace_bytes is not None and held < workspace_bytes:
         raise ValueError(f"{fn}: workspace tensor smaller than workspace_bytes")
     if -1 in devices:
         raise ValueError(f"{fn}: device tensor expected")
     device = torch.cuda.current_device()
-    if devices and devices != {device}:      # the work goes to the current device's stream
-        raise ValueError(f"{fn}: tensors on device {sorted(devices)}, the current device is {device}")
+    if devices.count(device) != len(devices):      # the work goes to the current device's stream
+        raise ValueError(f"{fn}: tensors on devices {sorted(set(devices))}, the current device is {device}")
     return (ptrs, None if workspace is None else workspace.data_ptr(), held if workspace_bytes is None else workspace_bytes,
             torch._C._cuda_getCurrentRawStream(device))
 

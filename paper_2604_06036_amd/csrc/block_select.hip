@@ -112,11 +112,11 @@ __global__ __launch_bounds__(256) void key_bounds_kernel(BoundsParams p) {
         lo[e] = fminf(lo[e], __uint_as_float(cs::lane_dpp<0x128>(__float_as_uint(lo[e]))));
       }
       if (LR <= 16) {
-        hi[e] = fmaxf(hi[e], cs::lane_xor16(hi[e]));
-        lo[e] = fminf(lo[e], cs::lane_xor16(lo[e]));
+        hi[e] = cs::with_lane16(hi[e], cs::larger);
+        lo[e] = cs::with_lane16(lo[e], cs::smaller);
       }
-      hi[e] = fmaxf(hi[e], cs::lane_xor32(hi[e]));
-      lo[e] = fminf(lo[e], cs::lane_xor32(lo[e]));
+      hi[e] = cs::with_lane32(hi[e], cs::larger);
+      lo[e] = cs::with_lane32(lo[e], cs::smaller);
     }
     const uint32_t byte = scale_byte(cs::lanes_max<64>(amax));
     const float inv = inverse_scale(byte == kNoNumber ? 127u : byte);

@@ -289,9 +289,9 @@ __device__ __forceinline__ void sweep(const Params& p, const Kind& kind, const L
         high = fmaxf(high, s[b][r]);
       }
     }
-    high = fmaxf(high, cs::lane_xor16(high));
-    high = fmaxf(high, cs::lane_xor32(high));
-    if (__any((high - sums.m) * c > kSlack)) {            // (-inf - -inf: no)
+    // (the row's lanes hold different keys; they share a maximum, and look at each other's only to raise it.  -inf - -inf: no)
+    if (__any((high - sums.m) * c > kSlack)) {
+      high = cs::with_lane32(cs::with_lane16(high, cs::larger), cs::larger);
       const float raised = fmaxf(sums.m, high);
       const float f = sums.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((sums.m - raised) * c);
 #pragma unroll
@@ -485,8 +485,7 @@ __global__ __launch_bounds__(64 * NW) void selected_attn_kernel(Params p) {
     }
     sums = kept;
   }
-  sums.l += cs::lane_xor16(sums.l);
-  sums.l += cs::lane_xor32(sums.l);
+  sums.l = cs::with_lane32(cs::with_lane16(sums.l, cs::plus), cs::plus);
 
   // ---- results
   const int64_t at_job = (static_cast<int64_t>(tile) * p.n_kv_heads + kvh) * p.pieces + piece;
@@ -723,9 +722,8 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
       const float a = fmaxf(fmaxf(s[b][0], s[b][1]), fmaxf(s[b][2], s[b][3]));
       high = fmaxf(high, mask[b] >> bit & 1 ? a : -INFINITY);
     }
-    high = fmaxf(high, cs::lane_xor16(high));
-    high = fmaxf(high, cs::lane_xor32(high));
-    if (__any((high - sums.m) * c > kSlack)) {             // (-inf - -inf: no)
+    if (__any((high - sums.m) * c > kSlack)) {             // (as above)
+      high = cs::with_lane32(cs::with_lane16(high, cs::larger), cs::larger);
       const float raised = fmaxf(sums.m, high);
       const float f = sums.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((sums.m - raised) * c);
 #pragma unroll
@@ -781,8 +779,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
       if (active >> (kStepGroups * i) & 1) compute(i);
     }
   }
-  sums.l += cs::lane_xor16(sums.l);
-  sums.l += cs::lane_xor32(sums.l);
+  sums.l = cs::with_lane32(cs::with_lane16(sums.l, cs::plus), cs::plus);
 
   // ---- results; where something is no number or infinite, again token by token, the waves in turn
   if (tid == 0) s_odd = 0;
@@ -817,8 +814,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
       kind.load_query(p.q, (static_cast<int64_t>(tok1) * p.n_q_heads + head1) * D, g);
       Sums<D> one;
       sweep<Again, D>(p, kind, locate, 0, 2, n_groups, i, live1 ? pos1 : -1, true, i, pos1, lds, lane, one);
-      one.l += cs::lane_xor16(one.l);
-      one.l += cs::lane_xor32(one.l);
+      one.l = cs::with_lane32(cs::with_lane16(one.l, cs::plus), cs::plus);
       if (live1) {
         Again::each4(one, g, [&](int ch, const float (&x)[4]) __attribute__((always_inline)) {
           float y[4] = {x[0], x[1], x[2], x[3]};

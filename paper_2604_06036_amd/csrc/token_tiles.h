@@ -54,15 +54,20 @@ inline int64_t most_token_tiles(int64_t n_q, int32_t n_streams, int tile) {
   return one + (n_q - one) / tile;
 }
 
-__device__ __forceinline__ float lane_xor32(float x) {
+// What an operation makes of a value and the one of lane ^ 32, lane ^ 16: the swaps leave both lanes' values in both lanes.
+template <class F>
+__device__ __forceinline__ float with_lane32(float x, const F& f) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+  return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-
-__device__ __forceinline__ float lane_xor16(float x) {
+template <class F>
+__device__ __forceinline__ float with_lane16(float x, const F& f) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float((threadIdx.x & 16) ? r[0] : r[1]);
+  return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
+__device__ __forceinline__ float plus(float a, float b) { return a + b; }
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float smaller(float a, float b) { return fminf(a, b); }
 
 template <int kCtrl>
 __device__ __forceinline__ uint32_t lane_dpp(uint32_t x) {
@@ -76,8 +81,14 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t x) {
   if (kLanes > 2) x = max(x, lane_dpp<0x4e>(x));
   if (kLanes > 4) x = max(x, lane_dpp<0x141>(x));
   if (kLanes > 8) x = max(x, lane_dpp<0x140>(x));
-  if (kLanes > 16) x = max(x, __float_as_uint(lane_xor16(__uint_as_float(x))));
-  if (kLanes > 32) x = max(x, __float_as_uint(lane_xor32(__uint_as_float(x))));
+  if (kLanes > 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = max(r[0], r[1]);
+  }
+  if (kLanes > 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    x = max(r[0], r[1]);
+  }
   return x;
 }
 
