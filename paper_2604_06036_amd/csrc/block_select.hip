@@ -154,7 +154,12 @@ struct SelectParams {
   int32_t max_blocks, n_streams, n_q_heads, n_kv_heads, group, n_sel, size, n_select, n_first, n_last, tile, pitch;
 };
 
-constexpr int kManyTokens = 8;           // a stream, on average, from which every wave has rows of its own
+// Which kernel: workgroups of 16 waves share a tile's blocks out among themselves, as long as all of them are on the card at once (two a
+// CU); past that pairs of waves with rows of their own do more for what they read.  28 on 4 heads, 276 blocks, wide / pairs: 64 tokens 7.6 /
+// 12.6 us, 256 8.2 / 12.8, 512 12.2 / 13.3, 768 (the first over 512 workgroups) 16.8 / 13.3, 1,024 21.1 / 13.6.  And a pair needs
+// the scores of two tokens at once: 1,250 blocks, 1,024 tokens 59 / 70 us, 938 blocks, 2,082 tokens 83 / 62 us.
+constexpr int kWideGroups = 512;
+constexpr int kPairTokens = 2;
 constexpr int kMostBlocks = 32768;       // whose scores a workgroup holds in LDS for one token
 constexpr int kTileScores = 8192;        // ... for a tile of tokens
 
@@ -528,10 +533,13 @@ extern "C" int cs_select_blocks(const void* q, const int8_t* bounds, const uint8
   while (gp < p.group) gp *= 2;
   p.pitch = n_sel;
   const int tok = 32 / gp < 8 ? 32 / gp : 8;
-  // Many tokens: as long as a wave's scores of one token fit beside those of the others.
-  const bool many = n_q >= static_cast<int64_t>(kManyTokens) * n_streams && static_cast<int64_t>(kPairs) * n_sel <= kTileScores;
-  p.tile = many ? kPairs * tok : tok;
-  while (p.tile > (many ? kPairs : 1) && static_cast<int64_t>(p.tile) * p.pitch > kTileScores) p.tile /= 2;
+  p.tile = tok;
+  while (p.tile > 1 && static_cast<int64_t>(p.tile) * p.pitch > kTileScores) p.tile /= 2;
+  const bool many = cs::most_token_tiles(n_q, n_streams, p.tile) * n_kv_heads > kWideGroups && static_cast<int64_t>(kPairs) * kPairTokens * n_sel <= kTileScores;
+  if (many) {
+    p.tile = kPairs * tok;
+    while (static_cast<int64_t>(p.tile) * p.pitch > kTileScores) p.tile /= 2;
+  }
   const int64_t tiles = cs::most_token_tiles(n_q, n_streams, p.tile), groups = tiles * n_kv_heads;
   if (groups > cs::kMostThreads / 1024) return CS_EUNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(groups));

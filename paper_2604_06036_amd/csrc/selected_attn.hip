@@ -314,8 +314,8 @@ __device__ __forceinline__ void sweep(const Params& p, const Kind& kind, const L
 }
 
 constexpr int kJoinBatch = 8;
-// What is joined: results of 16 rows, `ml` [way][16][2] and `o` [way][16][D].  A thread takes four channels of a row, kJoinBatch ways at a time.
-template <int D>
+// What is joined: results of R rows, `ml` [way][R][2] and `o` [way][R][D].  A thread takes four channels of a row, kJoinBatch ways at a time.
+template <int D, int R>
 __device__ __forceinline__ void join_rows(const float* ml, const float* o, int ways, int row, int ch, float c, float* m_out, float* l_out, float (&x)[4]) {
   float m = -INFINITY, l = 0.0f;
   x[0] = x[1] = x[2] = x[3] = 0.0f;
@@ -325,8 +325,8 @@ __device__ __forceinline__ void join_rows(const float* ml, const float* o, int w
 #pragma unroll
     for (int i = 0; i < kJoinBatch; ++i) {
       const int w = min(w0 + i, ways - 1);
-      stat[i] = *reinterpret_cast<const cs::f32v2*>(ml + (w * kRows + row) * 2);
-      v[i] = *reinterpret_cast<const f32x4*>(o + (w * kRows + row) * D + ch);
+      stat[i] = *reinterpret_cast<const cs::f32v2*>(ml + (w * R + row) * 2);
+      v[i] = *reinterpret_cast<const f32x4*>(o + (w * R + row) * D + ch);
     }
     float high = m;
 #pragma unroll
@@ -516,7 +516,7 @@ __global__ __launch_bounds__(64 * NW) void selected_attn_kernel(Params p) {
       const int row = i / (D / 4), ch = i % (D / 4) * 4;
       if (row >= t.count * p.group) continue;
       float m, l, x[4];
-      join_rows<D>(s_ml, s_o, NW, row, ch, c, &m, &l, x);
+      join_rows<D, kRows>(s_ml, s_o, NW, row, ch, c, &m, &l, x);
       if (p.pieces == 1) {
         write_row<D>(p, t.first + row / p.group, kvh * p.group + row % p.group, ch, m, l, x, Kind::kBf16);
       } else {
@@ -527,20 +527,19 @@ __global__ __launch_bounds__(64 * NW) void selected_attn_kernel(Params p) {
   }
 }
 
-// The pieces of a tile and kv head, joined.
-template <int D>
+// The pieces of a tile and kv head, joined: R rows a tile, four channels of one a thread.
+template <int D, int R>
 __global__ __launch_bounds__(256) void selected_join_kernel(Params p, int bf16) {
   const int kvh = static_cast<int>(blockIdx.x % p.n_kv_heads), tile = static_cast<int>(blockIdx.x / p.n_kv_heads);
   cs::TokenTile t;
   if (!cs::find_token_tile(p.cu_q, p.n_streams, p.n_q, p.tile, tile, &t)) return;
   if (min(p.kv_len[t.stream], p.max_blocks * CS_KV_BLOCK) <= 0) return;
   const int64_t at_job = (static_cast<int64_t>(tile) * p.n_kv_heads + kvh) * p.pieces;
-  for (int i = threadIdx.x; i < t.count * p.group * (D / 4); i += 256) {
-    const int row = i / (D / 4), ch = i % (D / 4) * 4;
-    float m, l, x[4];
-    join_rows<D>(p.ws_ml + at_job * kRows * 2, p.ws_o + at_job * kRows * D, p.pieces, row, ch, p.scale_log2e, &m, &l, x);
-    write_row<D>(p, t.first + row / p.group, kvh * p.group + row % p.group, ch, m, l, x, bf16 != 0);
-  }
+  const int i = blockIdx.y * 256 + threadIdx.x, row = i / (D / 4), ch = i % (D / 4) * 4;
+  if (row >= t.count * p.group) return;
+  float m, l, x[4];
+  join_rows<D, R>(p.ws_ml + at_job * R * 2, p.ws_o + at_job * R * D, p.pieces, row, ch, p.scale_log2e, &m, &l, x);
+  write_row<D>(p, t.first + row / p.group, kvh * p.group + row % p.group, ch, m, l, x, bf16 != 0);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -551,14 +550,14 @@ __global__ __launch_bounds__(256) void selected_join_kernel(Params p, int bf16) 
 // Rows go from memory to LDS directly (global_load_lds_dwordx4: lane l lands at base + 16 l), a step ahead, in two stages, one barrier a step.  Lanes choose which 16-byte chunk of a row they fetch, so that reads spread over the banks: row r of keys holds chunk c at
 // place c ^ row_place(r), of values at c ^ v_place(r).
 constexpr int kStepKeys = 32, kStepGroups = kStepKeys / CS_KV_BLOCK;
-constexpr int kRowsWave = kRows, kRowsWaves = 4;
+constexpr int kRowsWave = kRows, kRowsWaves = 4, kRowsGroup = kRowsWave * kRowsWaves;
 constexpr int kRowsListed = 512;         // list elements of a workgroup's tokens
 constexpr int kChunk = 1024;             // blocks whose readers are collected at once
 constexpr int kStages = 2;
 constexpr int kPlaces = 64;              // groups whose places are looked up at once, a lane each
 
 // Tokens of a workgroup: as many as fit, and as masks of 32 bits hold.
-inline int rows_tokens(int group) { return kRowsWaves * kRowsWave / group < 32 ? kRowsWaves * kRowsWave / group : 32; }
+inline int rows_tokens(int group) { return kRowsGroup / group < 32 ? kRowsGroup / group : 32; }
 
 template <int D>
 __device__ __forceinline__ int v_place(int r) { return D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); }
@@ -582,8 +581,9 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, g = lane >> 4;
   const int kvh = static_cast<int>(blockIdx.x % p.n_kv_heads);
+  const int job = static_cast<int>(blockIdx.x / p.n_kv_heads), piece = job % p.pieces, tile = job / p.pieces;
   cs::TokenTile t;
-  if (!cs::find_token_tile(p.cu_q, p.n_streams, p.n_q, p.tile, static_cast<int>(blockIdx.x / p.n_kv_heads), &t)) return;
+  if (!cs::find_token_tile(p.cu_q, p.n_streams, p.n_q, p.tile, tile, &t)) return;
   const int entries = min(p.kv_len[t.stream], p.max_blocks * CS_KV_BLOCK);
   if (entries <= 0) return;
   const int size = p.cache_blocks * CS_KV_BLOCK;
@@ -629,7 +629,10 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
     }
     __syncthreads();
   }
-  const int n_groups = __builtin_amdgcn_readfirstlane(count) * p.cache_blocks;
+  // this piece's groups, whole steps
+  const int all_groups = __builtin_amdgcn_readfirstlane(count) * p.cache_blocks;
+  const int a_piece = ((all_groups + kStepGroups - 1) / kStepGroups + p.pieces - 1) / p.pieces * kStepGroups;
+  const int begin = min(piece * a_piece, all_groups), n_groups = min(begin + a_piece, all_groups);
 
   // ---- the lane's row
   const int in_group = wave * kRowsWave + r16, bit = in_group / p.group;      // bit: the token, of the workgroup's
@@ -759,7 +762,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
   };
 
   // ---- the steps, kPlaces groups at a time
-  for (int g0 = 0; g0 < n_groups; g0 += kPlaces) {
+  for (int g0 = begin; g0 < n_groups; g0 += kPlaces) {
     const int here = min(kPlaces, n_groups - g0), steps = (here + kStepGroups - 1) / kStepGroups;
     const int gi = g0 + min(lane, here - 1), u = gi / p.cache_blocks;
     at_first = (s_list[u] * p.cache_blocks + (gi - u * p.cache_blocks)) * CS_KV_BLOCK;
@@ -782,6 +785,15 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
   sums.l = cs::with_lane32(cs::with_lane16(sums.l, cs::plus), cs::plus);
 
   // ---- results; where something is no number or infinite, again token by token, the waves in turn
+  const int64_t at_row = ((static_cast<int64_t>(tile) * p.n_kv_heads + kvh) * p.pieces + piece) * kRowsGroup;
+  const auto leave = [&](int token, int row, int ch, const Sums<D>& of, float (&y)[4]) __attribute__((always_inline)) {
+    if (p.pieces == 1) {
+      write_row<D>(p, token, kvh * p.group + row % p.group, ch, of.m, of.l, y, true);
+    } else {
+      if (ch == 0) *reinterpret_cast<cs::f32v2*>(p.ws_ml + (at_row + row) * 2) = cs::f32v2{of.m, of.l};
+      *reinterpret_cast<f32x4*>(p.ws_o + (at_row + row) * D + ch) = f32x4{y[0], y[1], y[2], y[3]};
+    }
+  };
   if (tid == 0) s_odd = 0;
   bool odd = false;
 #pragma unroll
@@ -813,12 +825,12 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
       Again kind;
       kind.load_query(p.q, (static_cast<int64_t>(tok1) * p.n_q_heads + head1) * D, g);
       Sums<D> one;
-      sweep<Again, D>(p, kind, locate, 0, 2, n_groups, i, live1 ? pos1 : -1, true, i, pos1, lds, lane, one);
+      sweep<Again, D>(p, kind, locate, begin, 2, n_groups, i, live1 ? pos1 : -1, true, i, pos1, lds, lane, one);
       one.l = cs::with_lane32(cs::with_lane16(one.l, cs::plus), cs::plus);
       if (live1) {
         Again::each4(one, g, [&](int ch, const float (&x)[4]) __attribute__((always_inline)) {
           float y[4] = {x[0], x[1], x[2], x[3]};
-          write_row<D>(p, tok1, head1, ch, one.m, one.l, y, true);
+          leave(tok1, i * p.group + r16, ch, one, y);
         });
       }
     }
@@ -827,7 +839,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
   if (!live) return;
   Again::each4(sums, g, [&](int ch, const float (&x)[4]) __attribute__((always_inline)) {
     float y[4] = {x[0], x[1], x[2], x[3]};
-    write_row<D>(p, tok, head, ch, sums.m, sums.l, y, true);
+    leave(tok, in_group, ch, sums, y);
   });
 }
 
@@ -841,11 +853,19 @@ struct Shape {
   bool rows;                             // the kernel for many tokens a stream
   int tile, pieces, waves;
   int64_t tiles;
+  size_t partials;                       // bytes of the pieces' results
 };
-constexpr int kGroupsWanted = 512;       // workgroups wanted of the few-rows kernel
+// Pieces, so that few tokens fill the card too.  A token over 16 / 32 blocks of 64: one piece 20 us, at most 4 11.4 / 14.9, 8 10.7 / 12.3.
+// 9 tokens over 16 blocks each, in the rows kernel: one piece 54 us, 8 17; 256 tokens 70 and 34; 1,024 tokens (two pieces) 80 and 75.
 constexpr int kMostPieces = 8;
-constexpr int kManyTokens = 8;           // a stream, on average, from which the rows kernel is taken
-Shape shape_of(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads, int32_t sel_block, int32_t n_select, bool bf16, int64_t stride_slot) {
+constexpr int kGroupsWanted = 512;       // workgroups wanted of the few-rows kernel
+constexpr int kRowsWanted = 1024;        // ... of the rows kernel, as many as are on the card at once (512: 1,024 tokens 84 us; 2,048: 2,082 tokens 125)
+constexpr int kRowsSteps = 4;            // steps of a piece of its sweep at least (2: the same)
+// Tokens a stream, on average, from which bf16 takes the rows kernel.  Few rows / rows kernel: one token 10.6 / 11.6 us, two 15.4 / 13.5; 16
+// streams of 2 tokens 22.3 / 18.9, of 8 30.6 / 25.5; 64 streams of 8 96 / 76.  (8 tokens of a stream over 8 blocks of 16 keys: 14.2 / 15.1.)
+constexpr int kManyTokens = 2;
+Shape shape_of(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t sel_block, int32_t n_select, bool bf16,
+               int64_t stride_slot) {
   Shape s;
   const int group = n_q_heads / n_kv_heads;
   s.rows = bf16 && n_q >= static_cast<int64_t>(kManyTokens) * n_streams && stride_slot < 1ll << 26;      // (offsets of a cache block in 32 bits)
@@ -853,7 +873,10 @@ Shape shape_of(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_h
     const int all = rows_tokens(group), by_lists = kRowsListed / n_select;
     s.tile = all < by_lists ? all : by_lists;
     s.tiles = cs::most_token_tiles(n_q, n_streams, s.tile);
-    s.pieces = 1;
+    const int64_t jobs = s.tiles * n_kv_heads, spare = kRowsWanted / jobs;
+    const int64_t steps = static_cast<int64_t>(n_select) * sel_block / (kStepKeys * kRowsSteps), most = spare < steps ? spare : steps;      // (lists that are all alike)
+    s.pieces = static_cast<int>(most < 1 ? 1 : most < kMostPieces ? most : kMostPieces);
+    s.partials = s.pieces == 1 ? 0 : static_cast<size_t>(jobs) * s.pieces * kRowsGroup * (head_dim + 2) * sizeof(float);
     return s;
   }
   s.tile = tile_of(group, n_select);
@@ -863,6 +886,7 @@ Shape shape_of(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_h
   s.pieces = static_cast<int>(most < 1 ? 1 : most < steps ? most : steps);
   const int64_t each = (steps + s.pieces - 1) / s.pieces;
   s.waves = each >= 4 ? 4 : each >= 2 ? 2 : 1;
+  s.partials = s.pieces == 1 ? 0 : static_cast<size_t>(jobs) * s.pieces * kRows * (head_dim + 2) * sizeof(float);
   return s;
 }
 
@@ -872,9 +896,10 @@ extern "C" size_t cs_selected_attn_workspace(int64_t n_q, int32_t n_streams, int
                                              int32_t sel_block, int32_t n_select) {
   if (n_q < 1 || n_streams < 1 || n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % n_kv_heads || n_q_heads / n_kv_heads > kRows) return 0;
   if (sel_block < 1 || n_select < 1 || n_select > CS_SELECT_MOST || head_dim < 1 || n_q >= 1ll << 26) return 0;
-  const Shape s = shape_of(n_q, n_streams, n_q_heads, n_kv_heads, sel_block, n_select, false, 0);
-  if (s.pieces == 1) return 0;
-  return static_cast<size_t>(s.tiles) * n_kv_heads * s.pieces * kRows * (head_dim + 2) * sizeof(float);
+  // (either type's)
+  const size_t rows = shape_of(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, sel_block, n_select, true, 0).partials;
+  const size_t few = shape_of(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, sel_block, n_select, false, 0).partials;
+  return rows > few ? rows : few;
 }
 
 extern "C" int cs_selected_attn(const void* q, const void* k_cache_layer, const void* v_cache_layer, const int32_t* cu_q, const int32_t* q_pos,
@@ -896,7 +921,7 @@ extern "C" int cs_selected_attn(const void* q, const void* k_cache_layer, const 
   if (n_q == 0 || n_streams == 0) return CS_OK;
   if (!q || !k_cache_layer || !v_cache_layer || !cu_q || !q_pos || !kv_len || !block_table || !selected || !out) return CS_EINVAL;
   if (!cs::aligned16(q) || !cs::aligned16(k_cache_layer) || !cs::aligned16(v_cache_layer) || !cs::aligned16(out)) return CS_EUNSUPPORTED;
-  const Shape s = shape_of(n_q, n_streams, n_q_heads, n_kv_heads, sel_block, n_select, dtype == CS_BF16, stride_slot);
+  const Shape s = shape_of(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, sel_block, n_select, dtype == CS_BF16, stride_slot);
   const size_t need = cs_selected_attn_workspace(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, sel_block, n_select);
   if (need && (!workspace || !cs::aligned16(workspace) || workspace_bytes < need)) return CS_EWORKSPACE;
   const int64_t groups = s.tiles * n_kv_heads * s.pieces;
@@ -913,7 +938,7 @@ extern "C" int cs_selected_attn(const void* q, const void* k_cache_layer, const 
   p.out = out;
   p.lse = lse;
   p.ws_o = static_cast<float*>(workspace);
-  p.ws_ml = need ? p.ws_o + groups * kRows * head_dim : nullptr;
+  p.ws_ml = s.partials ? p.ws_o + groups * (s.rows ? kRowsGroup : kRows) * head_dim : nullptr;
   p.n_q = n_q;
   p.stride_slot = stride_slot;
   p.stride_head = stride_head;
@@ -949,9 +974,13 @@ extern "C" int cs_selected_attn(const void* q, const void* k_cache_layer, const 
   if (s.pieces > 1) {
     const int status = cs::note_hip(hipGetLastError());
     if (status != CS_OK) return status;
-    const dim3 joins(static_cast<unsigned>(s.tiles * n_kv_heads));
-    if (head_dim == 128) hipLaunchKernelGGL(selected_join_kernel<128>, joins, dim3(256), 0, st, p, dtype == CS_BF16);
-    else hipLaunchKernelGGL(selected_join_kernel<64>, joins, dim3(256), 0, st, p, dtype == CS_BF16);
+    const int rows = s.rows ? kRowsGroup : kRows;
+    const dim3 joins(static_cast<unsigned>(s.tiles * n_kv_heads), static_cast<unsigned>(rows * (head_dim / 4) / 256));
+    const int bf16 = dtype == CS_BF16;
+    if (head_dim == 128 && s.rows) hipLaunchKernelGGL((selected_join_kernel<128, kRowsGroup>), joins, dim3(256), 0, st, p, bf16);
+    else if (head_dim == 128) hipLaunchKernelGGL((selected_join_kernel<128, kRows>), joins, dim3(256), 0, st, p, bf16);
+    else if (s.rows) hipLaunchKernelGGL((selected_join_kernel<64, kRowsGroup>), joins, dim3(256), 0, st, p, bf16);
+    else hipLaunchKernelGGL((selected_join_kernel<64, kRows>), joins, dim3(256), 0, st, p, bf16);
   }
   return cs::note_hip(hipGetLastError());
 }
