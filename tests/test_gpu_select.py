@@ -493,6 +493,29 @@ def test_selection_among_thousands_of_blocks(cs, n_blocks, nq):
         assert out[t, 0].tolist() == so.select(score.tolist(), n, want, 2, 3)
 
 
+@pytest.mark.parametrize("kv,nq,hq,hkv,d,dtype,size,n_select,n_first,n_last", [
+    ([3000, 0, 1700], [300, 0, 260], 28, 4, 128, "bf16", 16, 12, 1, 2), ([900], [300], 64, 4, 64, "bf16", 32, 5, 0, 1), ([2000], [280], 16, 16, 64, "f32", 16, 20, 1, 0),
+    ([16000], [520], 28, 4, 64, "bf16", 16, 30, 1, 2), ([700, 40, 1], [400, 130, 1], 8, 4, 128, "f32", 48, 3, 0, 0), ([8500], [515], 12, 4, 128, "bf16", 16, 256, 1, 2)])
+def test_selection_of_many_tokens(cs, kv, nq, hq, hkv, d, dtype, size, n_select, n_first, n_last):
+    """So many tokens that waves have rows of their own: the lists of calls of few tokens, and for some of them the oracle's."""
+    say("select, many tokens", kv, nq, hq, hkv, d, dtype, size, n_select, n_first, n_last)
+    c = Cache(cs, sum(kv) + d, hkv, d, kv, dtype)
+    qs = c.queries(nq, hq, where="any", extra=3)
+    bounds = c.bounds(size)
+    got = c.select(qs, size, n_select, n_first, n_last, bounds)
+    assert torch.all(got[sum(nq):] == -7)
+    at = 0
+    for s, n in enumerate(nq):
+        for a in range(at, at + n, 50):
+            m = min(50, at + n - a)
+            few = dict(hq=hq, n_q=m, q=qs["q"][a:a + m].contiguous(), q_pos=qs["q_pos"][a:a + m].contiguous(), cu_q=dev(np.array([0] * (s + 1) + [m] * (len(kv) - s), np.int32)))
+            assert torch.equal(c.select(few, size, n_select, n_first, n_last, bounds), got[a:a + m]), (s, a)
+        at += n
+    some = np.random.default_rng(1).permutation(sum(nq))[:12]
+    part = dict(hq=hq, n_q=len(some), q64=qs["q64"][some], pos=qs["pos"][some], stream=qs["stream"][some])
+    assert np.array_equal(got.cpu().numpy()[some], c.want_selected(part, size, n_select, n_first, n_last))
+
+
 def test_selection_of_equal_scores_and_odd_numbers(cs):
     """Equal blocks go by index; blocks without numbers come first; a query without numbers has equal scores; negative scores have an order."""
     say("select, ties and odd numbers")
@@ -567,6 +590,43 @@ def test_attention(cs, kv, nq, hq, hkv, d, dtype, size, n_select, where, layout,
     c.check_attention(qs, listed, size, out, stat)
     again, none = c.attend(qs, dev(listed), size, lse=False)
     assert none is None and torch.equal(out.view(torch.int16 if dtype == "bf16" else torch.int32), again.view(torch.int16 if dtype == "bf16" else torch.int32))
+
+
+@pytest.mark.parametrize("kv,nq,hq,hkv,d,dtype,size,n_select,layout", [
+    ([2000], [132], 256, 16, 64, "bf16", 16, 48, "slot"),           # one piece a tile, more places than are looked up at once
+    ([1500, 0, 300], [90, 0, 44], 256, 16, 128, "bf16", 32, 20, "head"),
+    ([1500, 600], [70, 70], 32, 4, 128, "bf16", 64, 8, "slot"),      # pieces
+    ([900], [20], 7, 1, 64, "bf16", 16, 90, "slot"),
+    ([300, 80, 5, 1, 20], [4, 0, 1, 1, 0], 7, 1, 128, "bf16", 16, 6, "slot"),      # several tokens in the kernel of few rows
+    ([900, 80, 5, 1, 20], [5, 0, 1, 0, 1], 8, 4, 64, "bf16", 64, 8, "head"),
+])
+@pytest.mark.parametrize("kind", ["sorted", "wild"])
+def test_attention_whole_and_in_pieces(cs, kv, nq, hq, hkv, d, dtype, size, n_select, layout, kind):
+    say("attention, pieces", kv, nq, hq, hkv, d, dtype, size, n_select, layout, kind)
+    c = Cache(cs, sum(kv) + d, hkv, d, kv, dtype, layout)
+    qs = c.queries(nq, hq, where="any", extra=2, gain=2.0)
+    listed = any_lists(c.rng, c, qs, size, n_select, kind)
+    out, stat = c.attend(qs, dev(listed), size)
+    c.check_attention(qs, listed, size, out, stat)
+    again, _ = c.attend(qs, dev(listed), size)
+    assert torch.equal(out.view(torch.int16), again.view(torch.int16))
+
+
+@pytest.mark.parametrize("nq", [[12, 3], [12, 0, 0, 0, 0, 0, 0, 0]])
+@pytest.mark.parametrize("hq,hkv,d", [(4, 2, 64), (7, 1, 128), (16, 16, 64)])
+def test_what_is_no_number_in_one_piece(cs, hq, hkv, d, nq):
+    """Blocks of 64 keys, so that the sweep is in pieces, of which some hold what is no number, before and behind the queries."""
+    say("attention, odd numbers in pieces", hq, hkv, d, nq)
+    c = Cache(cs, 7, hkv, d, [900] + [64] * (len(nq) - 1), "bf16")
+    for which, j, h, col, x in ((1, 40, 0, 3, np.nan), (1, 300, 0, 0, np.inf), (1, 301, 0, 1, -np.inf), (0, 500, 0, 5, np.nan), (1, 700, 0, d - 1, np.nan), (1, 899, 0, 2, np.inf)):
+        c.put(which, 0, j, h, col, x)
+    qs = c.queries(nq, hq, where="tail")
+    qs["pos"][:12] = [899, 39, 40, 299, 300, 498, 699, 898, 899, 450, 5, -1]
+    qs["q_pos"].copy_(dev(qs["pos"]))
+    listed = np.stack([np.stack([np.sort(c.rng.permutation(15)[:9]) for _ in range(hkv)]) for _ in range(sum(nq))]).astype(np.int32)
+    out, stat = c.attend(qs, dev(listed), 64)
+    c.check_attention(qs, listed, 64, out, stat)
+    assert np.isnan(f64(out)).any() and np.isinf(f64(out)).any()
 
 
 def test_all_blocks_are_the_window_attention(cs):
