@@ -658,30 +658,39 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
   constexpr int LR = D / 8, RL = 64 / LR;                  // lanes of a row, rows of a request
   const uint32_t mem = __builtin_amdgcn_readfirstlane(cs::lds_address(s_mem));
   const uint32_t row_bytes = static_cast<uint32_t>(p.stride_slot * 2);
-  uint32_t row_off[kAsks], k_off[kAsks], v_off[kAsks];
+  const auto row_of = [&](int j) __attribute__((always_inline)) { return 8 * (wave & 1) + j * RL + lane / LR; };
+  const auto k_part = [&](int j) __attribute__((always_inline)) { return 16u * (lane % LR ^ cs::row_place<D>(row_of(j))); };
+  const auto v_part = [&](int j) __attribute__((always_inline)) { return 16u * (lane % LR ^ v_place<D>(row_of(j))); };
+  uint32_t k_off[kAsks], v_off[kAsks];
 #pragma unroll
   for (int j = 0; j < kAsks; ++j) {
-    const int row = 8 * (wave & 1) + j * RL + lane / LR;
-    row_off[j] = static_cast<uint32_t>(row) * row_bytes;
-    k_off[j] = 16 * (lane % LR ^ cs::row_place<D>(row));
-    v_off[j] = 16 * (lane % LR ^ v_place<D>(row));
+    k_off[j] = row_of(j) * row_bytes + k_part(j);
+    v_off[j] = row_of(j) * row_bytes + v_part(j);
   }
-  // A lane's group, of those whose places are at hand: first entry, readers, offsets in bytes of its last row and of its cache block.
+  // A lane's group, of those whose places are at hand: first entry, readers, last row, offset in bytes of its cache block.
   int at_first = 0, at_last = 0;
   uint32_t at_mask = 0, at_low = 0, at_high = 0;
-  const auto request = [&](int i) __attribute__((always_inline)) {
+  const auto request = [&](int i, int stage) __attribute__((always_inline)) {
     const int from = kStepGroups * i + (wave >> 1);
     const uint64_t off64 = static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at_high), from))) << 32 |
                            static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at_low), from));
-    const uint32_t last_off = static_cast<uint32_t>(__builtin_amdgcn_readlane(at_last, from));
+    const int last = __builtin_amdgcn_readlane(at_last, from);
     const char* k = static_cast<const char*>(p.k) + off64;
     const char* v = static_cast<const char*>(p.v) + off64;
-    const uint32_t to = mem + (i % kStages) * kStage + wave * (1024 * kAsks);
+    const uint32_t to = mem + stage * kStage + wave * (1024 * kAsks);
+    if (last == CS_KV_BLOCK - 1) {
 #pragma unroll
-    for (int j = 0; j < kAsks; ++j) {
-      const uint32_t off = min(row_off[j], last_off);
-      cs::to_lds(off + k_off[j], k, to + 1024 * j);
-      cs::to_lds(off + v_off[j], v, to + kTensor + 1024 * j);
+      for (int j = 0; j < kAsks; ++j) {
+        cs::to_lds(k_off[j], k, to + 1024 * j);
+        cs::to_lds(v_off[j], v, to + kTensor + 1024 * j);
+      }
+    } else {                             // (rows past the last entry that anyone sees are that one)
+#pragma unroll
+      for (int j = 0; j < kAsks; ++j) {
+        const uint32_t off = min(row_of(j), last) * row_bytes;
+        cs::to_lds(off + k_part(j), k, to + 1024 * j);
+        cs::to_lds(off + v_part(j), v, to + kTensor + 1024 * j);
+      }
     }
   };
 
@@ -690,9 +699,16 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
   for (int db = 0; db < DB; ++db) sums.o[db] = f32x4{};
   sums.m = -INFINITY;
   sums.l = 0.0f;
-  // the lane's places in a stage
-  const int v_row = 4 * g + (r16 >> 2), k_at = r16 * D * 2, k_turn = cs::row_place<D>(r16), v_at = v_row * D * 2 + 16 * ((r16 >> 1) & 1) + 8 * (r16 & 1), v_turn = v_place<D>(v_row);
-  const auto compute = [&](int i) __attribute__((always_inline)) {
+  float total[4] = {};                   // sums of weights
+  // the lane's places in the first stage
+  const int v_row = 4 * g + (r16 >> 2);
+  const uint8_t *k_at[STEPS], *v_at[DB];
+#pragma unroll
+  for (int j = 0; j < STEPS; ++j) k_at[j] = s_mem + r16 * D * 2 + 16 * ((4 * j + g) ^ cs::row_place<D>(r16));
+#pragma unroll
+  for (int db = 0; db < DB; ++db) v_at[db] = s_mem + kTensor + v_row * D * 2 + 16 * ((r16 >> 1) & 1) + 8 * (r16 & 1) + 16 * ((2 * db) ^ v_place<D>(v_row));
+  const auto compute = [&](int i, auto which) __attribute__((always_inline)) {
+    constexpr int kHere = decltype(which)::value * kStage;
     int first[kStepGroups];
     uint32_t mask[kStepGroups];
 #pragma unroll
@@ -700,14 +716,12 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
       first[b] = __builtin_amdgcn_readlane(at_first, kStepGroups * i + b);
       mask[b] = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at_mask), kStepGroups * i + b));
     }
-    const uint8_t* k = s_mem + (i % kStages) * kStage;
-    const uint8_t* v = k + kTensor;
     f32x4 s[kStepGroups] = {};
 #pragma unroll
     for (int j = 0; j < STEPS; ++j)
 #pragma unroll
       for (int b = 0; b < kStepGroups; ++b)
-        s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8*>(k + k_at + b * 16 * D * 2 + 16 * ((4 * j + g) ^ k_turn)), query[j], s[b], 0, 0, 0);
+        s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8*>(k_at[j] + kHere + b * 16 * D * 2), query[j], s[b], 0, 0, 0);
     // A group that the lane's token does not read has the exponent -inf; only a group that ends behind one of the tokens is masked key
     // by key.
     if (max(first[0], first[1]) + CS_KV_BLOCK - 1 > least) {
@@ -733,11 +747,11 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
       for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int r = 0; r < 4; ++r) sums.o[db][r] *= f;
-      sums.l *= f;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) total[r] *= f;
       sums.m = raised;
     }
     const float base = sums.m == -INFINITY ? 0.0f : -sums.m * c;
-    float total[4] = {};
     // of the 32 keys of a product a lane's weights are of 4 g + 0..3 of two groups; a row's place does not change 16 rows further
 #pragma unroll
     for (int st = 0; st < kStepGroups / 2; ++st) {
@@ -751,14 +765,13 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
       const bf16x8 pf = __builtin_bit_cast(bf16x8, cs::u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])});
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        const uint8_t* at = v + v_at + 16 * ((2 * db) ^ v_turn) + 32 * st * D * 2;
+        const uint8_t* at = v_at[db] + kHere + 32 * st * D * 2;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * D * 2));
         const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         sums.o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, sums.o[db], 0, 0, 0);
       }
     }
-    sums.l += (total[0] + total[1]) + (total[2] + total[3]);
   };
 
   // ---- the steps, kPlaces groups at a time
@@ -771,18 +784,22 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
     const uint64_t off64 = static_cast<uint64_t>((static_cast<int64_t>(ids[cb]) * CS_KV_BLOCK * p.stride_slot + head_at) * 2);
     at_low = static_cast<uint32_t>(off64);
     at_high = static_cast<uint32_t>(off64 >> 32);
-    at_last = static_cast<int>(min(CS_KV_BLOCK - 1, top - cb * CS_KV_BLOCK) * row_bytes);
+    at_last = min(CS_KV_BLOCK - 1, top - cb * CS_KV_BLOCK);
     // (bit i: whether a token of this wave reads something of step i)
     const uint64_t groups = __ballot((at_mask & wave_mask) != 0), active = groups | groups >> 1;
     __syncthreads();                     // (the stages are free)
-    request(0);
-    for (int i = 0; i < steps; ++i) {
+    request(0, 0);
+    const auto step = [&](int i, auto which) __attribute__((always_inline)) {
       cs::rows_gate();
-      if (i + 1 < steps) request(i + 1);                   // (into the stage that everyone has read a step ago)
-      if (active >> (kStepGroups * i) & 1) compute(i);
+      if (i + 1 < steps) request(i + 1, 1 - decltype(which)::value);       // (into the stage that everyone has read a step ago)
+      if (active >> (kStepGroups * i) & 1) compute(i, which);
+    };
+    for (int i = 0; i < steps; i += 2) {
+      step(i, std::integral_constant<int, 0>());
+      if (i + 1 < steps) step(i + 1, std::integral_constant<int, 1>());
     }
   }
-  sums.l = cs::with_lane32(cs::with_lane16(sums.l, cs::plus), cs::plus);
+  sums.l = cs::with_lane32(cs::with_lane16((total[0] + total[1]) + (total[2] + total[3]), cs::plus), cs::plus);
 
   // ---- results; where something is no number or infinite, again token by token, the waves in turn
   const int64_t at_row = ((static_cast<int64_t>(tile) * p.n_kv_heads + kvh) * p.pieces + piece) * kRowsGroup;
