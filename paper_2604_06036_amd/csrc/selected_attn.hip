@@ -32,6 +32,7 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
 
 struct Params {
   const void* __restrict__ q;
@@ -702,11 +703,17 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
   float total[4] = {};                   // sums of weights
   // the lane's places in the first stage
   const int v_row = 4 * g + (r16 >> 2);
-  const uint8_t *k_at[STEPS], *v_at[DB];
+  uint32_t k_at[STEPS], v_at[DB];        // (LDS addresses, kept from being worked out again at every use)
 #pragma unroll
-  for (int j = 0; j < STEPS; ++j) k_at[j] = s_mem + r16 * D * 2 + 16 * ((4 * j + g) ^ cs::row_place<D>(r16));
+  for (int j = 0; j < STEPS; ++j) {
+    k_at[j] = mem + r16 * D * 2 + 16 * ((4 * j + g) ^ cs::row_place<D>(r16));
+    asm("" : "+v"(k_at[j]));
+  }
 #pragma unroll
-  for (int db = 0; db < DB; ++db) v_at[db] = s_mem + kTensor + v_row * D * 2 + 16 * ((r16 >> 1) & 1) + 8 * (r16 & 1) + 16 * ((2 * db) ^ v_place<D>(v_row));
+  for (int db = 0; db < DB; ++db) {
+    v_at[db] = mem + kTensor + v_row * D * 2 + 16 * ((r16 >> 1) & 1) + 8 * (r16 & 1) + 16 * ((2 * db) ^ v_place<D>(v_row));
+    asm("" : "+v"(v_at[db]));
+  }
   const auto compute = [&](int i, auto which) __attribute__((always_inline)) {
     constexpr int kHere = decltype(which)::value * kStage;
     int first[kStepGroups];
@@ -721,7 +728,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
     for (int j = 0; j < STEPS; ++j)
 #pragma unroll
       for (int b = 0; b < kStepGroups; ++b)
-        s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8*>(k_at[j] + kHere + b * 16 * D * 2), query[j], s[b], 0, 0, 0);
+        s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*((lds_bf16x8*)k_at[j] + (kHere + b * 16 * D * 2) / 16), query[j], s[b], 0, 0, 0);
     // A group that the lane's token does not read has the exponent -inf; only a group that ends behind one of the tokens is masked key
     // by key.
     if (max(first[0], first[1]) + CS_KV_BLOCK - 1 > least) {
@@ -765,9 +772,9 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
       const bf16x8 pf = __builtin_bit_cast(bf16x8, cs::u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])});
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        const uint8_t* at = v_at[db] + kHere + 32 * st * D * 2;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * D * 2));
+        lds_s16x4* at = (lds_s16x4*)v_at[db] + (kHere + 32 * st * D * 2) / 8;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at + 16 * D * 2 / 8);
         const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         sums.o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, sums.o[db], 0, 0, 0);
       }
