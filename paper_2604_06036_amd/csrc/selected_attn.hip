@@ -563,7 +563,8 @@ inline int rows_tokens(int group) { return kRowsGroup / group < 32 ? kRowsGroup 
 template <int D>
 __device__ __forceinline__ int v_place(int r) { return D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); }
 
-template <int D>
+// kPaired: the groups of a step are of one listed block (those of an even number of cache blocks).
+template <int D, bool kPaired>
 __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Params p) {
   constexpr int DB = D / 16, STEPS = D / 32;
   constexpr int kTensor = kStepKeys * D * 2;               // bytes of a step's keys, or values
@@ -638,6 +639,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
   // ---- the lane's row
   const int in_group = wave * kRowsWave + r16, bit = in_group / p.group;      // bit: the token, of the workgroup's
   const bool live = bit < t.count;
+  const uint32_t my_bit = live ? 1u << bit : 0;
   const int tok = t.first + (live ? bit : 0), head = kvh * p.group + (live ? in_group % p.group : 0);
   const int pos = live ? min(p.q_pos[tok], entries - 1) : -1;
   const int bits0 = wave * kRowsWave / p.group, bits1 = min((wave * kRowsWave + kRowsWave - 1) / p.group, t.count - 1);       // the wave's tokens
@@ -699,7 +701,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
 #pragma unroll
   for (int db = 0; db < DB; ++db) sums.o[db] = f32x4{};
   sums.m = -INFINITY;
-  sums.l = 0.0f;
+  float base = INFINITY;                 // the exponents' constant: - m c
   float total[4] = {};                   // sums of weights
   // the lane's places in the first stage
   const int v_row = 4 * g + (r16 >> 2);
@@ -717,11 +719,11 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
   const auto compute = [&](int i, auto which) __attribute__((always_inline)) {
     constexpr int kHere = decltype(which)::value * kStage;
     int first[kStepGroups];
-    uint32_t mask[kStepGroups];
+    bool reads[kStepGroups];
 #pragma unroll
     for (int b = 0; b < kStepGroups; ++b) {
-      first[b] = __builtin_amdgcn_readlane(at_first, kStepGroups * i + b);
-      mask[b] = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at_mask), kStepGroups * i + b));
+      first[b] = kPaired && b ? first[0] + CS_KV_BLOCK : __builtin_amdgcn_readlane(at_first, kStepGroups * i + b);
+      reads[b] = kPaired && b ? reads[0] : (static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at_mask), kStepGroups * i + b)) & my_bit) != 0;
     }
     f32x4 s[kStepGroups] = {};
 #pragma unroll
@@ -740,13 +742,15 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
           if (r > lim) s[b][r] = -INFINITY;
       }
     }
-    float high = -INFINITY;
-#pragma unroll
-    for (int b = 0; b < kStepGroups; ++b) {
-      const float a = fmaxf(fmaxf(s[b][0], s[b][1]), fmaxf(s[b][2], s[b][3]));
-      high = fmaxf(high, mask[b] >> bit & 1 ? a : -INFINITY);
+    float high = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), s[0][2]), s[0][3]);
+    if constexpr (kPaired) {
+      high = fmaxf(fmaxf(fmaxf(high, s[1][0]), fmaxf(s[1][1], s[1][2])), s[1][3]);
+      high = reads[0] ? high : -INFINITY;
+    } else {
+      const float other = fmaxf(fmaxf(fmaxf(s[1][0], s[1][1]), s[1][2]), s[1][3]);
+      high = fmaxf(reads[0] ? high : -INFINITY, reads[1] ? other : -INFINITY);
     }
-    if (__any((high - sums.m) * c > kSlack)) {             // (as above)
+    if (__any(fmaf(high, c, base) > kSlack)) {             // (as above; before the first one base is inf, and inf - inf no reason)
       high = cs::with_lane32(cs::with_lane16(high, cs::larger), cs::larger);
       const float raised = fmaxf(sums.m, high);
       const float f = sums.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((sums.m - raised) * c);
@@ -757,8 +761,8 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
 #pragma unroll
       for (int r = 0; r < 4; ++r) total[r] *= f;
       sums.m = raised;
+      base = -raised * c;
     }
-    const float base = sums.m == -INFINITY ? 0.0f : -sums.m * c;
     // of the 32 keys of a product a lane's weights are of 4 g + 0..3 of two groups; a row's place does not change 16 rows further
 #pragma unroll
     for (int st = 0; st < kStepGroups / 2; ++st) {
@@ -766,7 +770,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int b = 2 * st + e / 4;
-        x[e] = __builtin_amdgcn_exp2f(fmaf(s[b][e % 4], c, mask[b] >> bit & 1 ? base : -INFINITY));
+        x[e] = __builtin_amdgcn_exp2f(fmaf(s[b][e % 4], c, reads[b] ? base : -INFINITY));
         total[e % 4] += x[e];
       }
       const bf16x8 pf = __builtin_bit_cast(bf16x8, cs::u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])});
@@ -985,8 +989,11 @@ extern "C" int cs_selected_attn(const void* q, const void* k_cache_layer, const 
     else hipLaunchKernelGGL((selected_attn_kernel<KIND<D>, D, 1>), grid, dim3(64), 0, st, p);                              \
   } while (0)
   if (s.rows) {
-    if (head_dim == 128) hipLaunchKernelGGL(selected_rows_kernel<128>, grid, dim3(64 * kRowsWaves), 0, st, p);
-    else hipLaunchKernelGGL(selected_rows_kernel<64>, grid, dim3(64 * kRowsWaves), 0, st, p);
+    const bool paired = p.cache_blocks % kStepGroups == 0;
+    if (head_dim == 128 && paired) hipLaunchKernelGGL((selected_rows_kernel<128, true>), grid, dim3(64 * kRowsWaves), 0, st, p);
+    else if (head_dim == 128) hipLaunchKernelGGL((selected_rows_kernel<128, false>), grid, dim3(64 * kRowsWaves), 0, st, p);
+    else if (paired) hipLaunchKernelGGL((selected_rows_kernel<64, true>), grid, dim3(64 * kRowsWaves), 0, st, p);
+    else hipLaunchKernelGGL((selected_rows_kernel<64, false>), grid, dim3(64 * kRowsWaves), 0, st, p);
   } else if (dtype == CS_BF16) {
     if (head_dim == 128) CS_LAUNCH_SELECTED(Bf16, 128);
     else CS_LAUNCH_SELECTED(Bf16, 64);
