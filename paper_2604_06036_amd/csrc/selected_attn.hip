@@ -656,6 +656,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
   const int32_t* ids = p.block_table + static_cast<int64_t>(t.stream) * p.max_blocks;
   const int64_t head_at = static_cast<int64_t>(kvh) * p.stride_head;
   const float c = p.scale_log2e;
+  constexpr float kNone = 3.402823466e38f;                 // the constant without a maximum: any score is a reason to raise it, and -inf has weight 0
 
   // ---- this wave's part of a step's requests: half the rows of a group
   constexpr int LR = D / 8, RL = 64 / LR;                  // lanes of a row, rows of a request
@@ -701,7 +702,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
 #pragma unroll
   for (int db = 0; db < DB; ++db) sums.o[db] = f32x4{};
   sums.m = -INFINITY;
-  float base = INFINITY;                 // the exponents' constant: - m c
+  float base = kNone;                    // the exponents' constant: - m c
   float total[4] = {};                   // sums of weights
   // the lane's places in the first stage
   const int v_row = 4 * g + (r16 >> 2);
@@ -725,6 +726,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
       first[b] = kPaired && b ? first[0] + CS_KV_BLOCK : __builtin_amdgcn_readlane(at_first, kStepGroups * i + b);
       reads[b] = kPaired && b ? reads[0] : (static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at_mask), kStepGroups * i + b)) & my_bit) != 0;
     }
+    __builtin_amdgcn_s_setprio(1);       // (before waves that wait or ask: 98 -> 94 us)
     f32x4 s[kStepGroups] = {};
 #pragma unroll
     for (int j = 0; j < STEPS; ++j)
@@ -750,7 +752,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
       const float other = fmaxf(fmaxf(fmaxf(s[1][0], s[1][1]), s[1][2]), s[1][3]);
       high = fmaxf(reads[0] ? high : -INFINITY, reads[1] ? other : -INFINITY);
     }
-    if (__any(fmaf(high, c, base) > kSlack)) {             // (as above; before the first one base is inf, and inf - inf no reason)
+    if (__any(fmaf(high, c, base) > kSlack)) {             // (as above)
       high = cs::with_lane32(cs::with_lane16(high, cs::larger), cs::larger);
       const float raised = fmaxf(sums.m, high);
       const float f = sums.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((sums.m - raised) * c);
@@ -761,7 +763,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
 #pragma unroll
       for (int r = 0; r < 4; ++r) total[r] *= f;
       sums.m = raised;
-      base = -raised * c;
+      base = fminf(-raised * c, kNone);
     }
     // of the 32 keys of a product a lane's weights are of 4 g + 0..3 of two groups; a row's place does not change 16 rows further
 #pragma unroll
@@ -783,6 +785,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
         sums.o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, sums.o[db], 0, 0, 0);
       }
     }
+    __builtin_amdgcn_s_setprio(0);
   };
 
   // ---- the steps, kPlaces groups at a time
