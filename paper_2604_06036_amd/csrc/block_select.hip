@@ -159,7 +159,7 @@ struct SelectParams {
 // 12.6 us, 256 8.2 / 12.8, 512 12.2 / 13.3, 768 (the first over 512 workgroups) 16.8 / 13.3, 1,024 21.1 / 13.6.  And a pair needs
 // the scores of two tokens at once: 1,250 blocks, 1,024 tokens 59 / 70 us, 938 blocks, 2,082 tokens 83 / 62 us.
 constexpr int kWideGroups = 512;
-constexpr int kPairTokens = 2;
+constexpr int kPairTokens = 2, kPairBlocks = 1024;
 constexpr int kMostBlocks = 32768;       // whose scores a workgroup holds in LDS for one token
 constexpr int kTileScores = 8192;        // ... for a tile of tokens
 
@@ -170,41 +170,45 @@ __device__ __forceinline__ uint32_t ordered(float x) {
 }
 constexpr uint32_t kOdd = 0xfffffffeu;    // ... of a block that holds what is no number
 
-// The query's list from the scores of its n blocks, more than n_select: those of the first n_first, the last n_last, and the n_select -
-// n_first - n_last largest of the others.  `at(c)` is the lane's score of chunk c, of 64 blocks; fixed blocks and places past n have 0.
-// C: chunks (at least n / 64), or 0: counted when the kernel runs.  The threshold is found bit by bit from the first one in which the
-// scores differ, counting by ballots: the largest T with at least as many scores >= T as are wanted.
+// The largest T with at least `wanted` (> 0) scores >= T, and how many are > T.  `at(c)` is the lane's score of chunk c, 0 where it has none.
+// Found bit by bit from the first one in which the scores differ, counting by ballots.  C: chunks, or 0: counted when the kernel runs.
 template <int C, class F>
-__device__ __forceinline__ void write_list(const F& at, int n, int n_first, int n_last, int n_select, int32_t* out, int lane) {
-  const int chunks = C ? C : (n + 63) / 64, wanted = n_select - n_first - n_last;
-  uint32_t t = 0xffffffffu;                            // (nothing is wanted)
-  int above = 0;                                       // scores > T
-  if (wanted > 0) {
-    uint32_t high = 0, low = 0xffffffffu;
+__device__ __forceinline__ void threshold(const F& at, int chunks, int wanted, uint32_t* t_out, int* above_out) {
+  if (C) chunks = C;
+  uint32_t high = 0, low = 0xffffffffu;
 #pragma unroll(C ? C : 8)
-    for (int c = 0; c < chunks; ++c) {
-      const uint32_t x = at(c);
-      high = max(high, x);
-      low = min(low, x ? x : 0xffffffffu);
-    }
-    high = __builtin_amdgcn_readfirstlane(cs::lanes_max<64>(high));
-    low = ~__builtin_amdgcn_readfirstlane(cs::lanes_max<64>(~low));
-    const int first_bit = 31 - __clz(high ^ low);      // (-1: all are equal)
-    t = first_bit < 0 ? high : high & ~(0xffffffffu >> (31 - first_bit));
-    for (int bit = first_bit; bit >= 0; --bit) {
-      const uint32_t cand = t | 1u << bit;
-      int count = 0;
-#pragma unroll(C ? C : 8)
-      for (int c = 0; c < chunks; ++c) count += __popcll(__ballot(at(c) >= cand));
-      if (count >= wanted) {
-        t = cand;
-        if (count == wanted) break;
-      }
-    }
-#pragma unroll(C ? C : 8)
-    for (int c = 0; c < chunks; ++c) above += __popcll(__ballot(at(c) > t));
+  for (int c = 0; c < chunks; ++c) {
+    const uint32_t x = at(c);
+    high = max(high, x);
+    low = min(low, x ? x : 0xffffffffu);
   }
-  int ties = wanted - above, place = 0;
+  high = __builtin_amdgcn_readfirstlane(cs::lanes_max<64>(high));
+  low = ~__builtin_amdgcn_readfirstlane(cs::lanes_max<64>(~low));
+  const int first_bit = 31 - __clz(high ^ low);        // (-1: all are equal)
+  uint32_t t = first_bit < 0 ? high : high & ~(0xffffffffu >> (31 - first_bit));
+  for (int bit = first_bit; bit >= 0; --bit) {
+    const uint32_t cand = t | 1u << bit;
+    int count = 0;
+#pragma unroll(C ? C : 8)
+    for (int c = 0; c < chunks; ++c) count += __popcll(__ballot(at(c) >= cand));
+    if (count >= wanted) {
+      t = cand;
+      if (count == wanted) break;
+    }
+  }
+  int above = 0;
+#pragma unroll(C ? C : 8)
+  for (int c = 0; c < chunks; ++c) above += __popcll(__ballot(at(c) > t));
+  *t_out = t;
+  *above_out = above;
+}
+
+// The query's list from the scores of its n blocks, more than n_select: those of the first n_first, the last n_last, and the n_select -
+// n_first - n_last largest of the others, of which `above` are > t and the lowest ones = t follow.  Fixed blocks have the score 0.
+template <int C, class F>
+__device__ __forceinline__ void write_list(const F& at, int n, int n_first, int n_last, int n_select, uint32_t t, int above, int32_t* out, int lane) {
+  const int chunks = C ? C : (n + 63) / 64;
+  int ties = n_select - n_first - n_last - above, place = 0;
   const uint64_t below = (1ull << lane) - 1;
 #pragma unroll(C ? C : 8)
   for (int c = 0; c < chunks; ++c) {
@@ -220,16 +224,61 @@ __device__ __forceinline__ void write_list(const F& at, int n, int n_first, int 
   }
 }
 
-template <int C, class F>
-__device__ __forceinline__ void write_list_held(const F& key, int n, int n_first, int n_last, int n_select, int32_t* out, int lane) {
+// The same from scores in registers.  kNarrow, where a few are wanted of many: a bound is found first, from the lanes' largest scores alone;
+// what passes it moves into one register a lane, and the threshold is found there.  `score`: the row in LDS, not needed any more.  (1,563
+// blocks 22.7 -> 19.7 us; with 276 blocks it costs more than it saves, and in the kernel for many tokens registers.)
+constexpr int kFewWanted = 32, kSpare = 8;             // of 64 places; largest scores that may pass the bound beside those wanted
+template <int C, bool kNarrow, class F>
+__device__ __forceinline__ void write_list_held(const F& key, int n, int n_first, int n_last, int n_select, uint32_t* score, int32_t* out, int lane) {
   uint32_t held[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) held[c] = key(c * 64 + lane);
-  write_list<C>([&](int c) __attribute__((always_inline)) { return held[c]; }, n, n_first, n_last, n_select, out, lane);
+  const auto at = [&](int c) __attribute__((always_inline)) { return held[c]; };
+  const int wanted = n_select - n_first - n_last;
+  uint32_t t = 0xffffffffu;                            // (nothing is wanted)
+  int above = 0, passed = 65;
+  if (kNarrow && wanted > 0 && wanted <= kFewWanted) {
+    uint32_t most = held[0];
+#pragma unroll
+    for (int c = 1; c < C; ++c) most = max(most, held[c]);
+    const uint32_t high = __builtin_amdgcn_readfirstlane(cs::lanes_max<64>(most));
+    const uint32_t low = ~__builtin_amdgcn_readfirstlane(cs::lanes_max<64>(~most));
+    const int first_bit = 31 - __clz(high ^ low);
+    uint32_t bound = first_bit < 0 ? high : high & ~(0xffffffffu >> (31 - first_bit));
+    for (int bit = first_bit; bit >= 0; --bit) {
+      const uint32_t cand = bound | 1u << bit;
+      const int count = __popcll(__ballot(most >= cand));
+      if (count >= wanted) {
+        bound = cand;
+        if (count <= wanted + kSpare) break;
+      }
+    }
+    passed = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c) passed += __popcll(__ballot(held[c] >= bound));
+    if (passed <= 64) {
+      const uint64_t below = (1ull << lane) - 1;
+      int place = 0;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const uint64_t all = __ballot(held[c] >= bound);
+        if (held[c] >= bound) score[place + __popcll(all & below)] = held[c];
+        place += __popcll(all);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");              // (a wave's LDS operations are in order)
+      const uint32_t x = lane < passed ? score[lane] : 0u;
+      threshold<1>([&](int) __attribute__((always_inline)) { return x; }, 1, wanted, &t, &above);
+      t = max(t, bound);                 // (below it are others)
+      above = __popcll(__ballot(x > t));
+    }
+  }
+  if (passed > 64 && wanted > 0) threshold<C>(at, C, wanted, &t, &above);
+  write_list<C>(at, n, n_first, n_last, n_select, t, above, out, lane);
 }
 
 constexpr int kWide = 16;                // waves of a workgroup that takes few tokens
 constexpr int kRowsWaves = 8, kPairs = kRowsWaves / 2;     // ... many
+static_assert(kPairs * kPairTokens * kPairBlocks == kTileScores, "what a pair holds at least");
 
 // Tokens whose heads, padded to GP, are 32 rows (8 at most).
 template <int GP>
@@ -245,6 +294,10 @@ struct Query {
   static __device__ __forceinline__ uint32_t number(const cs::u32x4& x, int e) {
     const uint32_t w = x[kBf16 ? e / 2 : e];
     return kBf16 ? (e & 1 ? w & 0xffff0000u : w << 16) : w;
+  }
+  static constexpr float kWhole = 12582912.0f;
+  static __device__ __forceinline__ uint32_t lowest_bytes(const uint32_t (&x)[4]) {
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(x[3], x[2], 0x0c0c0400), __builtin_amdgcn_perm(x[1], x[0], 0x0c0c0400), 0x05040100);
   }
   __device__ __forceinline__ void ask(const SelectParams& p, int tok, int kvh, int lane) {
     const int64_t from = (static_cast<int64_t>(tok) * p.n_q_heads + static_cast<int64_t>(kvh) * p.group) * D;
@@ -268,13 +321,19 @@ struct Query {
     for (int j = 0; j < HELD; ++j) {
       const int c = j * 64 + lane, slot = c / CHUNKS;
       if (slot >= GP) continue;
-      uint32_t up[VE / 4] = {}, down[VE / 4] = {};
+      // A sum with 1.5 x 2^23 rounds to a whole number, whose lowest byte is the code.  (A query that holds what is no number: 0 throughout.)
+      uint32_t up[VE / 4], down[VE / 4];
 #pragma unroll
-      for (int e = 0; e < VE; ++e) {
-        // (a query that holds what is no number: 0 throughout)
-        const int code = byte == kNoNumber ? 0 : static_cast<int>(rintf(__uint_as_float(number(v[j], e)) * inv));
-        up[e / 4] |= static_cast<uint32_t>(max(code, 0)) << (8 * (e % 4));
-        down[e / 4] |= (static_cast<uint32_t>(min(code, 0)) & 0xffu) << (8 * (e % 4));
+      for (int w = 0; w < VE / 4; ++w) {
+        uint32_t u[4], d[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float code = byte == kNoNumber ? kWhole : fmaf(__uint_as_float(number(v[j], 4 * w + e)), inv, kWhole);
+          u[e] = __float_as_uint(fmaxf(code, kWhole));
+          d[e] = __float_as_uint(fminf(code, kWhole));
+        }
+        up[w] = lowest_bytes(u);
+        down[w] = lowest_bytes(d);
       }
       const int r = GP * (k / 2) + slot, row = 8 * (r / 4) + 4 * (k % 2) + r % 4;
       uint8_t* dst = rows + row * QROW + c % CHUNKS * VE;
@@ -309,22 +368,30 @@ __device__ __forceinline__ int candidates_of(const SelectParams& p, const cs::To
   return last < 0 ? 0 : last / p.size + 1;
 }
 
-// The list of token `tok` from its scores, by a wave.
-__device__ __forceinline__ void select_token(const SelectParams& p, const uint32_t* score, int tok, int kvh, int n, int lane) {
+// The list of token `tok` from its scores, by a wave.  kMost: blocks that it may be among (0: any number).
+template <int kMost>
+__device__ __forceinline__ void select_token(const SelectParams& p, uint32_t* score, int tok, int kvh, int n, int lane) {
   int32_t* out = p.selected + (static_cast<int64_t>(tok) * p.n_kv_heads + kvh) * p.n_select;
   if (n <= p.n_select) {
     for (int c = lane; c < p.n_select; c += 64) out[c] = c < n ? c : -1;
     return;
   }
   const auto key = [&](int b) __attribute__((always_inline)) -> uint32_t { return b < p.n_first || b >= n - p.n_last ? 0u : score[b]; };
-#define CS_LIST(C) write_list_held<C>(key, n, p.n_first, p.n_last, p.n_select, out, lane)
+#define CS_LIST(C) write_list_held<C, kMost == 0 && (C >= 16)>(key, n, p.n_first, p.n_last, p.n_select, score, out, lane)
   if (n <= 128) CS_LIST(2);
   else if (n <= 256) CS_LIST(4);
   else if (n <= 320) CS_LIST(5);
   else if (n <= 512) CS_LIST(8);
-  else if (n <= 1024) CS_LIST(16);
+  else if (kMost == 1024 || n <= 1024) CS_LIST(16);
   else if (n <= 2048) CS_LIST(32);
-  else write_list<0>([&](int c) __attribute__((always_inline)) { return key(c * 64 + lane); }, n, p.n_first, p.n_last, p.n_select, out, lane);
+  else {
+    const auto at = [&](int c) __attribute__((always_inline)) { return key(c * 64 + lane); };
+    uint32_t t = 0xffffffffu;            // (nothing is wanted)
+    int above = 0;
+    const int wanted = p.n_select - p.n_first - p.n_last;
+    if (wanted > 0) threshold<0>(at, (n + 63) / 64, wanted, &t, &above);
+    write_list<0>(at, n, p.n_first, p.n_last, p.n_select, t, above, out, lane);
+  }
 #undef CS_LIST
 }
 
@@ -371,7 +438,7 @@ __global__ __launch_bounds__(64 * kWide) void select_blocks_kernel(SelectParams 
     }
   }
   __syncthreads();
-  if (wave < t.count) select_token(p, s_score + wave * p.pitch, t.first + wave, kvh, __builtin_amdgcn_readlane(candidates, wave), lane);
+  if (wave < t.count) select_token<0>(p, s_score + wave * p.pitch, t.first + wave, kvh, __builtin_amdgcn_readlane(candidates, wave), lane);
 }
 
 // Many tokens a stream: two waves of a workgroup share 32 rows, four pairs take 64 columns a step, one wave of a pair the first 32 of them, the
@@ -435,7 +502,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void select_rows_kernel(SelectPara
     });
   }
   cs::rows_gate();                       // (also where no step has waited for the first request)
-  for (int i = half; i < mine; i += 2) select_token(p, score + i * p.pitch, t.first + first + i, kvh, __builtin_amdgcn_readlane(candidates, first + i), lane);
+  for (int i = half; i < mine; i += 2) select_token<kPairBlocks>(p, score + i * p.pitch, t.first + first + i, kvh, __builtin_amdgcn_readlane(candidates, first + i), lane);
 }
 
 }  // namespace
@@ -535,7 +602,7 @@ extern "C" int cs_select_blocks(const void* q, const int8_t* bounds, const uint8
   const int tok = 32 / gp < 8 ? 32 / gp : 8;
   p.tile = tok;
   while (p.tile > 1 && static_cast<int64_t>(p.tile) * p.pitch > kTileScores) p.tile /= 2;
-  const bool many = cs::most_token_tiles(n_q, n_streams, p.tile) * n_kv_heads > kWideGroups && static_cast<int64_t>(kPairs) * kPairTokens * n_sel <= kTileScores;
+  const bool many = cs::most_token_tiles(n_q, n_streams, p.tile) * n_kv_heads > kWideGroups && n_sel <= kPairBlocks;
   if (many) {
     p.tile = kPairs * tok;
     while (static_cast<int64_t>(p.tile) * p.pitch > kTileScores) p.tile /= 2;
