@@ -9,14 +9,16 @@
 //              index that stands twice counts once
 //   S^T        = K Q^T over 16 keys (bf16: v_mfma_f32_16x16x32_bf16, fp32: v_mfma_f32_16x16x4_f32), keys straight from memory in operand
 //              layout; a lane owns one row and 4 keys
-//   softmax    one pass, running maximum and sum in fp32; the reference maximum is raised when a tile exceeds it by more than 2^8.
+//   softmax    one pass, running maximum and sum in fp32; the reference is raised when a tile exceeds it by more than 2^8.  It is held as the
+//              rounded exponent that it stands for, m = round(scale log2(e) s): weights are 2^(scale log2(e) s - m), with one rounding, and
+//              what was summed against another m is taken over by 2^(m - m'), so that no rounding of m reaches the result.
 //              bf16: weights are rounded to bf16, which the products take (half a step is 2^-8 of a weight); their sum is not
 //   O^T       += V^T P^T; P^T is in operand layout as it is.  bf16 values pass through a wave's own part of LDS, whose transposing read
 //              gives the operand; fp32 values come from memory in operand layout
 // The waves of a workgroup take key tiles in turn and join their results at the end; pieces are joined by a second launch.  Few rows are bound
 // by latency (a token over 16 blocks of 64: 10.6 us, both launches), many tokens of their own windows by memory (64 tokens, 278 MB: 53 us,
-// 5.2 TB/s), fp32 by latency with 4 waves a SIMD (1,011 tokens of 16 heads of 64 on 4, 24 blocks of 16: 42 us; keys asked for a step ahead cost
-// registers, hence waves: 52; shared through LDS as below: 48).
+// 5.2 TB/s), fp32 by latency with 4 waves a SIMD (1,011 tokens of 16 heads of 64 on 4, 24 blocks of 16: 44 us; keys asked for a step ahead cost
+// registers, hence waves: 52; rows shared through LDS as below: 48).
 //
 // Entries that a query does not see have weight 0, and values there may be anything: addresses stop at the last entry that a token of the
 // tile sees, and where a sum comes out as no number or infinite, the sweep is done again token by token with the values that the token
@@ -48,16 +50,17 @@ struct Params {
   const int32_t* __restrict__ selected;  // [n_q][n_kv_heads][n_select]
   void* __restrict__ out;
   float* __restrict__ lse;
-  float* __restrict__ ws_ml;             // [tile][kv head][piece][16][2]: reference maximum (raw score), sum
+  float* __restrict__ ws_ml;             // [tile][kv head][piece][16][2]: reference exponent, sum
   float* __restrict__ ws_o;              // [tile][kv head][piece][16][D]: sums, not divided
   int64_t n_q, stride_slot, stride_head;
   int32_t max_blocks, n_streams, n_q_heads, n_kv_heads, group, tile, n_select, cache_blocks, pieces;
-  float scale_log2e;
+  float scale_log2e, scale_rest;         // scale log2(e), and what its rounding left
 };
 
 constexpr int kRows = 16;
 constexpr int kMostListed = 256;         // list elements of a tile
 constexpr float kSlack = 8.0f;           // log2 of how far weights may exceed the reference maximum's
+constexpr float kFar = 1e18f;            // a score, and a factor, past which the factor's rounding is left alone: products stay finite
 constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
@@ -73,7 +76,7 @@ __device__ __forceinline__ void store4(void* out, int64_t at, const float* x, bo
         cs::u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
 }
 
-__device__ __forceinline__ float log_sum(float m, float l, float c) { return l == 0.0f ? -INFINITY : (m * c + __builtin_amdgcn_logf(l)) * kLn2; }
+__device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2; }
 
 // ---- where the 16 keys of a group lie
 struct Group {
@@ -87,7 +90,7 @@ struct Group {
 template <int D>
 struct Sums {
   f32x4 o[D / 16];
-  float m, l;
+  float m, l;                            // reference exponent, sum of weights 2^(exponent - m)
 };
 
 // ---- bf16: 16 * GROUPS keys a step
@@ -219,15 +222,17 @@ struct F32 {
       }
   }
 
-  // (the sum over channels may run in any order: element e of the lanes' vectors is one step of it)
+  // The sum over channels may run in any order: element e of the lanes' vectors is one step of it, and a sum of its own, since four short
+  // sums round less than a long one.
   __device__ __forceinline__ void scores(const Tile& t, f32x4 (&s)[KB]) const {
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
-      s[b] = f32x4{};
+      f32x4 part[4] = {};
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.k[b][i][e], query[i][e], s[b], 0, 0, 0);
+        for (int e = 0; e < 4; ++e) part[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.k[b][i][e], query[i][e], part[e], 0, 0, 0);
+      s[b] = (part[0] + part[1]) + (part[2] + part[3]);
     }
   }
 
@@ -294,10 +299,10 @@ __device__ __forceinline__ void sweep(const Params& p, const Kind& kind, const L
       }
     }
     // (the row's lanes hold different keys; they share a maximum, and look at each other's only to raise it.  -inf - -inf: no)
-    if (__any((high - sums.m) * c > kSlack)) {
+    if (__any(fmaf(high, c, -sums.m) > kSlack)) {
       high = cs::with_lane32(cs::with_lane16(high, cs::larger), cs::larger);
-      const float raised = fmaxf(sums.m, high);
-      const float f = sums.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((sums.m - raised) * c);
+      const float raised = fmaxf(sums.m, high * c);
+      const float f = sums.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sums.m - raised);
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -305,12 +310,15 @@ __device__ __forceinline__ void sweep(const Params& p, const Kind& kind, const L
       sums.l *= f;
       sums.m = raised;
     }
-    const float base = sums.m == -INFINITY ? 0.0f : -sums.m * c;
+    const float base = sums.m == -INFINITY ? 0.0f : -sums.m;
 #pragma unroll
     for (int b = 0; b < KB; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, base));
+        float e = fmaf(s[b][r], c, base);
+        // (fp32: with the rounded factor alone a score of 20 would be off by 1e-6; what is infinite stays so)
+        if constexpr (!Kind::kBf16) e = fmaf(__builtin_amdgcn_fmed3f(s[b][r], -kFar, kFar), p.scale_rest, e);
+        s[b][r] = __builtin_amdgcn_exp2f(e);
         sums.l += s[b][r];
       }
     kind.add(tl, gr, s, sums, lds, lane, careful, limit);
@@ -320,7 +328,7 @@ __device__ __forceinline__ void sweep(const Params& p, const Kind& kind, const L
 constexpr int kJoinBatch = 8;
 // What is joined: results of R rows, `ml` [way][R][2] and `o` [way][R][D].  A thread takes four channels of a row, kJoinBatch ways at a time.
 template <int D, int R>
-__device__ __forceinline__ void join_rows(const float* ml, const float* o, int ways, int row, int ch, float c, float* m_out, float* l_out, float (&x)[4]) {
+__device__ __forceinline__ void join_rows(const float* ml, const float* o, int ways, int row, int ch, float* m_out, float* l_out, float (&x)[4]) {
   float m = -INFINITY, l = 0.0f;
   x[0] = x[1] = x[2] = x[3] = 0.0f;
   for (int w0 = 0; w0 < ways; w0 += kJoinBatch) {
@@ -335,7 +343,7 @@ __device__ __forceinline__ void join_rows(const float* ml, const float* o, int w
     float high = m;
 #pragma unroll
     for (int i = 0; i < kJoinBatch; ++i) high = fmaxf(high, stat[i].x);
-    const float back = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - high) * c);      // (without a maximum there are only zeros, or what is no number)
+    const float back = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - high);      // (without a maximum there are only zeros, or what is no number)
     l *= back;
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] *= back;
@@ -343,7 +351,7 @@ __device__ __forceinline__ void join_rows(const float* ml, const float* o, int w
 #pragma unroll
     for (int i = 0; i < kJoinBatch; ++i) {
       if (w0 + i >= ways) break;
-      const float f = stat[i].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((stat[i].x - m) * c);
+      const float f = stat[i].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(stat[i].x - m);
       l = fmaf(stat[i].y, f, l);
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] = fmaf(v[i][e], f, x[e]);
@@ -359,11 +367,12 @@ __device__ __forceinline__ void write_row(const Params& p, int tok, int head, in
 #pragma unroll
   for (int e = 0; e < 4; ++e) x[e] *= inv;
   store4(p.out, (static_cast<int64_t>(tok) * p.n_q_heads + head) * D + ch, x, bf16);
-  if (ch == 0 && p.lse) p.lse[static_cast<int64_t>(tok) * p.n_q_heads + head] = log_sum(m, l, p.scale_log2e);
+  if (ch == 0 && p.lse) p.lse[static_cast<int64_t>(tok) * p.n_q_heads + head] = log_sum(m, l);
 }
 
+// (fp32, head_dim 64: 128 registers, four waves a SIMD; without the bound 139 and 51 us where it takes 44)
 template <class Kind, int D, int NW>
-__global__ __launch_bounds__(64 * NW) void selected_attn_kernel(Params p) {
+__global__ __launch_bounds__(64 * NW, !Kind::kBf16 && D == 64 ? 4 : 1) void selected_attn_kernel(Params p) {
   constexpr int KB = Kind::KB;
   constexpr int kJoin = NW > 1 ? NW * kRows * (D + 2) * 4 : 16;          // results of the waves, where values were
   constexpr int kBytes = NW * Kind::kLds > kJoin ? NW * Kind::kLds : kJoin;
@@ -452,7 +461,6 @@ __global__ __launch_bounds__(64 * NW) void selected_attn_kernel(Params p) {
   const int32_t* ids = p.block_table + static_cast<int64_t>(t.stream) * p.max_blocks;
   const int64_t head_at = static_cast<int64_t>(kvh) * p.stride_head;
   uint8_t* lds = s_mem + wave * Kind::kLds;
-  const float c = p.scale_log2e;
 
   const auto locate = [&](int first_group, Group (&gr)[KB]) __attribute__((always_inline)) {
 #pragma unroll
@@ -520,7 +528,7 @@ __global__ __launch_bounds__(64 * NW) void selected_attn_kernel(Params p) {
       const int row = i / (D / 4), ch = i % (D / 4) * 4;
       if (row >= t.count * p.group) continue;
       float m, l, x[4];
-      join_rows<D, kRows>(s_ml, s_o, NW, row, ch, c, &m, &l, x);
+      join_rows<D, kRows>(s_ml, s_o, NW, row, ch, &m, &l, x);
       if (p.pieces == 1) {
         write_row<D>(p, t.first + row / p.group, kvh * p.group + row % p.group, ch, m, l, x, Kind::kBf16);
       } else {
@@ -542,7 +550,7 @@ __global__ __launch_bounds__(256) void selected_join_kernel(Params p, int bf16) 
   const int i = blockIdx.y * 256 + threadIdx.x, row = i / (D / 4), ch = i % (D / 4) * 4;
   if (row >= t.count * p.group) return;
   float m, l, x[4];
-  join_rows<D, R>(p.ws_ml + at_job * R * 2, p.ws_o + at_job * R * D, p.pieces, row, ch, p.scale_log2e, &m, &l, x);
+  join_rows<D, R>(p.ws_ml + at_job * R * 2, p.ws_o + at_job * R * D, p.pieces, row, ch, &m, &l, x);
   write_row<D>(p, t.first + row / p.group, kvh * p.group + row % p.group, ch, m, l, x, bf16 != 0);
 }
 
@@ -710,7 +718,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
 #pragma unroll
   for (int db = 0; db < DB; ++db) sums.o[db] = f32x4{};
   sums.m = -INFINITY;
-  float base = kNone;                    // the exponents' constant: - m c
+  float base = kNone;                    // the exponents' constant: - m
   float total[4] = {};                   // sums of weights
   // the lane's places in the first stage
   const int v_row = 4 * g + (r16 >> 2);
@@ -762,8 +770,8 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
     }
     if (__any(fmaf(high, c, base) > kSlack)) {             // (as above)
       high = cs::with_lane32(cs::with_lane16(high, cs::larger), cs::larger);
-      const float raised = fmaxf(sums.m, high);
-      const float f = sums.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((sums.m - raised) * c);
+      const float raised = fmaxf(sums.m, high * c);
+      const float f = sums.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sums.m - raised);
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -771,7 +779,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
 #pragma unroll
       for (int r = 0; r < 4; ++r) total[r] *= f;
       sums.m = raised;
-      base = fminf(-raised * c, kNone);
+      base = fminf(-raised, kNone);
     }
     // of the 32 keys of a product a lane's weights are of 4 g + 0..3 of two groups; a row's place does not change 16 rows further
 #pragma unroll
@@ -990,7 +998,9 @@ extern "C" int cs_selected_attn(const void* q, const void* k_cache_layer, const 
   p.n_select = n_select;
   p.cache_blocks = sel_block / CS_KV_BLOCK;
   p.pieces = s.pieces;
-  p.scale_log2e = softmax_scale * 1.4426950408889634f;
+  const double scale = static_cast<double>(softmax_scale) * 1.4426950408889634;
+  p.scale_log2e = static_cast<float>(scale);
+  p.scale_rest = p.scale_log2e < kFar ? static_cast<float>(scale - p.scale_log2e) : 0.0f;
   hipStream_t st = cs::as_stream(stream);
   const dim3 grid(static_cast<unsigned>(groups));
 #define CS_LAUNCH_SELECTED(KIND, D)                                                                                        \
