@@ -740,12 +740,12 @@ def test_rows_past_32_bits(cs):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_graphs_replayed_beside_eager_calls(cs, dtype):
-    """Two captured chains of different shapes that share a workspace, replayed in turn with eager calls and changed inputs between: each gives
+    """Captured chains of different shapes that share a workspace, replayed in turn with eager calls and changed inputs between: each gives
     what eager calls give, bit for bit."""
     say("graphs", dtype)
     c = Cache(cs, 21, 4, 128, [700, 333, 90], dtype)
     shapes = []
-    for nq, size, n_select in (([1, 1, 1], 64, 6), ([30, 11, 20], 16, 9)):
+    for nq, size, n_select in (([1, 1, 1], 64, 6), ([30, 11, 20], 16, 9), ([620, 300, 70], 16, 12)):
         qs = c.queries(nq, 28, where="tail")
         n_sel = c.n_sel(size)
         b, sc = torch.zeros((3, 4, n_sel, 2, 128), dtype=torch.int8, device=DEV), torch.zeros((3, 4, n_sel), dtype=torch.uint8, device=DEV)
