@@ -999,7 +999,7 @@ extern "C" int cs_selected_attn(const void* q, const void* k_cache_layer, const 
   p.cache_blocks = sel_block / CS_KV_BLOCK;
   p.pieces = s.pieces;
   const double scale = static_cast<double>(softmax_scale) * 1.4426950408889634;
-  p.scale_log2e = static_cast<float>(scale);
+  p.scale_log2e = static_cast<float>(scale < 3.4e38 ? scale : 3.4e38);
   p.scale_rest = p.scale_log2e < kFar ? static_cast<float>(scale - p.scale_log2e) : 0.0f;
   hipStream_t st = cs::as_stream(stream);
   const dim3 grid(static_cast<unsigned>(groups));
