@@ -180,7 +180,7 @@ template <int C, class F>
 __device__ __forceinline__ void threshold(const F& at, int chunks, int wanted, uint32_t* t_out, int* above_out) {
   if (C) chunks = C;
   uint32_t high = 0, low = 0xffffffffu;
-#pragma unroll(C ? C : 8)
+#pragma unroll(C ? C : 1)
   for (int c = 0; c < chunks; ++c) {
     const uint32_t x = at(c);
     high = max(high, x);
@@ -193,7 +193,7 @@ __device__ __forceinline__ void threshold(const F& at, int chunks, int wanted, u
   for (int bit = first_bit; bit >= 0; --bit) {
     const uint32_t cand = t | 1u << bit;
     int count = 0;
-#pragma unroll(C ? C : 8)
+#pragma unroll(C ? C : 1)
     for (int c = 0; c < chunks; ++c) count += __popcll(__ballot(at(c) >= cand));
     if (count >= wanted) {
       t = cand;
@@ -201,7 +201,7 @@ __device__ __forceinline__ void threshold(const F& at, int chunks, int wanted, u
     }
   }
   int above = 0;
-#pragma unroll(C ? C : 8)
+#pragma unroll(C ? C : 1)
   for (int c = 0; c < chunks; ++c) above += __popcll(__ballot(at(c) > t));
   *t_out = t;
   *above_out = above;
@@ -214,7 +214,7 @@ __device__ __forceinline__ void write_list(const F& at, int n, int n_first, int 
   const int chunks = C ? C : (n + 63) / 64;
   int ties = n_select - n_first - n_last - above, place = 0;
   const uint64_t below = (1ull << lane) - 1;
-#pragma unroll(C ? C : 8)
+#pragma unroll(C ? C : 1)
   for (int c = 0; c < chunks; ++c) {
     const uint32_t x = at(c);
     const int block = c * 64 + lane;

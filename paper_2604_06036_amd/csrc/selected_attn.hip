@@ -748,7 +748,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
     for (int j = 0; j < STEPS; ++j)
 #pragma unroll
       for (int b = 0; b < kStepGroups; ++b)
-        s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*((lds_bf16x8*)k_at[j] + (kHere + b * 16 * D * 2) / 16), query[j], s[b], 0, 0, 0);
+        s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*((lds_bf16x8*)static_cast<uintptr_t>(k_at[j]) + (kHere + b * 16 * D * 2) / 16), query[j], s[b], 0, 0, 0);
     // A group that the lane's token does not read has the exponent -inf; only a group that ends behind one of the tokens is masked key
     // by key.
     if (max(first[0], first[1]) + CS_KV_BLOCK - 1 > least) {
@@ -794,7 +794,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Param
       const bf16x8 pf = __builtin_bit_cast(bf16x8, cs::u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])});
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        lds_s16x4* at = (lds_s16x4*)v_at[db] + (kHere + 32 * st * D * 2) / 8;
+        lds_s16x4* at = (lds_s16x4*)static_cast<uintptr_t>(v_at[db]) + (kHere + 32 * st * D * 2) / 8;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at);
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at + 16 * D * 2 / 8);
         const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));

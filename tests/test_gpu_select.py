@@ -692,6 +692,30 @@ def test_a_query_without_numbers_keeps_to_its_heads(cs):
         c.check_attention(qs, listed, 16, out, stat)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq", [[1, 1], [3, 9]])
+def test_scores_of_minus_infinity_alone(cs, dtype, nq):
+    """An infinite key that all of a query's heads meet with the other sign: weight 0 beside others, and nothing seen where it is alone."""
+    say("attention, scores of -inf", dtype, nq)
+    c = Cache(cs, 10, 1, 64, [40, 90], dtype)
+    c.put(0, 0, 0, 0, 5, float("inf"))
+    qs = c.queries(nq, 4, where="tail")
+    qs["q"][:, :, 5] = -1.0
+    qs["q64"][:, :, 5] = -1.0
+    qs["pos"][: nq[0]] = 0 if nq[0] == 1 else [0, 7, 39]
+    qs["q_pos"].copy_(dev(qs["pos"]))
+    listed = np.tile(np.array([0, 1, 2], np.int32), (sum(nq), 1, 1))
+    out, stat = c.attend(qs, dev(listed), 16)
+    assert bool((out[0] == 0).all()) and bool((stat[0] == float("-inf")).all())
+    for t in range(1, sum(nq)):
+        s = int(qs["stream"][t])
+        rows = c.slots[s][so.seen(listed[t, 0], int(qs["pos"][t]), c.kv[s], 16)]
+        want, _ = so.attend(qs["q64"][t], np.where(np.isinf(c.x64[0][rows, 0]), 1e6, c.x64[0][rows, 0]), c.x64[1][rows, 0], 0.125)
+        # (scores below 2^6: weights off by under 2^-15; bf16 weights and results by b each)
+        tol = (2.0 ** -14 + 2 * (B if dtype == "bf16" else U)) * np.abs(c.x64[1][rows, 0]).max()
+        assert np.all(np.abs(f64(out)[t] - want) <= tol)
+
+
 # ------------------------------------------------------------------------------------------ how calls are made
 
 def test_rows_past_32_bits(cs):
