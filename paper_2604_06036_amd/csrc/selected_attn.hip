@@ -579,9 +579,10 @@ inline int rows_tokens(int group) { return kRowsGroup / group < 32 ? kRowsGroup 
 template <int D>
 __device__ __forceinline__ int v_place(int r) { return D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); }
 
-// kPaired: the groups of a step are of one listed block (those of an even number of cache blocks).
+// kPaired: the groups of a step are of one listed block (those of an even number of cache blocks).  Five workgroups a CU at head_dim 64 (32
+// streams of up to 389 tokens: four 86 us, five 81).
 template <int D, bool kPaired>
-__global__ __launch_bounds__(64 * kRowsWaves, 4) void selected_rows_kernel(Params p) {
+__global__ __launch_bounds__(64 * kRowsWaves, D == 64 ? 5 : 4) void selected_rows_kernel(Params p) {
   constexpr int DB = D / 16, STEPS = D / 32;
   constexpr int kTensor = kStepKeys * D * 2;               // bytes of a step's keys, or values
   constexpr int kStage = 2 * kTensor;
