@@ -128,8 +128,8 @@ __global__ __launch_bounds__(256) void norm_rope_write_kernel(NormRopeParams p) 
         ss = token_sum(mine ? ss : 0.0f, p.lanes_per_tok);
         float eps = p.eps;
         if (__builtin_expect(!(ss < INFINITY), 0)) {
-          // squares past the largest number (or what is none): the same with all elements 2^-70 times as large
-          eps = 0.0f;                    // (2^-140 of it, beside a mean square past 2^-20)
+          // squares past the largest number (or what is none): the same with all elements 2^-70 times as large, and eps with their squares
+          eps *= 0x1p-140f;
           ss = 0.0f;
 #pragma unroll
           for (int e = 0; e < kPairs; ++e) {
