@@ -108,10 +108,18 @@ __global__ __launch_bounds__(256) void norm_rope_write_kernel(NormRopeParams p) 
     for (int i = 0; i < kBatch; ++i) {
       const int h = h0 + i;
       if (!(h < h_end && (h < p.n_q_heads || slot >= 0))) continue;        // (the same for all lanes of a token)
+      if (h >= first_v) {                // (as they are: a conversion would make a signalling NaN a quiet one)
+        if (mine) {
+          Elem* dst = static_cast<Elem*>(p.v_cache) + static_cast<int64_t>(slot) * p.stride_slot + static_cast<int64_t>(h - first_v) * p.stride_head;
+          a[i].copy_to(dst + off_a);
+          b[i].copy_to(dst + off_b);
+        }
+        continue;
+      }
       float fa[kPairs], fb[kPairs];
       a[i].get(fa);
       b[i].get(fb);
-      const void* weight = h < p.n_q_heads ? p.q_weight : h < first_v ? p.k_weight : nullptr;
+      const void* weight = h < p.n_q_heads ? p.q_weight : p.k_weight;
       if (weight) {
         const int kind = h < p.n_q_heads ? 0 : 1;
         if (held != kind && mine) {
@@ -146,7 +154,7 @@ __global__ __launch_bounds__(256) void norm_rope_write_kernel(NormRopeParams p) 
           fb[e] = fb[e] * r * wb[e];
         }
       }
-      if (turned && h < first_v) {
+      if (turned) {
         float ya[kPairs], yb[kPairs];
         if (kStyle == CS_ROPE_HALF_SPLIT) {
 #pragma unroll
@@ -169,9 +177,7 @@ __global__ __launch_bounds__(256) void norm_rope_write_kernel(NormRopeParams p) 
       if (h < p.n_q_heads) {
         dst = static_cast<Elem*>(p.q_out) + tok * p.stride_q_out + static_cast<int64_t>(h) * p.head_dim;
       } else {
-        const bool is_v = h >= first_v;
-        dst = static_cast<Elem*>(is_v ? p.v_cache : p.k_cache) + static_cast<int64_t>(slot) * p.stride_slot +
-              static_cast<int64_t>(is_v ? h - first_v : h - p.n_q_heads) * p.stride_head;
+        dst = static_cast<Elem*>(p.k_cache) + static_cast<int64_t>(slot) * p.stride_slot + static_cast<int64_t>(h - p.n_q_heads) * p.stride_head;
       }
       Eight<kBf16>::store(dst + off_a, fa);
       Eight<kBf16>::store(dst + off_b, fb);

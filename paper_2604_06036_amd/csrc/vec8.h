@@ -20,6 +20,7 @@ struct Eight<true> {                     // eight bf16: one 16-byte vector
       f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
   }
+  __device__ __forceinline__ void copy_to(uint16_t* p) const { __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p)); }      // (bit for bit)
   static __device__ __forceinline__ void store(uint16_t* p, const float* f) {
     uint32_t w[4];
 #pragma unroll
@@ -40,6 +41,10 @@ struct Eight<false> {
   __device__ __forceinline__ void get(float* f) const {
     f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
     f[4] = __uint_as_float(w.x); f[5] = __uint_as_float(w.y); f[6] = __uint_as_float(w.z); f[7] = __uint_as_float(w.w);
+  }
+  __device__ __forceinline__ void copy_to(float* p) const {
+    __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
+    __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p + 4));
   }
   static __device__ __forceinline__ void store(float* p, const float* f) {
     __builtin_nontemporal_store(u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])},

@@ -1,10 +1,13 @@
-"""Corners of the operators of long windows: the largest epsilon of a norm beside squares that overflow (needs an MI355X)."""
+"""Corners of the operators of long windows: the largest epsilon of a norm beside squares that overflow, every bit pattern of a value (needs an
+MI355X)."""
 import numpy as np
 import pytest
+import torch
 
-from tests.test_gpu_select import cs, run_write, say  # noqa: F401 (cs: the fixture)
+from tests.test_gpu_select import cs, dev, pool, run_write, say  # noqa: F401 (cs: the fixture)
 
 pytestmark = pytest.mark.gpu
+DEV = "cuda"
 
 
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64), ("f32", 80), ("f32", 16)])
@@ -18,3 +21,28 @@ def test_write_of_an_epsilon_beside_squares_past_the_largest_number(cs, dtype, d
     x = rng.choice([-1.0, 1.0], (n, hq + 2 * hkv, d)) * rng.uniform(0.5, 1.0, (n, hq + 2 * hkv, d))
     x *= np.array([2e19, 1e20, 5e20, 1e22, 1e30, 2e38, 1e19, 3e18, 1e17, 1e10, 1.0, 4e19])[:, None, None]
     run_write(cs, 11, n, hq, hkv, d, 16, dtype, "one", 0, "slot", x=x.reshape(n, -1), eps=eps)
+
+
+@pytest.mark.parametrize("layout", ["slot", "head"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_values_are_copied_bit_for_bit(cs, dtype, layout):
+    """Every pattern of 16 bits (in fp32: as the upper half, the lower one drawn), signalling NaN and the smallest numbers among them."""
+    say("write, value bits", dtype, layout)
+    hkv, d, n = 4, 64, 256
+    bits = np.arange(1 << 16, dtype=np.uint32)
+    if dtype == "f32":
+        bits = (bits << 16 | np.random.default_rng(2).integers(0, 1 << 16, bits.size, dtype=np.uint32)).view(np.int32)
+    else:
+        bits = bits.astype(np.uint16).view(np.int16)
+    t, as_bits = (torch.bfloat16, torch.int16) if dtype == "bf16" else (torch.float32, torch.int32)
+    v = dev(bits.reshape(n, hkv * d)).view(t)
+    k = torch.ones_like(v)
+    slot = dev(np.random.default_rng(3).permutation(n).astype(np.int32))
+    kc, vc = (pool(layout, 1, n, hkv, d, t) for _ in range(2))
+    f = torch.full((d // 2,), 0.01, device=DEV)
+    for weight, pos in ((None, None), (torch.ones((d,), dtype=t, device=DEV), torch.arange(n, dtype=torch.int32, device=DEV))):
+        vc.zero_()
+        cs.cs_norm_rope_refresh_scatter(None, None, k, v, None, weight, slot, pos, None, f, kc, vc, n, 0, hkv, d, d, 0, hkv * d, hkv * d, kc.stride(1), kc.stride(2), 1e-6, 1.0, 0,
+                                        cs.CS_BF16 if dtype == "bf16" else cs.CS_F32)
+        got = vc[0].contiguous().view(as_bits)[slot.long()]
+        assert torch.equal(got, v.view(as_bits).reshape(n, hkv, d))
