@@ -816,7 +816,8 @@ int cs_select_blocks(const void* q, const int8_t* bounds, const uint8_t* scales,
  *  selected     in   int32 [n_q][n_kv_heads][n_select]
  *  lse          out  float [n_q][n_q_heads] or NULL: log sum_j exp(softmax_scale * q[t][h] . K_j) over the entries seen
  *  workspace         cs_selected_attn_workspace() bytes, 16-byte aligned (may be 0, then NULL is accepted); contents need not be
- *                    initialised.  Two calls that overlap in time must not share a workspace.
+ *                    initialised.  The bytes of the largest call serve calls of fewer tokens or streams too (other arguments the same), though
+ *                    these may use more of them.  Two calls that overlap in time must not share a workspace.
  * Errors: CS_EINVAL (null pointer, negative size, n_q_heads not a multiple of n_kv_heads, n_select < 1, softmax_scale not a positive finite
  *         number), CS_EUNSUPPORTED (head_dim not in {64,128}, block_size != 16, sel_block as above, n_select > CS_SELECT_MOST,
  *         n_q_heads/n_kv_heads > 16, strides not multiples of 16 bytes, alignment, unknown dtype, n_q >= 2^26, n_kv_heads > 65,535,

@@ -912,30 +912,48 @@ constexpr int kRowsSteps = 4;            // steps of a piece of its sweep at lea
 // Tokens a stream, on average, from which bf16 takes the rows kernel.  Few rows / rows kernel: one token 10.6 / 11.6 us, two 15.4 / 13.5; 16
 // streams of 2 tokens 22.3 / 18.9, of 8 30.6 / 25.5; 64 streams of 8 96 / 76.  (8 tokens of a stream over 8 blocks of 16 keys: 14.2 / 15.1.)
 constexpr int kManyTokens = 2;
+int most_pieces(int32_t sel_block, int32_t n_select, bool rows) {
+  const int64_t entries = static_cast<int64_t>(n_select) * sel_block;
+  const int64_t steps = rows ? entries / (kStepKeys * kRowsSteps) : (entries + 63) / 64;      // (rows: lists that are all alike)
+  return static_cast<int>(steps < 1 ? 1 : steps < kMostPieces ? steps : kMostPieces);
+}
+int pieces_of(int64_t jobs, int most, bool rows) {
+  const int64_t spare = (rows ? kRowsWanted : kGroupsWanted) / jobs;
+  return static_cast<int>(spare < 1 ? 1 : spare < most ? spare : most);
+}
+int rows_tile_of(int32_t group, int32_t n_select) {
+  const int all = rows_tokens(group), by_lists = kRowsListed / n_select;
+  return all < by_lists ? all : by_lists;
+}
+size_t partials_of(int64_t jobs, int pieces, int32_t head_dim, bool rows) {
+  return pieces == 1 ? 0 : static_cast<size_t>(jobs) * pieces * (rows ? kRowsGroup : kRows) * (head_dim + 2) * sizeof(float);
+}
+
 Shape shape_of(int64_t n_q, int32_t n_streams, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t sel_block, int32_t n_select, bool bf16,
                int64_t stride_slot) {
   Shape s;
   const int group = n_q_heads / n_kv_heads;
   s.rows = bf16 && n_q >= static_cast<int64_t>(kManyTokens) * n_streams && stride_slot < 1ll << 26;      // (offsets of a cache block in 32 bits)
-  if (s.rows) {
-    const int all = rows_tokens(group), by_lists = kRowsListed / n_select;
-    s.tile = all < by_lists ? all : by_lists;
-    s.tiles = cs::most_token_tiles(n_q, n_streams, s.tile);
-    const int64_t jobs = s.tiles * n_kv_heads, spare = kRowsWanted / jobs;
-    const int64_t steps = static_cast<int64_t>(n_select) * sel_block / (kStepKeys * kRowsSteps), most = spare < steps ? spare : steps;      // (lists that are all alike)
-    s.pieces = static_cast<int>(most < 1 ? 1 : most < kMostPieces ? most : kMostPieces);
-    s.partials = s.pieces == 1 ? 0 : static_cast<size_t>(jobs) * s.pieces * kRowsGroup * (head_dim + 2) * sizeof(float);
-    return s;
-  }
-  s.tile = tile_of(group, n_select);
+  s.tile = s.rows ? rows_tile_of(group, n_select) : tile_of(group, n_select);
   s.tiles = cs::most_token_tiles(n_q, n_streams, s.tile);
-  const int64_t jobs = s.tiles * n_kv_heads, steps = (static_cast<int64_t>(n_select) * sel_block + 63) / 64;
-  const int64_t spare = kGroupsWanted / jobs, most = spare < kMostPieces ? spare : kMostPieces;
-  s.pieces = static_cast<int>(most < 1 ? 1 : most < steps ? most : steps);
-  const int64_t each = (steps + s.pieces - 1) / s.pieces;
+  const int64_t jobs = s.tiles * n_kv_heads;
+  s.pieces = pieces_of(jobs, most_pieces(sel_block, n_select, s.rows), s.rows);
+  const int64_t each = ((static_cast<int64_t>(n_select) * sel_block + 63) / 64 + s.pieces - 1) / s.pieces;      // steps of a piece, few rows
   s.waves = each >= 4 ? 4 : each >= 2 ? 2 : 1;
-  s.partials = s.pieces == 1 ? 0 : static_cast<size_t>(jobs) * s.pieces * kRows * (head_dim + 2) * sizeof(float);
+  s.partials = partials_of(jobs, s.pieces, head_dim, s.rows);
   return s;
+}
+
+// Bytes that any call of up to n_q tokens and n_streams streams uses: fewer tokens are swept in more pieces, so this is the most over all
+// numbers of tiles (they go up one by one with the tokens, and down with the streams).
+size_t most_partials(int64_t n_q, int32_t n_streams, int32_t n_kv_heads, int32_t head_dim, int tile, int most, bool rows) {
+  const int64_t tiles = cs::most_token_tiles(n_q, n_streams, tile), in_pieces = (rows ? kRowsWanted : kGroupsWanted) / (2 * static_cast<int64_t>(n_kv_heads));
+  size_t bytes = 0;
+  for (int64_t t = 1; t <= tiles && t <= in_pieces; ++t) {
+    const size_t here = partials_of(t * n_kv_heads, pieces_of(t * n_kv_heads, most, rows), head_dim, rows);
+    bytes = here > bytes ? here : bytes;
+  }
+  return bytes;
 }
 
 }  // namespace
@@ -944,9 +962,11 @@ extern "C" size_t cs_selected_attn_workspace(int64_t n_q, int32_t n_streams, int
                                              int32_t sel_block, int32_t n_select) {
   if (n_q < 1 || n_streams < 1 || n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % n_kv_heads || n_q_heads / n_kv_heads > kRows) return 0;
   if (sel_block < 1 || n_select < 1 || n_select > CS_SELECT_MOST || head_dim < 1 || n_q >= 1ll << 26) return 0;
-  // (either type's)
-  const size_t rows = shape_of(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, sel_block, n_select, true, 0).partials;
-  const size_t few = shape_of(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, sel_block, n_select, false, 0).partials;
+  // (either type's, and either kernel's)
+  const int group = n_q_heads / n_kv_heads;
+  const size_t few = most_partials(n_q, n_streams, n_kv_heads, head_dim, tile_of(group, n_select), most_pieces(sel_block, n_select, false), false);
+  if (n_q < kManyTokens) return few;
+  const size_t rows = most_partials(n_q, n_streams, n_kv_heads, head_dim, rows_tile_of(group, n_select), most_pieces(sel_block, n_select, true), true);
   return rows > few ? rows : few;
 }
 
@@ -970,8 +990,7 @@ extern "C" int cs_selected_attn(const void* q, const void* k_cache_layer, const 
   if (!q || !k_cache_layer || !v_cache_layer || !cu_q || !q_pos || !kv_len || !block_table || !selected || !out) return CS_EINVAL;
   if (!cs::aligned16(q) || !cs::aligned16(k_cache_layer) || !cs::aligned16(v_cache_layer) || !cs::aligned16(out)) return CS_EUNSUPPORTED;
   const Shape s = shape_of(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, sel_block, n_select, dtype == CS_BF16, stride_slot);
-  const size_t need = cs_selected_attn_workspace(n_q, n_streams, n_q_heads, n_kv_heads, head_dim, sel_block, n_select);
-  if (need && (!workspace || !cs::aligned16(workspace) || workspace_bytes < need)) return CS_EWORKSPACE;
+  if (s.partials && (!workspace || !cs::aligned16(workspace) || workspace_bytes < s.partials)) return CS_EWORKSPACE;
   const int64_t groups = s.tiles * n_kv_heads * s.pieces;
   if (groups > cs::kMostThreads / 512) return CS_EUNSUPPORTED;
   Params p;

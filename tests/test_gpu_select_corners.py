@@ -1,10 +1,10 @@
-"""Corners of the operators of long windows: the largest epsilon of a norm beside squares that overflow, every bit pattern of a value (needs an
-MI355X)."""
+"""Corners of the operators of long windows: the largest epsilon of a norm beside squares that overflow, every bit pattern of a value, a
+workspace that calls of all sizes share (needs an MI355X)."""
 import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_select import cs, dev, pool, run_write, say  # noqa: F401 (cs: the fixture)
+from tests.test_gpu_select import Cache, any_lists, cs, dev, pool, run_write, say  # noqa: F401 (cs: the fixture)
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -46,3 +46,27 @@ def test_values_are_copied_bit_for_bit(cs, dtype, layout):
                                         cs.CS_BF16 if dtype == "bf16" else cs.CS_F32)
         got = vc[0].contiguous().view(as_bits)[slot.long()]
         assert torch.equal(got, v.view(as_bits).reshape(n, hkv, d))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_workspace_for_the_most_tokens_serves_fewer(cs, dtype):
+    """Sized once, for a whole window: shorter questions, single tokens and fewer streams after it use the same bytes, and get what they get with
+    bytes of their own."""
+    say("workspace of the largest call", dtype)
+    hq, hkv, d, size, n_select, kv = 28, 4, 128, 16, 12, [900, 700, 300]
+    c = Cache(cs, 41, hkv, d, kv, dtype)
+    most = cs.cs_selected_attn_workspace(2100, 3, hq, hkv, d, size, n_select)
+    ws = torch.full((max(16, most),), 255, dtype=torch.uint8, device=DEV)
+    for nq in ([1, 1, 1], [700, 700, 700], [30, 2, 0], [1, 0, 0], [200, 60, 11]):
+        for streams in (3, 1):
+            qs = c.queries(nq[:streams], hq, where="any")
+            listed = dev(any_lists(c.rng, c, qs, size, n_select, "sorted"))
+            out, stat = torch.full_like(qs["q"], 9.0), torch.full((qs["n_q"], hq), 9.0, device=DEV)
+            cs.cs_selected_attn(qs["q"], c.pool[0], c.pool[1], qs["cu_q"], qs["q_pos"], c.kv_len, c.table, c.max_blocks, 16, listed, size, n_select, out, stat, qs["n_q"], streams, hq, hkv,
+                                d, *c.stride, 0.1, c.code, ws if most else None)
+            own = cs.cs_selected_attn_workspace(qs["n_q"], streams, hq, hkv, d, size, n_select)
+            want, lse = torch.full_like(out, 9.0), torch.full_like(stat, 9.0)
+            cs.cs_selected_attn(qs["q"], c.pool[0], c.pool[1], qs["cu_q"], qs["q_pos"], c.kv_len, c.table, c.max_blocks, 16, listed, size, n_select, want, lse, qs["n_q"], streams, hq, hkv,
+                                d, *c.stride, 0.1, c.code, torch.full((max(16, own),), 255, dtype=torch.uint8, device=DEV))
+            torch.cuda.synchronize()
+            assert torch.equal(out, want) and torch.equal(stat, lse)
