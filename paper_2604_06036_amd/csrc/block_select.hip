@@ -12,6 +12,7 @@
 // scores that are compared are one power of two times whole numbers below 2^21, exact in fp32: lists are the same on any machine, in any order.
 #include <math.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "kv4.h"
@@ -511,6 +512,34 @@ __global__ __launch_bounds__(64 * kRowsWaves) void select_rows_kernel(SelectPara
   for (int i = half; i < mine; i += 2) select_token<kPairBlocks>(p, score + i * p.pitch, t.first + first + i, kvh, __builtin_amdgcn_readlane(candidates, first + i), lane);
 }
 
+// LDS that a workgroup of many tokens takes: a stage, then the queries, or the other stage and the scores.
+constexpr size_t rows_lds(int head_dim, size_t scores) {
+  const size_t stage = 64 * 2 * static_cast<size_t>(head_dim), queries = static_cast<size_t>(kPairs) * 32 * (2 * head_dim + 16);
+  return stage + (queries > stage + scores ? queries : stage + scores);
+}
+constexpr size_t kMostLdsWide = kMostBlocks * sizeof(uint32_t);
+template <int D>
+constexpr size_t kMostLdsRows = rows_lds(D, kTileScores * sizeof(uint32_t));
+
+// A kernel's limit on the LDS of a launch is the process's: it is raised once a device, to the most that any call takes, since a limit of one
+// call's own could be lowered by another thread's between this and the launch.
+template <void (*kKernel)(SelectParams), size_t kMostLds>
+int launch(const SelectParams& p, dim3 grid, int threads, size_t lds, hipStream_t st) {
+  if (lds > 32 * 1024) {
+    static std::atomic<uint64_t> raised{0};                // a bit a device
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    const uint64_t bit = device < 64 ? 1ull << device : 0;
+    if (e == hipSuccess && !(raised.load(std::memory_order_acquire) & bit)) {
+      e = hipFuncSetAttribute(reinterpret_cast<const void*>(kKernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMostLds));
+      if (e == hipSuccess) raised.fetch_or(bit, std::memory_order_release);
+    }
+    if (e != hipSuccess) return cs::note_hip(e);
+  }
+  hipLaunchKernelGGL(kKernel, grid, dim3(threads), lds, st, p);
+  return cs::note_hip(hipGetLastError());
+}
+
 }  // namespace
 
 extern "C" int cs_key_bounds(const void* k_cache_layer, const int32_t* from, const int32_t* kv_len, const int32_t* block_table,
@@ -616,23 +645,12 @@ extern "C" int cs_select_blocks(const void* q, const int8_t* bounds, const uint8
   const int64_t tiles = cs::most_token_tiles(n_q, n_streams, p.tile), groups = tiles * n_kv_heads;
   if (groups > cs::kMostThreads / 1024) return CS_EUNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(groups));
-  const size_t scores = static_cast<size_t>(p.tile) * p.pitch * sizeof(uint32_t), stage = 64 * 2 * static_cast<size_t>(head_dim);
-  const size_t queries = static_cast<size_t>(kPairs) * 32 * (2 * head_dim + 16);
-  const size_t lds = many ? stage + (queries > stage + scores ? queries : stage + scores) : scores;
+  const size_t scores = static_cast<size_t>(p.tile) * p.pitch * sizeof(uint32_t), lds = many ? rows_lds(head_dim, scores) : scores;
   hipStream_t st = cs::as_stream(stream);
-#define CS_LAUNCH_SELECT_KERNEL(KERNEL, THREADS)                                                                                           \
-  do {                                                                                                                                     \
-    if (lds > 32 * 1024) {                                                                                                                 \
-      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize,          \
-                                               static_cast<int>(lds));                                                                     \
-      if (e != hipSuccess) return cs::note_hip(e);                                                                                         \
-    }                                                                                                                                      \
-    hipLaunchKernelGGL(KERNEL, grid, dim3(THREADS), lds, st, p);                                                                           \
-  } while (0)
-#define CS_LAUNCH_SELECT(BF16, D, GP)                                                                    \
-  do {                                                                                                   \
-    if (many) CS_LAUNCH_SELECT_KERNEL((select_rows_kernel<BF16, D, GP>), 64 * kRowsWaves);               \
-    else CS_LAUNCH_SELECT_KERNEL((select_blocks_kernel<BF16, D, GP>), 64 * kWide);                       \
+#define CS_LAUNCH_SELECT(BF16, D, GP)                                                                                  \
+  do {                                                                                                                 \
+    if (many) return launch<select_rows_kernel<BF16, D, GP>, kMostLdsRows<D>>(p, grid, 64 * kRowsWaves, lds, st);      \
+    return launch<select_blocks_kernel<BF16, D, GP>, kMostLdsWide>(p, grid, 64 * kWide, lds, st);                      \
   } while (0)
 #define CS_LAUNCH_SELECT_GROUP(BF16, D)              \
   do {                                               \
@@ -650,7 +668,5 @@ extern "C" int cs_select_blocks(const void* q, const int8_t* bounds, const uint8
     else CS_LAUNCH_SELECT_GROUP(false, 64);
   }
 #undef CS_LAUNCH_SELECT_GROUP
-#undef CS_LAUNCH_SELECT_KERNEL
 #undef CS_LAUNCH_SELECT
-  return cs::note_hip(hipGetLastError());
 }

@@ -1,10 +1,14 @@
 """Corners of the operators of long windows: the largest epsilon of a norm beside squares that overflow, every bit pattern of a value, a
-workspace that calls of all sizes share (needs an MI355X)."""
+workspace that calls of all sizes share, calls from several threads (needs an MI355X)."""
+import math
+import threading
+
 import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_select import Cache, any_lists, cs, dev, pool, run_write, say  # noqa: F401 (cs: the fixture)
+from oracle import select_oracle as so
+from tests.test_gpu_select import Cache, any_lists, cs, dev, f64, pool, run_write, say  # noqa: F401 (cs: the fixture)
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -70,3 +74,60 @@ def test_a_workspace_for_the_most_tokens_serves_fewer(cs, dtype):
                                 d, *c.stride, 0.1, c.code, torch.full((max(16, own),), 255, dtype=torch.uint8, device=DEV))
             torch.cuda.synchronize()
             assert torch.equal(out, want) and torch.equal(stat, lse)
+
+
+def lists_by_sorting(q, bounds, scales, n, want, first, last):
+    """Lists of one stream and kv head from whole numbers in float64 (all below 2^24) by a stable sort.  q [nq][hq][d], n [nq] candidates."""
+    codes = torch.from_numpy(np.stack([so.query_codes(x) for x in f64(q)])).to(DEV, torch.float64)
+    nq, hq, d = codes.shape
+    hi, lo = bounds[:, 0].to(torch.float64), bounds[:, 1].to(torch.float64)
+    flat = codes.reshape(nq * hq, d)
+    score = (flat.clamp(min=0) @ hi.t().contiguous() + flat.clamp(max=0) @ lo.t().contiguous()).reshape(nq, hq, -1).amax(1) * torch.exp2(scales.to(torch.float64) - 127)
+    block = torch.arange(bounds.shape[0], device=DEV)[None]
+    score = torch.where((block < first) | (block >= n[:, None] - last), math.inf, score)
+    score = torch.where(block < n[:, None], score, -math.inf)
+    best = torch.sort(score, dim=1, descending=True, stable=True).indices[:, :want]
+    if best.shape[1] < want:
+        best = torch.cat([best, torch.full((nq, want - best.shape[1]), 1 << 30, device=DEV)], 1)
+    best = torch.where(torch.gather(torch.cat([score, torch.full((nq, 1), -math.inf, device=DEV, dtype=score.dtype)], 1), 1, best.clamp(max=score.shape[1])) == -math.inf, 1 << 30, best)
+    best = best.sort(1).values
+    return torch.where(best == 1 << 30, -1, best).to(torch.int32)
+
+
+def test_two_threads_choose_among_tables_of_different_lengths(cs):
+    """Launches of one kernel that ask for 40 and for 128 KB of LDS, from two threads at once: no call is refused, and every list is right."""
+    say("select, two threads")
+    d, hq, want = 64, 4, 20
+    work = []
+    for n_blocks in (32768, 10000, 9000):
+        gen = torch.Generator(device="cuda").manual_seed(n_blocks)
+        hi = torch.randint(-100, 128, (n_blocks, d), generator=gen, device=DEV)
+        bounds = torch.stack([hi, hi - 9], 1).to(torch.int8).contiguous()
+        scales = torch.full((n_blocks,), 120, dtype=torch.uint8, device=DEV)
+        q = torch.randn((1, hq, d), generator=gen, device=DEV).to(torch.bfloat16)
+        last = torch.tensor([16 * n_blocks - 1], dtype=torch.int32, device=DEV)
+        work.append((n_blocks, q, bounds, scales, torch.tensor([0, 1], dtype=torch.int32, device=DEV), last, last + 1))
+    torch.cuda.synchronize()
+    errors, lists = [], [[] for _ in work]
+
+    def calls(i):
+        n_blocks, q, bounds, scales, cu, last, kv = work[i]
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(60):
+                    out = torch.full((1, 1, want), -7, dtype=torch.int32, device=DEV)
+                    cs.cs_select_blocks(q, bounds, scales, cu, last, kv, n_blocks, 16, want, 2, 3, out, 1, 1, hq, 1, d, cs.CS_BF16)
+                    lists[i].append(out)
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:      # noqa: BLE001 (shown by the test's own thread)
+            errors.append((i, e))
+
+    threads = [threading.Thread(target=calls, args=(i,)) for i in range(len(work))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
+    for (n_blocks, q, bounds, scales, _, last, _), got in zip(work, lists):
+        want_list = lists_by_sorting(q, bounds, scales, last // 16 + 1, want, 2, 3)
+        assert all(torch.equal(x[:, 0], want_list) for x in got)
