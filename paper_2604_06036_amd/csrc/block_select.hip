@@ -232,6 +232,7 @@ __device__ __forceinline__ void write_list(const F& at, int n, int n_first, int 
 // The same from scores in registers.  kNarrow, where a few are wanted of many: a bound is found first, from the lanes' largest scores alone;
 // what passes it moves into one register a lane, and the threshold is found there.  `score`: the row in LDS, not needed any more.  (1,563
 // blocks 22.7 -> 19.7 us; with 276 blocks it costs more than it saves, and in the kernel for many tokens registers.)
+constexpr int kNarrowChunks = 12;        // chunks from which it is taken (64 tokens, 768 blocks, 12 chunks: 13.0 us without, 11.8 with)
 constexpr int kFewWanted = 32, kSpare = 8;             // of 64 places; largest scores that may pass the bound beside those wanted
 template <int C, bool kNarrow, class F>
 __device__ __forceinline__ void write_list_held(const F& key, int n, int n_first, int n_last, int n_select, uint32_t* score, int32_t* out, int lane) {
@@ -382,12 +383,20 @@ __device__ __forceinline__ void select_token(const SelectParams& p, uint32_t* sc
     return;
   }
   const auto key = [&](int b) __attribute__((always_inline)) -> uint32_t { return b < p.n_first || b >= n - p.n_last ? 0u : score[b]; };
-#define CS_LIST(C) write_list_held<C, kMost == 0 && (C >= 16)>(key, n, p.n_first, p.n_last, p.n_select, score, out, lane)
+  // As many registers as the list has chunks of 64 blocks, by a rule that leaves no window out: every number up to 8, then 12, 16, 24, 32, so
+  // that less than half again of what is counted is padding.  2,082 tokens, powers of two alone / this: 192 blocks 16.4 / 15.8 us, 276 23.3 /
+  // 19.5, 384 28.4 / 26.2, 448 29.7 / 28.4, 768 54.2 / 49.8; a token among 1,536 blocks 19.4 / 18.3.
+#define CS_LIST(C) write_list_held<C, kMost == 0 && (C >= kNarrowChunks)>(key, n, p.n_first, p.n_last, p.n_select, score, out, lane)
   if (n <= 128) CS_LIST(2);
+  else if (n <= 192) CS_LIST(3);
   else if (n <= 256) CS_LIST(4);
   else if (n <= 320) CS_LIST(5);
+  else if (n <= 384) CS_LIST(6);
+  else if (n <= 448) CS_LIST(7);
   else if (n <= 512) CS_LIST(8);
+  else if (n <= 768) CS_LIST(12);
   else if (kMost == 1024 || n <= 1024) CS_LIST(16);
+  else if (n <= 1536) CS_LIST(24);
   else if (n <= 2048) CS_LIST(32);
   else {
     const auto at = [&](int c) __attribute__((always_inline)) { return key(c * 64 + lane); };

@@ -1,5 +1,6 @@
 """Corners of the operators of long windows: the largest epsilon of a norm beside squares that overflow, every bit pattern of a value, a
-workspace that calls of all sizes share, calls from several threads (needs an MI355X)."""
+workspace that calls of all sizes share, calls from several threads, lists of
+as many blocks as registers hold (needs an MI355X)."""
 import math
 import threading
 
@@ -131,3 +132,24 @@ def test_two_threads_choose_among_tables_of_different_lengths(cs):
     for (n_blocks, q, bounds, scales, _, last, _), got in zip(work, lists):
         want_list = lists_by_sorting(q, bounds, scales, last // 16 + 1, want, 2, 3)
         assert all(torch.equal(x[:, 0], want_list) for x in got)
+
+
+@pytest.mark.parametrize("n_blocks", [127, 128, 129, 192, 193, 256, 257, 320, 321, 384, 385, 448, 449, 512, 513, 768, 769, 1024, 1025, 1536, 1537, 2048, 2049])
+@pytest.mark.parametrize("nq,want,first,last", [(3, 16, 1, 2), (4200, 7, 1, 1), (3, 90, 0, 0)])
+def test_selection_at_the_edges_of_lists_held(cs, n_blocks, nq, want, first, last):
+    """As many blocks as a wave's registers of a list hold, one more and one fewer, for few and for many tokens."""
+    say("select, lists held", n_blocks, nq, want)
+    d, hq = 64, 4
+    gen = torch.Generator(device="cuda").manual_seed(n_blocks)
+    hi = torch.randint(-100, 128, (n_blocks, d), generator=gen, device=DEV)
+    lo = hi - torch.randint(0, 28, hi.shape, generator=gen, device=DEV)
+    bounds = torch.stack([hi, lo], 1).to(torch.int8).contiguous()
+    scales = torch.randint(118, 123, (n_blocks,), generator=gen, device=DEV).to(torch.uint8)
+    bounds[n_blocks // 3] = bounds[n_blocks // 2]              # (equal scores)
+    scales[n_blocks // 3] = scales[n_blocks // 2]
+    q = torch.randn((nq, hq, d), generator=gen, device=DEV).to(torch.bfloat16)
+    pos = (16 * n_blocks - 1 - 16 * (torch.arange(nq, device=DEV) % (n_blocks // 2))).to(torch.int32)
+    out = torch.full((nq, 1, want), -7, dtype=torch.int32, device=DEV)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    cs.cs_select_blocks(q, bounds, scales, i32(0, nq), pos, i32(16 * n_blocks), n_blocks, 16, want, first, last, out, nq, 1, hq, 1, d, cs.CS_BF16)
+    assert torch.equal(out[:, 0], lists_by_sorting(q, bounds, scales, pos // 16 + 1, want, first, last))
