@@ -542,7 +542,8 @@ def cs_norm_rope_refresh_scatter(q, q_out, k_new, v_new, q_weight, k_weight, slo
     fn = "cs_norm_rope_refresh_scatter"
     el, i32 = _ELEMENT.get(dtype), torch.int32
     for t, stride, heads, what in ((q, stride_q, n_q_heads, "q"), (k_new, stride_k, n_kv_heads, "k_new"), (v_new, stride_v, n_kv_heads, "v_new")):
-        if t is not None and t.numel() < (n_tok - 1) * stride + heads * head_dim and not _span(t, n_tok, stride, heads * head_dim):
+        # (its own elements, where they lie behind one another, or what is behind its first one)
+        if t is not None and not (t.is_contiguous() and t.numel() >= (n_tok - 1) * stride + heads * head_dim) and not _span(t, n_tok, stride, heads * head_dim):
             raise ValueError(f"{fn}: {what} holds fewer than {n_tok} tokens")
     apart = q_out is not None and (q is None or q_out.data_ptr() != q.data_ptr())      # (else q_out is q, with its stride)
     p, _, _, stream = _held(fn, (
