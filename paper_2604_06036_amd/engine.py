@@ -567,8 +567,9 @@ class SelectStep(DeviceStep):
     cs_kv_rerotate_freqs; a layer is cs_norm_rope_refresh_scatter, cs_key_bounds, cs_select_blocks and cs_selected_attn.  `positions`,
     `axis_of_pair` (uint8 [rotary_dim/2]) as in Kv4Step.
 
-    `token` answers: a token a stream behind the window, in every layer.  Its rows go to `answer_blocks` cache blocks a stream that the step
-    keeps behind the window's own."""
+    `begin_token` and `token_layer` answer: a token a stream behind the window, layer by layer (`token`: all layers at once).  Its rows go to
+    what the window's last block leaves and to `answer_blocks` cache blocks a stream that the step keeps behind it; once these are full a
+    stream's tokens are not written, and `token_slot` says so."""
 
     def __init__(self, data: StepData, positions, inv_freq, axis_of_pair=None, rotary_dim: Optional[int] = None, q_weight=None, k_weight=None,
                  norm_eps: float = 1e-6, amplitude: float = 1.0, sel_block: int = 64, n_select: int = 16, n_first: int = 1, n_last: int = 2,
@@ -628,6 +629,7 @@ class SelectStep(DeviceStep):
         self.one_q = torch.empty((n, w.n_q_heads, w.head_dim), dtype=dtype, device=dev)
         self.one_selected = torch.empty((n, w.n_kv_heads, self.n_select), dtype=torch.int32, device=dev)
         self.ws_one = self._workspaces(n)
+        self.token_entry, self.token_slot, self.token_last = (torch.full((n,), -1, dtype=torch.int32, device=dev) for _ in range(3))
 
     def _workspaces(self, n_q):
         """Workspaces of selection and attention for n_q queries."""
@@ -690,22 +692,58 @@ class SelectStep(DeviceStep):
         for layer in range(self.data.workload.n_layers):
             self.refresh_and_attention(layer)
 
+    def begin_token(self):
+        """Places a token a stream behind the windows, in every layer's cache: `token_slot` int32 [n_streams] says where, -1 where a stream's
+        blocks are full.  Such a stream's token is not written and its window stays as it is; the others' windows grow by it (`kv_len`).
+        A token is this, then `token_layer` for every layer in turn."""
+        self.token_entry.copy_(self.kv_len)
+        slot, kv_len = _token_places(self.token_entry, self.room, self.block_table)
+        self.token_slot.copy_(slot)
+        self.kv_len.copy_(kv_len)
+        self.token_last.copy_(kv_len - 1)
+
+    def token_layer(self, layer: int, q, k_new, v_new, positions, out):
+        """A layer of the token that `begin_token` has placed: q [n_streams][n_q_heads][head_dim] as the projection leaves it, k_new and v_new
+        alike, positions int32 [n_streams] or [n_streams][3]; out like q.  The token reads itself too, where it is written."""
+        self._check_token(q, k_new, v_new, positions, ())
+        self._token_layer(layer, q, k_new, v_new, positions, out)
+
     def token(self, q, k_new, v_new, positions, out):
-        """One token a stream behind its window, in every layer: q [n_layers][n_streams][n_q_heads][head_dim] as the projections leave it,
-        k_new and v_new alike, positions int32 [n_streams] or [n_streams][3]; out like q.  Windows grow by the token (`kv_len`), which is read by
-        itself too; where a stream's blocks are full its rows are not written, and the window stays as it is.
-        (Layers at once, as the inputs of a step are: a model calls `_write` and `_read` layer by layer.)"""
-        import torch
-        w, cs = self.data.workload, self.cs
-        n, entry = w.n_streams, self.kv_len.clone()
-        place = entry.clamp(max=self.max_blocks * cs.CS_KV_BLOCK - 1).long()
-        slot = self.block_table.gather(1, (place // cs.CS_KV_BLOCK)[:, None])[:, 0] * cs.CS_KV_BLOCK + (place % cs.CS_KV_BLOCK).int()
-        slot = torch.where(entry < self.room, slot, -1)
-        self.kv_len.copy_(torch.where(slot >= 0, entry + 1, entry))
-        last = self.kv_len - 1
-        for layer in range(w.n_layers):
-            self._write(layer, q[layer], self.one_q, k_new[layer], v_new[layer], slot, positions, n)
-            self._read(layer, self.one_q, self.one_cu, last, entry, self.one_selected, out[layer], None, n, self.ws_one)
+        """A token in all layers at once, where their inputs are at hand: q [n_layers][n_streams][n_q_heads][head_dim], k_new and v_new
+        alike; out like q.  See `begin_token` and `token_layer`."""
+        n_layers = self.data.workload.n_layers
+        self._check_token(q, k_new, v_new, positions, (n_layers,))
+        self.begin_token()
+        for layer in range(n_layers):
+            self._token_layer(layer, q[layer], k_new[layer], v_new[layer], positions, out[layer])
+
+    def _token_layer(self, layer, q, k_new, v_new, positions, out):
+        n = self.data.workload.n_streams
+        self._write(layer, q, self.one_q, k_new, v_new, self.token_slot, positions, n)
+        self._read(layer, self.one_q, self.one_cu, self.token_last, self.token_entry, self.one_selected, out, None, n, self.ws_one)
+
+    def _check_token(self, q, k_new, v_new, positions, before):
+        w = self.data.workload
+        _check_token(q, k_new, v_new, positions, before + (w.n_streams,), w.n_q_heads, w.n_kv_heads, w.head_dim, 1 if self.axis_of_pair is None else 3)
+
+
+def _token_places(entry, room, block_table):
+    """Cache slots of a token behind windows of `entry` entries, -1 where a stream has no room (or no window yet: a negative length), and the lengths
+    with it."""
+    import torch
+    there = (entry >= 0) & (entry < room)
+    place = torch.where(there, entry, 0)
+    slot = block_table.gather(1, (place // synth.KV_BLOCK).long()[:, None])[:, 0] * synth.KV_BLOCK + place % synth.KV_BLOCK
+    return torch.where(there, slot, -1), entry + there.int()
+
+
+def _check_token(q, k_new, v_new, positions, rows, n_q_heads, n_kv_heads, head_dim, width):
+    for what, t, heads in (("q", q, n_q_heads), ("k_new", k_new, n_kv_heads), ("v_new", v_new, n_kv_heads)):
+        if tuple(t.shape) != rows + (heads, head_dim) or t.stride(-1) != 1 or heads > 1 and t.stride(-2) != head_dim:
+            raise ValueError(f"token: {what}: {list(rows + (heads, head_dim))} expected, the heads of a row behind one another")
+    # (a [3][n_streams] tensor would be read as other rows' positions)
+    if positions.numel() != width * rows[-1] or positions.dim() > 1 and int(positions.shape[-1]) != width:
+        raise ValueError(f"token: positions: int32 of {rows[-1]} rows of {width} expected")
 
 
 def _with_answer_blocks(data: StepData, extra: int) -> dict:
