@@ -1,6 +1,6 @@
-"""Corners of the operators of long windows: the largest epsilon of a norm beside squares that overflow, every bit pattern of a value, a
-workspace that calls of all sizes share, calls from several threads, lists of
-as many blocks as registers hold (needs an MI355X)."""
+"""Corners of the operators of long windows (needs an MI355X): the largest epsilon of a norm beside squares that overflow, every bit pattern of a
+value, a workspace that calls of all sizes share, calls from several threads, lists of as many blocks as registers hold, more blocks than are
+collected at once, rows that lie far apart."""
 import math
 import threading
 
@@ -153,3 +153,81 @@ def test_selection_at_the_edges_of_lists_held(cs, n_blocks, nq, want, first, las
     i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)
     cs.cs_select_blocks(q, bounds, scales, i32(0, nq), pos, i32(16 * n_blocks), n_blocks, 16, want, first, last, out, nq, 1, hq, 1, d, cs.CS_BF16)
     assert torch.equal(out[:, 0], lists_by_sorting(q, bounds, scales, pos // 16 + 1, want, first, last))
+
+
+@pytest.mark.parametrize("kv,nq,hq,hkv,d,size,n_select", [([40000, 17000], [37, 5], 7, 1, 128, 16, 24), ([40000], [40], 8, 4, 64, 16, 20), ([33000, 20], [9, 1], 4, 2, 64, 16, 128),
+                                                          ([35000], [700], 16, 16, 64, 16, 9)])
+def test_attention_over_more_blocks_than_are_collected_at_once(cs, kv, nq, hq, hkv, d, size, n_select):
+    """Windows of up to 2,500 blocks, whose readers are collected 1,024 at a time: lists in no order, with repeats, on both sides of every 1,024."""
+    say("attention, many candidates", kv, nq, hq, hkv, d, size, n_select)
+    c = Cache(cs, sum(kv) + d, hkv, d, kv, "bf16")
+    qs = c.queries(nq, hq, where="any", extra=2, gain=2.0)
+    listed = any_lists(c.rng, c, qs, size, n_select, "wild")
+    edges = np.array([1023, 1024, 1023, 2047, 2048, 0, 1025, 2048], np.int32)
+    for t in range(0, sum(nq), 2):
+        listed[t, :, :len(edges)] = c.rng.permutation(edges)
+    qs["pos"][: nq[0]: 3] = kv[0] - 1              # (the whole window in sight)
+    qs["pos"][1: nq[0]: 7] = [16 * 1024 - 1, 16 * 1024, 16 * 2048 + 3][: 3][c.rng.integers(0, 3)]
+    qs["q_pos"].copy_(dev(qs["pos"]))
+    out, stat = c.attend(qs, dev(listed), size)
+    some = np.unique(np.concatenate([np.arange(0, min(sum(nq), 40)), c.rng.integers(0, sum(nq), 20)]))
+    part = dict(qs, nq=None, n_q=len(some), q64=qs["q64"][some], pos=qs["pos"][some], stream=qs["stream"][some])
+    c.check_attention(part, listed[some], size, out[some], stat[some])
+    again, lse = c.attend(qs, dev(listed), size)
+    assert torch.equal(out.view(torch.int16), again.view(torch.int16)) and torch.equal(stat, lse)
+    assert bool((out[sum(nq):] == 9).all()) and bool((stat[sum(nq):] == 9).all())
+
+
+@pytest.mark.parametrize("stride", [(1 << 26) - 8, 1 << 26, (1 << 26) + 64])
+def test_attention_over_rows_that_lie_far_apart(cs, stride):
+    """Slots 2^26 elements apart, and a little less: both sides of what the many-token kernel's 32-bit offsets inside a cache block reach."""
+    say("attention, far rows", stride)
+    hkv, d = 2, 64
+    c = Cache(cs, 43, hkv, d, [33, 5], "bf16")
+    near, near_stride = c.pool, c.stride
+    n_slots = near[0].shape[0]
+    flat = torch.empty(((n_slots - 1) * stride + 2 * hkv * d,), dtype=torch.bfloat16, device=DEV)
+    far = [flat[i * hkv * d:].as_strided((n_slots, hkv, d), (stride, d, 1)) for i in range(2)]
+    for x, y in zip(far, near):
+        x.copy_(y)
+    for nq in ([1, 1], [30, 11]):
+        qs = c.queries(nq, 6, where="any")
+        listed = any_lists(c.rng, c, qs, 16, 5, "wild")
+        c.pool, c.stride = far, (stride, d)
+        bounds = c.bounds(16)
+        out, stat = c.attend(qs, dev(listed), 16)
+        c.pool, c.stride = near, near_stride
+        c.check_attention(qs, listed, 16, out, stat)
+        want = c.bounds(16)
+        assert torch.equal(bounds[0], want[0]) and torch.equal(bounds[1], want[1])
+
+
+def test_a_kernels_first_call_may_be_captured(cs):
+    """A choice that takes more LDS than launches do unasked, captured before its kernel has run: the limit is raised in the capture, and every
+    replay gives the list of the queries that are there by then."""
+    say("select, first call in a capture")
+    d, hq, hkv, n_blocks, want = 128, 48, 3, 20000, 9             # (fp32, heads in groups of 16: no other test has so many blocks for them)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    hi = torch.randint(-100, 128, (hkv, n_blocks, d), generator=gen, device=DEV)
+    bounds = torch.stack([hi, hi - 9], 2).to(torch.int8).contiguous()
+    scales = torch.randint(118, 123, (hkv, n_blocks), generator=gen, device=DEV).to(torch.uint8)
+    q, out = torch.zeros((2, hq, d), device=DEV), torch.zeros((2, hkv, want), dtype=torch.int32, device=DEV)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    cu, pos, kv = i32(0, 2), i32(16 * n_blocks - 1, 16 * n_blocks - 700), i32(16 * n_blocks)
+    call = lambda: cs.cs_select_blocks(q, bounds, scales, cu, pos, kv, n_blocks, 16, want, 1, 1, out, 2, 1, hq, hkv, d, cs.CS_F32)
+    torch.cuda.synchronize()
+    side, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        call()
+    for _ in range(3):
+        q.copy_(torch.randn(q.shape, generator=gen, device=DEV))
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        for h in range(hkv):
+            heads = q[:, h * 16:(h + 1) * 16].contiguous()
+            assert torch.equal(got[:, h], lists_by_sorting(heads, bounds[h], scales[h], pos // 16 + 1, want, 1, 1))
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(out, got)
