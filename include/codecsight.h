@@ -810,8 +810,9 @@ int cs_select_blocks(const void* q, const int8_t* bounds, const uint8_t* scales,
  * a block that stands twice counts once; indexes that are negative or lie behind the query are skipped; a query whose list leaves nothing
  * gets out 0, lse -inf.  Rows of a stream with kv_len <= 0, and from cu_q[n_streams] on, are left as they were.
  * CS_BF16: bf16 operands, fp32 scores, statistics and sums; weights are rounded to bf16.  CS_F32: fp32 throughout.  Keys and values that are
- * no numbers, or infinite, reach the queries that see them, and no others (a query all of whose scores are -inf sees nothing).  Weighted values are summed before they are divided, weights
- * up to 2^8: values past 2^120 / kv_len may overflow on the way.
+ * no numbers, or infinite, reach the queries that see them, and no others (a query all of whose scores are -inf sees nothing).  Weighted
+ * values are summed before they are divided, weights up to 2^8: values past 2^120 / kv_len may overflow on the way.  Scores (softmax_scale
+ * q . K) up to 2^28 in magnitude are in range; past 2^24 weights are up to 2^40, and past 2^28 a query may get what is no number, or out 0.
  *
  *  selected     in   int32 [n_q][n_kv_heads][n_select]
  *  lse          out  float [n_q][n_q_heads] or NULL: log sum_j exp(softmax_scale * q[t][h] . K_j) over the entries seen

@@ -231,3 +231,44 @@ def test_a_kernels_first_call_may_be_captured(cs):
         call()
         torch.cuda.synchronize()
         assert torch.equal(out, got)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("top", [2.0 ** 20, 2.0 ** 24, 2.0 ** 28 - 16])
+def test_attention_of_scores_up_to_the_documented_size(cs, dtype, sign, top):
+    """One key of every window leads all others by a half of its score: the answer is its value, though a score is only known to a multiple of up
+    to 16 and the reference that it is compared with is rounded too."""
+    say("attention, largest scores", dtype, sign, top)
+    d, kv = 64, [700, 90]
+    c = Cache(cs, 51, 2, d, kv, dtype)
+    keys = np.zeros((c.pool[0].shape[0], 2, d))
+    for s, n in enumerate(kv):
+        # (of the first channel alone, so that a score is one product)
+        lead, rest = (1.0, 0.5) if sign > 0 else (0.5, 1.0)
+        keys[c.slots[s], :, 0] = c.rng.uniform(0.7, 0.99, (n, 2)) * rest
+        keys[c.slots[s][n // 3], :, 0] = lead * c.rng.uniform(0.98, 0.999, 2) * (1 if sign > 0 else 0.65)
+    k64 = torch.from_numpy(keys.astype(np.float32)).to(c.t)
+    c.pool[0].copy_(k64)
+    keys = f64(k64)
+    for nq in ([1, 1], [23, 9]):
+        qs = c.queries(nq, 6, where="tail")
+        qs["pos"][:] = np.repeat(np.array(kv) - 1, nq)
+        qs["q_pos"].copy_(dev(qs["pos"]))
+        qs["q"].zero_()
+        qs["q"][..., 0] = sign * 8 * top * torch.from_numpy(c.rng.uniform(0.9, 0.99, (sum(nq), 6)).astype(np.float32)).to(DEV)
+        q = f64(qs["q"])
+        listed = np.tile(np.arange(44, dtype=np.int32), (sum(nq), 2, 1))
+        out, lse = c.attend(qs, dev(listed), 16, scale=0.125)
+        got, stat = f64(out), f64(lse)
+        for t, s in enumerate(qs["stream"]):
+            for g in range(2):
+                heads, best = slice(3 * g, 3 * g + 3), c.slots[s][kv[s] // 3]
+                scores = 0.125 * np.outer(q[t, heads, 0], keys[c.slots[s], g, 0])
+                assert np.all(scores.argmax(1) == kv[s] // 3) and np.all(np.abs(scores) < 2.0 ** 28)
+                want = c.x64[1][best, g]
+                # the weight is rounded before the product but not in the sum, and the result: half a step each, and three of fp32
+                half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+                assert np.all(np.abs(got[t, heads] - want) <= (2 * half + 3 * 2.0 ** -24) * 1.01 * np.abs(want))
+                # the score's product, the reference, its logarithm and their sum are rounded
+                assert np.all(np.abs(stat[t, heads] - scores.max(1)) <= 6 * 2.0 ** -24 * np.abs(scores.max(1)))
