@@ -55,7 +55,8 @@ struct BoundsParams {
 constexpr int kManyWaves = 1 << 20, kFewWaves = 1024;
 // A wave takes a block, lanes side by side on a row's channels, and goes on with the block `walkers` further.  Largest, smallest and greatest
 // magnitude are kept while the rows pass, UC cache blocks asked for at once; lanes that hold other rows of the same channels are joined at
-// the end.  Bound by memory: 32 windows of 17,630 entries at most, 4 heads of 128, 446 MB, take 91 us, 4.9 TB/s (a large copy: 5.1).
+// the end.  Bound by memory: 32 windows of 17,630 entries at most, 4 heads of 128, 446 MB, take 91 us, 4.9 TB/s (a large copy: 5.1); in
+// fp32, 892 MB, 164 us.
 template <bool kBf16, int D, int UC>
 __global__ __launch_bounds__(256) void key_bounds_kernel(BoundsParams p) {
   using Elem = typename std::conditional<kBf16, uint16_t, float>::type;
@@ -160,9 +161,9 @@ struct SelectParams {
 };
 
 // Which kernel: workgroups of 16 waves share a tile's blocks out among themselves, as long as all of them are on the card at once (two a
-// CU); past that pairs of waves with rows of their own do more for what they read.  28 on 4 heads, 276 blocks, wide / pairs: 64 tokens 7.6 /
-// 12.6 us, 256 8.2 / 12.8, 512 12.2 / 13.3, 768 (the first over 512 workgroups) 16.8 / 13.3, 1,024 21.1 / 13.6.  And a pair needs
-// the scores of two tokens at once: 1,250 blocks, 1,024 tokens 59 / 70 us, 938 blocks, 2,082 tokens 83 / 62 us.
+// CU); past that pairs of waves with rows of their own do more for what they read.  28 on 4 heads, 276 blocks, wide / pairs: 64 tokens 7.5 /
+// 12.2 us, 256 8.1 / 12.4, 512 12.0 / 12.8, 768 (the first over 512 workgroups) 16.6 / 12.7, 1,024 20.8 / 13.0.  And a pair needs
+// the scores of two tokens at once: 1,250 blocks, 1,024 tokens 50 / 64 us (pairs of one token each), 938 blocks, 2,082 tokens 81 / 61 us.
 constexpr int kWideGroups = 512;
 constexpr int kPairTokens = 2, kPairBlocks = 1024;
 constexpr int kMostBlocks = 32768;       // whose scores a workgroup holds in LDS for one token
@@ -231,7 +232,7 @@ __device__ __forceinline__ void write_list(const F& at, int n, int n_first, int 
 
 // The same from scores in registers.  kNarrow, where a few are wanted of many: a bound is found first, from the lanes' largest scores alone;
 // what passes it moves into one register a lane, and the threshold is found there.  `score`: the row in LDS, not needed any more.  (1,563
-// blocks 22.7 -> 19.7 us; with 276 blocks it costs more than it saves, and in the kernel for many tokens registers.)
+// blocks 22.7 -> 19.9 us; with 276 blocks it costs more than it saves, and in the kernel for many tokens registers.)
 constexpr int kNarrowChunks = 12;        // chunks from which it is taken (64 tokens, 768 blocks, 12 chunks: 13.0 us without, 11.8 with)
 constexpr int kFewWanted = 32, kSpare = 8;             // of 64 places; largest scores that may pass the bound beside those wanted
 template <int C, bool kNarrow, class F>
@@ -410,8 +411,8 @@ __device__ __forceinline__ void select_token(const SelectParams& p, uint32_t* sc
 }
 
 // Few tokens: a workgroup takes those of 32 rows and a kv head, its 16 waves the blocks in turn, 32 columns at a time; then each wave the
-// list of a token.  Bound by latency, of launch, queries, bounds, counting one after the other: a token among 276 blocks 6.6 us, 64 tokens 7.4, a
-// token among 1,563 blocks 19.8.  Rows are (token, head), the heads of a token padded to GP by the last of them and spread so that they are
+// list of a token.  Bound by latency, of launch, queries, bounds, counting one after the other: a token among 276 blocks 6.6 us, 64 tokens 7.5, a
+// token among 1,563 blocks 19.9.  Rows are (token, head), the heads of a token padded to GP by the last of them and spread so that they are
 // neighbouring registers of a lane.
 template <bool kBf16, int D, int GP>
 __global__ __launch_bounds__(64 * kWide) void select_blocks_kernel(SelectParams p) {

@@ -7,7 +7,8 @@
 // A lane owns 16 elements of a token's heads: eight pairs of the rotated part (8 and 8 elements, half a rotated part apart or
 // neighbours), or 16 neighbours past it.  It evaluates its cosines and sines once (double precision) and keeps them for every head of
 // its share; a head's lanes lie in one row of 16 of the wave, so the sum of squares is up to four lane exchanges, and nothing passes through
-// LDS.  Bound by memory: 22,804 tokens of 32 + 8 heads of 128 take 127 us, 4.4 TB/s (a large copy: 5.1); one token of 28 + 4 heads 4.4 us.
+// LDS.  Bound by memory: 22,804 tokens of 32 + 8 heads of 128 take 127 us, 4.4 TB/s (a large copy: 5.1),
+// in fp32 262 us, 4.3 TB/s; one token of 28 + 4 heads 4.4 us.
 #include <math.h>
 
 #include <type_traits>

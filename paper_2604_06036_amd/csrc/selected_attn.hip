@@ -564,7 +564,7 @@ __global__ __launch_bounds__(256) void selected_join_kernel(Params p, int bf16) 
 // c ^ row_place(r), of values at c ^ v_place(r).
 // Bound by the length of a step's chain (gate, scores, softmax, sums) with the four waves a SIMD that registers and LDS allow: 2,082 tokens of 28
 // heads of 128 on 4 over 16 blocks of 64 each take 90 us; matrix instructions are busy for 20 of them, vector instructions for 32, and LDS
-// reads for 21.  Deeper or wider did worse, since it costs waves (when this kernel took 112 to 116): three stages 152, a wave's scores a step
+// reads for 21; what the workgroups move from L2, 1.32 GB, takes 34 at 64 bytes a clock and CU.  Deeper or wider did worse, since it costs waves (when this kernel took 112 to 116): three stages 152, a wave's scores a step
 // ahead of its sums 171, 64 keys a step 126, 32 rows a wave 130.
 constexpr int kStepKeys = 32, kStepGroups = kStepKeys / CS_KV_BLOCK;
 constexpr int kRowsWave = kRows, kRowsWaves = 4, kRowsGroup = kRowsWave * kRowsWaves;
