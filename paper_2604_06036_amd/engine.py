@@ -696,11 +696,12 @@ class SelectStep(DeviceStep):
         """Places a token a stream behind the windows, in every layer's cache: `token_slot` int32 [n_streams] says where, -1 where a stream's
         blocks are full.  Such a stream's token is not written and its window stays as it is; the others' windows grow by it (`kv_len`).
         A token is this, then `token_layer` for every layer in turn."""
+        import torch
         self.token_entry.copy_(self.kv_len)
-        slot, kv_len = _token_places(self.token_entry, self.room, self.block_table)
+        slot, there = _token_places(self.token_entry, self.room, self.block_table)
         self.token_slot.copy_(slot)
-        self.kv_len.copy_(kv_len)
-        self.token_last.copy_(kv_len - 1)
+        self.kv_len.add_(there)
+        torch.sub(self.kv_len, 1, out=self.token_last)
 
     def token_layer(self, layer: int, q, k_new, v_new, positions, out):
         """A layer of the token that `begin_token` has placed: q [n_streams][n_q_heads][head_dim] as the projection leaves it, k_new and v_new
@@ -728,21 +729,23 @@ class SelectStep(DeviceStep):
 
 
 def _token_places(entry, room, block_table):
-    """Cache slots of a token behind windows of `entry` entries, -1 where a stream has no room (or no window yet: a negative length), and the lengths
-    with it."""
+    """Cache slots of a token behind windows of `entry` entries, -1 where a stream has no room (or no window yet: a negative length), and which
+    streams have."""
     import torch
-    there = (entry >= 0) & (entry < room)
-    place = torch.where(there, entry, 0)
-    slot = block_table.gather(1, (place // synth.KV_BLOCK).long()[:, None])[:, 0] * synth.KV_BLOCK + place % synth.KV_BLOCK
-    return torch.where(there, slot, -1), entry + there.int()
+    there = (entry < room).logical_and_(entry >= 0)
+    place = entry * there
+    block = block_table.gather(1, (place // synth.KV_BLOCK).long()[:, None])[:, 0]
+    return torch.where(there, torch.add(place % synth.KV_BLOCK, block, alpha=synth.KV_BLOCK), -1), there
 
 
 def _check_token(q, k_new, v_new, positions, rows, n_q_heads, n_kv_heads, head_dim, width):
+    """Refuses tensors of a token that hold fewer rows than `rows`, or rows of another shape."""
     for what, t, heads in (("q", q, n_q_heads), ("k_new", k_new, n_kv_heads), ("v_new", v_new, n_kv_heads)):
-        if tuple(t.shape) != rows + (heads, head_dim) or t.stride(-1) != 1 or heads > 1 and t.stride(-2) != head_dim:
+        if (t.dim() != len(rows) + 2 or tuple(t.shape[-2:]) != (heads, head_dim) or any(have < want for have, want in zip(t.shape, rows))
+                or t.stride(-1) != 1 or heads > 1 and t.stride(-2) != head_dim):
             raise ValueError(f"token: {what}: {list(rows + (heads, head_dim))} expected, the heads of a row behind one another")
     # (a [3][n_streams] tensor would be read as other rows' positions)
-    if positions.numel() != width * rows[-1] or positions.dim() > 1 and int(positions.shape[-1]) != width:
+    if positions.numel() < width * rows[-1] or positions.dim() > 1 and int(positions.shape[-1]) != width:
         raise ValueError(f"token: positions: int32 of {rows[-1]} rows of {width} expected")
 
 
